@@ -354,7 +354,8 @@ def _plain_append_to(cache, scales, new, s, tokens_last):
     if tokens_last:
         old = old.view(torch.uint8).transpose(3, 4).contiguous().view(E4M3)
     kept = old.float() * _power(127 + before - e)[..., None, None]
-    y = torch.where(fresh, x * _power(254 - e)[..., None, None], kept).clamp(-448, 448).to(E4M3).view(torch.uint8)
+    y = torch.where(fresh, x * _power(254 - e)[..., None, None], kept)
+    y = torch.where(torch.isfinite(y), y.clamp(-448, 448), math.nan).to(E4M3).view(torch.uint8)
     y = torch.where(fresh | older, y, old.view(torch.uint8))
     if tokens_last:
         y = y.transpose(3, 4)
