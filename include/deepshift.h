@@ -570,6 +570,137 @@ int64_t ds_conv2d_shift_noalloc_scratch_bytes(int64_t n, int64_t c, int64_t h, i
 ds_status ds_set_tuning(const char *name, int32_t value);
 ds_status ds_get_tuning(const char *name, int32_t *value);
 
+/* ---------------------------------------------------------------------------
+ * 8-bit operators of a language model's decoder layer: float8 numbers with
+ * power-of-two scales, for models whose weights are signed powers of two (every
+ * shift code is an E5M2 number exactly) or 8-bit floats.
+ *
+ * An 8-bit number q (E4M3: largest 448, no infinity; or E5M2) of a block with the
+ * scale byte e (E8M0) stands for q * 2^(e - 127). Activations have a scale for
+ * each row and 128 elements, weights one for each 128 x 128 elements, a cache one
+ * for each page of tokens and head. A quantiser takes the least power of two that
+ * brings the block's largest finite magnitude to at most 448 (2^0 for a block of
+ * zeros, 2^-48 in a cache), rounds to nearest even, and holds an element that is
+ * not finite as NaN, which has no say in its block's scale.
+ *
+ * Element types of the other tensors: ds_dtype. Strides (ld*) count elements from
+ * one row to the next; an 8-bit matrix's rows begin on 16 bytes, a multiple of 16
+ * apart, and are readable up to a multiple of 16 (their elements past the columns
+ * are never used, the quantisers write zeros up to a multiple of 8). No output may
+ * overlap another tensor of the call. Sums, norms and softmax statistics are held
+ * in 32 bits. Calls are asynchronous on `stream`, allocate nothing, keep nothing
+ * and may be captured; scratch is device memory of the caller's that a call may
+ * overwrite. Sizes of 0 rows, tokens or sequences are allowed and do nothing. */
+typedef enum ds_dtype {
+    DS_TYPE_F32 = 0,
+    DS_TYPE_F16 = 1,
+    DS_TYPE_BF16 = 2,
+    DS_TYPE_F8E4M3 = 3,
+    DS_TYPE_F8E5M2 = 4
+} ds_dtype;
+
+/* Root-mean-square norm. h = x + residual, rounded to `type` and stored (residual
+ * NULL: h = x, and h must be NULL); rstd[row] = 1 / sqrt(mean(h^2) + eps) (rstd may
+ * be NULL); y = h * rstd * weight, in `type` (y_type == type; scales and lds are
+ * ignored) or 8 bits (y_type DS_TYPE_F8E4M3). weight [cols]: `type` or float32.
+ * Up to 65536 columns. */
+ds_status ds_rms_norm(const void *x, const void *residual, const void *weight, void *y,
+                      uint8_t *scales, void *h, float *rstd, int64_t rows, int64_t cols,
+                      int64_t ldx, int64_t ldr, int64_t ldh, int64_t ldy, int64_t lds, float eps,
+                      int32_t type, int32_t weight_type, int32_t y_type, void *stream);
+
+/* Gradient of ds_rms_norm (an 8-bit output's rounding counts as the identity). With
+ * n = h * rstd and g = dy * weight: dx = rstd * (g - n * mean(g * n)) + dh, the
+ * gradient of x and of the residual alike (dh: the gradient that reaches h from
+ * elsewhere, or NULL), and dweight = sum over rows of dy * n, in weight's type (NULL:
+ * not wanted; with it scratch of ds_rms_norm_backward_scratch_bytes is). The sum is
+ * taken in the same order in every run. */
+ds_status ds_rms_norm_backward(const void *dy, const void *h, const void *weight,
+                               const float *rstd, const void *dh, void *dx, void *dweight,
+                               int64_t rows, int64_t cols, int64_t lddy, int64_t ldh,
+                               int64_t lddh, int64_t lddx, int32_t type, int32_t weight_type,
+                               void *scratch, int64_t scratch_bytes, void *stream);
+int64_t ds_rms_norm_backward_scratch_bytes(int64_t rows, int64_t cols);
+
+/* x [rows][cols], or silu(gate) * x with gate of the same shape and type (NULL: none),
+ * to 8 bits (E4M3) with a scale for each row and 128 elements. */
+ds_status ds_quantize_fp8(const void *x, const void *gate, uint8_t *y, uint8_t *scales,
+                          int64_t rows, int64_t cols, int64_t ldx, int64_t ldg, int64_t ldy,
+                          int64_t lds, int32_t type, void *stream);
+
+/* A weight matrix to 8 bits (E4M3) with scales [ceil(rows / 128)][ceil(cols / 128)]. */
+ds_status ds_quantize_weights_fp8(const void *w, uint8_t *w8, uint8_t *scales, int64_t rows,
+                                  int64_t cols, int64_t ldw, int64_t ldw8, int64_t lds,
+                                  int32_t type, void *stream);
+
+/* Packed shift codes (flags: DS_CODE_BITS) as E5M2 numbers +-2^-shift and 0, exactly;
+ * every scale of such a matrix is 2^0, the byte 127. */
+ds_status ds_shift_weights_to_fp8(const uint32_t *w_packed, uint8_t *w8, int64_t rows,
+                                  int64_t cols, int64_t ldw8, uint32_t flags, void *stream);
+
+/* y[m][n] = bias[n] + sum_k x8[m][k] * w8[n][k] of the scaled values: x8 E4M3 with
+ * scales [m][ceil(k / 128)], w8 of w_type (DS_TYPE_F8E4M3 or DS_TYPE_F8E5M2) with
+ * scales [ceil(n / 128)][ceil(k / 128)], bias float32 or NULL, y of y_type. */
+ds_status ds_linear_fp8(const uint8_t *x8, const uint8_t *x_scales, const uint8_t *w8,
+                        const uint8_t *w_scales, const float *bias, void *y, int64_t m, int64_t n,
+                        int64_t k, int64_t ldx, int64_t ldxs, int64_t ldw, int64_t ldws,
+                        int64_t ldy, int32_t w_type, int32_t y_type, void *stream);
+
+/* Its input gradient dx[m][k] = sum_n dy8[m][n] * w8[n][k] of the scaled values: dy8
+ * E4M3 with scales [m][ceil(n / 128)], the weights as in the forward product. scratch
+ * (256-byte aligned): ds_linear_fp8_backward_data_scratch_bytes. */
+ds_status ds_linear_fp8_backward_data(const uint8_t *dy8, const uint8_t *dy_scales,
+                                      const uint8_t *w8, const uint8_t *w_scales, void *dx,
+                                      int64_t m, int64_t n, int64_t k, int64_t lddy,
+                                      int64_t lddys, int64_t ldw, int64_t ldws, int64_t lddx,
+                                      int32_t w_type, int32_t dx_type, void *scratch,
+                                      int64_t scratch_bytes, void *stream);
+int64_t ds_linear_fp8_backward_data_scratch_bytes(int64_t m, int64_t n, int64_t k);
+
+/* A paged cache of keys and values in 8 bits (E4M3): k_cache [pages][heads][page][dim],
+ * v_cache [pages][heads][dim][page], scales [pages][heads] each, within 2^-48 .. 2^48 (an
+ * attention reads a scale outside as the nearest one inside). page: 16, 32, 64 or 128
+ * tokens; dim: a multiple of 16, at most 256. Row b of `table` [batch][columns] (ldt
+ * elements apart) lists the pages of sequence b in order.
+ *
+ * ds_kv_cache_append writes tokens 0 .. count[b] - 1 (count NULL: all) of k and v
+ * [batch][tokens][heads][dim] at positions start[b], start[b] + 1, .. of sequence b. A
+ * page's scale is the one its new tokens need; where it already holds tokens before
+ * start[b], the larger of that and its own, and what it holds is rounded again where the
+ * scale grows. Values past the scales' range are held as the largest number. Tokens of a
+ * column past the table, or of a page outside 0 .. pages - 1, are dropped. The pages that
+ * a call writes must be distinct. strides: of k and v in elements (sequence, token,
+ * head; host memory, read before the call returns); a vector's elements are consecutive. */
+ds_status ds_kv_cache_append(const void *k, const void *v, uint8_t *k_cache, uint8_t *v_cache,
+                             uint8_t *k_scales, uint8_t *v_scales, const int32_t *table,
+                             const int32_t *start, const int32_t *count, int64_t batch,
+                             int64_t tokens, int64_t heads, int64_t dim, int64_t page,
+                             int64_t pages, int64_t columns, int64_t ldt,
+                             const int64_t *k_strides, const int64_t *v_strides, int32_t type,
+                             void *stream);
+
+/* Causal attention of q [batch][tokens][heads * group][dim] (type DS_TYPE_F16 or
+ * DS_TYPE_BF16; query head h reads head h / group of the cache) over sequences of
+ * length[b] tokens in the cache, the last count[b] of which (count NULL: tokens) are the
+ * queries': query i < count[b] is at position length[b] - count[b] + i and sees the keys
+ * up to its own, the last `window` of them where window > 0. o (q's shape and type) =
+ * softmax(scale * q k) v; a query that sees no key, or i >= count[b], gets zeros. Keys on
+ * a page outside 0 .. pages - 1 are not seen (a page may leave a sequence that way). What
+ * pages hold past a sequence's end does not matter; a NaN among the values of a token
+ * that one query of a call sees reaches the queries of the same call and head that do not.
+ * scratch: ds_attention_fp8_scratch_bytes (0: none needed). */
+ds_status ds_attention_fp8(const void *q, const uint8_t *k_cache, const uint8_t *v_cache,
+                           const uint8_t *k_scales, const uint8_t *v_scales, const int32_t *table,
+                           const int32_t *length, const int32_t *count, void *o, int64_t batch,
+                           int64_t tokens, int64_t heads, int64_t group, int64_t dim,
+                           int64_t page, int64_t pages, int64_t columns, int64_t ldt,
+                           const int64_t *q_strides, const int64_t *o_strides, float scale,
+                           int64_t window, int32_t type, void *scratch, int64_t scratch_bytes,
+                           void *stream);
+int64_t ds_attention_fp8_scratch_bytes(int64_t batch, int64_t tokens, int64_t heads,
+                                       int64_t group, int64_t dim, int64_t page,
+                                       int64_t columns);
+
 /* Static text for a status code. */
 const char *ds_status_string(ds_status status);
 

@@ -19,6 +19,7 @@ _P = ctypes.c_void_p
 _I64 = ctypes.c_int64
 _I32 = ctypes.c_int32
 _U32 = ctypes.c_uint32
+_F32 = ctypes.c_float
 
 SIGNATURES = {
     "ds_packed_row_words": (_I64, [_I64]),
@@ -58,6 +59,18 @@ SIGNATURES = {
     "ds_conv2d_shift_backward_data_scratch_bytes": (_I64, [_I64] * 7 + [_I32] * 4),
     "ds_conv2d_shift_backward_data_ws": (ctypes.c_int, [_P, _P, _P] + [_I64] * 7 + [_I32] * 4 + [_I32, _U32, _P, _I64, _P]),
     "ds_jit_conv_matrix_cores": (_I32, [_P]),
+    "ds_rms_norm": (ctypes.c_int, [_P] * 7 + [_I64] * 7 + [_F32] + [_I32] * 3 + [_P]),
+    "ds_rms_norm_backward": (ctypes.c_int, [_P] * 7 + [_I64] * 6 + [_I32] * 2 + [_P, _I64, _P]),
+    "ds_rms_norm_backward_scratch_bytes": (_I64, [_I64] * 2),
+    "ds_quantize_fp8": (ctypes.c_int, [_P] * 4 + [_I64] * 6 + [_I32, _P]),
+    "ds_quantize_weights_fp8": (ctypes.c_int, [_P] * 3 + [_I64] * 5 + [_I32, _P]),
+    "ds_shift_weights_to_fp8": (ctypes.c_int, [_P] * 2 + [_I64] * 3 + [_U32, _P]),
+    "ds_linear_fp8": (ctypes.c_int, [_P] * 6 + [_I64] * 8 + [_I32] * 2 + [_P]),
+    "ds_linear_fp8_backward_data": (ctypes.c_int, [_P] * 5 + [_I64] * 8 + [_I32] * 2 + [_P, _I64, _P]),
+    "ds_linear_fp8_backward_data_scratch_bytes": (_I64, [_I64] * 3),
+    "ds_kv_cache_append": (ctypes.c_int, [_P] * 9 + [_I64] * 8 + [_P] * 2 + [_I32, _P]),
+    "ds_attention_fp8": (ctypes.c_int, [_P] * 9 + [_I64] * 9 + [_P] * 2 + [_F32, _I64, _I32, _P, _I64, _P]),
+    "ds_attention_fp8_scratch_bytes": (_I64, [_I64] * 7),
     "ds_set_tuning": (ctypes.c_int, [ctypes.c_char_p, _I32]),
     "ds_get_tuning": (ctypes.c_int, [ctypes.c_char_p, _P]),
     "ds_status_string": (ctypes.c_char_p, [ctypes.c_int]),

@@ -1,0 +1,142 @@
+// What the 8-bit operators share: float8 numbers with power-of-two block scales.
+//
+// A block of numbers y is held as bytes q and one scale byte e (E8M0, a biased
+// exponent): y = q * 2^(e - 127). A power of two costs the matrix instructions
+// nothing (their block scale operand applies it), is exact in every format here,
+// and moving a block to another scale is a change of its elements' exponents.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "common.hpp"
+
+namespace ds {
+
+constexpr int kScaleBlock = 128;   // elements of a row that share a scale
+
+// The element types of the unquantised tensors.
+inline int float_bytes(int32_t type) { return type == DS_TYPE_F32 ? 4 : type == DS_TYPE_F16 || type == DS_TYPE_BF16 ? 2 : 0; }
+
+// The status of a call whose launches are enqueued.
+inline ds_status launched(const char *what)
+{
+    const hipError_t e = hipGetLastError();
+    if (e == hipSuccess) return ok();
+    return fail(DS_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
+}
+
+// Bytes that `rows` rows of `row` bytes span when they begin `pitch` bytes apart.
+inline int64_t span(int64_t rows, int64_t pitch, int64_t row) { return rows <= 0 ? 0 : (rows - 1) * pitch + row; }
+
+// A tensor of a call: checked to lie in device memory; an output overlaps no other.
+struct Tensor {
+    const void *p;
+    int64_t bytes;
+    const char *name;
+    bool out;
+};
+
+inline ds_status check_tensors(std::initializer_list<Tensor> list)
+{
+    for (const Tensor &t : list) {
+        if (!t.out || !t.p) continue;
+        for (const Tensor &o : list)
+            if (&o != &t && overlap(t.p, t.bytes, o.p, o.bytes))
+                return fail(DS_ERR_INVALID_ARG, "%s overlaps %s", t.name, o.name);
+    }
+    for (const Tensor &t : list)
+        if (t.p && t.bytes > 0 && !device_range_ok(t.p, t.bytes))
+            return fail(DS_ERR_INVALID_ARG, "%s is not a device buffer of %lld bytes", t.name, (long long)t.bytes);
+    return DS_SUCCESS;
+}
+
+#if defined(__HIPCC__)
+
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// 2^(e - 127) for e in 1 .. 254.
+__device__ __forceinline__ float power_of_two(uint32_t e) { return __uint_as_float(e << 23); }
+
+// The scale byte of the least power of two that brings `amax` (finite, >= 0) to at
+// most 448 = 1.75 * 2^8, the largest E4M3 number: a mantissa above 1.75 carries into
+// the exponent. Not limited to a byte from below: the caller does that.
+__device__ __forceinline__ int scale_byte(float amax) { return int((__float_as_uint(amax) + 0x1fffffu) >> 23) - 8; }
+
+// The scale byte of a block of activations or weights: 2^0 for a block of zeros.
+__device__ __forceinline__ int block_scale(float amax) { return amax == 0.f ? 127 : max(scale_byte(amax), 1); }
+
+// |v|, or 0 where v is infinite or NaN: such an element is held as NaN and has no
+// say in its block's scale.
+__device__ __forceinline__ float finite_abs(float v)
+{
+    const float a = fabsf(v);
+    return a < __builtin_inff() ? a : 0.f;
+}
+
+// Four floats as E4M3 bytes, rounded to nearest even (beyond +-448, infinite or NaN: NaN).
+__device__ __forceinline__ int to_fp8x4(float a, float b, float c, float d)
+{
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return __builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true);
+}
+
+// Eight consecutive elements as floats. Rows may begin anywhere (16-byte loads need
+// no alignment on this machine); `n` < 8 reads the first n, the others are 0.
+template <typename T>
+__device__ __forceinline__ void load8(const T *p, int n, float (&v)[8])
+{
+    if (n >= 8) {
+        T t[8];
+        __builtin_memcpy(t, p, sizeof t);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = float(t[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? float(p[i]) : 0.f;
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void store8(T *p, int n, const float (&v)[8])
+{
+    if (n >= 8) {
+        T t[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i] = T(v[i]);
+        __builtin_memcpy(p, t, sizeof t);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) p[i] = T(v[i]);
+    }
+}
+
+// Sum / maximum over aligned groups of N lanes (N a power of two up to 64), in every lane.
+template <int N>
+__device__ __forceinline__ float lanes_sum(float v)
+{
+#pragma unroll
+    for (int o = N / 2; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+}
+
+template <int N>
+__device__ __forceinline__ float lanes_max(float v)
+{
+#pragma unroll
+    for (int o = N / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+    return v;
+}
+
+#endif  // __HIPCC__
+
+}  // namespace ds

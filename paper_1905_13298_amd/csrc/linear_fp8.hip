@@ -1,0 +1,271 @@
+// The product of 8-bit matrices with power-of-two block scales, and its input gradient.
+//
+//   y[m][n] = bias[n] + sum over blocks b of 128 of
+//             2^(xs[m][b] + ws[n / 128][b] - 254) * sum_{k in b} x8[m][k] * w8[n][k]
+//
+// x8 in E4M3 with a scale for each row and 128 elements, w8 in E4M3 or E5M2 with a
+// scale for each 128 x 128 elements. The scales are the matrix instruction's own block
+// scale operands, so they cost no instruction and the sums stay in 32-bit accumulators
+// from the first element to the last.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "conv_plan.hpp"
+#include "fp8.hpp"
+
+namespace ds {
+
+namespace {
+
+struct LinearParams {
+    const uint8_t *x, *xs, *w, *ws;
+    const float *bias;
+    void *y;
+    int m, n, k, kblocks;
+    int64_t ldx, ldxs, ldw, ldws, ldy;
+};
+
+// 16 bytes of a row from element k on; bytes past `cols` are 0 (the row's first bytes
+// are read in place of a piece that begins past the end).
+__device__ __forceinline__ i32x4 row16(const uint8_t *row, int k, int cols)
+{
+    const int n = cols - k;
+    i32x4 v = *reinterpret_cast<const i32x4 *>(row + (n > 0 ? k : 0));
+    if (n < 16) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int left = n - 4 * i;
+            v[i] = left >= 4 ? v[i] : left <= 0 ? 0 : v[i] & int((1u << (8 * left)) - 1u);
+        }
+    }
+    return v;
+}
+
+__device__ __forceinline__ i32x8 row32(const uint8_t *row, int k, int cols)
+{
+    const i32x4 a = row16(row, k, cols), b = row16(row, k + 16, cols);
+    return i32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+}
+
+// 8 of a lane's 32 elements as 16-bit floats, exactly (WF 0: E4M3, 1: E5M2).
+template <int WF>
+__device__ __forceinline__ f16x8 widen(i32x8 v, int i)
+{
+    f16x8 o;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        f16x2 a, b;
+        if constexpr (WF == 0) {
+            a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v[2 * i + j], 1.f, false);
+            b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v[2 * i + j], 1.f, true);
+        } else {
+            a = __builtin_amdgcn_cvt_scalef32_pk_f16_bf8(v[2 * i + j], 1.f, false);
+            b = __builtin_amdgcn_cvt_scalef32_pk_f16_bf8(v[2 * i + j], 1.f, true);
+        }
+        o[4 * j] = a[0];
+        o[4 * j + 1] = a[1];
+        o[4 * j + 2] = b[0];
+        o[4 * j + 3] = b[1];
+    }
+    return o;
+}
+
+// c + one block's products. The 8-bit instruction aligns the products of each 8 elements with
+// the largest of them and drops what lies 2^-14 below it, which an output of 16 bits does
+// not show and one of 32 does: such an output (FULL) is formed from the same numbers as
+// 16-bit floats, whose products and sums keep 24 bits, the scales applied afterwards.
+template <int WF, bool FULL>
+__device__ __forceinline__ f32x4 mma(i32x8 w, i32x8 x, f32x4 c, int ws, int xs)
+{
+    if constexpr (FULL) {
+        f32x4 part{};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) part = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen<WF>(w, i), widen<0>(x, i), part, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c[i] += ldexpf(part[i], ws + xs - 254);
+        return c;
+    } else {
+        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, c, WF, 0, 0, ws, 0, xs);
+    }
+}
+
+// Few rows of x: the weights go from memory to registers, once. A block takes 16 rows of
+// w and MT x 16 rows of x; its waves take every WAVES-th block of 128 of the reduction
+// and add their sums in LDS. The weights are the instruction's first operand, so that a
+// lane ends up with four consecutive outputs of one row of y.
+template <typename O, int WF, int MT, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES)
+linear_rows_kernel(const LinearParams p)
+{
+    __shared__ f32x4 sums[WAVES][MT][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+    const int n0 = int(blockIdx.x) * 16, m0 = int(blockIdx.y) * 16 * MT;
+    const uint8_t *wrow = p.w + int64_t(min(n0 + r, p.n - 1)) * p.ldw;
+    const uint8_t *wsrow = p.ws + int64_t(n0 / kScaleBlock) * p.ldws;
+    const uint8_t *xrow[MT], *xsrow[MT];
+    f32x4 acc[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        const int64_t m = min(m0 + t * 16 + r, p.m - 1);
+        xrow[t] = p.x + m * p.ldx;
+        xsrow[t] = p.xs + m * p.ldxs;
+        acc[t] = f32x4{};
+    }
+    for (int b = wave; b < p.kblocks; b += WAVES) {
+        const int k = b * kScaleBlock + g * 32;
+        const i32x8 w = row32(wrow, k, p.k);
+        const int ws = wsrow[b];
+#pragma unroll
+        for (int t = 0; t < MT; ++t) acc[t] = mma<WF, sizeof(O) == 4>(w, row32(xrow[t], k, p.k), acc[t], ws, xsrow[t][b]);
+    }
+#pragma unroll
+    for (int t = 0; t < MT; ++t) sums[wave][t][lane] = acc[t];
+    __syncthreads();
+    for (int t = wave; t < MT; t += WAVES) {
+        f32x4 s = sums[0][t][lane];
+#pragma unroll
+        for (int i = 1; i < WAVES; ++i) s += sums[i][t][lane];
+        const int m = m0 + t * 16 + r, n = n0 + g * 4;
+        if (m >= p.m) continue;
+        O *y = static_cast<O *>(p.y) + m * p.ldy + n;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (n + i < p.n) y[i] = O(s[i] + (p.bias ? p.bias[n + i] : 0.f));
+    }
+}
+
+// w8 [n][k] to [k][n] (rows of ldt bytes, filled up with zeros): 64 x 64 bytes a block.
+__global__ void __launch_bounds__(256)
+transpose8_kernel(const uint8_t *__restrict__ w, uint8_t *__restrict__ t, int n, int k, int64_t ldw, int64_t ldt)
+{
+    __shared__ uint8_t tile[64][68];
+    const int k0 = int(blockIdx.x) * 64, n0 = int(blockIdx.y) * 64;
+    const int row = int(threadIdx.x >> 2), piece = int(threadIdx.x & 3) * 16;
+    i32x4 v{};
+    if (n0 + row < n) v = row16(w + (n0 + row) * ldw, k0 + piece, k);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<int *>(&tile[row][piece + 4 * i]) = v[i];
+    __syncthreads();
+    if (k0 + row >= k || n0 + piece >= ldt) return;
+    i32x4 o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t word = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) word |= uint32_t(tile[piece + 4 * i + j][row]) << (8 * j);
+        o[i] = int(word);
+    }
+    *reinterpret_cast<i32x4 *>(t + (k0 + row) * ldt + n0 + piece) = o;
+}
+
+// The weights' scales [rows][cols] to [cols][rows].
+__global__ void __launch_bounds__(256)
+transpose_scales_kernel(const uint8_t *__restrict__ s, uint8_t *__restrict__ t, int rows, int cols, int64_t lds)
+{
+    const int i = int(blockIdx.x) * 256 + int(threadIdx.x);
+    if (i < rows * cols) t[(i % cols) * rows + i / cols] = s[(i / cols) * lds + i % cols];
+}
+
+template <typename O>
+void run_linear(const LinearParams &p, bool e5m2, hipStream_t s)
+{
+    const bool one = p.m <= 16;
+    const dim3 grid(uint32_t((p.n + 15) / 16), uint32_t((p.m + (one ? 15 : 63)) / (one ? 16 : 64)));
+    const auto k = e5m2 ? (one ? linear_rows_kernel<O, 1, 1, 8> : linear_rows_kernel<O, 1, 4, 8>)
+                        : (one ? linear_rows_kernel<O, 0, 1, 8> : linear_rows_kernel<O, 0, 4, 8>);
+    hipLaunchKernelGGL(k, grid, dim3(512), 0, s, p);
+}
+
+int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+int64_t blocks_of(int64_t v) { return (v + kScaleBlock - 1) / kScaleBlock; }
+
+ds_status check_linear(const char *a, int64_t m, int64_t n, int64_t k, int64_t in, int64_t out, const void *x8, const void *w8,
+                       int64_t ldx, int64_t ldxs, int64_t ldw, int64_t ldws, int64_t ldy, int32_t w_type, int32_t y_type)
+{
+    if (m < 0 || n <= 0 || k <= 0) return fail(DS_ERR_INVALID_SHAPE, "m must be >= 0, n and k > 0");
+    if (m > kMaxElems / 64 || n > kMaxElems / 64 || k > kMaxElems / 64)
+        return fail(DS_ERR_UNSUPPORTED, "2^25 or more rows or columns");
+    if (w_type != DS_TYPE_F8E4M3 && w_type != DS_TYPE_F8E5M2) return fail(DS_ERR_INVALID_ARG, "w_type must be DS_TYPE_F8E4M3 or DS_TYPE_F8E5M2");
+    if (!float_bytes(y_type)) return fail(DS_ERR_INVALID_ARG, "y_type must be DS_TYPE_F32, DS_TYPE_F16 or DS_TYPE_BF16");
+    if (ldx < up(in, 16) || ldx % 16 || reinterpret_cast<uintptr_t>(x8) % 16 || ldw < up(k, 16) || ldw % 16 ||
+        reinterpret_cast<uintptr_t>(w8) % 16)
+        return fail(DS_ERR_INVALID_ARG, "8-bit rows must begin on 16 bytes and be a multiple of 16 apart, at least the columns");
+    if (ldxs < blocks_of(in) || ldws < blocks_of(k)) return fail(DS_ERR_INVALID_ARG, "fewer scales in a row than blocks of 128");
+    if (ldy < out) return fail(DS_ERR_INVALID_ARG, "a row of %s is shorter than its columns", a);
+    return DS_SUCCESS;
+}
+
+void launch(const LinearParams &p, int32_t w_type, int32_t y_type, hipStream_t s)
+{
+    const bool e5m2 = w_type == DS_TYPE_F8E5M2;
+    if (y_type == DS_TYPE_F32) run_linear<float>(p, e5m2, s);
+    else if (y_type == DS_TYPE_F16) run_linear<_Float16>(p, e5m2, s);
+    else run_linear<__bf16>(p, e5m2, s);
+}
+
+}  // namespace
+
+}  // namespace ds
+
+using namespace ds;
+
+extern "C" ds_status ds_linear_fp8(const uint8_t *x8, const uint8_t *x_scales, const uint8_t *w8, const uint8_t *w_scales,
+                                   const float *bias, void *y, int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldxs,
+                                   int64_t ldw, int64_t ldws, int64_t ldy, int32_t w_type, int32_t y_type, void *stream)
+{
+    if (m != 0 && (!x8 || !x_scales || !w8 || !w_scales || !y))
+        return fail(DS_ERR_NULL_POINTER, "x8, w8, their scales and y must not be NULL");
+    if (ds_status st = check_linear("y", m, n, k, k, n, x8, w8, ldx, ldxs, ldw, ldws, ldy, w_type, y_type)) return st;
+    if (m == 0) return ok();
+    const int64_t es = float_bytes(y_type);
+    if (ds_status st = check_tensors({{x8, span(m, ldx, up(k, 16)), "x8", false},
+                                      {x_scales, span(m, ldxs, blocks_of(k)), "x_scales", false},
+                                      {w8, span(n, ldw, up(k, 16)), "w8", false},
+                                      {w_scales, span(blocks_of(n), ldws, blocks_of(k)), "w_scales", false},
+                                      {bias, n * 4, "bias", false},
+                                      {y, span(m, ldy * es, n * es), "y", true}}))
+        return st;
+    const LinearParams p{x8, x_scales, w8, w_scales, bias, y, int(m), int(n), int(k), int(blocks_of(k)), ldx, ldxs, ldw, ldws, ldy};
+    launch(p, w_type, y_type, static_cast<hipStream_t>(stream));
+    return launched("ds_linear_fp8");
+}
+
+extern "C" int64_t ds_linear_fp8_backward_data_scratch_bytes(int64_t m, int64_t n, int64_t k)
+{
+    if (m <= 0 || n <= 0 || k <= 0 || n > kMaxElems / 64 || k > kMaxElems / 64) return 0;
+    return up(k * up(n, 16), 256) + up(blocks_of(k) * blocks_of(n), 256);
+}
+
+extern "C" ds_status ds_linear_fp8_backward_data(const uint8_t *dy8, const uint8_t *dy_scales, const uint8_t *w8,
+                                                 const uint8_t *w_scales, void *dx, int64_t m, int64_t n, int64_t k,
+                                                 int64_t lddy, int64_t lddys, int64_t ldw, int64_t ldws, int64_t lddx,
+                                                 int32_t w_type, int32_t dx_type, void *scratch, int64_t scratch_bytes,
+                                                 void *stream)
+{
+    if (m != 0 && (!dy8 || !dy_scales || !w8 || !w_scales || !dx))
+        return fail(DS_ERR_NULL_POINTER, "dy8, w8, their scales and dx must not be NULL");
+    if (ds_status st = check_linear("dx", m, n, k, n, k, dy8, w8, lddy, lddys, ldw, ldws, lddx, w_type, dx_type)) return st;
+    if (m == 0) return ok();
+    const int64_t need = ds_linear_fp8_backward_data_scratch_bytes(m, n, k), es = float_bytes(dx_type);
+    if (!scratch) return fail(DS_ERR_NULL_POINTER, "scratch must not be NULL");
+    if (scratch_bytes < need) return fail(DS_ERR_BUFFER_TOO_SMALL, "scratch has %lld bytes, %lld are needed", (long long)scratch_bytes, (long long)need);
+    if (reinterpret_cast<uintptr_t>(scratch) % 256) return fail(DS_ERR_INVALID_ARG, "scratch is not 256-byte aligned");
+    if (ds_status st = check_tensors({{dy8, span(m, lddy, up(n, 16)), "dy8", false},
+                                      {dy_scales, span(m, lddys, blocks_of(n)), "dy_scales", false},
+                                      {w8, span(n, ldw, up(k, 16)), "w8", false},
+                                      {w_scales, span(blocks_of(n), ldws, blocks_of(k)), "w_scales", false},
+                                      {dx, span(m, lddx * es, k * es), "dx", true},
+                                      {scratch, need, "scratch", true}}))
+        return st;
+    const auto s = static_cast<hipStream_t>(stream);
+    const int64_t ldt = up(n, 16);
+    uint8_t *wt = static_cast<uint8_t *>(scratch), *wst = wt + up(k * ldt, 256);
+    const int nb = int(blocks_of(n)), kb = int(blocks_of(k));
+    hipLaunchKernelGGL(transpose8_kernel, dim3(uint32_t((k + 63) / 64), uint32_t((n + 63) / 64)), dim3(256), 0, s, w8, wt,
+                       int(n), int(k), ldw, ldt);
+    hipLaunchKernelGGL(transpose_scales_kernel, dim3(uint32_t((nb * kb + 255) / 256)), dim3(256), 0, s, w_scales, wst, nb, kb, ldws);
+    const LinearParams p{dy8, dy_scales, wt, wst, nullptr, dx, int(m), int(k), int(n), nb, lddy, lddys, ldt, int64_t(nb), lddx};
+    launch(p, w_type, dx_type, s);
+    return launched("ds_linear_fp8_backward_data");
+}

@@ -1,0 +1,538 @@
+// Root-mean-square norm with the residual's addition and an 8-bit output, its
+// gradient, and the quantisers: of activations (with or without a SiLU gate), of
+// weight matrices, and of shift codes.
+//
+// All are streaming passes bound by memory bandwidth: every input is read once and
+// every output written once. A thread holds 8 consecutive elements, so 16 lanes hold
+// the 128 elements that share a scale and its maximum is four steps between lanes.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "conv_plan.hpp"
+#include "fastdiv.hpp"
+#include "fp8.hpp"
+
+namespace ds {
+
+namespace {
+
+// ---------------------------------------------------------------------------
+// Norm. h = x + residual (rounded to x's type, as it is stored), rstd = 1 / sqrt(mean
+// h^2 + eps), y = h * rstd * weight, in 8 bits or in x's type.
+
+struct NormParams {
+    int64_t rows, ldx, ldr, ldh, ldy, lds;
+    int cols;
+    float eps;
+};
+
+// Sum of `v` over the TPR threads of a row; `red` holds a float per wave.
+template <int TPR>
+__device__ __forceinline__ float row_sum(float v, float *red)
+{
+    v = lanes_sum<64>(v);
+    if constexpr (TPR > 64) {
+        const int wave = threadIdx.x >> 6;
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) red[wave] = v;
+        __syncthreads();
+        v = 0.f;
+#pragma unroll
+        for (int i = 0; i < TPR / 64; ++i) v += red[i];
+    }
+    return v;
+}
+
+template <int TPR>
+constexpr int row_block() { return TPR < 256 ? 256 : TPR; }
+
+// TPR threads hold a row in registers, NV vectors of 8 elements each.
+template <typename T, typename W, int TPR, int NV, bool QUANT>
+__global__ void __launch_bounds__(row_block<TPR>())
+norm_kernel(const T *__restrict__ x, const T *__restrict__ residual, const W *__restrict__ weight, void *__restrict__ y,
+            uint8_t *__restrict__ scales, T *__restrict__ h, float *__restrict__ rstd, const NormParams p)
+{
+    __shared__ float red[row_block<TPR>() / 64];
+    constexpr int kRowsPerBlock = row_block<TPR>() / TPR;
+    const int t = int(threadIdx.x) % TPR;
+    const int64_t row = int64_t(blockIdx.x) * kRowsPerBlock + int(threadIdx.x) / TPR;
+    if (kRowsPerBlock > 1 && row >= p.rows) return;    // whole waves: no barrier follows
+    float v[NV][8];
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * TPR + t) * 8, n = p.cols - c;
+        if (n > 0) {
+            load8(x + row * p.ldx + c, n, v[i]);
+            if (residual) {
+                float r[8];
+                load8(residual + row * p.ldr + c, n, r);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[i][e] = float(T(v[i][e] + r[e]));
+                store8(h + row * p.ldh + c, n, v[i]);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum = fmaf(v[i][e], v[i][e], sum);
+    }
+    sum = row_sum<TPR>(sum, red);
+    const float r = 1.f / sqrtf(sum / float(p.cols) + p.eps);
+    if (rstd && t == 0) rstd[row] = r;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * TPR + t) * 8, n = p.cols - c;
+        float w[8] = {};
+        if (n > 0) load8(weight + c, n, w);
+        float amax = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            v[i][e] = v[i][e] * r * w[e];
+            amax = fmaxf(amax, finite_abs(v[i][e]));
+        }
+        if constexpr (QUANT) {
+            const int e = block_scale(lanes_max<16>(amax));
+            const float s = power_of_two(254 - e);
+            if (n > 0) {
+                i32x2 q;
+                q[0] = to_fp8x4(v[i][0] * s, v[i][1] * s, v[i][2] * s, v[i][3] * s);
+                q[1] = to_fp8x4(v[i][4] * s, v[i][5] * s, v[i][6] * s, v[i][7] * s);
+                *reinterpret_cast<i32x2 *>(static_cast<uint8_t *>(y) + row * p.ldy + c) = q;
+                if ((t & 15) == 0) scales[row * p.lds + c / kScaleBlock] = uint8_t(e);
+            }
+        } else if (n > 0) {
+            store8(static_cast<T *>(y) + row * p.ldy + c, n, v[i]);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Gradient. With n = h * rstd and g = dy * weight: dx = rstd * (g - n * mean(g * n)) +
+// dh (the gradient of x and of the residual alike), dweight = sum over rows of dy * n.
+// The rounding to 8 bits counts as the identity. A block takes every `gridDim.x`-th
+// row (or group of rows) and keeps its share of dweight in registers; the shares are
+// added by a second launch, always in the same order.
+
+struct NormGradParams {
+    int64_t rows, lddy, ldh, lddh, lddx;
+    int cols;
+};
+
+template <typename T, typename W, int TPR, int NV>
+__global__ void __launch_bounds__(row_block<TPR>())
+norm_grad_kernel(const T *__restrict__ dy, const T *__restrict__ h, const W *__restrict__ weight,
+                 const float *__restrict__ rstd, const T *__restrict__ dh, T *__restrict__ dx, float *__restrict__ part,
+                 const NormGradParams p)
+{
+    constexpr int kRowsPerBlock = row_block<TPR>() / TPR;
+    __shared__ float red[row_block<TPR>() / 64];
+    const int t = int(threadIdx.x) % TPR, sub = int(threadIdx.x) / TPR;
+    float w[NV][8], dw[NV][8];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * TPR + t) * 8, n = p.cols - c;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[i][e] = dw[i][e] = 0.f;
+        if (n > 0) load8(weight + c, n, w[i]);
+    }
+    const float inv = 1.f / float(p.cols);
+    for (int64_t row = int64_t(blockIdx.x) * kRowsPerBlock + sub; row < p.rows; row += int64_t(gridDim.x) * kRowsPerBlock) {
+        const float r = rstd[row];
+        float d[NV][8], n8[NV][8];
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * TPR + t) * 8, n = p.cols - c;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) d[i][e] = n8[i][e] = 0.f;
+            if (n > 0) {
+                load8(dy + row * p.lddy + c, n, d[i]);
+                load8(h + row * p.ldh + c, n, n8[i]);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                n8[i][e] *= r;
+                dw[i][e] = fmaf(d[i][e], n8[i][e], dw[i][e]);
+                d[i][e] *= w[i][e];
+                sum = fmaf(d[i][e], n8[i][e], sum);
+            }
+        }
+        const float mean = row_sum<TPR>(sum, red) * inv;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * TPR + t) * 8, n = p.cols - c;
+            if (n <= 0) continue;
+            float o[8] = {};
+            if (dh) load8(dh + row * p.lddh + c, n, o);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = fmaf(r, d[i][e] - n8[i][e] * mean, o[e]);
+            store8(dx + row * p.lddx + c, n, o);
+        }
+    }
+    if (!part) return;
+    const int64_t base = (int64_t(blockIdx.x) * kRowsPerBlock + sub) * p.cols;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * TPR + t) * 8, n = p.cols - c;
+        if (n > 0) store8(part + base + c, n, dw[i]);
+    }
+}
+
+// dweight[c] = sum over `parts` rows of part: a block adds 64 columns, 4 threads a column.
+template <typename W>
+__global__ void __launch_bounds__(256)
+norm_grad_weight_kernel(const float *__restrict__ part, W *__restrict__ dweight, int parts, int cols)
+{
+    __shared__ float red[256];
+    const int c = int(blockIdx.x) * 64 + int(threadIdx.x & 63);
+    float sum = 0.f;
+    if (c < cols)
+        for (int i = int(threadIdx.x >> 6); i < parts; i += 4) sum += part[int64_t(i) * cols + c];
+    red[threadIdx.x] = sum;
+    __syncthreads();
+    if (threadIdx.x < 64 && c < cols) dweight[c] = W(red[threadIdx.x] + red[threadIdx.x + 64] + red[threadIdx.x + 128] + red[threadIdx.x + 192]);
+}
+
+// ---------------------------------------------------------------------------
+// Quantisers.
+
+struct QuantParams {
+    int64_t ldx, ldg, ldy, lds;
+    int cols, blocks;            // blocks of 128 in the whole tensor
+    FastDiv per_row;             // blocks of a row
+};
+
+// x, or silu(gate) * x, in 8 bits: 16 lanes per block of 128.
+template <typename T, bool GATE>
+__global__ void __launch_bounds__(256)
+quantize_kernel(const T *__restrict__ x, const T *__restrict__ gate, uint8_t *__restrict__ y, uint8_t *__restrict__ scales,
+                const QuantParams p)
+{
+    const int b = int(blockIdx.x) * 16 + int(threadIdx.x >> 4);
+    const int bc = min(b, p.blocks - 1);
+    const int64_t row = fdiv(bc, p.per_row);
+    const int blk = bc - int(row) * int(p.per_row.d);
+    const int c = blk * kScaleBlock + int(threadIdx.x & 15) * 8, n = p.cols - c;
+    float v[8] = {};
+    if (n > 0) {
+        load8(x + row * p.ldx + c, n, v);
+        if constexpr (GATE) {
+            float g[8];
+            load8(gate + row * p.ldg + c, n, g);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = g[e] / (1.f + __expf(-g[e])) * v[e];
+        }
+    }
+    float amax = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) amax = fmaxf(amax, finite_abs(v[e]));
+    const int e = block_scale(lanes_max<16>(amax));
+    if (b >= p.blocks || n <= 0) return;
+    const float s = power_of_two(254 - e);
+    i32x2 q;
+    q[0] = to_fp8x4(v[0] * s, v[1] * s, v[2] * s, v[3] * s);
+    q[1] = to_fp8x4(v[4] * s, v[5] * s, v[6] * s, v[7] * s);
+    *reinterpret_cast<i32x2 *>(y + row * p.ldy + c) = q;
+    if ((threadIdx.x & 15) == 0) scales[row * p.lds + blk] = uint8_t(e);
+}
+
+// A weight matrix in 8 bits, a scale for each 128 x 128 elements: one block each, a
+// thread 8 rows' 8 elements (rows threadIdx / 16 + 16 i).
+template <typename T>
+__global__ void __launch_bounds__(256)
+quantize_weights_kernel(const T *__restrict__ w, uint8_t *__restrict__ y, uint8_t *__restrict__ scales, int rows, int cols,
+                        int64_t ldw, int64_t ldy, int64_t lds)
+{
+    __shared__ float red[4];
+    const int c = int(blockIdx.x) * kScaleBlock + int(threadIdx.x & 15) * 8, n = cols - c;
+    const int r0 = int(blockIdx.y) * kScaleBlock + int(threadIdx.x >> 4);
+    float v[8][8];
+    float amax = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int r = r0 + 16 * i;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
+        if (r < rows && n > 0) load8(w + r * ldw + c, n, v[i]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) amax = fmaxf(amax, finite_abs(v[i][e]));
+    }
+    amax = lanes_max<64>(amax);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = amax;
+    __syncthreads();
+    const int e = block_scale(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
+    const float s = power_of_two(254 - e);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int r = r0 + 16 * i;
+        if (r >= rows || n <= 0) continue;
+        i32x2 q;
+        q[0] = to_fp8x4(v[i][0] * s, v[i][1] * s, v[i][2] * s, v[i][3] * s);
+        q[1] = to_fp8x4(v[i][4] * s, v[i][5] * s, v[i][6] * s, v[i][7] * s);
+        *reinterpret_cast<i32x2 *>(y + r * ldy + c) = q;
+    }
+    if (threadIdx.x == 0) scales[int64_t(blockIdx.y) * lds + blockIdx.x] = uint8_t(e);
+}
+
+// Shift codes as E5M2 numbers, which hold +-2^0 .. +-2^-14 and 0 exactly (2^-14 is
+// the least normal one): exponent field 15 - shift, mantissa 0. 8 codes a thread.
+__global__ void __launch_bounds__(256)
+shift_to_fp8_kernel(const uint32_t *__restrict__ wp, uint8_t *__restrict__ y, int cols, int wpr, int64_t ldy, const CodeFmt fmt)
+{
+    const int64_t row = blockIdx.y;
+    const int c = (int(blockIdx.x) * 256 + int(threadIdx.x)) * 8;
+    if (c >= cols) return;
+    uint32_t q[2] = {};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t code = c + i < cols ? fmt.at(wp + row * wpr, c + i) : 15u, sh = code & 15u;
+        const uint32_t byte = sh == 15u ? 0u : (code >> 4) << 7 | (15u - sh) << 2;
+        q[i >> 2] |= byte << (8 * (i & 3));
+    }
+    *reinterpret_cast<i32x2 *>(y + row * ldy + c) = i32x2{int(q[0]), int(q[1])};
+}
+
+// ---------------------------------------------------------------------------
+
+// Threads and vectors per row: a wave holds rows of up to 1024 elements, four waves
+// up to 16384, sixteen up to 65536.
+template <typename F>
+bool for_row_layout(int64_t cols, F &&f)
+{
+#define DS_TRY(TPR, NV) \
+    if (cols <= int64_t(TPR) * NV * 8) return f(std::integral_constant<int, TPR>{}, std::integral_constant<int, NV>{}), true
+    DS_TRY(64, 1);
+    DS_TRY(64, 2);
+    DS_TRY(256, 1);
+    DS_TRY(256, 2);
+    DS_TRY(256, 4);
+    DS_TRY(256, 8);
+    DS_TRY(1024, 4);
+    DS_TRY(1024, 8);
+#undef DS_TRY
+    return false;
+}
+constexpr int64_t kMaxCols = 65536;
+
+// f with the element type of `type`, and of weights (x's type or float32).
+template <typename F>
+void for_type(int32_t type, F &&f)
+{
+    if (type == DS_TYPE_F32) f(float{});
+    else if (type == DS_TYPE_F16) f(_Float16{});
+    else f(__bf16{});
+}
+
+template <typename F>
+void for_types(int32_t type, int32_t wtype, F &&f)
+{
+    for_type(type, [&](auto t) {
+        if (wtype == DS_TYPE_F32) f(t, float{});
+        else f(t, t);
+    });
+}
+
+ds_status check_rows(int64_t rows, int64_t cols, int32_t type)
+{
+    if (rows < 0 || cols <= 0) return fail(DS_ERR_INVALID_SHAPE, "rows must be >= 0 and cols > 0");
+    if (!float_bytes(type)) return fail(DS_ERR_INVALID_ARG, "type must be DS_TYPE_F32, DS_TYPE_F16 or DS_TYPE_BF16");
+    if (rows > kMaxElems || cols > kMaxElems || prod({std::max<int64_t>(rows, 1), cols}) > (int64_t(1) << 40))
+        return fail(DS_ERR_UNSUPPORTED, "2^31 or more rows or columns, or over 2^40 elements");
+    return DS_SUCCESS;
+}
+
+// An 8-bit matrix: rows that begin on 16 bytes (and so are readable to a multiple of 16).
+ds_status check_rows8(const void *p, int64_t cols, int64_t ld, int64_t lds, int64_t blocks)
+{
+    if (ld < (cols + 15) / 16 * 16 || ld % 16 || reinterpret_cast<uintptr_t>(p) % 16)
+        return fail(DS_ERR_INVALID_ARG, "8-bit rows must begin on 16 bytes and be a multiple of 16 apart, at least the columns");
+    if (lds < blocks) return fail(DS_ERR_INVALID_ARG, "fewer scales in a row than blocks of 128");
+    return DS_SUCCESS;
+}
+
+int64_t blocks_of(int64_t cols) { return (cols + kScaleBlock - 1) / kScaleBlock; }
+
+// Blocks of the gradient's launch, a row of dweight's shares each (times the rows that
+// a block takes at once).
+int norm_grad_blocks(int64_t rows, int64_t cols)
+{
+    const int64_t per = cols <= 1024 ? 4 : 1;
+    return int(std::min<int64_t>((rows + per - 1) / per, 512));
+}
+
+}  // namespace
+
+}  // namespace ds
+
+using namespace ds;
+
+extern "C" ds_status ds_rms_norm(const void *x, const void *residual, const void *weight, void *y, uint8_t *scales, void *h,
+                                 float *rstd, int64_t rows, int64_t cols, int64_t ldx, int64_t ldr, int64_t ldh,
+                                 int64_t ldy, int64_t lds, float eps, int32_t type, int32_t weight_type, int32_t y_type,
+                                 void *stream)
+{
+    if (rows != 0 && (!x || !weight || !y || (residual && !h)))
+        return fail(DS_ERR_NULL_POINTER, "x, weight, y (and h with a residual) must not be NULL");
+    if (rows != 0 && h && !residual) return fail(DS_ERR_INVALID_ARG, "h is written with a residual only");
+    if (ds_status st = check_rows(rows, cols, type)) return st;
+    if (cols > kMaxCols) return fail(DS_ERR_UNSUPPORTED, "more than %lld columns", (long long)kMaxCols);
+    if (weight_type != type && weight_type != DS_TYPE_F32) return fail(DS_ERR_INVALID_ARG, "weight must have x's type or float32");
+    if (y_type != type && y_type != DS_TYPE_F8E4M3) return fail(DS_ERR_INVALID_ARG, "y must have x's type or DS_TYPE_F8E4M3");
+    if (!(eps >= 0.f)) return fail(DS_ERR_INVALID_ARG, "eps must be >= 0");
+    const bool quant = y_type == DS_TYPE_F8E4M3;
+    if (ldx < cols || (residual && (ldr < cols || ldh < cols)) || (!quant && ldy < cols))
+        return fail(DS_ERR_INVALID_ARG, "a row's stride is shorter than the row");
+    if (quant) {
+        if (rows != 0 && !scales) return fail(DS_ERR_NULL_POINTER, "an 8-bit y needs scales");
+        if (ds_status st = check_rows8(y, cols, ldy, lds, blocks_of(cols))) return st;
+    }
+    if (rows == 0) return ok();
+    const int64_t es = float_bytes(type), row = cols * es;
+    if (ds_status st = check_tensors({{x, span(rows, ldx * es, row), "x", false},
+                                      {residual, span(rows, ldr * es, row), "residual", false},
+                                      {weight, cols * float_bytes(weight_type), "weight", false},
+                                      {y, quant ? span(rows, ldy, (cols + 7) / 8 * 8) : span(rows, ldy * es, row), "y", true},
+                                      {quant ? scales : nullptr, span(rows, lds, blocks_of(cols)), "scales", true},
+                                      {h, span(rows, ldh * es, row), "h", true},
+                                      {rstd, rows * 4, "rstd", true}}))
+        return st;
+    const NormParams p{rows, ldx, ldr, ldh, ldy, lds, int(cols), eps};
+    for_types(type, weight_type, [&](auto t, auto w) {
+        using T = decltype(t);
+        using W = decltype(w);
+        for_row_layout(cols, [&](auto tpr, auto nv) {
+            constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value;
+            const auto k = quant ? norm_kernel<T, W, TPR, NV, true> : norm_kernel<T, W, TPR, NV, false>;
+            constexpr int block = row_block<TPR>(), per = block / TPR;
+            hipLaunchKernelGGL(k, dim3(uint32_t((rows + per - 1) / per)), dim3(block), 0, static_cast<hipStream_t>(stream),
+                               static_cast<const T *>(x), static_cast<const T *>(residual), static_cast<const W *>(weight), y,
+                               scales, static_cast<T *>(h), rstd, p);
+        });
+    });
+    return launched("ds_rms_norm");
+}
+
+extern "C" int64_t ds_rms_norm_backward_scratch_bytes(int64_t rows, int64_t cols)
+{
+    if (rows <= 0 || cols <= 0 || cols > kMaxCols) return 0;
+    return int64_t(norm_grad_blocks(rows, cols)) * (cols <= 1024 ? 4 : 1) * cols * 4;
+}
+
+extern "C" ds_status ds_rms_norm_backward(const void *dy, const void *h, const void *weight, const float *rstd, const void *dh,
+                                          void *dx, void *dweight, int64_t rows, int64_t cols, int64_t lddy, int64_t ldh,
+                                          int64_t lddh, int64_t lddx, int32_t type, int32_t weight_type, void *scratch,
+                                          int64_t scratch_bytes, void *stream)
+{
+    if (rows != 0 && (!dy || !h || !weight || !rstd || !dx))
+        return fail(DS_ERR_NULL_POINTER, "dy, h, weight, rstd and dx must not be NULL");
+    if (ds_status st = check_rows(rows, cols, type)) return st;
+    if (cols > kMaxCols) return fail(DS_ERR_UNSUPPORTED, "more than %lld columns", (long long)kMaxCols);
+    if (weight_type != type && weight_type != DS_TYPE_F32) return fail(DS_ERR_INVALID_ARG, "weight must have dy's type or float32");
+    if (lddy < cols || ldh < cols || (dh && lddh < cols) || lddx < cols)
+        return fail(DS_ERR_INVALID_ARG, "a row's stride is shorter than the row");
+    const int64_t need = dweight ? ds_rms_norm_backward_scratch_bytes(rows, cols) : 0;
+    if (need > 0 && !scratch) return fail(DS_ERR_NULL_POINTER, "dweight needs scratch");
+    if (need > scratch_bytes) return fail(DS_ERR_BUFFER_TOO_SMALL, "scratch has %lld bytes, %lld are needed", (long long)scratch_bytes, (long long)need);
+    const int64_t es = float_bytes(type), row = cols * es;
+    if (ds_status st = check_tensors({{dy, span(rows, lddy * es, row), "dy", false},
+                                      {h, span(rows, ldh * es, row), "h", false},
+                                      {weight, cols * float_bytes(weight_type), "weight", false},
+                                      {rstd, rows * 4, "rstd", false},
+                                      {dh, span(rows, lddh * es, row), "dh", false},
+                                      {dx, span(rows, lddx * es, row), "dx", true},
+                                      {dweight, cols * float_bytes(weight_type), "dweight", true},
+                                      {need ? scratch : nullptr, need, "scratch", true}}))
+        return st;
+    const auto s = static_cast<hipStream_t>(stream);
+    const int blocks = norm_grad_blocks(rows, cols), parts = blocks * (cols <= 1024 ? 4 : 1);
+    const NormGradParams p{rows, lddy, ldh, lddh, lddx, int(cols)};
+    for_types(type, weight_type, [&](auto t, auto w) {
+        using T = decltype(t);
+        using W = decltype(w);
+        if (rows > 0)
+            for_row_layout(cols, [&](auto tpr, auto nv) {
+                constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value;
+                hipLaunchKernelGGL((norm_grad_kernel<T, W, TPR, NV>), dim3(blocks), dim3(row_block<TPR>()), 0, s,
+                                   static_cast<const T *>(dy), static_cast<const T *>(h), static_cast<const W *>(weight), rstd,
+                                   static_cast<const T *>(dh), static_cast<T *>(dx),
+                                   dweight ? static_cast<float *>(scratch) : nullptr, p);
+            });
+        if (dweight)
+            hipLaunchKernelGGL(norm_grad_weight_kernel<W>, dim3(uint32_t((cols + 63) / 64)), dim3(256), 0, s,
+                               static_cast<const float *>(scratch), static_cast<W *>(dweight), rows > 0 ? parts : 0, int(cols));
+    });
+    return launched("ds_rms_norm_backward");
+}
+
+extern "C" ds_status ds_quantize_fp8(const void *x, const void *gate, uint8_t *y, uint8_t *scales, int64_t rows, int64_t cols,
+                                     int64_t ldx, int64_t ldg, int64_t ldy, int64_t lds, int32_t type, void *stream)
+{
+    if (rows != 0 && (!x || !y || !scales)) return fail(DS_ERR_NULL_POINTER, "x, y and scales must not be NULL");
+    if (ds_status st = check_rows(rows, cols, type)) return st;
+    if (ldx < cols || (gate && ldg < cols)) return fail(DS_ERR_INVALID_ARG, "a row's stride is shorter than the row");
+    const int64_t nb = blocks_of(cols);
+    if (ds_status st = check_rows8(y, cols, ldy, lds, nb)) return st;
+    if (prod({std::max<int64_t>(rows, 1), nb}) > kMaxElems) return fail(DS_ERR_UNSUPPORTED, "2^31 or more scales");
+    if (rows == 0) return ok();
+    const int64_t es = float_bytes(type), row = cols * es;
+    if (ds_status st = check_tensors({{x, span(rows, ldx * es, row), "x", false},
+                                      {gate, span(rows, ldg * es, row), "gate", false},
+                                      {y, span(rows, ldy, (cols + 7) / 8 * 8), "y", true},
+                                      {scales, span(rows, lds, nb), "scales", true}}))
+        return st;
+    const QuantParams p{ldx, ldg, ldy, lds, int(cols), int(rows * nb), make_fastdiv(uint32_t(nb))};
+    for_type(type, [&](auto t) {
+        using T = decltype(t);
+        const auto k = gate ? quantize_kernel<T, true> : quantize_kernel<T, false>;
+        hipLaunchKernelGGL(k, dim3(uint32_t((rows * nb + 15) / 16)), dim3(256), 0, static_cast<hipStream_t>(stream),
+                           static_cast<const T *>(x), static_cast<const T *>(gate), y, scales, p);
+    });
+    return launched("ds_quantize_fp8");
+}
+
+extern "C" ds_status ds_quantize_weights_fp8(const void *w, uint8_t *w8, uint8_t *scales, int64_t rows, int64_t cols,
+                                             int64_t ldw, int64_t ldw8, int64_t lds, int32_t type, void *stream)
+{
+    if (!w || !w8 || !scales) return fail(DS_ERR_NULL_POINTER, "w, w8 and scales must not be NULL");
+    if (rows == 0) return fail(DS_ERR_INVALID_SHAPE, "rows must be > 0");
+    if (ds_status st = check_rows(rows, cols, type)) return st;
+    if (ldw < cols) return fail(DS_ERR_INVALID_ARG, "a row's stride is shorter than the row");
+    const int64_t nb = blocks_of(cols), rb = blocks_of(rows);
+    if (ds_status st = check_rows8(w8, cols, ldw8, lds, nb)) return st;
+    if (rb > 65535) return fail(DS_ERR_UNSUPPORTED, "more than 65535 x 128 rows");
+    const int64_t es = float_bytes(type);
+    if (ds_status st = check_tensors({{w, span(rows, ldw * es, cols * es), "w", false},
+                                      {w8, span(rows, ldw8, (cols + 7) / 8 * 8), "w8", true},
+                                      {scales, span(rb, lds, nb), "scales", true}}))
+        return st;
+    for_type(type, [&](auto t) {
+        using T = decltype(t);
+        hipLaunchKernelGGL(quantize_weights_kernel<T>, dim3(uint32_t(nb), uint32_t(rb)), dim3(256), 0,
+                           static_cast<hipStream_t>(stream), static_cast<const T *>(w), w8, scales, int(rows), int(cols), ldw,
+                           ldw8, lds);
+    });
+    return launched("ds_quantize_weights_fp8");
+}
+
+extern "C" ds_status ds_shift_weights_to_fp8(const uint32_t *w_packed, uint8_t *w8, int64_t rows, int64_t cols, int64_t ldw8,
+                                             uint32_t flags, void *stream)
+{
+    if (!w_packed || !w8) return fail(DS_ERR_NULL_POINTER, "w_packed and w8 must not be NULL");
+    if (rows <= 0 || cols <= 0) return fail(DS_ERR_INVALID_SHAPE, "rows and cols must be > 0");
+    if (flags & ~0xF00u) return fail(DS_ERR_INVALID_ARG, "unknown flags 0x%x", flags);
+    const int bits = flags_code_bits(flags);
+    if (bits < 0) return fail(DS_ERR_INVALID_ARG, "DS_CODE_BITS must be 2..5 (or 0 for 5)");
+    if (prod({rows, cols}) < 0 || prod({rows, cols}) > kMaxElems || rows > 65535)
+        return fail(DS_ERR_UNSUPPORTED, "2^31 or more weights, or more than 65535 rows");
+    if (ds_status st = check_rows8(w8, cols, ldw8, 0, 0)) return st;
+    const int64_t wpr = row_words_bits(cols, bits);
+    if (ds_status st = check_tensors({{w_packed, rows * wpr * 4, "w_packed", false},
+                                      {w8, span(rows, ldw8, (cols + 7) / 8 * 8), "w8", true}}))
+        return st;
+    hipLaunchKernelGGL(shift_to_fp8_kernel, dim3(uint32_t((cols + 2047) / 2048), uint32_t(rows)), dim3(256), 0,
+                       static_cast<hipStream_t>(stream), w_packed, w8, int(cols), int(wpr), ldw8, code_fmt(bits));
+    return launched("ds_shift_weights_to_fp8");
+}

@@ -2,7 +2,10 @@
 
 PyTorch provides the device memory and the stream; every computation runs in
 the HIP library. Tensors must be contiguous int32 CUDA (ROCm) tensors; packed
-weights are int32 tensors holding the uint32 words bit for bit.
+weights are int32 tensors holding the uint32 words bit for bit. The 8-bit
+operators (rms_norm .. attention_fp8) take floating-point tensors whose rows may
+be strided: float32, float16 and bfloat16, float8_e4m3fn or float8_e5m2 with
+float8_e8m0fnu scales (powers of two).
 """
 from __future__ import annotations
 
@@ -21,7 +24,9 @@ __all__ = ["DeepShiftError", "code_bits_flag", "describe_conv2d", "packed_row_wo
            "DS_JIT_RESIDUAL", "JitConv", "jit_conv_image", "conv2d_shift_backward_data",
            "linear_shift_backward_data", "describe_conv2d_backward_data", "JitConvBackwardData",
            "layer_plan", "run_layer_plan", "set_tuning", "get_tuning", "tuning", "DS_MUL_I24",
-           "JitConvMul", "jit_conv_mul_image", "DS_ACT_I16", "DS_ACT_I8", "act_bits_flag"]
+           "JitConvMul", "jit_conv_mul_image", "DS_ACT_I16", "DS_ACT_I8", "act_bits_flag",
+           "rms_norm", "rms_norm_backward", "quantize_fp8", "quantize_weights_fp8", "shift_weights_to_fp8",
+           "linear_fp8", "linear_fp8_backward_data", "kv_cache", "kv_cache_append", "attention_fp8"]
 
 DS_RELU = 1
 
@@ -770,3 +775,313 @@ class JitConvMul(JitConv):
             return 5.5 + max(self.sac / self.ROWS_SAC_PER_US, weight_bytes / 1.75e6)
         fill = nq / (-(-nq // 256) * 256)
         return (40.0 if self.linear else 25.0) + self.sac / (self.RUNTIME_SAC_PER_US * fill) + weight_bytes / 4e6
+
+
+# ---------------------------------------------------------------------------
+# 8-bit operators of a decoder layer.
+
+_TYPE = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.float8_e4m3fn: 3, torch.float8_e5m2: 4}
+_FLOATS = (torch.bfloat16, torch.float16, torch.float32)
+_E4M3, _E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+
+
+def _dev_as(t, name: str, dtypes, shape=None):
+    """t: a device tensor of one of `dtypes` and of `shape`."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a device tensor")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t
+
+
+def _rows(t, name: str, dtypes, shape=None):
+    """t as a matrix whose rows' elements are consecutive, and its row stride."""
+    _dev_as(t, name, dtypes, shape)
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have two dimensions")
+    if t.stride(1) != 1 and t.shape[1] > 1:
+        raise ValueError(f"the elements of a row of {name} must be consecutive")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _rows8(t, name: str, dtypes, shape=None):
+    """An 8-bit matrix whose rows begin on 16 bytes, and its row stride: t, or a copy laid out so."""
+    ld = _rows(t, name, dtypes, shape)
+    if ld % 16 or t.data_ptr() % 16 or ld < (t.shape[1] + 15) // 16 * 16:
+        if t.shape[0] == 1 and not t.data_ptr() % 16 and not t.shape[1] % 16:
+            return t, t.shape[1]
+        c = _empty8(t.shape[0], t.shape[1], t.dtype, t.device)
+        c.copy_(t)
+        return c, c.stride(0)
+    return t, ld
+
+
+def _empty8(rows: int, cols: int, dtype, dev):
+    """Room for an 8-bit matrix with rows on 16 bytes."""
+    pitch = (cols + 15) & -16
+    t = torch.empty((rows, pitch), dtype=dtype, device=dev)
+    return t if pitch == cols else t[:, :cols]
+
+
+def _blocks(n: int) -> int:
+    return (n + 127) // 128
+
+
+def _same_device(dev, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != dev:
+            raise ValueError(f"{name} is on {t.device}, not on {dev}")
+
+
+def rms_norm(x, weight, residual=None, eps: float = 1e-6, quantize: bool = True):
+    """Root-mean-square norm of the rows of x [rows, cols] (+ residual): (y, scales, h, rstd).
+
+    h = x + residual in x's type (x itself without a residual), rstd = 1 / sqrt(mean(h^2) + eps)
+    (float32), y = h * rstd * weight: float8_e4m3fn with `scales` [rows, ceil(cols / 128)]
+    (float8_e8m0fnu), or x's type (scales None) with quantize=False. weight: x's type or float32."""
+    ldx = _rows(x, "x", _FLOATS)
+    rows, cols = x.shape
+    dev = x.device
+    _dev_as(weight, "weight", (x.dtype, torch.float32), (cols,))
+    if weight.stride(0) != 1 and cols > 1:
+        raise ValueError("weight must be contiguous")
+    ldr, h = 0, x
+    if residual is not None:
+        ldr = _rows(residual, "residual", (x.dtype,), (rows, cols))
+        h = torch.empty((rows, cols), dtype=x.dtype, device=dev)
+    _same_device(dev, weight=weight, residual=residual)
+    scales = torch.empty((rows, _blocks(cols)), dtype=_E8M0, device=dev) if quantize else None
+    y = _empty8(rows, cols, _E4M3, dev) if quantize else torch.empty((rows, cols), dtype=x.dtype, device=dev)
+    rstd = torch.empty(rows, dtype=torch.float32, device=dev)
+    with _on(dev):
+        call("ds_rms_norm", _ptr(x), _ptr(residual), _ptr(weight), _ptr(y), _ptr(scales),
+             None if residual is None else _ptr(h), _ptr(rstd), rows, cols, ldx, ldr, cols, (cols + 15) & -16 if quantize else cols, _blocks(cols),
+             eps, _TYPE[x.dtype], _TYPE[weight.dtype], _TYPE[y.dtype], _stream(dev))
+    return y, scales, h, rstd
+
+
+def rms_norm_backward(dy, h, weight, rstd, dh=None):
+    """Gradients (dx, dweight) of rms_norm from the gradient dy of y; dx is that of x and of the
+    residual alike. h, rstd: what rms_norm returned; dh: the gradient that reaches h from elsewhere.
+    An 8-bit output's rounding counts as the identity."""
+    ldy = _rows(dy, "dy", _FLOATS)
+    rows, cols = dy.shape
+    dev = dy.device
+    ldh = _rows(h, "h", (dy.dtype,), (rows, cols))
+    lddh = 0 if dh is None else _rows(dh, "dh", (dy.dtype,), (rows, cols))
+    _dev_as(weight, "weight", (dy.dtype, torch.float32), (cols,))
+    _dev_as(rstd, "rstd", (torch.float32,), (rows,))
+    if (weight.stride(0) != 1 and cols > 1) or (rstd.stride(0) != 1 and rows > 1):
+        raise ValueError("weight and rstd must be contiguous")
+    _same_device(dev, h=h, weight=weight, rstd=rstd, dh=dh)
+    dx = torch.empty((rows, cols), dtype=dy.dtype, device=dev)
+    dw = torch.empty(cols, dtype=weight.dtype, device=dev)
+    with _on(dev):
+        scratch, size = _scratch8("ds_rms_norm_backward_scratch_bytes", (rows, cols), dev)
+        call("ds_rms_norm_backward", _ptr(dy), _ptr(h), _ptr(weight), _ptr(rstd), _ptr(dh), _ptr(dx), _ptr(dw), rows, cols,
+             ldy, ldh, lddh, cols, _TYPE[dy.dtype], _TYPE[weight.dtype], _ptr(scratch), size, _stream(dev))
+    return dx, dw
+
+
+def _scratch8(entry: str, shape, dev):
+    """A call's scratch, which it cannot do without."""
+    size = getattr(lib(), entry)(*shape)
+    return (torch.empty(size, dtype=torch.uint8, device=dev), size) if size > 0 else (None, 0)
+
+
+def quantize_fp8(x, gate=None):
+    """x [rows, cols], or silu(gate) * x, in 8 bits: (float8_e4m3fn [rows, cols], float8_e8m0fnu scales
+    [rows, ceil(cols / 128)]). A scale is the least power of two that brings its 128 elements to at most 448."""
+    ldx = _rows(x, "x", _FLOATS)
+    rows, cols = x.shape
+    dev = x.device
+    ldg = 0 if gate is None else _rows(gate, "gate", (x.dtype,), (rows, cols))
+    _same_device(dev, gate=gate)
+    y = _empty8(rows, cols, _E4M3, dev)
+    scales = torch.empty((rows, _blocks(cols)), dtype=_E8M0, device=dev)
+    with _on(dev):
+        call("ds_quantize_fp8", _ptr(x), _ptr(gate), _ptr(y), _ptr(scales), rows, cols, ldx, ldg, (cols + 15) & -16,
+             _blocks(cols), _TYPE[x.dtype], _stream(dev))
+    return y, scales
+
+
+def quantize_weights_fp8(w):
+    """A weight matrix [rows, cols] in 8 bits: (float8_e4m3fn, float8_e8m0fnu scales
+    [ceil(rows / 128), ceil(cols / 128)])."""
+    ldw = _rows(w, "w", _FLOATS)
+    rows, cols = w.shape
+    dev = w.device
+    w8 = _empty8(rows, cols, _E4M3, dev)
+    scales = torch.empty((_blocks(rows), _blocks(cols)), dtype=_E8M0, device=dev)
+    with _on(dev):
+        call("ds_quantize_weights_fp8", _ptr(w), _ptr(w8), _ptr(scales), rows, cols, ldw, (cols + 15) & -16, _blocks(cols),
+             _TYPE[w.dtype], _stream(dev))
+    return w8, scales
+
+
+def shift_weights_to_fp8(w_packed, cols: int, code_bits: int = 5):
+    """Packed shift codes [rows, words] as 8-bit weights: float8_e5m2 [rows, cols] holding each +-2^-shift and 0
+    exactly, and scales of 1."""
+    _dev_i32(w_packed, "w_packed")
+    rows, words = w_packed.shape
+    if words != packed_row_words(cols, code_bits):
+        raise ValueError(f"w_packed must have {packed_row_words(cols, code_bits)} words a row, got {words}")
+    dev = w_packed.device
+    w8 = _empty8(rows, cols, torch.float8_e5m2, dev)
+    with _on(dev):
+        call("ds_shift_weights_to_fp8", _ptr(w_packed), _ptr(w8), rows, cols, (cols + 15) & -16, code_bits_flag(code_bits),
+             _stream(dev))
+    return w8, torch.full((_blocks(rows), _blocks(cols)), 127, dtype=torch.uint8, device=dev).view(_E8M0)
+
+
+def _weights8(w8, w_scales, dev):
+    w8, ldw = _rows8(w8, "w8", (_E4M3, torch.float8_e5m2))
+    n, k = w8.shape
+    ldws = _rows(w_scales, "w_scales", (_E8M0,), (_blocks(n), _blocks(k)))
+    _same_device(dev, w8=w8, w_scales=w_scales)
+    return w8, n, k, ldw, ldws
+
+
+def linear_fp8(x8, x_scales, w8, w_scales, bias=None, out_dtype=torch.bfloat16):
+    """y [m, n] = x w^T (+ bias, float32) of 8-bit matrices: x8 [m, k] float8_e4m3fn with scales
+    [m, ceil(k / 128)] (quantize_fp8, rms_norm), w8 [n, k] float8_e4m3fn or float8_e5m2 with scales
+    [ceil(n / 128), ceil(k / 128)] (quantize_weights_fp8, shift_weights_to_fp8). 8-bit rows that do not
+    begin on 16 bytes are copied first."""
+    x8, ldx = _rows8(x8, "x8", (_E4M3,))
+    dev = x8.device
+    w8, n, k, ldw, ldws = _weights8(w8, w_scales, dev)
+    m = x8.shape[0]
+    if x8.shape[1] != k:
+        raise ValueError(f"x8 has {x8.shape[1]} columns, w8 {k}")
+    ldxs = _rows(x_scales, "x_scales", (_E8M0,), (m, _blocks(k)))
+    if bias is not None and not _dev_as(bias, "bias", (torch.float32,), (n,)).is_contiguous():
+        raise ValueError("bias must be contiguous")
+    _same_device(dev, x_scales=x_scales, bias=bias)
+    if out_dtype not in _FLOATS:
+        raise TypeError("out_dtype must be float32, float16 or bfloat16")
+    y = torch.empty((m, n), dtype=out_dtype, device=dev)
+    with _on(dev):
+        call("ds_linear_fp8", _ptr(x8), _ptr(x_scales), _ptr(w8), _ptr(w_scales), _ptr(bias), _ptr(y), m, n, k, ldx, ldxs,
+             ldw, ldws, n, _TYPE[w8.dtype], _TYPE[out_dtype], _stream(dev))
+    return y
+
+
+def linear_fp8_backward_data(dy8, dy_scales, w8, w_scales, out_dtype=torch.bfloat16):
+    """Input gradient of linear_fp8: dx [m, k] = dy w, with dy8 [m, n] float8_e4m3fn and scales
+    [m, ceil(n / 128)] (quantize_fp8 of the gradient)."""
+    dy8, lddy = _rows8(dy8, "dy8", (_E4M3,))
+    dev = dy8.device
+    w8, n, k, ldw, ldws = _weights8(w8, w_scales, dev)
+    m = dy8.shape[0]
+    if dy8.shape[1] != n:
+        raise ValueError(f"dy8 has {dy8.shape[1]} columns, w8 {n} rows")
+    ldys = _rows(dy_scales, "dy_scales", (_E8M0,), (m, _blocks(n)))
+    _same_device(dev, dy_scales=dy_scales)
+    if out_dtype not in _FLOATS:
+        raise TypeError("out_dtype must be float32, float16 or bfloat16")
+    dx = torch.empty((m, k), dtype=out_dtype, device=dev)
+    with _on(dev):
+        scratch, size = _scratch8("ds_linear_fp8_backward_data_scratch_bytes", (m, n, k), dev)
+        call("ds_linear_fp8_backward_data", _ptr(dy8), _ptr(dy_scales), _ptr(w8), _ptr(w_scales), _ptr(dx), m, n, k, lddy,
+             ldys, ldw, ldws, k, _TYPE[w8.dtype], _TYPE[out_dtype], _ptr(scratch), size, _stream(dev))
+    return dx
+
+
+def kv_cache(pages: int, heads: int, page: int, dim: int, device="cuda:0"):
+    """An empty paged 8-bit cache: (k_cache [pages, heads, page, dim], v_cache [pages, heads, dim, page],
+    k_scales [pages, heads], v_scales [pages, heads])."""
+    if page not in (16, 32, 64, 128) or dim <= 0 or dim % 16 or dim > 256 or pages <= 0 or heads <= 0:
+        raise ValueError("page must be 16, 32, 64 or 128, dim a multiple of 16 up to 256, pages and heads > 0")
+    new = lambda *s: torch.zeros(s, dtype=torch.uint8, device=device)  # noqa: E731
+    return (new(pages, heads, page, dim).view(_E4M3), new(pages, heads, dim, page).view(_E4M3),
+            new(pages, heads).view(_E8M0), new(pages, heads).view(_E8M0))
+
+
+def _check_cache(k_cache, v_cache, k_scales, v_scales, table, batch: int):
+    """(pages, heads, page, dim) of a cache and the row stride of its table."""
+    _dev_as(k_cache, "k_cache", (_E4M3,))
+    if k_cache.dim() != 4:
+        raise ValueError("k_cache must be [pages, heads, page, dim]")
+    pages, heads, page, dim = k_cache.shape
+    _dev_as(v_cache, "v_cache", (_E4M3,), (pages, heads, dim, page))
+    _dev_as(k_scales, "k_scales", (_E8M0,), (pages, heads))
+    _dev_as(v_scales, "v_scales", (_E8M0,), (pages, heads))
+    if not (k_cache.is_contiguous() and v_cache.is_contiguous() and k_scales.is_contiguous() and v_scales.is_contiguous()):
+        raise ValueError("a cache and its scales must be contiguous")
+    ldt = _rows(table, "table", (torch.int32,))
+    if table.shape[0] != batch:
+        raise ValueError(f"table has {table.shape[0]} rows for {batch} sequences")
+    return pages, heads, page, dim, ldt
+
+
+def _per_sequence(t, name: str, batch: int):
+    if t is not None and not _dev_as(t, name, (torch.int32,), (batch,)).is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _vectors(t, name: str):
+    """Element strides (sequence, token, head) of vectors [batch, tokens, heads, dim]."""
+    if t.stride(3) != 1:
+        raise ValueError(f"the elements of a vector of {name} must be consecutive")
+    return (ctypes.c_int64 * 3)(*t.stride()[:3])
+
+
+def kv_cache_append(k, v, k_cache, v_cache, k_scales, v_scales, table, start, count=None):
+    """Writes k and v [batch, tokens, heads, dim] into a paged 8-bit cache, in place: tokens 0 .. count[b] - 1
+    (all without count) at positions start[b], start[b] + 1, .. of sequence b, whose pages row b of `table`
+    [batch, columns] lists (all int32 device tensors). A page's scale grows where its new tokens need it, and
+    what it holds is rounded again. Tokens past the table, or on a page outside the cache, are dropped."""
+    _dev_as(k, "k", _FLOATS)
+    if k.dim() != 4:
+        raise ValueError("k must be [batch, tokens, heads, dim]")
+    _dev_as(v, "v", (k.dtype,), k.shape)
+    batch, tokens = k.shape[:2]
+    pages, heads, page, dim, ldt = _check_cache(k_cache, v_cache, k_scales, v_scales, table, batch)
+    if tuple(k.shape[2:]) != (heads, dim):
+        raise ValueError(f"k has heads and dim {tuple(k.shape[2:])}, the cache {(heads, dim)}")
+    _per_sequence(_required(start, "start"), "start", batch)
+    _per_sequence(count, "count", batch)
+    dev = k.device
+    _same_device(dev, v=v, k_cache=k_cache, v_cache=v_cache, k_scales=k_scales, v_scales=v_scales, table=table,
+                 start=start, count=count)
+    with _on(dev):
+        call("ds_kv_cache_append", _ptr(k), _ptr(v), _ptr(k_cache), _ptr(v_cache), _ptr(k_scales), _ptr(v_scales), _ptr(table),
+             _ptr(start), _ptr(count), batch, tokens, heads, dim, page, pages, table.shape[1], ldt, _vectors(k, "k"),
+             _vectors(v, "v"), _TYPE[k.dtype], _stream(dev))
+
+
+def _required(t, name: str):
+    if t is None:
+        raise TypeError(f"{name} must be a device tensor")
+    return t
+
+
+def attention_fp8(q, k_cache, v_cache, k_scales, v_scales, table, length, count=None, scale: float | None = None,
+                  window: int = 0):
+    """Causal attention of q [batch, tokens, query heads, dim] (float16 or bfloat16) over a paged 8-bit cache: o, of
+    q's shape and type. Sequence b has length[b] tokens in the cache, the last count[b] of them (all `tokens`
+    without count) the queries'; query head h reads head h // (query heads / heads). A query sees the keys up to
+    its own position, the last `window` of them where window > 0; one that sees none gets zeros. scale: 1 / sqrt(dim)
+    without one. table, length, count: int32 device tensors."""
+    _dev_as(q, "q", (torch.bfloat16, torch.float16))
+    if q.dim() != 4:
+        raise ValueError("q must be [batch, tokens, heads, dim]")
+    batch, tokens, hq, qdim = q.shape
+    pages, heads, page, dim, ldt = _check_cache(k_cache, v_cache, k_scales, v_scales, table, batch)
+    if qdim != dim or hq % heads:
+        raise ValueError(f"q has {hq} heads of {qdim}, the cache {heads} of {dim}")
+    _per_sequence(_required(length, "length"), "length", batch)
+    _per_sequence(count, "count", batch)
+    dev = q.device
+    _same_device(dev, k_cache=k_cache, v_cache=v_cache, k_scales=k_scales, v_scales=v_scales, table=table, length=length,
+                 count=count)
+    o = torch.empty((batch, tokens, hq, dim), dtype=q.dtype, device=dev)
+    shape = (batch, tokens, heads, hq // heads, dim, page, table.shape[1])
+    with _on(dev):
+        scratch, size = _scratch8("ds_attention_fp8_scratch_bytes", shape, dev)
+        call("ds_attention_fp8", _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(k_scales), _ptr(v_scales), _ptr(table),
+             _ptr(length), _ptr(count), _ptr(o), *shape[:6], pages, shape[6], ldt, _vectors(q, "q"), _vectors(o, "o"),
+             1 / math.sqrt(dim) if scale is None else scale, window, _TYPE[q.dtype], _ptr(scratch), size, _stream(dev))
+    return o
