@@ -135,6 +135,163 @@ linear_rows_kernel(const LinearParams p)
     }
 }
 
+// Four scale bytes of a row, of blocks b .. b + 3 (those past the last hold anything).
+__device__ __forceinline__ uint32_t scales4(const uint8_t *row, int b, int blocks)
+{
+    uint32_t v = 0;
+    if (blocks >= 4) {
+        const int at = min(b, blocks - 4);
+        __builtin_memcpy(&v, row + at, 4);
+        return v >> (8 * min(b - at, 3));
+    }
+    for (int i = 0; i < blocks; ++i) v |= uint32_t(row[i]) << (8 * i);
+    return v;
+}
+
+typedef __attribute__((address_space(3))) void *lds_ptr_t;
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const uint8_t *p, int64_t bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p), 0, int(bytes), 0x00020000);
+}
+
+// 16 bytes a lane from a buffer to LDS (the lanes' pieces one after the other).
+__device__ __forceinline__ void to_lds(__amdgpu_buffer_rsrc_t from, uint8_t *to, int lane_offset, int offset)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_ptr_t)to, 16, lane_offset, offset, 0, 0);
+}
+
+// Many rows of x: a block forms BN outputs of BM rows of y, 128 elements of the reduction
+// at a time, which go from memory to LDS without registers, one step ahead of the
+// products. A row's eight 16-byte pieces are kept in an order of its own, so that the
+// lanes of a read find theirs in different banks.
+template <typename O, int WF, int BN, int BM, int WN, int WM>
+__global__ void __launch_bounds__(64 * WN * WM)
+linear_tile_kernel(const LinearParams p, int tiles_n, int tiles_m)
+{
+    constexpr int kWaves = WN * WM, NT = BN / WN / 16, MT = BM / WM / 16;
+    constexpr int kStage = (BN + BM) * 128, kLoadsW = BN / 8 / kWaves, kLoadsX = BM / 8 / kWaves, kGroup = 8;
+    __shared__ __align__(16) uint8_t lds[2 * kStage];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), r = lane & 15, g = lane >> 4;
+    // Blocks are dealt to the 8 XCDs in turn: each takes a run of tiles, kGroup rows of
+    // tiles at a time, so that those in flight share their inputs in its L2.
+    const int tiles = tiles_n * tiles_m, share = (tiles + 7) >> 3, at = (int(blockIdx.x) & 7) * share + (int(blockIdx.x) >> 3);
+    if ((int(blockIdx.x) >> 3) >= share || at >= tiles) return;
+    const int band = at / (kGroup * tiles_n), in = at - band * kGroup * tiles_n, deep = min(kGroup, tiles_m - band * kGroup);
+    const int n0 = in / deep * BN, m0 = (band * kGroup + in % deep) * BM;
+    const int wn = wave % WN, wm = wave / WN;
+
+    const uint8_t *wbase = p.w + n0 * p.ldw, *xbase = p.x + m0 * p.ldx;
+    const int krow = (p.k + 15) & ~15;
+    const __amdgpu_buffer_rsrc_t wr = rows_rsrc(wbase, (min(BN, p.n - n0) - 1) * p.ldw + krow);
+    const __amdgpu_buffer_rsrc_t xr = rows_rsrc(xbase, (min(BM, p.m - m0) - 1) * p.ldx + krow);
+    const int ldw = int(p.ldw), ldx = int(p.ldx);
+    const int lrow = wave * 8 + (lane >> 3), piece = ((lane & 7) ^ (lrow & 7)) * 16;
+    int wv[kLoadsW], xv[kLoadsX];      // rows past the last read it instead
+#pragma unroll
+    for (int i = 0; i < kLoadsW; ++i) wv[i] = min(i * kWaves * 8 + lrow, p.n - 1 - n0) * ldw + piece;
+#pragma unroll
+    for (int i = 0; i < kLoadsX; ++i) xv[i] = min(i * kWaves * 8 + lrow, p.m - 1 - m0) * ldx + piece;
+    auto fetch = [&](int step, int buf) {
+        const int k = step * 128;
+#pragma unroll
+        for (int i = 0; i < kLoadsW; ++i)
+            to_lds(wr, lds + buf * kStage + (i * kWaves + wave) * 1024, wv[i], k);
+#pragma unroll
+        for (int i = 0; i < kLoadsX; ++i)
+            to_lds(xr, lds + buf * kStage + (BN / 8 + i * kWaves + wave) * 1024, xv[i], k);
+    };
+    // The last step of a reduction that ends inside a block of 128: through registers,
+    // with zeros past its end.
+    auto fetch_end = [&](int step, int buf) {
+        const int k = step * 128 + piece;
+        for (int i = 0; i < kLoadsW + kLoadsX; ++i) {
+            const bool w = i < kLoadsW;
+            const int row = ((w ? i : i - kLoadsW) * kWaves + wave) * 8 + (lane >> 3);
+            const uint8_t *src = w ? wbase + min(row, p.n - 1 - n0) * p.ldw : xbase + min(row, p.m - 1 - m0) * p.ldx;
+            *reinterpret_cast<i32x4 *>(lds + buf * kStage + (w ? 0 : BN * 128) + row * 128 + (lane & 7) * 16) = row16(src, k, p.k);
+        }
+    };
+    const uint8_t *xsrow[MT];
+    uint32_t xs[MT], xsn[MT], ws, wsn;
+    const uint8_t *wsrow = p.ws + int64_t((n0 + wn * NT * 16) / kScaleBlock) * p.ldws;
+    if (n0 + wn * NT * 16 >= p.n) wsrow = p.ws;
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        xsrow[t] = p.xs + min(m0 + (wm * MT + t) * 16 + r, p.m - 1) * p.ldxs;
+        xsn[t] = scales4(xsrow[t], 0, p.kblocks);
+    }
+    wsn = scales4(wsrow, 0, p.kblocks);
+    f32x4 acc[NT][MT];
+#pragma unroll
+    for (int a = 0; a < NT; ++a)
+#pragma unroll
+        for (int b = 0; b < MT; ++b) acc[a][b] = f32x4{};
+
+    const int full = p.k / 128;
+    if (full > 0) fetch(0, 0);
+    else fetch_end(0, 0);
+    const int so = r * 128 + ((2 * g) ^ (r & 7)) * 16, s1 = r * 128 + ((2 * g + 1) ^ (r & 7)) * 16;
+    for (int step = 0; step < p.kblocks; ++step) {
+        const int buf = step & 1;
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if ((step & 3) == 0) {
+#pragma unroll
+            for (int t = 0; t < MT; ++t) xs[t] = xsn[t];
+            ws = wsn;
+            if (step + 4 < p.kblocks) {
+#pragma unroll
+                for (int t = 0; t < MT; ++t) xsn[t] = scales4(xsrow[t], step + 4, p.kblocks);
+                wsn = scales4(wsrow, step + 4, p.kblocks);
+            }
+        }
+        if (step + 1 < full) fetch(step + 1, buf ^ 1);
+        else if (step + 1 < p.kblocks) fetch_end(step + 1, buf ^ 1);
+        const uint8_t *wt = lds + buf * kStage + wn * NT * 2048, *xt = lds + buf * kStage + BN * 128 + wm * MT * 2048;
+        auto frag = [&](const uint8_t *base, int t) {
+            const i32x4 a = *reinterpret_cast<const i32x4 *>(base + t * 2048 + so), b = *reinterpret_cast<const i32x4 *>(base + t * 2048 + s1);
+            return i32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+        };
+        i32x8 wf[NT];
+#pragma unroll
+        for (int a = 0; a < NT; ++a) wf[a] = frag(wt, a);
+#pragma unroll
+        for (int b = 0; b < MT; ++b) {
+            const i32x8 xf = frag(xt, b);
+#pragma unroll
+            for (int a = 0; a < NT; ++a) acc[a][b] = mma<WF, sizeof(O) == 4>(wf[a], xf, acc[a][b], int(ws & 255), int(xs[b] & 255));
+        }
+        ws >>= 8;
+#pragma unroll
+        for (int t = 0; t < MT; ++t) xs[t] >>= 8;
+    }
+#pragma unroll
+    for (int b = 0; b < MT; ++b) {
+        const int m = m0 + (wm * MT + b) * 16 + r;
+        if (m >= p.m) continue;
+#pragma unroll
+        for (int a = 0; a < NT; ++a) {
+            const int n = n0 + (wn * NT + a) * 16 + g * 4;
+            O *y = static_cast<O *>(p.y) + m * p.ldy + n;
+            f32x4 v = acc[a][b];
+            if (p.bias) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] += p.bias[min(n + i, p.n - 1)];
+            }
+            O o[4] = {O(v[0]), O(v[1]), O(v[2]), O(v[3])};
+            if (n + 4 <= p.n) {
+                __builtin_memcpy(y, o, sizeof o);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (n + i < p.n) y[i] = o[i];
+            }
+        }
+    }
+}
+
 // w8 [n][k] to [k][n] (rows of ldt bytes, filled up with zeros): 64 x 64 bytes a block.
 __global__ void __launch_bounds__(256)
 transpose8_kernel(const uint8_t *__restrict__ w, uint8_t *__restrict__ t, int n, int k, int64_t ldw, int64_t ldt)
@@ -167,14 +324,36 @@ transpose_scales_kernel(const uint8_t *__restrict__ s, uint8_t *__restrict__ t, 
     if (i < rows * cols) t[(i % cols) * rows + i / cols] = s[(i / cols) * lds + i % cols];
 }
 
+template <typename O, int WF, int BN, int BM, int WN, int WM>
+void run_tiles(const LinearParams &p, hipStream_t s)
+{
+    const int tn = (p.n + BN - 1) / BN, tm = (p.m + BM - 1) / BM;
+    hipLaunchKernelGGL((linear_tile_kernel<O, WF, BN, BM, WN, WM>), dim3(uint32_t((int64_t(tn) * tm + 7) / 8 * 8)), dim3(64 * WN * WM), 0, s, p, tn, tm);
+}
+
+template <typename O, int WF>
+void run_linear(const LinearParams &p, hipStream_t s)
+{
+    // The tiles' 32-bit offsets reach 256 rows.
+    const bool reach = p.ldx <= (1 << 22) && p.ldw <= (1 << 22);
+    if (p.m > 64 && reach) {
+        const int64_t t256 = int64_t((p.n + 255) / 256) * ((p.m + 255) / 256);
+        if constexpr (sizeof(O) == 2) {
+            if (t256 >= 192) return run_tiles<O, WF, 256, 256, 4, 2>(p, s);
+        }
+        return run_tiles<O, WF, 128, 128, 2, 2>(p, s);
+    }
+    const bool one = p.m <= 16;
+    const dim3 grid(uint32_t((p.n + 15) / 16), uint32_t((p.m + (one ? 15 : 63)) / (one ? 16 : 64)));
+    const auto k = one ? linear_rows_kernel<O, WF, 1, 8> : linear_rows_kernel<O, WF, 4, 8>;
+    hipLaunchKernelGGL(k, grid, dim3(512), 0, s, p);
+}
+
 template <typename O>
 void run_linear(const LinearParams &p, bool e5m2, hipStream_t s)
 {
-    const bool one = p.m <= 16;
-    const dim3 grid(uint32_t((p.n + 15) / 16), uint32_t((p.m + (one ? 15 : 63)) / (one ? 16 : 64)));
-    const auto k = e5m2 ? (one ? linear_rows_kernel<O, 1, 1, 8> : linear_rows_kernel<O, 1, 4, 8>)
-                        : (one ? linear_rows_kernel<O, 0, 1, 8> : linear_rows_kernel<O, 0, 4, 8>);
-    hipLaunchKernelGGL(k, grid, dim3(512), 0, s, p);
+    if (e5m2) run_linear<O, 1>(p, s);
+    else run_linear<O, 0>(p, s);
 }
 
 int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
