@@ -116,7 +116,7 @@ append_kernel(const T *__restrict__ k, const T *__restrict__ v, uint8_t *__restr
 
 // ---------------------------------------------------------------------------
 // Attention. A kv head's queries are its `rows` = tokens x group vectors, and a wave
-// handles MT x 16 of them with 64 keys at a time:
+// handles 16 of them at a time with 64 keys:
 //
 //   S^T = K Q^T (the matrix instruction's rows are keys, its columns queries), so that a
 //   lane holds 16 consecutive keys of one query;
@@ -170,49 +170,137 @@ __device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __bui
 // v if it is finite or +inf, 0 for -inf: what a row without keys subtracts.
 __device__ __forceinline__ float or_zero(float v) { return v == -__builtin_inff() ? 0.f : v; }
 
-// Block: 4 waves, the same rows, every fourth step of the block's share of the keys.
-template <typename T, int DP, int MT>
+// The weights of 64 keys for one query a lane (16 of them in this lane): s holds the
+// products, key `run` + i in [low, high) counts. The running maximum m moves only when it
+// is passed by more than 2^8, so that the sums are hardly ever rescaled: weights reach 2^8
+// at most, far inside the range of a 16-bit float.
+constexpr float kSlack = 8.f;
+
+template <typename Rescale>
+__device__ __forceinline__ void weights(f32x4 (&s)[4], float &m, float &l, float sk, float lv, float iv, bool page, int run, int low,
+                                        int high, f16x8 (&pf)[2], Rescale &&rescale)
+{
+    const bool whole = page && run >= low && run + 16 <= high;
+    float top = -__builtin_inff();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        float t = fmaf(s[i >> 2][i & 3], sk, lv);
+        if (!whole) t = page && run + i >= low && run + i < high ? t : -__builtin_inff();
+        s[i >> 2][i & 3] = t;
+        top = fmaxf(top, t);
+    }
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const bool grown = top > m + kSlack;
+    if (__any(grown)) {
+        const float mn = grown ? top : m, alpha = __builtin_amdgcn_exp2f(m - or_zero(mn));
+        m = mn;
+        l *= alpha;
+        rescale(alpha);
+    }
+    const float sub = or_zero(m);
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const float e = __builtin_amdgcn_exp2f(s[i >> 2][i & 3] - sub);
+        sum += e;
+        pf[i >> 3][i & 7] = _Float16(e);
+    }
+    l = fmaf(sum, iv, l);
+}
+
+// Bytes of the 4 keys from `key` on that lie in [low, high).
+__device__ __forceinline__ int key_mask(int key, int low, int high)
+{
+    const int upto = high - key, past = low - key;
+    uint32_t mask = upto >= 4 ? 0xffffffffu : upto <= 0 ? 0u : (1u << (8 * upto)) - 1u;
+    if (past > 0) mask &= past >= 4 ? 0u : 0xffffffffu << (8 * past);
+    return int(mask);
+}
+
+// The factors of a page's scales: of its keys' products (times the softmax scale), the
+// logarithm of its values', and one over that.
+struct PageScale {
+    float sk, lv, iv;
+};
+
+__device__ __forceinline__ PageScale page_scale(int ek, int ev, float scale)
+{
+    ek = min(max(ek, kCacheLow), kCacheHigh);
+    ev = min(max(ev, kCacheLow), kCacheHigh);
+    return PageScale{power_of_two(uint32_t(ek)) * scale, float(ev - 127), power_of_two(uint32_t(254 - ev))};
+}
+
+// What the queries of 16 rows of a kv head see.
+struct Sequence {
+    int length, count, first;
+    __device__ __forceinline__ Sequence(const AttentionParams &p, int b)
+    {
+        length = int(min(int64_t(max(p.length[b], 0)), int64_t(p.columns) << p.page_shift));
+        count = min(p.count ? max(p.count[b], 0) : p.tokens, min(p.tokens, length));
+        first = length - count;            // position of the first query
+    }
+};
+
+// A lane's query: row `row` of head h, its keys [low, high), its elements as the first
+// product's second operand.
+template <typename T, int DP>
+__device__ __forceinline__ bool load_query(const AttentionParams &p, const Sequence &seq, int b, int h, int row, int g, int &low, int &high,
+                                           typename Vec8<T>::type (&qf)[DP / 32])
+{
+    const int t = row / p.group, hq = h * p.group + row - t * p.group;
+    const bool live = row < p.rows && t < seq.count;
+    high = live ? seq.first + t + 1 : 0;
+    low = live && p.window ? max(high - p.window, 0) : 0;
+    const T *src = static_cast<const T *>(p.q) + b * p.qb + (live ? t * p.qt + hq * p.qh : 0);
+#pragma unroll
+    for (int c = 0; c < DP / 32; ++c) {
+        const int d = g * (DP / 4) + c * 8;
+        typename Vec8<T>::type x{};
+        if (live && d < p.dim) __builtin_memcpy(&x, src + d, 16);
+        qf[c] = x;
+    }
+    return live;
+}
+
+// Four of a row's results, to o or (unnormalised) to the split's part.
+template <typename T>
+__device__ __forceinline__ void store_row(const AttentionParams &p, int b, int h, int row, float *part, int d, f32x4 o, float inv)
+{
+    if (part) {
+        __builtin_memcpy(part + d, &o, 16);
+        return;
+    }
+    const int t = row / p.group, hq = h * p.group + row - t * p.group;
+    T *out = static_cast<T *>(p.o) + b * p.ob + t * p.ot + hq * p.oh + d;
+    T x[4] = {T(o[0] * inv), T(o[1] * inv), T(o[2] * inv), T(o[3] * inv)};
+    __builtin_memcpy(out, x, 8);
+}
+
+__device__ __forceinline__ float inverse(float total) { return total > 0.f ? 1.f / total : total == 0.f ? 0.f : total; }
+
+// Up to 16 queries of a kv head (tokens being decoded): a block of 4 waves takes a share of
+// the keys, each wave every fourth 64 of it straight from memory to registers, and joins
+// them at its end.
+template <typename T, int DP>
 __global__ void __launch_bounds__(256)
-attention_kernel(const AttentionParams p)
+attention_few_kernel(const AttentionParams p)
 {
     constexpr int kWaves = 4;
     constexpr int QC = DP / 32;            // chunks of 32 of the first product's contraction
     constexpr int KB = DP / 64;            // 16-byte loads of a lane's part of a key
     constexpr int DT = DP / 16;            // tiles of 16 dimensions of the second product
     typedef typename Vec8<T>::type v8;
-    __shared__ float ml[2][kWaves][MT * 16];
-    __shared__ f32x4 osum[kWaves][64];
+    __shared__ float ml[2][kWaves][16];
+    __shared__ f32x4 osum[kWaves][DT][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), r = lane & 15, g = lane >> 4;
-    const int split = int(blockIdx.x), tile = int(blockIdx.y), bh = int(blockIdx.z), b = bh / p.heads, h = bh - b * p.heads;
+    const int split = int(blockIdx.x), bh = int(blockIdx.y), b = bh / p.heads, h = bh - b * p.heads;
     const int D = p.dim, page = 1 << p.page_shift;
-    const int64_t held = int64_t(p.columns) * page;
-    const int length = int(min(int64_t(max(p.length[b], 0)), held));
-    const int count = min(p.count ? max(p.count[b], 0) : p.tokens, min(p.tokens, length));
-    const int first = length - count;      // position of the first query
-
-    // This lane's queries, one of each tile: the keys [low, high) they see.
-    v8 qf[MT][QC];
-    int low[MT], high[MT];
-    int tlo = 0x7fffffff, thi = 0;
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-        const int row = (tile * MT + mt) * 16 + r, t = row / p.group, hq = h * p.group + row - t * p.group;
-        const bool live = row < p.rows && t < count;
-        high[mt] = live ? first + t + 1 : 0;
-        low[mt] = live && p.window ? max(high[mt] - p.window, 0) : 0;
-        if (live) {
-            tlo = min(tlo, low[mt]);
-            thi = max(thi, high[mt]);
-        }
-        const T *src = static_cast<const T *>(p.q) + b * p.qb + (live ? t * p.qt + hq * p.qh : 0);
-#pragma unroll
-        for (int c = 0; c < QC; ++c) {
-            const int d = g * (DP / 4) + c * 8;
-            v8 x{};
-            if (live && d < D) __builtin_memcpy(&x, src + d, 16);
-            qf[mt][c] = x;
-        }
-    }
+    const Sequence seq(p, b);
+    v8 qf[QC];
+    int low, high;
+    const bool live = load_query<T, DP>(p, seq, b, h, r, g, low, high, qf);
+    int tlo = live ? low : 0x7fffffff, thi = high;
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) {
         tlo = min(tlo, __shfl_xor(tlo, o));
@@ -224,25 +312,20 @@ attention_kernel(const AttentionParams p)
     const int each = (s1 - s0 + p.splits - 1) / p.splits;
     const int from = s0 + split * each, to = min(s1, from + each);
 
-    f32x4 acc[MT][DT];
-    float m[MT], l[MT];
+    f32x4 acc[DT];
+    float m = -__builtin_inff(), l = 0.f;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-        m[mt] = -__builtin_inff();
-        l[mt] = 0.f;
-#pragma unroll
-        for (int d = 0; d < DT; ++d) acc[mt][d] = f32x4{};
-    }
+    for (int d = 0; d < DT; ++d) acc[d] = f32x4{};
     // Page of the 16 keys from `key` on (they share it), or -1 where there is none.
     auto page_of = [&](int key) {
         const int col = key >> p.page_shift;
         const int pid = key < thi ? p.table[b * p.ldt + col] : -1;
         return unsigned(pid) < unsigned(p.pages) ? pid : -1;
     };
+    int kp = page_of((from + wave) * kStep + (r >> 2) * 16), vp = page_of((from + wave) * kStep + g * 16);
     for (int step = from + wave; step < to; step += kWaves) {
         const int base = step * kStep;
         const int krun = base + (r >> 2) * 16, vrun = base + g * 16;
-        const int kp = page_of(krun), vp = page_of(vrun);
         const int64_t kat = (int64_t(max(kp, 0)) * p.heads + h) * page, vat = int64_t(max(vp, 0)) * p.heads + h;
         const uint8_t *krow = p.kc + (kat + (krun & (page - 1)) + (r & 3)) * D;
         const uint8_t *vrow = p.vc + (vat * D + r) * page + (vrun & (page - 1));
@@ -254,149 +337,270 @@ attention_kernel(const AttentionParams p)
                 const int d = g * (DP / 4) + i * 16;
                 kraw[t][i] = kp >= 0 && d < D ? *reinterpret_cast<const i32x4 *>(krow + t * 4 * D + d) : i32x4{};
             }
+        const int ek = p.ks[vat], ev = p.vs[vat];
 #pragma unroll
         for (int d = 0; d < DT; ++d)
             vraw[d] = vp >= 0 && d * 16 < D ? *reinterpret_cast<const i32x4 *>(vrow + d * 16 * page) : i32x4{};
-        const int ek = min(max(int(p.ks[vat]), kCacheLow), kCacheHigh), ev = min(max(int(p.vs[vat]), kCacheLow), kCacheHigh);
-        const float sk = power_of_two(uint32_t(ek)) * p.scale, lv = float(ev - 127), iv = power_of_two(uint32_t(254 - ev));
+        const bool held = vp >= 0;
+        kp = page_of(krun + kWaves * kStep);
+        vp = page_of(vrun + kWaves * kStep);
+        f32x4 s[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            s[t] = f32x4{};
+#pragma unroll
+            for (int c = 0; c < QC; ++c) s[t] = mma(widen<T>(kraw[t][c >> 1][(c & 1) * 2], kraw[t][c >> 1][(c & 1) * 2 + 1]), qf[c], s[t]);
+        }
+        const PageScale ps = page_scale(ek, ev, p.scale);
+        f16x8 pf[2];
+        weights(s, m, l, ps.sk, ps.lv, ps.iv, held, vrun, low, high, pf, [&](float alpha) {
+#pragma unroll
+            for (int d = 0; d < DT; ++d) acc[d] *= alpha;
+        });
         if (base + kStep > thi || base < tlo) {
             // Keys that no query sees may hold anything: their values count as 0.
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                const int upto = thi - vrun - 4 * w, past = tlo - vrun - 4 * w;
-                uint32_t mask = upto >= 4 ? 0xffffffffu : upto <= 0 ? 0u : (1u << (8 * upto)) - 1u;
-                if (past > 0) mask &= past >= 4 ? 0u : 0xffffffffu << (8 * past);
+                const int mask = key_mask(vrun + 4 * w, tlo, thi);
 #pragma unroll
-                for (int d = 0; d < DT; ++d) vraw[d][w] &= int(mask);
+                for (int d = 0; d < DT; ++d) vraw[d][w] &= mask;
             }
         }
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) acc[d] = mma(widen<_Float16>(vraw[d][2 * c], vraw[d][2 * c + 1]), pf[c], acc[d]);
+    }
+    // The waves' sums together: a lane's l is its own keys'.
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (g == 0) {
+        ml[0][wave][r] = m;
+        ml[1][wave][r] = l;
+    }
+    __syncthreads();
+    float top = ml[0][0][r];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, ml[0][w][r]);
+    const float sub = or_zero(top), mine = __builtin_amdgcn_exp2f(m - sub);
+    float total = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) total = fmaf(ml[1][w][r], __builtin_amdgcn_exp2f(ml[0][w][r] - sub), total);
+#pragma unroll
+    for (int d = 0; d < DT; ++d) osum[wave][d][lane] = acc[d] * mine;
+    __syncthreads();
+    if (r >= p.rows) return;
+    float *part = p.part ? p.part + ((int64_t(bh) * p.rows + r) * p.splits + split) * (D + 2) : nullptr;
+    if (part && wave == 0 && g == 0) {
+        part[D] = top;
+        part[D + 1] = total;
+    }
+    const float inv = inverse(total);
+    for (int d = wave; d < DT; d += kWaves) {
+        if (d * 16 >= D) continue;
+        f32x4 o = osum[0][d][lane];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) o += osum[w][d][lane];
+        store_row<T>(p, b, h, r, part, d * 16 + g * 4, o, inv);
+    }
+}
+
+// 16 bytes a lane from memory to LDS, one after the other.
+__device__ __forceinline__ void to_lds(const uint8_t *from, uint8_t *to)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+}
+
+// Many queries of a kv head: the block's 4 waves have MT x 16 of them each and share the
+// keys, which go from memory to LDS, 64 ahead of the products. Wave w fetches the w-th 16
+// of 64: its keys as rows whose 16-byte pieces are kept in an order of their own (no two
+// lanes of a read meet in a bank), its values as 16 keys of one dimension after the other.
+template <typename T, int DP, int MT>
+__global__ void __launch_bounds__(256, MT == 1 || DP <= 128 ? 2 : 1)
+attention_many_kernel(const AttentionParams p, int bhs)
+{
+    constexpr int kWaves = 4, QC = DP / 32, DT = DP / 16, kPieces = DP / 16;
+    constexpr int kRun = 16 * DP, kStage = 2 * kWaves * kRun;
+    typedef typename Vec8<T>::type v8;
+    __shared__ __align__(16) uint8_t lds[2 * kStage];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), r = lane & 15, g = lane >> 4;
+    // An eighth of the work to each XCD, a head's blocks together, so that they read its
+    // keys through one L2; the last rows, which see the most keys, first.
+    const int per = p.row_tiles * p.splits, blocks = bhs * per, share = (blocks + 7) >> 3;
+    const int at = (int(blockIdx.x) & 7) * share + (int(blockIdx.x) >> 3);
+    if ((int(blockIdx.x) >> 3) >= share || at >= blocks) return;
+    const int bh = at / per, rest = at - bh * per, tile = p.row_tiles - 1 - rest / p.splits, split = rest % p.splits;
+    const int b = bh / p.heads, h = bh - b * p.heads;
+    const int D = p.dim, page = 1 << p.page_shift;
+    const Sequence seq(p, b);
+    v8 qf[MT][QC];
+    int low[MT], high[MT], row[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        row[t] = ((tile * kWaves + wave) * MT + t) * 16 + r;
+        load_query<T, DP>(p, seq, b, h, row[t], g, low[t], high[t], qf[t]);
+    }
+    // The block's keys: from the first that its first query sees to its last query's own.
+    const int t0 = tile * kWaves * MT * 16 / p.group, t1 = min(((tile + 1) * kWaves * MT * 16 - 1) / p.group, seq.count - 1);
+    const int thi = t0 < seq.count ? seq.first + t1 + 1 : 0, tlo = p.window ? max(seq.first + t0 + 1 - p.window, 0) : 0;
+    const int s0 = thi > 0 ? tlo / kStep : 0, s1 = (thi + kStep - 1) / kStep;
+    const int each = (s1 - s0 + p.splits - 1) / p.splits;
+    const int from = s0 + split * each, to = min(s1, from + each);
+
+    f32x4 acc[MT][DT];
+    float m[MT], l[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        m[t] = -__builtin_inff();
+        l[t] = 0.f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) acc[t][d] = f32x4{};
+    }
+    auto page_of = [&](int key) {
+        const int pid = key < thi ? p.table[b * p.ldt + (key >> p.page_shift)] : -1;
+        return unsigned(pid) < unsigned(p.pages) ? pid : -1;
+    };
+    // 16 keys on page pid (lane group `wave`'s) to LDS.
+    auto fetch = [&](int step, int pids, int buf) {
+        const int run = step * kStep + wave * 16, pid = max(__builtin_amdgcn_readlane(pids, wave * 16), 0);
+        const int64_t at = int64_t(pid) * p.heads + h;
+        const int slot = run & (page - 1);
+        uint8_t *to = lds + buf * kStage + wave * kRun;
+        const uint8_t *k = p.kc + (at * page + slot) * D, *v = p.vc + at * D * page + slot;
+#pragma unroll
+        for (int i = 0; i < kRun / 1024; ++i) {
+            const int key = (i * 64 + lane) / kPieces, piece = ((lane % kPieces) ^ ((key & 3) | (wave & 1) << 2)) & (kPieces - 1);
+            to_lds(k + key * D + (piece * 16 < D ? piece * 16 : 0), to + i * 1024);
+        }
+#pragma unroll
+        for (int i = 0; i < kRun / 1024; ++i) {
+            const int d = i * 64 + lane;
+            to_lds(v + int64_t(d < D ? d : 0) * page, to + kWaves * kRun + i * 1024);
+        }
+    };
+    int pids = -1, next = -1, eks = 0, evs = 0;
+    if (from < to) {
+        pids = page_of(from * kStep + g * 16);
+        next = from + 1 < to ? page_of((from + 1) * kStep + g * 16) : -1;
+        fetch(from, pids, 0);
+        const int64_t at = int64_t(max(pids, 0)) * p.heads + h;
+        eks = p.ks[at];
+        evs = p.vs[at];
+    }
+    for (int step = from; step < to; ++step) {
+        const int buf = (step - from) & 1, base = step * kStep, run = base + g * 16;
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        const PageScale ps = page_scale(eks, evs, p.scale);
+        const bool held = pids >= 0;
+        if (step + 1 < to) {
+            fetch(step + 1, next, buf ^ 1);
+            pids = next;
+            const int64_t at = int64_t(max(pids, 0)) * p.heads + h;
+            eks = p.ks[at];
+            evs = p.vs[at];
+            next = step + 2 < to ? page_of(base + 2 * kStep + g * 16) : -1;
+        }
+        const uint8_t *kt = lds + buf * kStage + (r >> 2) * kRun, *vt = lds + buf * kStage + (kWaves + g) * kRun + r * 16;
         f32x4 s[MT][4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) s[mt][t] = f32x4{};
+            const uint8_t *krow = kt + (t * 4 + (r & 3)) * DP;
+            const int order = ((r & 3) | ((r >> 2) & 1) << 2) & (kPieces - 1);
 #pragma unroll
-            for (int c = 0; c < QC; ++c) {
-                const v8 kf = widen<T>(kraw[t][c >> 1][(c & 1) * 2], kraw[t][c >> 1][(c & 1) * 2 + 1]);
+            for (int c = 0; c < QC; c += 2) {
+                const i32x4 raw = *reinterpret_cast<const i32x4 *>(krow + ((g * (kPieces / 4) + c / 2) ^ order) * 16);
+                const v8 k0 = widen<T>(raw[0], raw[1]), k1 = widen<T>(raw[2], raw[3]);
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) s[mt][t] = mma(kf, qf[mt][c], s[mt][t]);
+                for (int mt = 0; mt < MT; ++mt) {
+                    s[mt][t] = mma(k0, qf[mt][c], s[mt][t]);
+                    s[mt][t] = mma(k1, qf[mt][c + 1], s[mt][t]);
+                }
             }
         }
         f16x8 pf[MT][2];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            const bool whole = vp >= 0 && vrun >= low[mt] && vrun + 16 <= high[mt];
-            float top = -__builtin_inff();
+        for (int mt = 0; mt < MT; ++mt)
+            weights(s[mt], m[mt], l[mt], ps.sk, ps.lv, ps.iv, held, run, low[mt], high[mt], pf[mt], [&](float alpha) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                float t = fmaf(s[mt][i >> 2][i & 3], sk, lv);
-                if (!whole) t = vp >= 0 && vrun + i >= low[mt] && vrun + i < high[mt] ? t : -__builtin_inff();
-                s[mt][i >> 2][i & 3] = t;
-                top = fmaxf(top, t);
+                for (int d = 0; d < DT; ++d) acc[mt][d] *= alpha;
+            });
+        const bool edge = base + kStep > thi || base < tlo;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+            i32x4 raw = *reinterpret_cast<const i32x4 *>(vt + d * 256);
+            if (edge) {
+#pragma unroll
+                for (int w = 0; w < 4; ++w) raw[w] &= held ? key_mask(run + 4 * w, tlo, thi) : 0;
             }
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float mn = fmaxf(m[mt], top), sub = or_zero(mn), alpha = __builtin_amdgcn_exp2f(m[mt] - sub);
-            m[mt] = mn;
-            float sum = 0.f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float e = __builtin_amdgcn_exp2f(s[mt][i >> 2][i & 3] - sub);
-                sum += e;
-                pf[mt][i >> 3][i & 7] = _Float16(e);
-            }
-            l[mt] = fmaf(l[mt], alpha, sum * iv);
-#pragma unroll
-            for (int d = 0; d < DT; ++d) acc[mt][d] *= alpha;
-        }
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                const f16x8 vf = widen<_Float16>(vraw[d][2 * c], vraw[d][2 * c + 1]);
+                const f16x8 vf = widen<_Float16>(raw[2 * c], raw[2 * c + 1]);
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) acc[mt][d] = mma(vf, pf[mt][c], acc[mt][d]);
             }
+        }
     }
-    // The waves' sums together: a lane's l is its own keys'.
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
         l[mt] += __shfl_xor(l[mt], 16);
         l[mt] += __shfl_xor(l[mt], 32);
-        if (g == 0) {
-            ml[0][wave][mt * 16 + r] = m[mt];
-            ml[1][wave][mt * 16 + r] = l[mt];
+        if (row[mt] >= p.rows) continue;
+        float *part = p.part ? p.part + ((int64_t(bh) * p.rows + row[mt]) * p.splits + split) * (D + 2) : nullptr;
+        if (part && g == 0) {
+            part[D] = m[mt];
+            part[D + 1] = l[mt];
         }
-    }
-    __syncthreads();
+        const float inv = inverse(l[mt]);
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-        const int row = (tile * MT + mt) * 16 + r, t = row / p.group, hq = h * p.group + row - t * p.group;
-        float top = ml[0][0][mt * 16 + r];
-#pragma unroll
-        for (int w = 1; w < kWaves; ++w) top = fmaxf(top, ml[0][w][mt * 16 + r]);
-        const float sub = or_zero(top), mine = __builtin_amdgcn_exp2f(m[mt] - sub);
-        float total = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) total = fmaf(ml[1][w][mt * 16 + r], __builtin_amdgcn_exp2f(ml[0][w][mt * 16 + r] - sub), total);
-        const float inv = total > 0.f ? 1.f / total : total == 0.f ? 0.f : total;
-        float *part = p.part + ((int64_t(bh) * p.rows + min(row, p.rows - 1)) * p.splits + split) * (D + 2);
-        if (p.part && row < p.rows && wave == 0 && g == 0) {
-            part[D] = top;
-            part[D + 1] = total;
-        }
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-            osum[wave][lane] = acc[mt][d] * mine;
-            __syncthreads();
-            if (wave == (d & (kWaves - 1)) && row < p.rows && d * 16 + g * 4 < D) {
-                f32x4 o = osum[0][lane];
-#pragma unroll
-                for (int w = 1; w < kWaves; ++w) o += osum[w][lane];
-                if (p.part) {
-                    __builtin_memcpy(part + d * 16 + g * 4, &o, 16);
-                } else {
-                    T *out = static_cast<T *>(p.o) + b * p.ob + t * p.ot + hq * p.oh + d * 16 + g * 4;
-                    T x[4] = {T(o[0] * inv), T(o[1] * inv), T(o[2] * inv), T(o[3] * inv)};
-                    __builtin_memcpy(out, x, 8);
-                }
-            }
-            __syncthreads();
-        }
+        for (int d = 0; d < DT; ++d)
+            if (d * 16 < D) store_row<T>(p, b, h, row[mt], part, d * 16 + g * 4, acc[mt][d], inv);
     }
 }
 
-// The splits of a row together: a wave per row.
-template <typename T>
+// The splits of a row together: a block of 4 waves per row, LANES lanes (4 dimensions each)
+// per split, so that 16 or 8 or 4 splits are read at once.
+template <typename T, int LANES>
 __global__ void __launch_bounds__(256)
-attention_join_kernel(const AttentionParams p, int64_t rows_of_all)
+attention_join_kernel(const AttentionParams p)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t at = int64_t(blockIdx.x) * 4 + int(threadIdx.x >> 6);
-    if (at >= rows_of_all) return;
-    const int D = p.dim;
+    constexpr int kAtOnce = 256 / LANES;
+    __shared__ float red[2][4];
+    __shared__ f32x4 sums[256];
+    const int64_t at = blockIdx.x;
+    const int D = p.dim, d = int(threadIdx.x % LANES) * 4, mine = int(threadIdx.x) / LANES;
     const float *part = p.part + at * p.splits * (D + 2);
     float top = -__builtin_inff();
-    for (int s = lane; s < p.splits; s += 64) top = fmaxf(top, part[s * (D + 2) + D]);
-    const float sub = or_zero(lanes_max<64>(top));
+    for (int s = threadIdx.x; s < p.splits; s += 256) top = fmaxf(top, part[s * (D + 2) + D]);
+    top = lanes_max<64>(top);
+    if ((threadIdx.x & 63) == 0) red[0][threadIdx.x >> 6] = top;
+    __syncthreads();
+    const float sub = or_zero(fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3])));
     float total = 0.f;
+    for (int s = threadIdx.x; s < p.splits; s += 256)
+        total = fmaf(part[s * (D + 2) + D + 1], __builtin_amdgcn_exp2f(part[s * (D + 2) + D] - sub), total);
+    total = lanes_sum<64>(total);
+    if ((threadIdx.x & 63) == 0) red[1][threadIdx.x >> 6] = total;
     f32x4 o{};
-    for (int s = 0; s < p.splits; ++s) {
-        const float *q = part + s * (D + 2), f = __builtin_amdgcn_exp2f(q[D] - sub);
-        total = fmaf(q[D + 1], f, total);
-        if (f != 0.f && lane * 4 < D) {
+    if (d < D) {
+#pragma unroll 4
+        for (int s = mine; s < p.splits; s += kAtOnce) {
+            const float f = __builtin_amdgcn_exp2f(part[s * (D + 2) + D] - sub);
             f32x4 x;
-            __builtin_memcpy(&x, q + lane * 4, 16);
+            __builtin_memcpy(&x, part + s * (D + 2) + d, 16);
             o += x * f;
         }
     }
-    const float inv = total > 0.f ? 1.f / total : total == 0.f ? 0.f : total;
+    sums[threadIdx.x] = o;
+    __syncthreads();
+    if (mine != 0 || d >= D) return;
+#pragma unroll
+    for (int i = 1; i < kAtOnce; ++i) o += sums[i * LANES + threadIdx.x];
     const int64_t bh = at / p.rows;
-    const int row = int(at - bh * p.rows), t = row / p.group, b = int(bh / p.heads), hq = int(bh - int64_t(b) * p.heads) * p.group + row - t * p.group;
-    if (lane * 4 >= D) return;
-    T *out = static_cast<T *>(p.o) + b * p.ob + t * p.ot + hq * p.oh + lane * 4;
-    T x[4] = {T(o[0] * inv), T(o[1] * inv), T(o[2] * inv), T(o[3] * inv)};
-    __builtin_memcpy(out, x, 8);
+    store_row<T>(p, int(bh / p.heads), int(bh % p.heads), int(at - bh * p.rows), nullptr, d, o, inverse(red[1][0] + red[1][1] + red[1][2] + red[1][3]));
 }
 
 bool page_ok(int64_t page) { return page == 16 || page == 32 || page == 64 || page == 128; }
@@ -415,19 +619,20 @@ ds_status check_cache(int64_t batch, int64_t tokens, int64_t heads, int64_t dim,
 }
 
 struct Plan {
-    int mt, splits, row_tiles;
+    int mt, splits, row_tiles;      // mt 0: few queries of a head
     int64_t rows;
 };
 
-// How a call is split. MT: 16 rows a wave, more where there are more rows.
+// How a call is split: over the rows first, then over the keys until there are about 512
+// blocks of at least 8 steps of 64 keys.
 Plan plan_attention(int64_t batch, int64_t tokens, int64_t heads, int64_t group, int64_t dim, int64_t columns, int64_t page)
 {
     Plan a;
     a.rows = tokens * group;
-    a.mt = a.rows <= 16 ? 1 : a.rows <= 32 || dim > 128 ? 2 : 4;
-    a.row_tiles = int((a.rows + 16 * a.mt - 1) / (16 * a.mt));
+    a.mt = a.rows <= 16 ? 0 : a.rows <= 64 || dim > 128 ? 1 : 2;
+    a.row_tiles = a.mt ? int((a.rows + 64 * a.mt - 1) / (64 * a.mt)) : 1;
     const int64_t blocks = std::max<int64_t>(batch * heads * a.row_tiles, 1), steps = (columns * page + kStep - 1) / kStep;
-    a.splits = int(std::max<int64_t>(1, std::min<int64_t>({2048 / blocks, (steps + 7) / 8, 256})));
+    a.splits = int(std::max<int64_t>(1, std::min<int64_t>({(a.mt ? 1024 : 1024) / blocks, (steps + 7) / 8, 256})));
     return a;
 }
 
@@ -439,14 +644,13 @@ int64_t part_floats(const Plan &a, int64_t batch, int64_t heads, int64_t dim)
 template <typename T, int DP>
 void run_attention(const AttentionParams &p, const Plan &a, int64_t batch, hipStream_t s)
 {
-    const dim3 grid(uint32_t(a.splits), uint32_t(a.row_tiles), uint32_t(batch * p.heads));
-    if (a.mt == 1) hipLaunchKernelGGL((attention_kernel<T, DP, 1>), grid, dim3(256), 0, s, p);
-    else if (a.mt == 2 || DP > 128) hipLaunchKernelGGL((attention_kernel<T, DP, 2>), grid, dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((attention_kernel<T, DP, (DP > 128 ? 2 : 4)>), grid, dim3(256), 0, s, p);
-    if (a.splits > 1) {
-        const int64_t rows = batch * p.heads * a.rows;
-        hipLaunchKernelGGL(attention_join_kernel<T>, dim3(uint32_t((rows + 3) / 4)), dim3(256), 0, s, p, rows);
-    }
+    const int bhs = int(batch * p.heads);
+    const dim3 many(uint32_t((int64_t(bhs) * a.row_tiles * a.splits + 7) / 8 * 8));
+    if (a.mt == 0) hipLaunchKernelGGL((attention_few_kernel<T, DP>), dim3(a.splits, bhs), dim3(256), 0, s, p);
+    else if (a.mt == 1 || DP > 128) hipLaunchKernelGGL((attention_many_kernel<T, DP, 1>), many, dim3(256), 0, s, p, bhs);
+    else hipLaunchKernelGGL((attention_many_kernel<T, DP, (DP > 128 ? 1 : 2)>), many, dim3(256), 0, s, p, bhs);
+    if (a.splits > 1)
+        hipLaunchKernelGGL((attention_join_kernel<T, DP / 4>), dim3(uint32_t(bhs * a.rows)), dim3(256), 0, s, p);
 }
 
 template <typename T>
@@ -534,7 +738,7 @@ extern "C" ds_status ds_attention_fp8(const void *q, const uint8_t *k_cache, con
     if (batch * heads > 65535) return fail(DS_ERR_UNSUPPORTED, "more than 65535 sequences times heads");
     if (group > 65535 || tokens * group > kMaxElems / 64) return fail(DS_ERR_UNSUPPORTED, "too many queries of a head");
     const Plan a = plan_attention(batch, tokens, heads, group, dim, columns, page);
-    if (a.row_tiles > 65535) return fail(DS_ERR_UNSUPPORTED, "too many queries of a head");
+    if (batch * heads * a.rows * a.splits > kMaxElems / 2) return fail(DS_ERR_UNSUPPORTED, "too many queries");
     int64_t bytes[2];
     for (int i = 0; i < 2; ++i) {
         const int64_t *s = i ? o_strides : q_strides;
