@@ -405,12 +405,6 @@ attention_few_kernel(const AttentionParams p)
     }
 }
 
-// 16 bytes a lane from memory to LDS, one after the other.
-__device__ __forceinline__ void to_lds(const uint8_t *from, uint8_t *to)
-{
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)to, 16, 0, 0);
-}
-
 // Many queries of a kv head: the block's 4 waves have MT x 16 of them each and share the
 // keys, which go from memory to LDS, 64 ahead of the products. Wave w fetches the w-th 16
 // of 64: its keys as rows whose 16-byte pieces are kept in an order of their own (no two
@@ -456,32 +450,31 @@ attention_many_kernel(const AttentionParams p, int bhs)
 #pragma unroll
         for (int d = 0; d < DT; ++d) acc[t][d] = f32x4{};
     }
-    auto page_of = [&](int key) {
-        const int pid = key < thi ? p.table[b * p.ldt + (key >> p.page_shift)] : -1;
-        return unsigned(pid) < unsigned(p.pages) ? pid : -1;
-    };
+    auto entry = [&](int key) { return key < thi ? p.table[b * p.ldt + (key >> p.page_shift)] : -1; };
+    auto on_page = [&](int pid) { return unsigned(pid) < unsigned(p.pages) ? pid : -1; };
+    const uint32_t base_lds = __builtin_amdgcn_readfirstlane(lds_address(lds));
     // 16 keys on page pid (lane group `wave`'s) to LDS.
     auto fetch = [&](int step, int pids, int buf) {
         const int run = step * kStep + wave * 16, pid = max(__builtin_amdgcn_readlane(pids, wave * 16), 0);
         const int64_t at = int64_t(pid) * p.heads + h;
         const int slot = run & (page - 1);
-        uint8_t *to = lds + buf * kStage + wave * kRun;
+        const uint32_t to = base_lds + buf * kStage + wave * kRun;
         const uint8_t *k = p.kc + (at * page + slot) * D, *v = p.vc + at * D * page + slot;
 #pragma unroll
         for (int i = 0; i < kRun / 1024; ++i) {
             const int key = (i * 64 + lane) / kPieces, piece = ((lane % kPieces) ^ ((key & 3) | (wave & 1) << 2)) & (kPieces - 1);
-            to_lds(k + key * D + (piece * 16 < D ? piece * 16 : 0), to + i * 1024);
+            to_lds16(to + i * 1024, k + key * D + (piece * 16 < D ? piece * 16 : 0));
         }
 #pragma unroll
         for (int i = 0; i < kRun / 1024; ++i) {
             const int d = i * 64 + lane;
-            to_lds(v + int64_t(d < D ? d : 0) * page, to + kWaves * kRun + i * 1024);
+            to_lds16(to + kWaves * kRun + i * 1024, v + int64_t(d < D ? d : 0) * page);
         }
     };
     int pids = -1, next = -1, eks = 0, evs = 0;
     if (from < to) {
-        pids = page_of(from * kStep + g * 16);
-        next = from + 1 < to ? page_of((from + 1) * kStep + g * 16) : -1;
+        pids = on_page(entry(from * kStep + g * 16));
+        next = from + 1 < to ? entry((from + 1) * kStep + g * 16) : -1;
         fetch(from, pids, 0);
         const int64_t at = int64_t(max(pids, 0)) * p.heads + h;
         eks = p.ks[at];
@@ -489,18 +482,17 @@ attention_many_kernel(const AttentionParams p, int bhs)
     }
     for (int step = from; step < to; ++step) {
         const int buf = (step - from) & 1, base = step * kStep, run = base + g * 16;
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
+        wait_all();
+        barrier();
         const PageScale ps = page_scale(eks, evs, p.scale);
         const bool held = pids >= 0;
         if (step + 1 < to) {
-            fetch(step + 1, next, buf ^ 1);
-            pids = next;
+            pids = on_page(next);
+            fetch(step + 1, pids, buf ^ 1);
             const int64_t at = int64_t(max(pids, 0)) * p.heads + h;
             eks = p.ks[at];
             evs = p.vs[at];
-            next = step + 2 < to ? page_of(base + 2 * kStep + g * 16) : -1;
+            next = step + 2 < to ? entry(base + 2 * kStep + g * 16) : -1;
         }
         const uint8_t *kt = lds + buf * kStage + (r >> 2) * kRun, *vt = lds + buf * kStage + (kWaves + g) * kRun + r * 16;
         f32x4 s[MT][4];

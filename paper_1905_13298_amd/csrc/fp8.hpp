@@ -120,6 +120,44 @@ __device__ __forceinline__ void store8(T *p, int n, const float (&v)[8])
     }
 }
 
+// 16 bytes a lane from memory to LDS, the lanes' pieces one after the other from `to` on
+// (an LDS address, the same in every lane). No register takes part: the data have arrived
+// behind wait_all() and, for other waves, a barrier. In assembly, since the compiler takes
+// every later read of LDS to need what such a load brings, and waits for it there.
+__device__ __forceinline__ void to_lds16(uint32_t to, const uint8_t *from)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(to), "v"(from) : "memory", "m0");
+}
+
+__device__ __forceinline__ void to_lds16(uint32_t to, __amdgpu_buffer_rsrc_t from, int lane_offset, int offset)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                 :
+                 : "s"(to), "v"(lane_offset), "s"(from), "s"(offset)
+                 : "memory", "m0");
+}
+
+__device__ __forceinline__ uint32_t lds_address(const void *p)
+{
+    return uint32_t(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void *)p));
+}
+
+// Everything that the wave has loaded and read is there.
+__device__ __forceinline__ void wait_all()
+{
+    asm volatile("" : : : "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070);      // vmcnt(0) lgkmcnt(0)
+    asm volatile("" : : : "memory");
+}
+
+// The waves' barrier, without the wait for memory that __syncthreads() implies.
+__device__ __forceinline__ void barrier()
+{
+    asm volatile("" : : : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" : : : "memory");
+}
+
 // Sum / maximum over aligned groups of N lanes (N a power of two up to 64), in every lane.
 template <int N>
 __device__ __forceinline__ float lanes_sum(float v)

@@ -135,30 +135,27 @@ linear_rows_kernel(const LinearParams p)
     }
 }
 
-// Four scale bytes of a row, of blocks b .. b + 3 (those past the last hold anything).
-__device__ __forceinline__ uint32_t scales4(const uint8_t *row, int b, int blocks)
+// Four scale bytes of a row, of blocks b .. b + 3 (those past the last hold anything): as
+// they are read, and in place once they are there.
+__device__ __forceinline__ uint32_t load_scales4(const uint8_t *row, int b, int blocks)
 {
     uint32_t v = 0;
     if (blocks >= 4) {
-        const int at = min(b, blocks - 4);
-        __builtin_memcpy(&v, row + at, 4);
-        return v >> (8 * min(b - at, 3));
+        __builtin_memcpy(&v, row + min(b, blocks - 4), 4);
+    } else {
+        for (int i = 0; i < blocks; ++i) v |= uint32_t(row[i]) << (8 * i);
     }
-    for (int i = 0; i < blocks; ++i) v |= uint32_t(row[i]) << (8 * i);
     return v;
 }
 
-typedef __attribute__((address_space(3))) void *lds_ptr_t;
+__device__ __forceinline__ uint32_t place_scales4(uint32_t v, int b, int blocks)
+{
+    return blocks >= 4 ? v >> (8 * max(b - (blocks - 4), 0)) : v;
+}
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const uint8_t *p, int64_t bytes)
 {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p), 0, int(bytes), 0x00020000);
-}
-
-// 16 bytes a lane from a buffer to LDS (the lanes' pieces one after the other).
-__device__ __forceinline__ void to_lds(__amdgpu_buffer_rsrc_t from, uint8_t *to, int lane_offset, int offset)
-{
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_ptr_t)to, 16, lane_offset, offset, 0, 0);
 }
 
 // Many rows of x: a block forms BN outputs of BM rows of y, 128 elements of the reduction
@@ -192,14 +189,15 @@ linear_tile_kernel(const LinearParams p, int tiles_n, int tiles_m)
     for (int i = 0; i < kLoadsW; ++i) wv[i] = min(i * kWaves * 8 + lrow, p.n - 1 - n0) * ldw + piece;
 #pragma unroll
     for (int i = 0; i < kLoadsX; ++i) xv[i] = min(i * kWaves * 8 + lrow, p.m - 1 - m0) * ldx + piece;
+    const uint32_t base_lds = __builtin_amdgcn_readfirstlane(lds_address(lds));
     auto fetch = [&](int step, int buf) {
         const int k = step * 128;
 #pragma unroll
         for (int i = 0; i < kLoadsW; ++i)
-            to_lds(wr, lds + buf * kStage + (i * kWaves + wave) * 1024, wv[i], k);
+            to_lds16(base_lds + buf * kStage + (i * kWaves + wave) * 1024, wr, wv[i], k);
 #pragma unroll
         for (int i = 0; i < kLoadsX; ++i)
-            to_lds(xr, lds + buf * kStage + (BN / 8 + i * kWaves + wave) * 1024, xv[i], k);
+            to_lds16(base_lds + buf * kStage + (BN / 8 + i * kWaves + wave) * 1024, xr, xv[i], k);
     };
     // The last step of a reduction that ends inside a block of 128: through registers,
     // with zeros past its end.
@@ -219,9 +217,9 @@ linear_tile_kernel(const LinearParams p, int tiles_n, int tiles_m)
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
         xsrow[t] = p.xs + min(m0 + (wm * MT + t) * 16 + r, p.m - 1) * p.ldxs;
-        xsn[t] = scales4(xsrow[t], 0, p.kblocks);
+        xsn[t] = load_scales4(xsrow[t], 0, p.kblocks);
     }
-    wsn = scales4(wsrow, 0, p.kblocks);
+    wsn = load_scales4(wsrow, 0, p.kblocks);
     f32x4 acc[NT][MT];
 #pragma unroll
     for (int a = 0; a < NT; ++a)
@@ -234,17 +232,16 @@ linear_tile_kernel(const LinearParams p, int tiles_n, int tiles_m)
     const int so = r * 128 + ((2 * g) ^ (r & 7)) * 16, s1 = r * 128 + ((2 * g + 1) ^ (r & 7)) * 16;
     for (int step = 0; step < p.kblocks; ++step) {
         const int buf = step & 1;
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
+        wait_all();
+        barrier();
         if ((step & 3) == 0) {
 #pragma unroll
-            for (int t = 0; t < MT; ++t) xs[t] = xsn[t];
-            ws = wsn;
+            for (int t = 0; t < MT; ++t) xs[t] = place_scales4(xsn[t], step, p.kblocks);
+            ws = place_scales4(wsn, step, p.kblocks);
             if (step + 4 < p.kblocks) {
 #pragma unroll
-                for (int t = 0; t < MT; ++t) xsn[t] = scales4(xsrow[t], step + 4, p.kblocks);
-                wsn = scales4(wsrow, step + 4, p.kblocks);
+                for (int t = 0; t < MT; ++t) xsn[t] = load_scales4(xsrow[t], step + 4, p.kblocks);
+                wsn = load_scales4(wsrow, step + 4, p.kblocks);
             }
         }
         if (step + 1 < full) fetch(step + 1, buf ^ 1);
