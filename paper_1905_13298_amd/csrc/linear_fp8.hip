@@ -83,7 +83,7 @@ __device__ __forceinline__ f32x4 mma(i32x8 w, i32x8 x, f32x4 c, int ws, int xs)
 #pragma unroll
         for (int i = 0; i < 4; ++i) part = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen<WF>(w, i), widen<0>(x, i), part, 0, 0, 0);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) c[i] += ldexpf(part[i], ws + xs - 254);
+        for (int i = 0; i < 4; ++i) c[i] += ldexpf(part[i], (ws & 255) + (xs & 255) - 254);
         return c;
     } else {
         return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, c, WF, 0, 0, ws, 0, xs);
@@ -163,12 +163,13 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const uint8_t *p, in
 // products. A row's eight 16-byte pieces are kept in an order of its own, so that the
 // lanes of a read find theirs in different banks.
 template <typename O, int WF, int BN, int BM, int WN, int WM>
-__global__ void __launch_bounds__(64 * WN * WM)
+__global__ void __launch_bounds__(64 * WN * WM, 1)
 linear_tile_kernel(const LinearParams p, int tiles_n, int tiles_m)
 {
     constexpr int kWaves = WN * WM, NT = BN / WN / 16, MT = BM / WM / 16;
     constexpr int kStage = (BN + BM) * 128, kLoadsW = BN / 8 / kWaves, kLoadsX = BM / 8 / kWaves, kGroup = 8;
     __shared__ __align__(16) uint8_t lds[2 * kStage];
+    __shared__ uint32_t scales[2][BM + BN / 128];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), r = lane & 15, g = lane >> 4;
     // Blocks are dealt to the 8 XCDs in turn: each takes a run of tiles, kGroup rows of
     // tiles at a time, so that those in flight share their inputs in its L2.
@@ -183,7 +184,7 @@ linear_tile_kernel(const LinearParams p, int tiles_n, int tiles_m)
     const __amdgpu_buffer_rsrc_t wr = rows_rsrc(wbase, (min(BN, p.n - n0) - 1) * p.ldw + krow);
     const __amdgpu_buffer_rsrc_t xr = rows_rsrc(xbase, (min(BM, p.m - m0) - 1) * p.ldx + krow);
     const int ldw = int(p.ldw), ldx = int(p.ldx);
-    const int lrow = wave * 8 + (lane >> 3), piece = ((lane & 7) ^ (lrow & 7)) * 16;
+    const int lrow = wave * 8 + (lane >> 3), piece = ((lane & 7) ^ ((lrow >> 1) & 7)) * 16;
     int wv[kLoadsW], xv[kLoadsX];      // rows past the last read it instead
 #pragma unroll
     for (int i = 0; i < kLoadsW; ++i) wv[i] = min(i * kWaves * 8 + lrow, p.n - 1 - n0) * ldw + piece;
@@ -203,6 +204,7 @@ linear_tile_kernel(const LinearParams p, int tiles_n, int tiles_m)
     // with zeros past its end.
     auto fetch_end = [&](int step, int buf) {
         const int k = step * 128 + piece;
+#pragma unroll 1
         for (int i = 0; i < kLoadsW + kLoadsX; ++i) {
             const bool w = i < kLoadsW;
             const int row = ((w ? i : i - kLoadsW) * kWaves + wave) * 8 + (lane >> 3);
@@ -210,16 +212,29 @@ linear_tile_kernel(const LinearParams p, int tiles_n, int tiles_m)
             *reinterpret_cast<i32x4 *>(lds + buf * kStage + (w ? 0 : BN * 128) + row * 128 + (lane & 7) * 16) = row16(src, k, p.k);
         }
     };
-    const uint8_t *xsrow[MT];
-    uint32_t xs[MT], xsn[MT], ws, wsn;
-    const uint8_t *wsrow = p.ws + int64_t((n0 + wn * NT * 16) / kScaleBlock) * p.ldws;
-    if (n0 + wn * NT * 16 >= p.n) wsrow = p.ws;
+    // The scales of four steps of the block's rows, a thread a row (of w's, by 128): read
+    // four steps ahead, in LDS from the step before their first.
+    constexpr int kScaleRows = BM + BN / 128;
+    static_assert(kScaleRows <= 2 * 64 * kWaves, "two rows a thread at most");
+    const uint8_t *srow[2];
+    uint32_t ahead4[2];
 #pragma unroll
-    for (int t = 0; t < MT; ++t) {
-        xsrow[t] = p.xs + min(m0 + (wm * MT + t) * 16 + r, p.m - 1) * p.ldxs;
-        xsn[t] = load_scales4(xsrow[t], 0, p.kblocks);
+    for (int i = 0; i < 2; ++i) {
+        const int row = int(threadIdx.x) + i * 64 * kWaves;
+        srow[i] = row < BM ? p.xs + min(m0 + row, p.m - 1) * p.ldxs : p.ws + min(n0 / 128 + row - BM, (p.n - 1) / 128) * p.ldws;
     }
-    wsn = load_scales4(wsrow, 0, p.kblocks);
+    auto scale_row = [&](int i) { return i == 0 ? kScaleRows >= 64 * kWaves || int(threadIdx.x) < kScaleRows : int(threadIdx.x) + 64 * kWaves < kScaleRows; };
+    auto fetch_scales = [&](int step) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (scale_row(i)) ahead4[i] = load_scales4(srow[i], step, p.kblocks);
+    };
+    auto keep_scales = [&](int step) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (scale_row(i)) scales[(step >> 2) & 1][threadIdx.x + i * 64 * kWaves] = place_scales4(ahead4[i], step, p.kblocks);
+    };
+    uint32_t xs[MT], ws;
     f32x4 acc[NT][MT];
 #pragma unroll
     for (int a = 0; a < NT; ++a)
@@ -227,39 +242,68 @@ linear_tile_kernel(const LinearParams p, int tiles_n, int tiles_m)
         for (int b = 0; b < MT; ++b) acc[a][b] = f32x4{};
 
     const int full = p.k / 128;
-    if (full > 0) fetch(0, 0);
-    else fetch_end(0, 0);
-    const int so = r * 128 + ((2 * g) ^ (r & 7)) * 16, s1 = r * 128 + ((2 * g + 1) ^ (r & 7)) * 16;
+    auto stage = [&](int step, int buf) {
+        if (step < full) fetch(step, buf);
+        else if (step < p.kblocks) fetch_end(step, buf);
+    };
+    fetch_scales(0);
+    stage(0, 0);
+    stage(1, 1);
+    keep_scales(0);
+    if (p.kblocks > 4) fetch_scales(4);
+    wait_all();
+    barrier();
+    const int so = r * 128 + (g ^ (r >> 1)) * 16, s1 = so ^ 64;      // pieces g and g + 4
+    auto frag = [&](const uint8_t *base, int t) {
+        const i32x4 a = *reinterpret_cast<const i32x4 *>(base + t * 2048 + so), b = *reinterpret_cast<const i32x4 *>(base + t * 2048 + s1);
+        return i32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    };
+    const uint8_t *const wt = lds + wn * NT * 2048, *const xt = lds + BN * 128 + wm * MT * 2048;
+    i32x8 wf[NT], x;
+#pragma unroll
+    for (int a = 0; a < NT; ++a) wf[a] = frag(wt, a);
+    x = frag(xt, 0);
+    // A step: rows of tiles of x one after the other, the next one's elements read ahead.
+    // Before the last row's products every element of this step has been read: one barrier
+    // says so and that the next step's have arrived. Behind it, the step after the next is
+    // sent for, and each of the last products is followed by the read of the next step's
+    // weights into the registers that it leaves.
     for (int step = 0; step < p.kblocks; ++step) {
         const int buf = step & 1;
-        wait_all();
-        barrier();
         if ((step & 3) == 0) {
+            const uint32_t *from = scales[(step >> 2) & 1];
 #pragma unroll
-            for (int t = 0; t < MT; ++t) xs[t] = place_scales4(xsn[t], step, p.kblocks);
-            ws = place_scales4(wsn, step, p.kblocks);
-            if (step + 4 < p.kblocks) {
-#pragma unroll
-                for (int t = 0; t < MT; ++t) xsn[t] = load_scales4(xsrow[t], step + 4, p.kblocks);
-                wsn = load_scales4(wsrow, step + 4, p.kblocks);
-            }
+            for (int t = 0; t < MT; ++t) xs[t] = from[(wm * MT + t) * 16 + r];
+            ws = from[BM + wn * NT / 8];
         }
-        if (step + 1 < full) fetch(step + 1, buf ^ 1);
-        else if (step + 1 < p.kblocks) fetch_end(step + 1, buf ^ 1);
-        const uint8_t *wt = lds + buf * kStage + wn * NT * 2048, *xt = lds + buf * kStage + BN * 128 + wm * MT * 2048;
-        auto frag = [&](const uint8_t *base, int t) {
-            const i32x4 a = *reinterpret_cast<const i32x4 *>(base + t * 2048 + so), b = *reinterpret_cast<const i32x4 *>(base + t * 2048 + s1);
-            return i32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-        };
-        i32x8 wf[NT];
-#pragma unroll
-        for (int a = 0; a < NT; ++a) wf[a] = frag(wt, a);
-#pragma unroll
-        for (int b = 0; b < MT; ++b) {
-            const i32x8 xf = frag(xt, b);
-#pragma unroll
-            for (int a = 0; a < NT; ++a) acc[a][b] = mma<WF, sizeof(O) == 4>(wf[a], xf, acc[a][b], int(ws & 255), int(xs[b] & 255));
+        // The next four steps' before the barrier that precedes their first.
+        if ((step & 3) == 2 && step + 2 < p.kblocks) {
+            keep_scales(step + 2);
+            if (step + 6 < p.kblocks) fetch_scales(step + 6);
         }
+        const uint8_t *const xb = xt + buf * kStage, *const wnext = wt + (buf ^ 1) * kStage;
+#pragma unroll
+        for (int b = 0; b + 1 < MT; ++b) {
+            const i32x8 ahead = frag(xb, b + 1);
+#pragma unroll
+            for (int a = 0; a < NT; ++a) acc[a][b] = mma<WF, sizeof(O) == 4>(wf[a], x, acc[a][b], int(ws), int(xs[b]));
+            x = ahead;
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (step + 1 < p.kblocks) {
+            wait_all();
+            barrier();
+            stage(step + 2, buf);
+        }
+        // (After the last step these reads are of LDS that nothing uses any more.)
+        const i32x8 ahead = frag(xt + (buf ^ 1) * kStage, 0);
+#pragma unroll
+        for (int a = 0; a < NT; ++a) {
+            acc[a][MT - 1] = mma<WF, sizeof(O) == 4>(wf[a], x, acc[a][MT - 1], int(ws), int(xs[MT - 1]));
+            wf[a] = frag(wnext, a);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        x = ahead;
         ws >>= 8;
 #pragma unroll
         for (int t = 0; t < MT; ++t) xs[t] >>= 8;
@@ -336,7 +380,7 @@ void run_linear(const LinearParams &p, hipStream_t s)
     if (p.m > 64 && reach) {
         const int64_t t256 = int64_t((p.n + 255) / 256) * ((p.m + 255) / 256);
         if constexpr (sizeof(O) == 2) {
-            if (t256 >= 192) return run_tiles<O, WF, 256, 256, 4, 2>(p, s);
+            if (t256 >= 192) return run_tiles<O, WF, 256, 256, 2, 2>(p, s);
         }
         return run_tiles<O, WF, 128, 128, 2, 2>(p, s);
     }
