@@ -143,7 +143,8 @@ struct AttentionParams {
     int64_t ldt, qb, qt, qh, ob, ot, oh;
     int columns, pages, tokens, heads, group, dim, page_shift;
     int window, splits, rows, row_tiles;
-    float scale;                 // softmax scale * log2(e)
+    float scale;                 // |softmax scale| * log2(e)
+    int negative;                // the scale is: the queries are taken with the other sign
 };
 
 template <typename T> struct Vec8;
@@ -170,55 +171,7 @@ __device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __bui
 // v if it is finite or +inf, 0 for -inf: what a row without keys subtracts.
 __device__ __forceinline__ float or_zero(float v) { return v == -__builtin_inff() ? 0.f : v; }
 
-// The weights of 64 keys for one query a lane (16 of them in this lane): s holds the
-// products, key `run` + i in [low, high) counts. The running maximum m moves only when it
-// is passed by more than 2^8, so that the sums are hardly ever rescaled: weights reach 2^8
-// at most, far inside the range of a 16-bit float.
-constexpr float kSlack = 8.f;
-
-template <typename Rescale>
-__device__ __forceinline__ void weights(f32x4 (&s)[4], float &m, float &l, float sk, float lv, float iv, bool page, int run, int low,
-                                        int high, f16x8 (&pf)[2], Rescale &&rescale)
-{
-    const bool whole = page && run >= low && run + 16 <= high;
-    float top = -__builtin_inff();
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        float t = fmaf(s[i >> 2][i & 3], sk, lv);
-        if (!whole) t = page && run + i >= low && run + i < high ? t : -__builtin_inff();
-        s[i >> 2][i & 3] = t;
-        top = fmaxf(top, t);
-    }
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
-    const bool grown = top > m + kSlack;
-    if (__any(grown)) {
-        const float mn = grown ? top : m, alpha = __builtin_amdgcn_exp2f(m - or_zero(mn));
-        m = mn;
-        l *= alpha;
-        rescale(alpha);
-    }
-    const float sub = or_zero(m);
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const float e = __builtin_amdgcn_exp2f(s[i >> 2][i & 3] - sub);
-        sum += e;
-        pf[i >> 3][i & 7] = _Float16(e);
-    }
-    l = fmaf(sum, iv, l);
-}
-
-// Bytes of the 4 keys from `key` on that lie in [low, high).
-__device__ __forceinline__ int key_mask(int key, int low, int high)
-{
-    const int upto = high - key, past = low - key;
-    uint32_t mask = upto >= 4 ? 0xffffffffu : upto <= 0 ? 0u : (1u << (8 * upto)) - 1u;
-    if (past > 0) mask &= past >= 4 ? 0u : 0xffffffffu << (8 * past);
-    return int(mask);
-}
-
-// The factors of a page's scales: of its keys' products (times the softmax scale), the
+// The factors of a page's scales: of its keys' products (times the softmax scale, > 0), the
 // logarithm of its values', and one over that.
 struct PageScale {
     float sk, lv, iv;
@@ -228,7 +181,73 @@ __device__ __forceinline__ PageScale page_scale(int ek, int ev, float scale)
 {
     ek = min(max(ek, kCacheLow), kCacheHigh);
     ev = min(max(ev, kCacheLow), kCacheHigh);
-    return PageScale{power_of_two(uint32_t(ek)) * scale, float(ev - 127), power_of_two(uint32_t(254 - ev))};
+    return PageScale{fmaxf(power_of_two(uint32_t(ek)) * scale, 0x1p-126f), float(ev - 127), power_of_two(uint32_t(254 - ev))};
+}
+
+// The weights of 64 keys for MT queries a lane (16 of the keys in this lane): s holds the
+// products, key `run` + i in [low, high) counts. With a page's factors the same for all 16,
+// and sk > 0, the largest product has the largest exponent. The running maximum m moves only
+// when it is passed by more than 2^8, so that the sums are hardly ever rescaled: weights
+// reach 2^8 at most, far inside the range of a 16-bit float. What is rare stands in two
+// branches, so that the rest may be mixed with the products around it.
+constexpr float kSlack = 8.f;
+
+template <int MT, typename Rescale>
+__device__ __forceinline__ void weights(f32x4 (&s)[MT][4], float (&m)[MT], float (&l)[MT], const PageScale &ps, bool page, int run,
+                                        const int (&low)[MT], const int (&high)[MT], f16x8 (&pf)[MT][2], Rescale &&rescale)
+{
+    bool whole = page;
+#pragma unroll
+    for (int t = 0; t < MT; ++t) whole = whole && run >= low[t] && run + 16 <= high[t];
+    if (!__all(whole)) {
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                s[t][i >> 2][i & 3] = page && run + i >= low[t] && run + i < high[t] ? s[t][i >> 2][i & 3] : -__builtin_inff();
+    }
+    float top[MT];
+    bool grown = false;
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        top[t] = s[t][0][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top[t] = fmaxf(top[t], s[t][i >> 2][i & 3]);
+        top[t] = fmaf(top[t], ps.sk, ps.lv);
+        top[t] = fmaxf(top[t], __shfl_xor(top[t], 16));
+        top[t] = fmaxf(top[t], __shfl_xor(top[t], 32));
+        grown = grown || top[t] > m[t] + kSlack;
+    }
+    if (__any(grown)) {
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            const float mn = top[t] > m[t] + kSlack ? top[t] : m[t], alpha = __builtin_amdgcn_exp2f(m[t] - or_zero(mn));
+            m[t] = mn;
+            l[t] *= alpha;
+            rescale(t, alpha);
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        const float off = ps.lv - or_zero(m[t]);
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float e = __builtin_amdgcn_exp2f(fmaf(s[t][i >> 2][i & 3], ps.sk, off));
+            sum += e;
+            pf[t][i >> 3][i & 7] = _Float16(e);
+        }
+        l[t] = fmaf(sum, ps.iv, l[t]);
+    }
+}
+
+// Bytes of the 4 keys from `key` on that lie in [low, high).
+__device__ __forceinline__ int key_mask(int key, int low, int high)
+{
+    const int upto = high - key, past = low - key;
+    uint32_t mask = upto >= 4 ? 0xffffffffu : upto <= 0 ? 0u : (1u << (8 * upto)) - 1u;
+    if (past > 0) mask &= past >= 4 ? 0u : 0xffffffffu << (8 * past);
+    return int(mask);
 }
 
 // What the queries of 16 rows of a kv head see.
@@ -243,8 +262,8 @@ struct Sequence {
 };
 
 // A lane's query: row `row` of head h, its keys [low, high), its elements as the first
-// product's second operand.
-template <typename T, int DP>
+// product's second operand (chunk c: elements c * CHUNK + g * GROUP .. + 7).
+template <typename T, int DP, int CHUNK, int GROUP>
 __device__ __forceinline__ bool load_query(const AttentionParams &p, const Sequence &seq, int b, int h, int row, int g, int &low, int &high,
                                            typename Vec8<T>::type (&qf)[DP / 32])
 {
@@ -255,10 +274,10 @@ __device__ __forceinline__ bool load_query(const AttentionParams &p, const Seque
     const T *src = static_cast<const T *>(p.q) + b * p.qb + (live ? t * p.qt + hq * p.qh : 0);
 #pragma unroll
     for (int c = 0; c < DP / 32; ++c) {
-        const int d = g * (DP / 4) + c * 8;
+        const int d = c * CHUNK + g * GROUP;
         typename Vec8<T>::type x{};
         if (live && d < p.dim) __builtin_memcpy(&x, src + d, 16);
-        qf[c] = x;
+        qf[c] = p.negative ? -x : x;
     }
     return live;
 }
@@ -298,9 +317,9 @@ attention_few_kernel(const AttentionParams p)
     const int D = p.dim, page = 1 << p.page_shift;
     const Sequence seq(p, b);
     v8 qf[QC];
-    int low, high;
-    const bool live = load_query<T, DP>(p, seq, b, h, r, g, low, high, qf);
-    int tlo = live ? low : 0x7fffffff, thi = high;
+    int low[1], high[1];
+    const bool live = load_query<T, DP, 8, DP / 4>(p, seq, b, h, r, g, low[0], high[0], qf);
+    int tlo = live ? low[0] : 0x7fffffff, thi = high[0];
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) {
         tlo = min(tlo, __shfl_xor(tlo, o));
@@ -313,7 +332,7 @@ attention_few_kernel(const AttentionParams p)
     const int from = s0 + split * each, to = min(s1, from + each);
 
     f32x4 acc[DT];
-    float m = -__builtin_inff(), l = 0.f;
+    float m[1] = {-__builtin_inff()}, l[1] = {0.f};
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] = f32x4{};
     // Page of the 16 keys from `key` on (they share it), or -1 where there is none.
@@ -344,16 +363,15 @@ attention_few_kernel(const AttentionParams p)
         const bool held = vp >= 0;
         kp = page_of(krun + kWaves * kStep);
         vp = page_of(vrun + kWaves * kStep);
-        f32x4 s[4];
+        f32x4 s[1][4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            s[t] = f32x4{};
+        for (int c = 0; c < QC; ++c)
 #pragma unroll
-            for (int c = 0; c < QC; ++c) s[t] = mma(widen<T>(kraw[t][c >> 1][(c & 1) * 2], kraw[t][c >> 1][(c & 1) * 2 + 1]), qf[c], s[t]);
-        }
+            for (int t = 0; t < 4; ++t)
+                s[0][t] = mma(widen<T>(kraw[t][c >> 1][(c & 1) * 2], kraw[t][c >> 1][(c & 1) * 2 + 1]), qf[c], c == 0 ? f32x4{} : s[0][t]);
         const PageScale ps = page_scale(ek, ev, p.scale);
-        f16x8 pf[2];
-        weights(s, m, l, ps.sk, ps.lv, ps.iv, held, vrun, low, high, pf, [&](float alpha) {
+        f16x8 pf[1][2];
+        weights<1>(s, m, l, ps, held, vrun, low, high, pf, [&](int, float alpha) {
 #pragma unroll
             for (int d = 0; d < DT; ++d) acc[d] *= alpha;
         });
@@ -367,22 +385,22 @@ attention_few_kernel(const AttentionParams p)
             }
         }
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
+        for (int c = 0; c < 2; ++c)
 #pragma unroll
-            for (int c = 0; c < 2; ++c) acc[d] = mma(widen<_Float16>(vraw[d][2 * c], vraw[d][2 * c + 1]), pf[c], acc[d]);
+            for (int d = 0; d < DT; ++d) acc[d] = mma(widen<_Float16>(vraw[d][2 * c], vraw[d][2 * c + 1]), pf[0][c], acc[d]);
     }
     // The waves' sums together: a lane's l is its own keys'.
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
+    l[0] += __shfl_xor(l[0], 16);
+    l[0] += __shfl_xor(l[0], 32);
     if (g == 0) {
-        ml[0][wave][r] = m;
-        ml[1][wave][r] = l;
+        ml[0][wave][r] = m[0];
+        ml[1][wave][r] = l[0];
     }
     __syncthreads();
     float top = ml[0][0][r];
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) top = fmaxf(top, ml[0][w][r]);
-    const float sub = or_zero(top), mine = __builtin_amdgcn_exp2f(m - sub);
+    const float sub = or_zero(top), mine = __builtin_amdgcn_exp2f(m[0] - sub);
     float total = 0.f;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) total = fmaf(ml[1][w][r], __builtin_amdgcn_exp2f(ml[0][w][r] - sub), total);
@@ -406,15 +424,16 @@ attention_few_kernel(const AttentionParams p)
 }
 
 // Many queries of a kv head: the block's 4 waves have MT x 16 of them each and share the
-// keys, which go from memory to LDS, 64 ahead of the products. Wave w fetches the w-th 16
-// of 64: its keys as rows whose 16-byte pieces are kept in an order of their own (no two
-// lanes of a read meet in a bank), its values as 16 keys of one dimension after the other.
+// keys, 64 at a time. Wave w reads the w-th 16 of them a step ahead, turns them into 16-bit
+// floats, once for the whole block, and puts them into LDS: keys as rows [key][dim], values
+// as rows [dim][key] with the 16-byte pieces of a row in an order of its own, so that the
+// lanes of a read (0-3, 12-15, 20-27 at once, and so on) meet in no bank.
 template <typename T, int DP, int MT>
-__global__ void __launch_bounds__(256, MT == 1 || DP <= 128 ? 2 : 1)
+__global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1)
 attention_many_kernel(const AttentionParams p, int bhs)
 {
-    constexpr int kWaves = 4, QC = DP / 32, DT = DP / 16, kPieces = DP / 16;
-    constexpr int kRun = 16 * DP, kStage = 2 * kWaves * kRun;
+    constexpr int kWaves = 4, QC = DP / 32, DT = DP / 16, kLoads = DP / 64;
+    constexpr int kKeys = kStep * DP * 2, kStage = 2 * kKeys;     // bytes of a step's keys, and with its values
     typedef typename Vec8<T>::type v8;
     __shared__ __align__(16) uint8_t lds[2 * kStage];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), r = lane & 15, g = lane >> 4;
@@ -429,10 +448,13 @@ attention_many_kernel(const AttentionParams p, int bhs)
     const Sequence seq(p, b);
     v8 qf[MT][QC];
     int low[MT], high[MT], row[MT];
+    bool live[MT];
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
         row[t] = ((tile * kWaves + wave) * MT + t) * 16 + r;
-        load_query<T, DP>(p, seq, b, h, row[t], g, low[t], high[t], qf[t]);
+        live[t] = load_query<T, DP, 32, 8>(p, seq, b, h, row[t], g, low[t], high[t], qf[t]);
+        // A row without a query sees every key, which costs less than no key, and is 0 in the end.
+        if (!live[t]) high[t] = 0x7fffffff;
     }
     // The block's keys: from the first that its first query sees to its last query's own.
     const int t0 = tile * kWaves * MT * 16 / p.group, t1 = min(((tile + 1) * kWaves * MT * 16 - 1) / p.group, seq.count - 1);
@@ -450,97 +472,113 @@ attention_many_kernel(const AttentionParams p, int bhs)
 #pragma unroll
         for (int d = 0; d < DT; ++d) acc[t][d] = f32x4{};
     }
-    auto entry = [&](int key) { return key < thi ? p.table[b * p.ldt + (key >> p.page_shift)] : -1; };
+    // The table's entry of a lane group's 16 keys of a step; a page of the cache or -1.
+    auto entry = [&](int step) {
+        const int key = step * kStep + g * 16;
+        return step < to && key < thi ? p.table[b * p.ldt + (key >> p.page_shift)] : -1;
+    };
     auto on_page = [&](int pid) { return unsigned(pid) < unsigned(p.pages) ? pid : -1; };
-    const uint32_t base_lds = __builtin_amdgcn_readfirstlane(lds_address(lds));
-    // 16 keys on page pid (lane group `wave`'s) to LDS.
-    auto fetch = [&](int step, int pids, int buf) {
-        const int run = step * kStep + wave * 16, pid = max(__builtin_amdgcn_readlane(pids, wave * 16), 0);
-        const int64_t at = int64_t(pid) * p.heads + h;
-        const int slot = run & (page - 1);
-        const uint32_t to = base_lds + buf * kStage + wave * kRun;
+    i32x4 kraw[kLoads], vraw[kLoads];
+    // This wave's 16 keys of a step, from the page of lane group `wave`: dimension `lane` of
+    // the values, and of the keys a piece of 16 dimensions of one key.
+    auto fetch = [&](int step, int pids) {
+        const int pid = __builtin_amdgcn_readlane(pids, wave * 16), run = step * kStep + wave * 16, slot = run & (page - 1);
+        const int64_t at = int64_t(max(pid, 0)) * p.heads + h;
         const uint8_t *k = p.kc + (at * page + slot) * D, *v = p.vc + at * D * page + slot;
 #pragma unroll
-        for (int i = 0; i < kRun / 1024; ++i) {
-            const int key = (i * 64 + lane) / kPieces, piece = ((lane % kPieces) ^ ((key & 3) | (wave & 1) << 2)) & (kPieces - 1);
-            to_lds16(to + i * 1024, k + key * D + (piece * 16 < D ? piece * 16 : 0));
-        }
-#pragma unroll
-        for (int i = 0; i < kRun / 1024; ++i) {
-            const int d = i * 64 + lane;
-            to_lds16(to + kWaves * kRun + i * 1024, v + int64_t(d < D ? d : 0) * page);
+        for (int i = 0; i < kLoads; ++i) {
+            const int key = (i * 64 + lane) / DT, d = (lane % DT) * 16, vd = i * 64 + lane;
+            kraw[i] = pid >= 0 && d < D ? *reinterpret_cast<const i32x4 *>(k + key * D + d) : i32x4{};
+            vraw[i] = pid >= 0 && vd < D ? *reinterpret_cast<const i32x4 *>(v + int64_t(vd) * page) : i32x4{};
         }
     };
-    int pids = -1, next = -1, eks = 0, evs = 0;
+    // The order of a key's pieces, from its number in 64: the keys of a read differ in the
+    // last two bits and the first two. Rows of 128 bytes share a bank row by twos.
+    auto order = [](int key) { return ((key & 3) | (key >> 4) << 2) >> (DP < 128 ? 1 : 0); };
+    auto put = [&](int step, int buf) {
+        const int run = step * kStep + wave * 16;
+        uint8_t *const ks = lds + buf * kStage, *const vs = ks + kKeys;
+        if (run + 16 > thi || run < tlo) {
+            // Keys that no query sees may hold anything: their values count as 0.
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const int mask = key_mask(run + 4 * w, tlo, thi);
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) vraw[i][w] &= mask;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int key = wave * 16 + (i * 64 + lane) / DT, piece = (lane % DT) * 2, d = i * 64 + lane;
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                *reinterpret_cast<v8 *>(ks + key * DP * 2 + ((piece + c) ^ order(key)) * 16) = widen<T>(kraw[i][2 * c], kraw[i][2 * c + 1]);
+                *reinterpret_cast<f16x8 *>(vs + d * 128 + ((c * 4 + wave) ^ ((d >> 1) & 7)) * 16) = widen<_Float16>(vraw[i][2 * c], vraw[i][2 * c + 1]);
+            }
+        }
+    };
+    int pids = -1, next = -1, ek = 0, ev = 0;
     if (from < to) {
-        pids = on_page(entry(from * kStep + g * 16));
-        next = from + 1 < to ? entry((from + 1) * kStep + g * 16) : -1;
-        fetch(from, pids, 0);
+        pids = on_page(entry(from));
+        next = entry(from + 1);
         const int64_t at = int64_t(max(pids, 0)) * p.heads + h;
-        eks = p.ks[at];
-        evs = p.vs[at];
+        ek = p.ks[at];
+        ev = p.vs[at];
+        fetch(from, pids);
+        put(from, 0);
     }
+    const int korder = order((r >> 2) * 16 + (r & 3));
     for (int step = from; step < to; ++step) {
-        const int buf = (step - from) & 1, base = step * kStep, run = base + g * 16;
-        wait_all();
+        const int buf = (step - from) & 1, run = step * kStep + g * 16;
+        wait_lds();
         barrier();
-        const PageScale ps = page_scale(eks, evs, p.scale);
+        const PageScale ps = page_scale(ek, ev, p.scale);
         const bool held = pids >= 0;
         if (step + 1 < to) {
             pids = on_page(next);
-            fetch(step + 1, pids, buf ^ 1);
+            fetch(step + 1, pids);
             const int64_t at = int64_t(max(pids, 0)) * p.heads + h;
-            eks = p.ks[at];
-            evs = p.vs[at];
-            next = step + 2 < to ? entry(base + 2 * kStep + g * 16) : -1;
+            ek = p.ks[at];
+            ev = p.vs[at];
+            next = entry(step + 2);
         }
-        const uint8_t *kt = lds + buf * kStage + (r >> 2) * kRun, *vt = lds + buf * kStage + (kWaves + g) * kRun + r * 16;
+        const uint8_t *const kt = lds + buf * kStage + ((r >> 2) * 16 + (r & 3)) * DP * 2, *const vt = lds + buf * kStage + kKeys + r * 128;
+        // (Products into the same sum stand apart: one takes as long as two follow each other.)
         f32x4 s[MT][4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
+        for (int c = 0; c < QC; ++c)
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) s[mt][t] = f32x4{};
-            const uint8_t *krow = kt + (t * 4 + (r & 3)) * DP;
-            const int order = ((r & 3) | ((r >> 2) & 1) << 2) & (kPieces - 1);
+            for (int t = 0; t < 4; ++t) {
+                const v8 kf = *reinterpret_cast<const v8 *>(kt + t * 4 * DP * 2 + ((c * 4 + g) ^ korder) * 16);
 #pragma unroll
-            for (int c = 0; c < QC; c += 2) {
-                const i32x4 raw = *reinterpret_cast<const i32x4 *>(krow + ((g * (kPieces / 4) + c / 2) ^ order) * 16);
-                const v8 k0 = widen<T>(raw[0], raw[1]), k1 = widen<T>(raw[2], raw[3]);
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    s[mt][t] = mma(k0, qf[mt][c], s[mt][t]);
-                    s[mt][t] = mma(k1, qf[mt][c + 1], s[mt][t]);
-                }
+                for (int mt = 0; mt < MT; ++mt) s[mt][t] = mma(kf, qf[mt][c], c == 0 ? f32x4{} : s[mt][t]);
             }
-        }
         f16x8 pf[MT][2];
+        weights<MT>(s, m, l, ps, held, run, low, high, pf, [&](int mt, float alpha) {
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-            weights(s[mt], m[mt], l[mt], ps.sk, ps.lv, ps.iv, held, run, low[mt], high[mt], pf[mt], [&](float alpha) {
+            for (int d = 0; d < DT; ++d) acc[mt][d] *= alpha;
+        });
 #pragma unroll
-                for (int d = 0; d < DT; ++d) acc[mt][d] *= alpha;
-            });
-        const bool edge = base + kStep > thi || base < tlo;
+        for (int c = 0; c < 2; ++c)
 #pragma unroll
-        for (int d = 0; d < DT; ++d) {
-            i32x4 raw = *reinterpret_cast<const i32x4 *>(vt + d * 256);
-            if (edge) {
-#pragma unroll
-                for (int w = 0; w < 4; ++w) raw[w] &= held ? key_mask(run + 4 * w, tlo, thi) : 0;
-            }
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const f16x8 vf = widen<_Float16>(raw[2 * c], raw[2 * c + 1]);
+            for (int d = 0; d < DT; ++d) {
+                const f16x8 vf = *reinterpret_cast<const f16x8 *>(vt + d * 16 * 128 + ((c * 4 + g) ^ ((r >> 1) & 7)) * 16);
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) acc[mt][d] = mma(vf, pf[mt][c], acc[mt][d]);
             }
-        }
+        if (step + 1 < to) put(step + 1, buf ^ 1);
     }
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
         l[mt] += __shfl_xor(l[mt], 16);
         l[mt] += __shfl_xor(l[mt], 32);
         if (row[mt] >= p.rows) continue;
+        if (!live[mt]) {
+            m[mt] = -__builtin_inff();
+            l[mt] = 0.f;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) acc[mt][d] = f32x4{};
+        }
         float *part = p.part ? p.part + ((int64_t(bh) * p.rows + row[mt]) * p.splits + split) * (D + 2) : nullptr;
         if (part && g == 0) {
             part[D] = m[mt];
@@ -624,7 +662,7 @@ Plan plan_attention(int64_t batch, int64_t tokens, int64_t heads, int64_t group,
     a.mt = a.rows <= 16 ? 0 : a.rows <= 64 || dim > 128 ? 1 : 2;
     a.row_tiles = a.mt ? int((a.rows + 64 * a.mt - 1) / (64 * a.mt)) : 1;
     const int64_t blocks = std::max<int64_t>(batch * heads * a.row_tiles, 1), steps = (columns * page + kStep - 1) / kStep;
-    a.splits = int(std::max<int64_t>(1, std::min<int64_t>({(a.mt ? 1024 : 1024) / blocks, (steps + 7) / 8, 256})));
+    a.splits = int(std::max<int64_t>(1, std::min<int64_t>({(a.mt ? 512 : 1024) / blocks, (steps + 7) / 8, 256})));
     return a;
 }
 
@@ -752,7 +790,7 @@ extern "C" ds_status ds_attention_fp8(const void *q, const uint8_t *k_cache, con
                             need ? static_cast<float *>(scratch) : nullptr, ldt, q_strides[0], q_strides[1], q_strides[2],
                             o_strides[0], o_strides[1], o_strides[2], int(columns), int(pages), int(tokens), int(heads),
                             int(group), int(dim), shift, int(window), a.splits, int(a.rows), a.row_tiles,
-                            scale * 1.44269504f};
+                            std::fabs(scale) * 1.44269504f, scale < 0};
     const auto s = static_cast<hipStream_t>(stream);
     if (type == DS_TYPE_F16) run_attention<_Float16>(p, a, batch, s);
     else run_attention<__bf16>(p, a, batch, s);

@@ -120,15 +120,10 @@ __device__ __forceinline__ void store8(T *p, int n, const float (&v)[8])
     }
 }
 
-// 16 bytes a lane from memory to LDS, the lanes' pieces one after the other from `to` on
+// 16 bytes a lane from a buffer to LDS, the lanes' pieces one after the other from `to` on
 // (an LDS address, the same in every lane). No register takes part: the data have arrived
 // behind wait_all() and, for other waves, a barrier. In assembly, since the compiler takes
 // every later read of LDS to need what such a load brings, and waits for it there.
-__device__ __forceinline__ void to_lds16(uint32_t to, const uint8_t *from)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(to), "v"(from) : "memory", "m0");
-}
-
 __device__ __forceinline__ void to_lds16(uint32_t to, __amdgpu_buffer_rsrc_t from, int lane_offset, int offset)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
@@ -147,6 +142,14 @@ __device__ __forceinline__ void wait_all()
 {
     asm volatile("" : : : "memory");
     __builtin_amdgcn_s_waitcnt(0x0070);      // vmcnt(0) lgkmcnt(0)
+    asm volatile("" : : : "memory");
+}
+
+// What the wave has written to LDS is there; loads from memory may be on their way.
+__device__ __forceinline__ void wait_lds()
+{
+    asm volatile("" : : : "memory");
+    __builtin_amdgcn_s_waitcnt(0xc07f);      // lgkmcnt(0)
     asm volatile("" : : : "memory");
 }
 
