@@ -168,6 +168,9 @@ __device__ __forceinline__ typename Vec8<T>::type widen(int lo, int hi)
 __device__ __forceinline__ f32x4 mma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
+__device__ __forceinline__ f32x16 mma32(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mma32(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+
 // v if it is finite or +inf, 0 for -inf: what a row without keys subtracts.
 __device__ __forceinline__ float or_zero(float v) { return v == -__builtin_inff() ? 0.f : v; }
 
@@ -184,61 +187,53 @@ __device__ __forceinline__ PageScale page_scale(int ek, int ev, float scale)
     return PageScale{fmaxf(power_of_two(uint32_t(ek)) * scale, 0x1p-126f), float(ev - 127), power_of_two(uint32_t(254 - ev))};
 }
 
-// The weights of 64 keys for MT queries a lane (16 of the keys in this lane): s holds the
-// products, key `run` + i in [low, high) counts. With a page's factors the same for all 16,
-// and sk > 0, the largest product has the largest exponent. The running maximum m moves only
-// when it is passed by more than 2^8, so that the sums are hardly ever rescaled: weights
-// reach 2^8 at most, far inside the range of a 16-bit float. What is rare stands in two
-// branches, so that the rest may be mixed with the products around it.
+// The running maximum m of a row moves only when it is passed by more than 2^8, so that the
+// sums are hardly ever rescaled: weights reach 2^8 at most, far inside the range of a 16-bit
+// float.
 constexpr float kSlack = 8.f;
 
-template <int MT, typename Rescale>
-__device__ __forceinline__ void weights(f32x4 (&s)[MT][4], float (&m)[MT], float (&l)[MT], const PageScale &ps, bool page, int run,
-                                        const int (&low)[MT], const int (&high)[MT], f16x8 (&pf)[MT][2], Rescale &&rescale)
+// A row's maximum and sum once `top` is known, and the factor of its sums (rescale): in a
+// branch that is rarely taken.
+template <typename Rescale>
+__device__ __forceinline__ void raise(float &m, float &l, float top, Rescale &&rescale)
 {
-    bool whole = page;
-#pragma unroll
-    for (int t = 0; t < MT; ++t) whole = whole && run >= low[t] && run + 16 <= high[t];
-    if (!__all(whole)) {
-#pragma unroll
-        for (int t = 0; t < MT; ++t)
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                s[t][i >> 2][i & 3] = page && run + i >= low[t] && run + i < high[t] ? s[t][i >> 2][i & 3] : -__builtin_inff();
-    }
-    float top[MT];
-    bool grown = false;
-#pragma unroll
-    for (int t = 0; t < MT; ++t) {
-        top[t] = s[t][0][0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) top[t] = fmaxf(top[t], s[t][i >> 2][i & 3]);
-        top[t] = fmaf(top[t], ps.sk, ps.lv);
-        top[t] = fmaxf(top[t], __shfl_xor(top[t], 16));
-        top[t] = fmaxf(top[t], __shfl_xor(top[t], 32));
-        grown = grown || top[t] > m[t] + kSlack;
-    }
+    const bool grown = top > m + kSlack;
     if (__any(grown)) {
-#pragma unroll
-        for (int t = 0; t < MT; ++t) {
-            const float mn = top[t] > m[t] + kSlack ? top[t] : m[t], alpha = __builtin_amdgcn_exp2f(m[t] - or_zero(mn));
-            m[t] = mn;
-            l[t] *= alpha;
-            rescale(t, alpha);
-        }
+        const float mn = grown ? top : m, alpha = __builtin_amdgcn_exp2f(m - or_zero(mn));
+        m = mn;
+        l *= alpha;
+        rescale(alpha);
     }
+}
+
+// The weights of 64 keys for one query a lane (16 of the keys in this lane): s holds the
+// products, key `run` + i in [low, high) counts. With a page's factors the same for all 16,
+// and sk > 0, the largest product has the largest exponent.
+template <typename Rescale>
+__device__ __forceinline__ void weights(f32x4 (&s)[4], float &m, float &l, const PageScale &ps, bool page, int run, int low, int high,
+                                        f16x8 (&pf)[2], Rescale &&rescale)
+{
+    if (!__all(page && run >= low && run + 16 <= high)) {
 #pragma unroll
-    for (int t = 0; t < MT; ++t) {
-        const float off = ps.lv - or_zero(m[t]);
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float e = __builtin_amdgcn_exp2f(fmaf(s[t][i >> 2][i & 3], ps.sk, off));
-            sum += e;
-            pf[t][i >> 3][i & 7] = _Float16(e);
-        }
-        l[t] = fmaf(sum, ps.iv, l[t]);
+        for (int i = 0; i < 16; ++i)
+            s[i >> 2][i & 3] = page && run + i >= low && run + i < high ? s[i >> 2][i & 3] : -__builtin_inff();
     }
+    float top = s[0][0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i >> 2][i & 3]);
+    top = fmaf(top, ps.sk, ps.lv);
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    raise(m, l, top, rescale);
+    const float off = ps.lv - or_zero(m);
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const float e = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], ps.sk, off));
+        sum += e;
+        pf[i >> 3][i & 7] = _Float16(e);
+    }
+    l = fmaf(sum, ps.iv, l);
 }
 
 // Bytes of the 4 keys from `key` on that lie in [low, high).
@@ -263,9 +258,9 @@ struct Sequence {
 
 // A lane's query: row `row` of head h, its keys [low, high), its elements as the first
 // product's second operand (chunk c: elements c * CHUNK + g * GROUP .. + 7).
-template <typename T, int DP, int CHUNK, int GROUP>
+template <typename T, int DP, int CHUNK, int GROUP, int N>
 __device__ __forceinline__ bool load_query(const AttentionParams &p, const Sequence &seq, int b, int h, int row, int g, int &low, int &high,
-                                           typename Vec8<T>::type (&qf)[DP / 32])
+                                           typename Vec8<T>::type (&qf)[N])
 {
     const int t = row / p.group, hq = h * p.group + row - t * p.group;
     const bool live = row < p.rows && t < seq.count;
@@ -273,7 +268,7 @@ __device__ __forceinline__ bool load_query(const AttentionParams &p, const Seque
     low = live && p.window ? max(high - p.window, 0) : 0;
     const T *src = static_cast<const T *>(p.q) + b * p.qb + (live ? t * p.qt + hq * p.qh : 0);
 #pragma unroll
-    for (int c = 0; c < DP / 32; ++c) {
+    for (int c = 0; c < N; ++c) {
         const int d = c * CHUNK + g * GROUP;
         typename Vec8<T>::type x{};
         if (live && d < p.dim) __builtin_memcpy(&x, src + d, 16);
@@ -317,9 +312,9 @@ attention_few_kernel(const AttentionParams p)
     const int D = p.dim, page = 1 << p.page_shift;
     const Sequence seq(p, b);
     v8 qf[QC];
-    int low[1], high[1];
-    const bool live = load_query<T, DP, 8, DP / 4>(p, seq, b, h, r, g, low[0], high[0], qf);
-    int tlo = live ? low[0] : 0x7fffffff, thi = high[0];
+    int low, high;
+    const bool live = load_query<T, DP, 8, DP / 4, QC>(p, seq, b, h, r, g, low, high, qf);
+    int tlo = live ? low : 0x7fffffff, thi = high;
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) {
         tlo = min(tlo, __shfl_xor(tlo, o));
@@ -332,7 +327,7 @@ attention_few_kernel(const AttentionParams p)
     const int from = s0 + split * each, to = min(s1, from + each);
 
     f32x4 acc[DT];
-    float m[1] = {-__builtin_inff()}, l[1] = {0.f};
+    float m = -__builtin_inff(), l = 0.f;
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] = f32x4{};
     // Page of the 16 keys from `key` on (they share it), or -1 where there is none.
@@ -363,15 +358,15 @@ attention_few_kernel(const AttentionParams p)
         const bool held = vp >= 0;
         kp = page_of(krun + kWaves * kStep);
         vp = page_of(vrun + kWaves * kStep);
-        f32x4 s[1][4];
+        f32x4 s[4];
 #pragma unroll
         for (int c = 0; c < QC; ++c)
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-                s[0][t] = mma(widen<T>(kraw[t][c >> 1][(c & 1) * 2], kraw[t][c >> 1][(c & 1) * 2 + 1]), qf[c], c == 0 ? f32x4{} : s[0][t]);
+                s[t] = mma(widen<T>(kraw[t][c >> 1][(c & 1) * 2], kraw[t][c >> 1][(c & 1) * 2 + 1]), qf[c], c == 0 ? f32x4{} : s[t]);
         const PageScale ps = page_scale(ek, ev, p.scale);
-        f16x8 pf[1][2];
-        weights<1>(s, m, l, ps, held, vrun, low, high, pf, [&](int, float alpha) {
+        f16x8 pf[2];
+        weights(s, m, l, ps, held, vrun, low, high, pf, [&](float alpha) {
 #pragma unroll
             for (int d = 0; d < DT; ++d) acc[d] *= alpha;
         });
@@ -387,20 +382,20 @@ attention_few_kernel(const AttentionParams p)
 #pragma unroll
         for (int c = 0; c < 2; ++c)
 #pragma unroll
-            for (int d = 0; d < DT; ++d) acc[d] = mma(widen<_Float16>(vraw[d][2 * c], vraw[d][2 * c + 1]), pf[0][c], acc[d]);
+            for (int d = 0; d < DT; ++d) acc[d] = mma(widen<_Float16>(vraw[d][2 * c], vraw[d][2 * c + 1]), pf[c], acc[d]);
     }
     // The waves' sums together: a lane's l is its own keys'.
-    l[0] += __shfl_xor(l[0], 16);
-    l[0] += __shfl_xor(l[0], 32);
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
     if (g == 0) {
-        ml[0][wave][r] = m[0];
-        ml[1][wave][r] = l[0];
+        ml[0][wave][r] = m;
+        ml[1][wave][r] = l;
     }
     __syncthreads();
     float top = ml[0][0][r];
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) top = fmaxf(top, ml[0][w][r]);
-    const float sub = or_zero(top), mine = __builtin_amdgcn_exp2f(m[0] - sub);
+    const float sub = or_zero(top), mine = __builtin_amdgcn_exp2f(m - sub);
     float total = 0.f;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) total = fmaf(ml[1][w][r], __builtin_amdgcn_exp2f(ml[0][w][r] - sub), total);
@@ -423,20 +418,26 @@ attention_few_kernel(const AttentionParams p)
     }
 }
 
-// Many queries of a kv head: the block's 4 waves have MT x 16 of them each and share the
-// keys, 64 at a time. Wave w reads the w-th 16 of them a step ahead, turns them into 16-bit
-// floats, once for the whole block, and puts them into LDS: keys as rows [key][dim], values
-// as rows [dim][key] with the 16-byte pieces of a row in an order of its own, so that the
-// lanes of a read (0-3, 12-15, 20-27 at once, and so on) meet in no bank.
-template <typename T, int DP, int MT>
-__global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1)
+// Many queries of a kv head: a block's waves have 32 of them each and share the keys, 64 at a
+// time. A wave reads its part of them a step ahead, turns them into 16-bit floats, once for
+// the whole block, and puts them into LDS: keys as rows [key][dim], values as rows [dim][key],
+// the 16-byte pieces of a row in an order of its own, so that the lanes of a read (0-3, 12-15,
+// 20-27 at once, and so on) meet in no bank.
+//
+// The products are 32 x 32: one query a lane and 32 keys of it, 8 of each 16, and twice the
+// work an instruction, which one wave can issue without a pause (it issues at most one 16 x 16
+// x 32 in 32 clocks where two waves reach one in 16). Row 8 w + 4 hf + e of tile tt is key
+// 32 tt + 16 (w / 2) + 8 hf + 4 (w % 2) + e: lane half hf then holds the keys that it
+// contracts in the second product.
+template <typename T, int DP, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, DP <= 128 ? 2 : 1)
 attention_many_kernel(const AttentionParams p, int bhs)
 {
-    constexpr int kWaves = 4, QC = DP / 32, DT = DP / 16, kLoads = DP / 64;
-    constexpr int kKeys = kStep * DP * 2, kStage = 2 * kKeys;     // bytes of a step's keys, and with its values
+    constexpr int QC = DP / 16, DT = DP / 32, kLoads = DP / 64, kRuns = 4 / WAVES;
+    constexpr int kKeys = kStep * DP * 2;      // bytes of a step's keys, or values
     typedef typename Vec8<T>::type v8;
-    __shared__ __align__(16) uint8_t lds[2 * kStage];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), r = lane & 15, g = lane >> 4;
+    __shared__ __align__(16) uint8_t lds[2][2 * kKeys];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), r = lane & 31, hf = lane >> 5, g = lane >> 4;
     // An eighth of the work to each XCD, a head's blocks together, so that they read its
     // keys through one L2; the last rows, which see the most keys, first.
     const int per = p.row_tiles * p.splits, blocks = bhs * per, share = (blocks + 7) >> 3;
@@ -446,74 +447,72 @@ attention_many_kernel(const AttentionParams p, int bhs)
     const int b = bh / p.heads, h = bh - b * p.heads;
     const int D = p.dim, page = 1 << p.page_shift;
     const Sequence seq(p, b);
-    v8 qf[MT][QC];
-    int low[MT], high[MT], row[MT];
-    bool live[MT];
-#pragma unroll
-    for (int t = 0; t < MT; ++t) {
-        row[t] = ((tile * kWaves + wave) * MT + t) * 16 + r;
-        live[t] = load_query<T, DP, 32, 8>(p, seq, b, h, row[t], g, low[t], high[t], qf[t]);
-        // A row without a query sees every key, which costs less than no key, and is 0 in the end.
-        if (!live[t]) high[t] = 0x7fffffff;
-    }
+    v8 qf[QC];
+    int low, high;
+    const int row = (tile * WAVES + wave) * 32 + r;
+    const bool live = load_query<T, DP, 16, 8, QC>(p, seq, b, h, row, hf, low, high, qf);
+    // A row without a query sees every key, which costs less than no key, and is 0 in the end.
+    if (!live) high = 0x7fffffff;
     // The block's keys: from the first that its first query sees to its last query's own.
-    const int t0 = tile * kWaves * MT * 16 / p.group, t1 = min(((tile + 1) * kWaves * MT * 16 - 1) / p.group, seq.count - 1);
+    const int t0 = tile * WAVES * 32 / p.group, t1 = min(((tile + 1) * WAVES * 32 - 1) / p.group, seq.count - 1);
     const int thi = t0 < seq.count ? seq.first + t1 + 1 : 0, tlo = p.window ? max(seq.first + t0 + 1 - p.window, 0) : 0;
     const int s0 = thi > 0 ? tlo / kStep : 0, s1 = (thi + kStep - 1) / kStep;
     const int each = (s1 - s0 + p.splits - 1) / p.splits;
     const int from = s0 + split * each, to = min(s1, from + each);
 
-    f32x4 acc[MT][DT];
-    float m[MT], l[MT];
+    f32x16 acc[DT];
+    float m = -__builtin_inff(), l = 0.f;
 #pragma unroll
-    for (int t = 0; t < MT; ++t) {
-        m[t] = -__builtin_inff();
-        l[t] = 0.f;
-#pragma unroll
-        for (int d = 0; d < DT; ++d) acc[t][d] = f32x4{};
-    }
-    // The table's entry of a lane group's 16 keys of a step; a page of the cache or -1.
+    for (int d = 0; d < DT; ++d) acc[d] = f32x16{};
+    // The table's entry of the g-th 16 keys of a step; a page of the cache or -1.
     auto entry = [&](int step) {
         const int key = step * kStep + g * 16;
         return step < to && key < thi ? p.table[b * p.ldt + (key >> p.page_shift)] : -1;
     };
     auto on_page = [&](int pid) { return unsigned(pid) < unsigned(p.pages) ? pid : -1; };
-    i32x4 kraw[kLoads], vraw[kLoads];
-    // This wave's 16 keys of a step, from the page of lane group `wave`: dimension `lane` of
-    // the values, and of the keys a piece of 16 dimensions of one key.
+    i32x4 kraw[kRuns][kLoads], vraw[kRuns][kLoads];
+    // This wave's runs of 16 keys of a step: of the values dimension `lane`, of the keys a
+    // piece of 16 dimensions of one key.
     auto fetch = [&](int step, int pids) {
-        const int pid = __builtin_amdgcn_readlane(pids, wave * 16), run = step * kStep + wave * 16, slot = run & (page - 1);
-        const int64_t at = int64_t(max(pid, 0)) * p.heads + h;
-        const uint8_t *k = p.kc + (at * page + slot) * D, *v = p.vc + at * D * page + slot;
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int key = (i * 64 + lane) / DT, d = (lane % DT) * 16, vd = i * 64 + lane;
-            kraw[i] = pid >= 0 && d < D ? *reinterpret_cast<const i32x4 *>(k + key * D + d) : i32x4{};
-            vraw[i] = pid >= 0 && vd < D ? *reinterpret_cast<const i32x4 *>(v + int64_t(vd) * page) : i32x4{};
-        }
-    };
-    // The order of a key's pieces, from its number in 64: the keys of a read differ in the
-    // last two bits and the first two. Rows of 128 bytes share a bank row by twos.
-    auto order = [](int key) { return ((key & 3) | (key >> 4) << 2) >> (DP < 128 ? 1 : 0); };
-    auto put = [&](int step, int buf) {
-        const int run = step * kStep + wave * 16;
-        uint8_t *const ks = lds + buf * kStage, *const vs = ks + kKeys;
-        if (run + 16 > thi || run < tlo) {
-            // Keys that no query sees may hold anything: their values count as 0.
+        for (int q = 0; q < kRuns; ++q) {
+            const int which = wave * kRuns + q, pid = __builtin_amdgcn_readlane(pids, which * 16);
+            const int slot = (step * kStep + which * 16) & (page - 1);
+            const int64_t at = int64_t(max(pid, 0)) * p.heads + h;
+            const uint8_t *k = p.kc + (at * page + slot) * D, *v = p.vc + at * D * page + slot;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const int mask = key_mask(run + 4 * w, tlo, thi);
-#pragma unroll
-                for (int i = 0; i < kLoads; ++i) vraw[i][w] &= mask;
+            for (int i = 0; i < kLoads; ++i) {
+                const int key = (i * 64 + lane) / (DP / 16), d = (lane % (DP / 16)) * 16, vd = i * 64 + lane;
+                kraw[q][i] = pid >= 0 && d < D ? *reinterpret_cast<const i32x4 *>(k + key * D + d) : i32x4{};
+                vraw[q][i] = pid >= 0 && vd < D ? *reinterpret_cast<const i32x4 *>(v + int64_t(vd) * page) : i32x4{};
             }
         }
+    };
+    // The order of a key's pieces: its row in a tile, from 16 on again. Rows of 128 bytes
+    // share a bank row by twos.
+    auto order = [](int key) { return ((key & 3) | ((key >> 3) & 1) << 2 | ((key >> 2) & 1) << 3) >> (DP < 128 ? 1 : 0); };
+    auto put = [&](int step, int buf) {
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int key = wave * 16 + (i * 64 + lane) / DT, piece = (lane % DT) * 2, d = i * 64 + lane;
+        for (int q = 0; q < kRuns; ++q) {
+            const int which = wave * kRuns + q, run = step * kStep + which * 16;
+            uint8_t *const ks = lds[buf], *const vs = ks + kKeys;
+            if (run + 16 > thi || run < tlo) {
+                // Keys that no query sees may hold anything: their values count as 0.
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                *reinterpret_cast<v8 *>(ks + key * DP * 2 + ((piece + c) ^ order(key)) * 16) = widen<T>(kraw[i][2 * c], kraw[i][2 * c + 1]);
-                *reinterpret_cast<f16x8 *>(vs + d * 128 + ((c * 4 + wave) ^ ((d >> 1) & 7)) * 16) = widen<_Float16>(vraw[i][2 * c], vraw[i][2 * c + 1]);
+                for (int w = 0; w < 4; ++w) {
+                    const int mask = key_mask(run + 4 * w, tlo, thi);
+#pragma unroll
+                    for (int i = 0; i < kLoads; ++i) vraw[q][i][w] &= mask;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int key = which * 16 + (i * 64 + lane) / (DP / 16), piece = (lane % (DP / 16)) * 2, d = i * 64 + lane;
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    *reinterpret_cast<v8 *>(ks + key * DP * 2 + ((piece + c) ^ order(key)) * 16) = widen<T>(kraw[q][i][2 * c], kraw[q][i][2 * c + 1]);
+                    *reinterpret_cast<f16x8 *>(vs + d * 128 + ((which * 2 + c) ^ ((d >> 1) & 7)) * 16) = widen<_Float16>(vraw[q][i][2 * c], vraw[q][i][2 * c + 1]);
+                }
             }
         }
     };
@@ -527,13 +526,14 @@ attention_many_kernel(const AttentionParams p, int bhs)
         fetch(from, pids);
         put(from, 0);
     }
-    const int korder = order((r >> 2) * 16 + (r & 3));
+    const int krow = (r >> 4) * 16 + ((r >> 2) & 1) * 8 + ((r >> 3) & 1) * 4 + (r & 3);     // row r's key in tile 0
     for (int step = from; step < to; ++step) {
-        const int buf = (step - from) & 1, run = step * kStep + g * 16;
+        const int buf = (step - from) & 1, base = step * kStep;
         wait_lds();
         barrier();
         const PageScale ps = page_scale(ek, ev, p.scale);
-        const bool held = pids >= 0;
+        const bool held = __all(pids >= 0);
+        const int now = pids;
         if (step + 1 < to) {
             pids = on_page(next);
             fetch(step + 1, pids);
@@ -542,53 +542,88 @@ attention_many_kernel(const AttentionParams p, int bhs)
             ev = p.vs[at];
             next = entry(step + 2);
         }
-        const uint8_t *const kt = lds + buf * kStage + ((r >> 2) * 16 + (r & 3)) * DP * 2, *const vt = lds + buf * kStage + kKeys + r * 128;
-        // (Products into the same sum stand apart: one takes as long as two follow each other.)
-        f32x4 s[MT][4];
+        const uint8_t *const kt = lds[buf] + krow * DP * 2, *const vt = lds[buf] + kKeys + r * 128;
+        f32x16 s[2];
 #pragma unroll
         for (int c = 0; c < QC; ++c)
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const v8 kf = *reinterpret_cast<const v8 *>(kt + t * 4 * DP * 2 + ((c * 4 + g) ^ korder) * 16);
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) s[mt][t] = mma(kf, qf[mt][c], c == 0 ? f32x4{} : s[mt][t]);
+            for (int t = 0; t < 2; ++t) {
+                const v8 kf = *reinterpret_cast<const v8 *>(kt + t * 32 * DP * 2 + ((c * 2 + hf) ^ order(krow)) * 16);
+                s[t] = mma32(kf, qf[c], c == 0 ? f32x16{} : s[t]);
             }
-        f16x8 pf[MT][2];
-        weights<MT>(s, m, l, ps, held, run, low, high, pf, [&](int mt, float alpha) {
+        // Element i of s[t]: key 16 (2 t + i / 8) + 8 hf + i % 8.
+        if (!held || !__all(base >= low && base + kStep <= high)) {
 #pragma unroll
-            for (int d = 0; d < DT; ++d) acc[mt][d] *= alpha;
+            for (int q = 0; q < 4; ++q) {
+                const bool there = __builtin_amdgcn_readlane(now, q * 16) >= 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int key = base + q * 16 + hf * 8 + i;
+                    float &v = reinterpret_cast<float *>(&s[q >> 1])[(q & 1) * 8 + i];
+                    v = there && key >= low && key < high ? v : -__builtin_inff();
+                }
+            }
+        }
+        float sk[4], lv[4], iv[4], top = -__builtin_inff();
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            sk[q] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ps.sk), q * 16));
+            lv[q] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ps.lv), q * 16));
+            iv[q] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ps.iv), q * 16));
+            float most = s[q >> 1][(q & 1) * 8];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) most = fmaxf(most, s[q >> 1][(q & 1) * 8 + i]);
+            top = fmaxf(top, fmaf(most, sk[q], lv[q]));
+        }
+        top = fmaxf(top, __shfl_xor(top, 32));
+        raise(m, l, top, [&](float alpha) {
+#pragma unroll
+            for (int d = 0; d < DT; ++d) acc[d] *= alpha;
         });
+        const float sub = or_zero(m);
+        f16x8 pf[4];
 #pragma unroll
-        for (int c = 0; c < 2; ++c)
+        for (int q = 0; q < 4; ++q) {
+            const float off = lv[q] - sub;
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float e = __builtin_amdgcn_exp2f(fmaf(s[q >> 1][(q & 1) * 8 + i], sk[q], off));
+                sum += e;
+                pf[q][i] = _Float16(e);
+            }
+            l = fmaf(sum, iv[q], l);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
-                const f16x8 vf = *reinterpret_cast<const f16x8 *>(vt + d * 16 * 128 + ((c * 4 + g) ^ ((r >> 1) & 7)) * 16);
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) acc[mt][d] = mma(vf, pf[mt][c], acc[mt][d]);
+                const f16x8 vf = *reinterpret_cast<const f16x8 *>(vt + d * 32 * 128 + ((q * 2 + hf) ^ ((r >> 1) & 7)) * 16);
+                acc[d] = mma32(vf, pf[q], acc[d]);
             }
         if (step + 1 < to) put(step + 1, buf ^ 1);
     }
+    l += __shfl_xor(l, 32);
+    if (row >= p.rows) return;
+    if (!live) {
+        m = -__builtin_inff();
+        l = 0.f;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-        l[mt] += __shfl_xor(l[mt], 16);
-        l[mt] += __shfl_xor(l[mt], 32);
-        if (row[mt] >= p.rows) continue;
-        if (!live[mt]) {
-            m[mt] = -__builtin_inff();
-            l[mt] = 0.f;
-#pragma unroll
-            for (int d = 0; d < DT; ++d) acc[mt][d] = f32x4{};
-        }
-        float *part = p.part ? p.part + ((int64_t(bh) * p.rows + row[mt]) * p.splits + split) * (D + 2) : nullptr;
-        if (part && g == 0) {
-            part[D] = m[mt];
-            part[D + 1] = l[mt];
-        }
-        const float inv = inverse(l[mt]);
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-            if (d * 16 < D) store_row<T>(p, b, h, row[mt], part, d * 16 + g * 4, acc[mt][d], inv);
+        for (int d = 0; d < DT; ++d) acc[d] = f32x16{};
     }
+    float *part = p.part ? p.part + ((int64_t(bh) * p.rows + row) * p.splits + split) * (D + 2) : nullptr;
+    if (part && hf == 0) {
+        part[D] = m;
+        part[D + 1] = l;
+    }
+    const float inv = inverse(l);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const int at = d * 32 + w * 8 + hf * 4;
+            if (at < D) store_row<T>(p, b, h, row, part, at, f32x4{acc[d][4 * w], acc[d][4 * w + 1], acc[d][4 * w + 2], acc[d][4 * w + 3]}, inv);
+        }
 }
 
 // The splits of a row together: a block of 4 waves per row, LANES lanes (4 dimensions each)
@@ -649,20 +684,20 @@ ds_status check_cache(int64_t batch, int64_t tokens, int64_t heads, int64_t dim,
 }
 
 struct Plan {
-    int mt, splits, row_tiles;      // mt 0: few queries of a head
+    int waves, splits, row_tiles;      // waves 0: few queries of a head
     int64_t rows;
 };
 
 // How a call is split: over the rows first, then over the keys until there are about 512
-// blocks of at least 8 steps of 64 keys.
-Plan plan_attention(int64_t batch, int64_t tokens, int64_t heads, int64_t group, int64_t dim, int64_t columns, int64_t page)
+// blocks (1024 of few queries) of at least 8 steps of 64 keys.
+Plan plan_attention(int64_t batch, int64_t tokens, int64_t heads, int64_t group, int64_t columns, int64_t page)
 {
     Plan a;
     a.rows = tokens * group;
-    a.mt = a.rows <= 16 ? 0 : a.rows <= 64 || dim > 128 ? 1 : 2;
-    a.row_tiles = a.mt ? int((a.rows + 64 * a.mt - 1) / (64 * a.mt)) : 1;
+    a.waves = a.rows <= 16 ? 0 : a.rows <= 64 ? 2 : 4;
+    a.row_tiles = a.waves ? int((a.rows + 32 * a.waves - 1) / (32 * a.waves)) : 1;
     const int64_t blocks = std::max<int64_t>(batch * heads * a.row_tiles, 1), steps = (columns * page + kStep - 1) / kStep;
-    a.splits = int(std::max<int64_t>(1, std::min<int64_t>({(a.mt ? 512 : 1024) / blocks, (steps + 7) / 8, 256})));
+    a.splits = int(std::max<int64_t>(1, std::min<int64_t>({(a.waves ? 512 : 1024) / blocks, (steps + 7) / 8, 256})));
     return a;
 }
 
@@ -676,9 +711,9 @@ void run_attention(const AttentionParams &p, const Plan &a, int64_t batch, hipSt
 {
     const int bhs = int(batch * p.heads);
     const dim3 many(uint32_t((int64_t(bhs) * a.row_tiles * a.splits + 7) / 8 * 8));
-    if (a.mt == 0) hipLaunchKernelGGL((attention_few_kernel<T, DP>), dim3(a.splits, bhs), dim3(256), 0, s, p);
-    else if (a.mt == 1 || DP > 128) hipLaunchKernelGGL((attention_many_kernel<T, DP, 1>), many, dim3(256), 0, s, p, bhs);
-    else hipLaunchKernelGGL((attention_many_kernel<T, DP, (DP > 128 ? 1 : 2)>), many, dim3(256), 0, s, p, bhs);
+    if (a.waves == 0) hipLaunchKernelGGL((attention_few_kernel<T, DP>), dim3(a.splits, bhs), dim3(256), 0, s, p);
+    else if (a.waves == 2) hipLaunchKernelGGL((attention_many_kernel<T, DP, 2>), many, dim3(128), 0, s, p, bhs);
+    else hipLaunchKernelGGL((attention_many_kernel<T, DP, 4>), many, dim3(256), 0, s, p, bhs);
     if (a.splits > 1)
         hipLaunchKernelGGL((attention_join_kernel<T, DP / 4>), dim3(uint32_t(bhs * a.rows)), dim3(256), 0, s, p);
 }
@@ -746,7 +781,7 @@ extern "C" int64_t ds_attention_fp8_scratch_bytes(int64_t batch, int64_t tokens,
                                                   int64_t page, int64_t columns)
 {
     if (batch <= 0 || tokens <= 0 || heads <= 0 || group <= 0 || dim <= 0 || page <= 0 || columns <= 0) return 0;
-    return 4 * part_floats(plan_attention(batch, tokens, heads, group, dim, columns, page), batch, heads, dim);
+    return 4 * part_floats(plan_attention(batch, tokens, heads, group, columns, page), batch, heads, dim);
 }
 
 extern "C" ds_status ds_attention_fp8(const void *q, const uint8_t *k_cache, const uint8_t *v_cache, const uint8_t *k_scales,
@@ -767,7 +802,7 @@ extern "C" ds_status ds_attention_fp8(const void *q, const uint8_t *k_cache, con
     if (batch == 0 || tokens == 0) return ok();
     if (batch * heads > 65535) return fail(DS_ERR_UNSUPPORTED, "more than 65535 sequences times heads");
     if (group > 65535 || tokens * group > kMaxElems / 64) return fail(DS_ERR_UNSUPPORTED, "too many queries of a head");
-    const Plan a = plan_attention(batch, tokens, heads, group, dim, columns, page);
+    const Plan a = plan_attention(batch, tokens, heads, group, columns, page);
     if (batch * heads * a.rows * a.splits > kMaxElems / 2) return fail(DS_ERR_UNSUPPORTED, "too many queries");
     int64_t bytes[2];
     for (int i = 0; i < 2; ++i) {
