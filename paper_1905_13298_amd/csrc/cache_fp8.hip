@@ -7,6 +7,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "conv_plan.hpp"
 #include "fp8.hpp"
@@ -189,26 +190,41 @@ __device__ __forceinline__ PageScale page_scale(int ek, int ev, float scale)
 
 // The running maximum m of a row moves only when it is passed by more than 2^8, so that the
 // sums are hardly ever rescaled: weights reach 2^8 at most, far inside the range of a 16-bit
-// float.
+// float. So the exponents are formed with the old maximum, and where none is above 8 they
+// stay.
 constexpr float kSlack = 8.f;
 
-// A row's maximum and sum once `top` is known, and the factor of its sums (rescale): in a
-// branch that is rarely taken.
-template <typename Rescale>
-__device__ __forceinline__ void raise(float &m, float &l, float top, Rescale &&rescale)
+// `top`: the largest of a row's new exponents, relative to the maximum (0 in its place where
+// there is none yet). Moves the maximum where it has to, in a branch that is rarely taken: then
+// shift(by) takes `by` off the exponents and rescale(alpha) multiplies the sums.
+template <typename Shift, typename Rescale>
+__device__ __forceinline__ void raise(float &m, float &l, float top, Shift &&shift, Rescale &&rescale)
 {
-    const bool grown = top > m + kSlack;
+    const bool none = m == -__builtin_inff(), grown = none ? top > m : top > kSlack;
     if (__any(grown)) {
-        const float mn = grown ? top : m, alpha = __builtin_amdgcn_exp2f(m - or_zero(mn));
-        m = mn;
+        const float by = grown ? top : 0.f, alpha = grown ? (none ? 0.f : __builtin_amdgcn_exp2f(-top)) : 1.f;
+        m = none ? (grown ? top : m) : m + by;
         l *= alpha;
+        shift(by);
         rescale(alpha);
     }
 }
 
+// The larger of a lane's value and that of the lane 32 (16) further, in both.
+__device__ __forceinline__ float max_over_32(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+__device__ __forceinline__ float max_over_16(float v)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
 // The weights of 64 keys for one query a lane (16 of the keys in this lane): s holds the
-// products, key `run` + i in [low, high) counts. With a page's factors the same for all 16,
-// and sk > 0, the largest product has the largest exponent.
+// products, key `run` + i in [low, high) counts.
 template <typename Rescale>
 __device__ __forceinline__ void weights(f32x4 (&s)[4], float &m, float &l, const PageScale &ps, bool page, int run, int low, int high,
                                         f16x8 (&pf)[2], Rescale &&rescale)
@@ -218,20 +234,23 @@ __device__ __forceinline__ void weights(f32x4 (&s)[4], float &m, float &l, const
         for (int i = 0; i < 16; ++i)
             s[i >> 2][i & 3] = page && run + i >= low && run + i < high ? s[i >> 2][i & 3] : -__builtin_inff();
     }
-    float top = s[0][0];
-#pragma unroll
-    for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i >> 2][i & 3]);
-    top = fmaf(top, ps.sk, ps.lv);
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
-    raise(m, l, top, rescale);
     const float off = ps.lv - or_zero(m);
-    float sum = 0.f;
+    float e[16], top = -__builtin_inff(), sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) e[i] = fmaf(s[i >> 2][i & 3], ps.sk, off);
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) top = fmaxf(top, fmaxf(e[i], e[i + 1]));
+    raise(m, l, max_over_32(max_over_16(top)),
+          [&](float by) {
+#pragma unroll
+              for (int i = 0; i < 16; ++i) e[i] -= by;
+          },
+          rescale);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-        const float e = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], ps.sk, off));
-        sum += e;
-        pf[i >> 3][i & 7] = _Float16(e);
+        e[i] = __builtin_amdgcn_exp2f(e[i]);
+        sum += e[i];
+        pf[i >> 3][i & 7] = _Float16(e[i]);
     }
     l = fmaf(sum, ps.iv, l);
 }
@@ -429,22 +448,24 @@ attention_few_kernel(const AttentionParams p)
 // x 32 in 32 clocks where two waves reach one in 16). Row 8 w + 4 hf + e of tile tt is key
 // 32 tt + 16 (w / 2) + 8 hf + 4 (w % 2) + e: lane half hf then holds the keys that it
 // contracts in the second product.
-template <typename T, int DP, int WAVES>
+// ONE: a page holds whole steps (64 or 128 tokens), so that a step has one scale.
+template <typename T, int DP, int WAVES, bool ONE>
 __global__ void __launch_bounds__(64 * WAVES, DP <= 128 ? 2 : 1)
 attention_many_kernel(const AttentionParams p, int bhs)
 {
-    constexpr int QC = DP / 16, DT = DP / 32, kLoads = DP / 64, kRuns = 4 / WAVES;
+    constexpr int QC = DP / 16, DT = DP / 32, kLoads = DP / 64, kRuns = 4 / WAVES, kScales = ONE ? 1 : 4;
     constexpr int kKeys = kStep * DP * 2;      // bytes of a step's keys, or values
     typedef typename Vec8<T>::type v8;
     __shared__ __align__(16) uint8_t lds[2][2 * kKeys];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), r = lane & 31, hf = lane >> 5, g = lane >> 4;
     // An eighth of the work to each XCD, a head's blocks together, so that they read its
-    // keys through one L2; the last rows, which see the most keys, first.
+    // keys through one L2, the same head of every sequence next, whose lengths may differ; the
+    // last rows, which see the most keys, first.
     const int per = p.row_tiles * p.splits, blocks = bhs * per, share = (blocks + 7) >> 3;
     const int at = (int(blockIdx.x) & 7) * share + (int(blockIdx.x) >> 3);
     if ((int(blockIdx.x) >> 3) >= share || at >= blocks) return;
-    const int bh = at / per, rest = at - bh * per, tile = p.row_tiles - 1 - rest / p.splits, split = rest % p.splits;
-    const int b = bh / p.heads, h = bh - b * p.heads;
+    const int unit = at / per, rest = at - unit * per, tile = p.row_tiles - 1 - rest / p.splits, split = rest % p.splits;
+    const int batch = bhs / p.heads, h = unit / batch, b = unit - h * batch, bh = b * p.heads + h;
     const int D = p.dim, page = 1 << p.page_shift;
     const Sequence seq(p, b);
     v8 qf[QC];
@@ -465,92 +486,139 @@ attention_many_kernel(const AttentionParams p, int bhs)
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] = f32x16{};
     // The table's entry of the g-th 16 keys of a step; a page of the cache or -1.
+    const int *const table = p.table + b * p.ldt;
     auto entry = [&](int step) {
-        const int key = step * kStep + g * 16;
-        return step < to && key < thi ? p.table[b * p.ldt + (key >> p.page_shift)] : -1;
+        const int key = step * kStep + (ONE ? 0 : g * 16);
+        return step < to && key < thi ? table[key >> p.page_shift] : -1;
     };
     auto on_page = [&](int pid) { return unsigned(pid) < unsigned(p.pages) ? pid : -1; };
+    auto on_pages = [&](int pids) { return ONE ? __builtin_amdgcn_readfirstlane(pids) >= 0 : bool(__all(pids >= 0)); };
     i32x4 kraw[kRuns][kLoads], vraw[kRuns][kLoads];
     // This wave's runs of 16 keys of a step: of the values dimension `lane`, of the keys a
-    // piece of 16 dimensions of one key.
+    // piece of 16 dimensions of one key (what lies past `dim` is read somewhere inside). Where
+    // there is no page, page 0 is read instead.
+    uint32_t koff[kLoads], voff[kLoads];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+        koff[i] = uint32_t((i * 64 + lane) / (DP / 16) * D + min(lane % (DP / 16) * 16, D - 16));
+        voff[i] = uint32_t(min(i * 64 + lane, D - 1) * page);
+    }
+    const uint8_t *const kh = p.kc + int64_t(h) * D * page, *const vh = p.vc + int64_t(h) * D * page;
+    const int64_t page_bytes = int64_t(p.heads) * D * page;
     auto fetch = [&](int step, int pids) {
 #pragma unroll
         for (int q = 0; q < kRuns; ++q) {
-            const int which = wave * kRuns + q, pid = __builtin_amdgcn_readlane(pids, which * 16);
+            const int which = wave * kRuns + q, pid = ONE ? __builtin_amdgcn_readfirstlane(pids) : __builtin_amdgcn_readlane(pids, which * 16);
             const int slot = (step * kStep + which * 16) & (page - 1);
-            const int64_t at = int64_t(max(pid, 0)) * p.heads + h;
-            const uint8_t *k = p.kc + (at * page + slot) * D, *v = p.vc + at * D * page + slot;
+            const int64_t at = max(pid, 0) * page_bytes;
+            const uint8_t *k = kh + at + slot * D, *v = vh + at + slot;
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
-                const int key = (i * 64 + lane) / (DP / 16), d = (lane % (DP / 16)) * 16, vd = i * 64 + lane;
-                kraw[q][i] = pid >= 0 && d < D ? *reinterpret_cast<const i32x4 *>(k + key * D + d) : i32x4{};
-                vraw[q][i] = pid >= 0 && vd < D ? *reinterpret_cast<const i32x4 *>(v + int64_t(vd) * page) : i32x4{};
+                kraw[q][i] = *reinterpret_cast<const i32x4 *>(k + koff[i]);
+                vraw[q][i] = *reinterpret_cast<const i32x4 *>(v + voff[i]);
             }
         }
     };
     // The order of a key's pieces: its row in a tile, from 16 on again. Rows of 128 bytes
     // share a bank row by twos.
     auto order = [](int key) { return ((key & 3) | ((key >> 3) & 1) << 2 | ((key >> 2) & 1) << 3) >> (DP < 128 ? 1 : 0); };
-    auto put = [&](int step, int buf) {
+    // Keys that no query sees may hold anything: their values count as 0. So does what was
+    // read of a key past `dim`.
+    auto clear = [&](int step, int pids) {
+        if (__builtin_expect(D == DP && step * kStep >= tlo && step * kStep + kStep <= thi && on_pages(pids), 1)) return;
 #pragma unroll
         for (int q = 0; q < kRuns; ++q) {
             const int which = wave * kRuns + q, run = step * kStep + which * 16;
-            uint8_t *const ks = lds[buf], *const vs = ks + kKeys;
-            if (run + 16 > thi || run < tlo) {
-                // Keys that no query sees may hold anything: their values count as 0.
+            const bool there = __builtin_amdgcn_readlane(pids, which * 16) >= 0;
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const int mask = key_mask(run + 4 * w, tlo, thi);
+            for (int w = 0; w < 4; ++w) {
+                const int mask = there ? key_mask(run + 4 * w, tlo, thi) : 0;
 #pragma unroll
-                    for (int i = 0; i < kLoads; ++i) vraw[q][i][w] &= mask;
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                const int key = which * 16 + (i * 64 + lane) / (DP / 16), piece = (lane % (DP / 16)) * 2, d = i * 64 + lane;
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    *reinterpret_cast<v8 *>(ks + key * DP * 2 + ((piece + c) ^ order(key)) * 16) = widen<T>(kraw[q][i][2 * c], kraw[q][i][2 * c + 1]);
-                    *reinterpret_cast<f16x8 *>(vs + d * 128 + ((which * 2 + c) ^ ((d >> 1) & 7)) * 16) = widen<_Float16>(vraw[q][i][2 * c], vraw[q][i][2 * c + 1]);
+                for (int i = 0; i < kLoads; ++i) {
+                    vraw[q][i][w] &= mask;
+                    if (lane % (DP / 16) * 16 >= D) kraw[q][i][w] = 0;
                 }
             }
         }
     };
-    int pids = -1, next = -1, ek = 0, ev = 0;
-    if (from < to) {
-        pids = on_page(entry(from));
-        next = entry(from + 1);
-        const int64_t at = int64_t(max(pids, 0)) * p.heads + h;
+    // Part u of what fetch() read, to LDS: 8 keys or values a lane.
+    constexpr int kParts = kRuns * kLoads * 4;
+    auto put = [&](int u, int buf) {
+        const int q = u / (kLoads * 4), i = u / 4 % kLoads, c = u / 2 % 2, which = wave * kRuns + q;
+        uint8_t *const ks = lds[buf], *const vs = ks + kKeys;
+        if (u % 2 == 0) {
+            const int key = which * 16 + (i * 64 + lane) / (DP / 16), piece = (lane % (DP / 16)) * 2;
+            *reinterpret_cast<v8 *>(ks + key * DP * 2 + ((piece + c) ^ order(key)) * 16) = widen<T>(kraw[q][i][2 * c], kraw[q][i][2 * c + 1]);
+        } else {
+            const int d = i * 64 + lane;
+            *reinterpret_cast<f16x8 *>(vs + d * 128 + ((which * 2 + c) ^ ((d >> 1) & 7)) * 16) = widen<_Float16>(vraw[q][i][2 * c], vraw[q][i][2 * c + 1]);
+        }
+    };
+    // Pages of this step and the next, the table's entry of the one after, and this step's
+    // scales. Those of the next step are read before its successor's keys, so that waiting
+    // for them waits for nothing else.
+    int pid0 = -1, pid1 = -1, next = -1, ek = 0, ev = 0;
+    auto look_ahead = [&](int step) {
+        const int64_t at = int64_t(max(pid1, 0)) * p.heads + h;
         ek = p.ks[at];
         ev = p.vs[at];
-        fetch(from, pids);
-        put(from, 0);
+        next = entry(step);
+        asm volatile("" : : : "memory");
+    };
+    if (from < to) {
+        pid1 = on_page(entry(from));
+        fetch(from, pid1);
+        look_ahead(from + 1);
+        clear(from, pid1);
+#pragma unroll
+        for (int u = 0; u < kParts; ++u) put(u, 0);
+        pid0 = pid1;
+        pid1 = on_page(next);
+        next = entry(from + 2);
+        fetch(from + 1, pid1);
     }
+    // A step mixes what does not depend on each other, product by product (each is issued in
+    // a few clocks and takes 32): into the first products the transfer of the next step's keys
+    // to LDS, into the second ones the weights that the products after them need. What they
+    // read from LDS is read eight products ahead.
+    constexpr int kFirst = 2 * QC, kSecond = 4 * DT, kAhead = 8;
     const int krow = (r >> 4) * 16 + ((r >> 2) & 1) * 8 + ((r >> 3) & 1) * 4 + (r & 3);     // row r's key in tile 0
-    for (int step = from; step < to; ++step) {
-        const int buf = (step - from) & 1, base = step * kStep;
+    auto body = [&](int step, auto which_buf) {
+        constexpr int buf = decltype(which_buf)::value;
+        const int base = step * kStep;
         wait_lds();
         barrier();
-        const PageScale ps = page_scale(ek, ev, p.scale);
-        const bool held = __all(pids >= 0);
-        const int now = pids;
-        if (step + 1 < to) {
-            pids = on_page(next);
-            fetch(step + 1, pids);
-            const int64_t at = int64_t(max(pids, 0)) * p.heads + h;
-            ek = p.ks[at];
-            ev = p.vs[at];
-            next = entry(step + 2);
-        }
         const uint8_t *const kt = lds[buf] + krow * DP * 2, *const vt = lds[buf] + kKeys + r * 128;
+        auto key_part = [&](int n) { return *reinterpret_cast<const v8 *>(kt + (n % 2) * 32 * DP * 2 + ((n / 2 * 2 + hf) ^ order(krow)) * 16); };
+        auto value_part = [&](int n) {
+            return *reinterpret_cast<const f16x8 *>(vt + n % DT * 32 * 128 + ((n / DT * 2 + hf) ^ ((r >> 1) & 7)) * 16);
+        };
+        v8 kf[kAhead];
+#pragma unroll
+        for (int n = 0; n < kAhead; ++n) kf[n] = key_part(n);
+        const PageScale ps = page_scale(ek, ev, p.scale);
+        const bool held = on_pages(pid0);
+        const int now = pid0;
+        if (step + 1 < to) clear(step + 1, pid1);
         f32x16 s[2];
 #pragma unroll
-        for (int c = 0; c < QC; ++c)
+        for (int n = 0; n < kFirst; ++n) {
+            s[n % 2] = mma32(kf[n % kAhead], qf[n / 2], n < 2 ? f32x16{} : s[n % 2]);
+            if (n + kAhead < kFirst) kf[n % kAhead] = key_part(n + kAhead);
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const v8 kf = *reinterpret_cast<const v8 *>(kt + t * 32 * DP * 2 + ((c * 2 + hf) ^ order(krow)) * 16);
-                s[t] = mma32(kf, qf[c], c == 0 ? f32x16{} : s[t]);
-            }
+            for (int u = n * kParts / kFirst; u < (n + 1) * kParts / kFirst; ++u) put(u, buf ^ 1);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        f16x8 vf[kAhead];
+#pragma unroll
+        for (int n = 0; n < kAhead; ++n) vf[n] = value_part(n);
+        pid0 = pid1;
+        if (step + 1 < to) {
+            const int pid2 = on_page(next);
+            look_ahead(step + 3);
+            pid1 = pid2;
+            fetch(step + 2, pid2);
+        }
         // Element i of s[t]: key 16 (2 t + i / 8) + 8 hf + i % 8.
         if (!held || !__all(base >= low && base + kStep <= high)) {
 #pragma unroll
@@ -564,44 +632,61 @@ attention_many_kernel(const AttentionParams p, int bhs)
                 }
             }
         }
-        float sk[4], lv[4], iv[4], top = -__builtin_inff();
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            sk[q] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ps.sk), q * 16));
-            lv[q] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ps.lv), q * 16));
-            iv[q] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ps.iv), q * 16));
-            float most = s[q >> 1][(q & 1) * 8];
-#pragma unroll
-            for (int i = 1; i < 8; ++i) most = fmaxf(most, s[q >> 1][(q & 1) * 8 + i]);
-            top = fmaxf(top, fmaf(most, sk[q], lv[q]));
-        }
-        top = fmaxf(top, __shfl_xor(top, 32));
-        raise(m, l, top, [&](float alpha) {
-#pragma unroll
-            for (int d = 0; d < DT; ++d) acc[d] *= alpha;
-        });
+        float sk[kScales], lv[kScales], iv[kScales], top = -__builtin_inff();
         const float sub = or_zero(m);
+#pragma unroll
+        for (int j = 0; j < kScales; ++j) {
+            auto of = [&](float v) { return ONE ? v : __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), j * 16)); };
+            sk[j] = of(ps.sk);
+            lv[j] = of(ps.lv);
+            iv[j] = of(ps.iv);
+            constexpr int kN = 32 / kScales;
+            const float off = lv[j] - sub;
+#pragma unroll
+            for (int i = j * kN; i < (j + 1) * kN; ++i) s[i / 16][i % 16] = fmaf(s[i / 16][i % 16], sk[j], off);
+#pragma unroll
+            for (int i = j * kN; i < (j + 1) * kN; i += 2) top = fmaxf(top, fmaxf(s[i / 16][i % 16], s[i / 16][i % 16 + 1]));
+        }
+        raise(m, l, max_over_32(top),
+              [&](float by) {
+#pragma unroll
+                  for (int i = 0; i < 32; ++i) s[i / 16][i % 16] -= by;
+              },
+              [&](float alpha) {
+#pragma unroll
+                  for (int d = 0; d < DT; ++d) acc[d] *= alpha;
+              });
+        // (The sum is of the 32-bit weights: of a page whose scale is far below the largest one's
+        // nothing may be left in 16 bits, where its values do not count but its weights do.)
         f16x8 pf[4];
+        float sum[4] = {};
+        auto weigh = [&](int q, int i) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const float off = lv[q] - sub;
-            float sum = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float e = __builtin_amdgcn_exp2f(fmaf(s[q >> 1][(q & 1) * 8 + i], sk[q], off));
-                sum += e;
-                pf[q][i] = _Float16(e);
+            for (int k = 0; k < 2; ++k) {
+                const float e = __builtin_amdgcn_exp2f(s[q >> 1][(q & 1) * 8 + i + k]);
+                sum[q] += e;
+                pf[q][i + k] = _Float16(e);
             }
-            l = fmaf(sum, iv[q], l);
+        };
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) weigh(0, i);
+#pragma unroll
+        for (int n = 0; n < kSecond; ++n) {
+            const int q = n / DT, d = n % DT;
+            acc[d] = mma32(vf[n % kAhead], pf[q], acc[d]);
+            if (n + kAhead < kSecond) vf[n % kAhead] = value_part(n + kAhead);
+            if (q < 3) {
+#pragma unroll
+                for (int i = d * 4 / DT * 2; i < (d + 1) * 4 / DT * 2; i += 2) weigh(q + 1, i);
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-#pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                const f16x8 vf = *reinterpret_cast<const f16x8 *>(vt + d * 32 * 128 + ((q * 2 + hf) ^ ((r >> 1) & 7)) * 16);
-                acc[d] = mma32(vf, pf[q], acc[d]);
-            }
-        if (step + 1 < to) put(step + 1, buf ^ 1);
+        for (int q = 0; q < 4; ++q) l = fmaf(sum[q], iv[q * kScales / 4], l);
+    };
+    for (int step = from; step < to; step += 2) {
+        body(step, std::integral_constant<int, 0>{});
+        if (step + 1 < to) body(step + 1, std::integral_constant<int, 1>{});
     }
     l += __shfl_xor(l, 32);
     if (row >= p.rows) return;
@@ -712,8 +797,12 @@ void run_attention(const AttentionParams &p, const Plan &a, int64_t batch, hipSt
     const int bhs = int(batch * p.heads);
     const dim3 many(uint32_t((int64_t(bhs) * a.row_tiles * a.splits + 7) / 8 * 8));
     if (a.waves == 0) hipLaunchKernelGGL((attention_few_kernel<T, DP>), dim3(a.splits, bhs), dim3(256), 0, s, p);
-    else if (a.waves == 2) hipLaunchKernelGGL((attention_many_kernel<T, DP, 2>), many, dim3(128), 0, s, p, bhs);
-    else hipLaunchKernelGGL((attention_many_kernel<T, DP, 4>), many, dim3(256), 0, s, p, bhs);
+    else {
+        const bool one = (1 << p.page_shift) % kStep == 0;
+        const auto k = a.waves == 2 ? (one ? attention_many_kernel<T, DP, 2, true> : attention_many_kernel<T, DP, 2, false>)
+                                    : (one ? attention_many_kernel<T, DP, 4, true> : attention_many_kernel<T, DP, 4, false>);
+        hipLaunchKernelGGL(k, many, dim3(64 * a.waves), 0, s, p, bhs);
+    }
     if (a.splits > 1)
         hipLaunchKernelGGL((attention_join_kernel<T, DP / 4>), dim3(uint32_t(bhs * a.rows)), dim3(256), 0, s, p);
 }
