@@ -44,11 +44,47 @@ __device__ __forceinline__ float row_sum(float v, float *red)
     return v;
 }
 
+// Eight consecutive elements as they are stored.
+template <typename T>
+struct Eight {
+    T v[8];
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = T(0.f);
+    }
+    __device__ __forceinline__ float at(int i) const { return float(v[i]); }
+    // The first n (or all, as always where WHOLE) of those at p + at.
+    template <bool WHOLE>
+    __device__ __forceinline__ void load(const T *p, uint32_t at, int n)
+    {
+        if (WHOLE || n >= 8) {
+            __builtin_memcpy(v, p + at, sizeof v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < n) v[i] = p[at + i];
+        }
+    }
+    template <bool WHOLE>
+    __device__ __forceinline__ void store(T *p, uint32_t at, int n) const
+    {
+        if (WHOLE || n >= 8) {
+            __builtin_memcpy(p + at, v, sizeof v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < n) p[at + i] = v[i];
+        }
+    }
+};
+
 template <int TPR>
 constexpr int row_block() { return TPR < 256 ? 256 : TPR; }
 
-// TPR threads hold a row in registers, NV vectors of 8 elements each.
-template <typename T, typename W, int TPR, int NV, bool QUANT>
+// TPR threads hold a row in registers, NV vectors of 8 elements each. WHOLE: rows of a
+// multiple of 8 elements. Weights are read with the row, not behind its sum.
+template <typename T, typename W, int TPR, int NV, bool QUANT, bool WHOLE>
 __global__ void __launch_bounds__(row_block<TPR>())
 norm_kernel(const T *__restrict__ x, const T *__restrict__ residual, const W *__restrict__ weight, void *__restrict__ y,
             uint8_t *__restrict__ scales, T *__restrict__ h, float *__restrict__ rstd, const NormParams p)
@@ -56,28 +92,34 @@ norm_kernel(const T *__restrict__ x, const T *__restrict__ residual, const W *__
     __shared__ float red[row_block<TPR>() / 64];
     constexpr int kRowsPerBlock = row_block<TPR>() / TPR;
     const int t = int(threadIdx.x) % TPR;
-    const int64_t row = int64_t(blockIdx.x) * kRowsPerBlock + int(threadIdx.x) / TPR;
+    const int64_t row = int64_t(blockIdx.x) * kRowsPerBlock + __builtin_amdgcn_readfirstlane(int(threadIdx.x) / TPR);
     if (kRowsPerBlock > 1 && row >= p.rows) return;    // whole waves: no barrier follows
-    float v[NV][8];
+    const T *const xr = x + row * p.ldx, *const rr = residual + row * p.ldr;
+    T *const hr = h + row * p.ldh;
+    Eight<T> v[NV], r8[NV];
+    Eight<W> w[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * TPR + t) * 8, n = p.cols - c;
+        v[i].clear();
+        r8[i].clear();
+        w[i].clear();
+        if (n <= 0) continue;
+        v[i].template load<WHOLE>(xr, c, n);
+        if (residual) r8[i].template load<WHOLE>(rr, c, n);
+        w[i].template load<WHOLE>(weight, c, n);
+    }
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int c = (i * TPR + t) * 8, n = p.cols - c;
-        if (n > 0) {
-            load8(x + row * p.ldx + c, n, v[i]);
-            if (residual) {
-                float r[8];
-                load8(residual + row * p.ldr + c, n, r);
+        if (residual) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[i][e] = float(T(v[i][e] + r[e]));
-                store8(h + row * p.ldh + c, n, v[i]);
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
+            for (int e = 0; e < 8; ++e) v[i].v[e] = T(v[i].at(e) + r8[i].at(e));
+            if (n > 0) v[i].template store<WHOLE>(hr, c, n);
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum = fmaf(v[i][e], v[i][e], sum);
+        for (int e = 0; e < 8; ++e) sum = fmaf(v[i].at(e), v[i].at(e), sum);
     }
     sum = row_sum<TPR>(sum, red);
     const float r = 1.f / sqrtf(sum / float(p.cols) + p.eps);
@@ -85,26 +127,24 @@ norm_kernel(const T *__restrict__ x, const T *__restrict__ residual, const W *__
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int c = (i * TPR + t) * 8, n = p.cols - c;
-        float w[8] = {};
-        if (n > 0) load8(weight + c, n, w);
-        float amax = 0.f;
+        float o[8], amax = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            v[i][e] = v[i][e] * r * w[e];
-            amax = fmaxf(amax, finite_abs(v[i][e]));
+            o[e] = v[i].at(e) * r * w[i].at(e);
+            amax = fmaxf(amax, finite_abs(o[e]));
         }
         if constexpr (QUANT) {
             const int e = block_scale(lanes_max<16>(amax));
             const float s = power_of_two(254 - e);
             if (n > 0) {
                 i32x2 q;
-                q[0] = to_fp8x4(v[i][0] * s, v[i][1] * s, v[i][2] * s, v[i][3] * s);
-                q[1] = to_fp8x4(v[i][4] * s, v[i][5] * s, v[i][6] * s, v[i][7] * s);
+                q[0] = to_fp8x4(o[0] * s, o[1] * s, o[2] * s, o[3] * s);
+                q[1] = to_fp8x4(o[4] * s, o[5] * s, o[6] * s, o[7] * s);
                 *reinterpret_cast<i32x2 *>(static_cast<uint8_t *>(y) + row * p.ldy + c) = q;
                 if ((t & 15) == 0) scales[row * p.lds + c / kScaleBlock] = uint8_t(e);
             }
         } else if (n > 0) {
-            store8(static_cast<T *>(y) + row * p.ldy + c, n, v[i]);
+            store8(static_cast<T *>(y) + row * p.ldy + c, WHOLE ? 8 : n, o);
         }
     }
 }
@@ -121,55 +161,92 @@ struct NormGradParams {
     int cols;
 };
 
-template <typename T, typename W, int TPR, int NV>
-__global__ void __launch_bounds__(row_block<TPR>())
+// WHOLE: rows of a multiple of 8 elements. (Without the loads of single elements the wide
+// rows' 128 registers a thread are enough.)
+template <typename T, typename W, int TPR, int NV, bool WHOLE>
+__global__ void __launch_bounds__(row_block<TPR>(), NV == 1 && TPR > 64 ? 4 : 1)
 norm_grad_kernel(const T *__restrict__ dy, const T *__restrict__ h, const W *__restrict__ weight,
                  const float *__restrict__ rstd, const T *__restrict__ dh, T *__restrict__ dx, float *__restrict__ part,
                  const NormGradParams p)
 {
     constexpr int kRowsPerBlock = row_block<TPR>() / TPR;
-    __shared__ float red[row_block<TPR>() / 64];
-    const int t = int(threadIdx.x) % TPR, sub = int(threadIdx.x) / TPR;
-    float w[NV][8], dw[NV][8];
+    __shared__ float red[2][row_block<TPR>() / 64];
+    const int t = int(threadIdx.x) % TPR, sub = __builtin_amdgcn_readfirstlane(int(threadIdx.x) / TPR);
+    Eight<W> w[NV];
+    float dw[NV][8];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int c = (i * TPR + t) * 8, n = p.cols - c;
+        w[i].clear();
+        if (n > 0) w[i].template load<WHOLE>(weight, c, n);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[i][e] = dw[i][e] = 0.f;
-        if (n > 0) load8(weight + c, n, w[i]);
+        for (int e = 0; e < 8; ++e) dw[i][e] = 0.f;
     }
     const float inv = 1.f / float(p.cols);
-    for (int64_t row = int64_t(blockIdx.x) * kRowsPerBlock + sub; row < p.rows; row += int64_t(gridDim.x) * kRowsPerBlock) {
-        const float r = rstd[row];
-        float d[NV][8], n8[NV][8];
-        float sum = 0.f;
+    const int64_t step = int64_t(gridDim.x) * kRowsPerBlock, first = int64_t(blockIdx.x) * kRowsPerBlock + sub;
+    // The next row's elements are on their way while this one's are reduced; they stay as they
+    // were stored, in half the registers. What lies past the columns stays 0. (Two rows ahead:
+    // the same time.)
+    struct Row {
+        Eight<T> dy[NV], h[NV], dh[NV];
+        float r;
+    };
+    Row next;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (i * TPR + t) * 8, n = p.cols - c;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) d[i][e] = n8[i][e] = 0.f;
-            if (n > 0) {
-                load8(dy + row * p.lddy + c, n, d[i]);
-                load8(h + row * p.ldh + c, n, n8[i]);
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                n8[i][e] *= r;
-                dw[i][e] = fmaf(d[i][e], n8[i][e], dw[i][e]);
-                d[i][e] *= w[i][e];
-                sum = fmaf(d[i][e], n8[i][e], sum);
-            }
-        }
-        const float mean = row_sum<TPR>(sum, red) * inv;
+    for (int i = 0; i < NV; ++i) {
+        next.dy[i].clear();
+        next.h[i].clear();
+        next.dh[i].clear();
+    }
+    next.r = 0.f;
+    auto fetch = [&](int64_t row) {
+        if (row >= p.rows) return;
+        next.r = rstd[row];
+        const T *const dyr = dy + row * p.lddy, *const hr = h + row * p.ldh, *const dhr = dh + row * p.lddh;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (i * TPR + t) * 8, n = p.cols - c;
             if (n <= 0) continue;
-            float o[8] = {};
-            if (dh) load8(dh + row * p.lddh + c, n, o);
+            next.dy[i].template load<WHOLE>(dyr, c, n);
+            next.h[i].template load<WHOLE>(hr, c, n);
+            if (dh) next.dh[i].template load<WHOLE>(dhr, c, n);
+        }
+    };
+    fetch(first);
+    int turn = 0;
+    for (int64_t row = first; row < p.rows; row += step, turn ^= 1) {
+        const Row x = next;
+        fetch(row + step);
+        float sum = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = fmaf(r, d[i][e] - n8[i][e] * mean, o[e]);
-            store8(dx + row * p.lddx + c, n, o);
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float d = x.dy[i].at(e), n = x.h[i].at(e) * x.r;
+                dw[i][e] = fmaf(d, n, dw[i][e]);
+                sum = fmaf(d * w[i].at(e), n, sum);
+            }
+        sum = lanes_sum<64>(sum);
+        if constexpr (TPR > 64) {
+            // Two sets of sums in turn: a wave is at most one row ahead of the slowest.
+            if ((threadIdx.x & 63) == 0) red[turn][threadIdx.x >> 6] = sum;
+            wait_lds();
+            barrier();
+            sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < TPR / 64; ++i) sum += red[turn][i];
+        }
+        const float mean = sum * inv;
+        T *const out = dx + row * p.lddx;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * TPR + t) * 8, n = p.cols - c;
+            if (n <= 0) continue;
+            float o[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                o[e] = fmaf(x.r, x.dy[i].at(e) * w[i].at(e) - x.h[i].at(e) * x.r * mean, x.dh[i].at(e));
+            store8(out + uint32_t(c), WHOLE ? 8 : n, o);
         }
     }
     if (!part) return;
@@ -181,19 +258,26 @@ norm_grad_kernel(const T *__restrict__ dy, const T *__restrict__ h, const W *__r
     }
 }
 
-// dweight[c] = sum over `parts` rows of part: a block adds 64 columns, 4 threads a column.
+// dweight[c] = sum over `parts` rows of part: a block adds 32 columns, 32 threads a column.
 template <typename W>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(1024)
 norm_grad_weight_kernel(const float *__restrict__ part, W *__restrict__ dweight, int parts, int cols)
 {
-    __shared__ float red[256];
-    const int c = int(blockIdx.x) * 64 + int(threadIdx.x & 63);
+    __shared__ float red[32][33];
+    const int x = int(threadIdx.x & 31), y = int(threadIdx.x >> 5), c = int(blockIdx.x) * 32 + x;
     float sum = 0.f;
-    if (c < cols)
-        for (int i = int(threadIdx.x >> 6); i < parts; i += 4) sum += part[int64_t(i) * cols + c];
-    red[threadIdx.x] = sum;
+    if (c < cols) {
+#pragma unroll 8
+        for (int i = y; i < parts; i += 32) sum += part[int64_t(i) * cols + c];
+    }
+    red[y][x] = sum;
     __syncthreads();
-    if (threadIdx.x < 64 && c < cols) dweight[c] = W(red[threadIdx.x] + red[threadIdx.x + 64] + red[threadIdx.x + 128] + red[threadIdx.x + 192]);
+    // Column y of the block, its 32 sums across half a wave.
+    sum = red[x][y];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 32);
+    const int out = int(blockIdx.x) * 32 + y;
+    if (x == 0 && out < cols) dweight[out] = W(sum);
 }
 
 // ---------------------------------------------------------------------------
@@ -298,7 +382,7 @@ shift_to_fp8_kernel(const uint32_t *__restrict__ wp, uint8_t *__restrict__ y, in
 // ---------------------------------------------------------------------------
 
 // Threads and vectors per row: a wave holds rows of up to 1024 elements, four waves
-// up to 16384, sixteen up to 65536.
+// up to 2048, eight up to 8192, sixteen up to 65536.
 template <typename F>
 bool for_row_layout(int64_t cols, F &&f)
 {
@@ -307,9 +391,9 @@ bool for_row_layout(int64_t cols, F &&f)
     DS_TRY(64, 1);
     DS_TRY(64, 2);
     DS_TRY(256, 1);
-    DS_TRY(256, 2);
-    DS_TRY(256, 4);
-    DS_TRY(256, 8);
+    DS_TRY(512, 1);
+    DS_TRY(512, 2);
+    DS_TRY(1024, 2);
     DS_TRY(1024, 4);
     DS_TRY(1024, 8);
 #undef DS_TRY
@@ -405,7 +489,8 @@ extern "C" ds_status ds_rms_norm(const void *x, const void *residual, const void
         using W = decltype(w);
         for_row_layout(cols, [&](auto tpr, auto nv) {
             constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value;
-            const auto k = quant ? norm_kernel<T, W, TPR, NV, true> : norm_kernel<T, W, TPR, NV, false>;
+            const auto k = cols % 8 ? (quant ? norm_kernel<T, W, TPR, NV, true, false> : norm_kernel<T, W, TPR, NV, false, false>)
+                                    : (quant ? norm_kernel<T, W, TPR, NV, true, true> : norm_kernel<T, W, TPR, NV, false, true>);
             constexpr int block = row_block<TPR>(), per = block / TPR;
             hipLaunchKernelGGL(k, dim3(uint32_t((rows + per - 1) / per)), dim3(block), 0, static_cast<hipStream_t>(stream),
                                static_cast<const T *>(x), static_cast<const T *>(residual), static_cast<const W *>(weight), y,
@@ -455,13 +540,13 @@ extern "C" ds_status ds_rms_norm_backward(const void *dy, const void *h, const v
         if (rows > 0)
             for_row_layout(cols, [&](auto tpr, auto nv) {
                 constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value;
-                hipLaunchKernelGGL((norm_grad_kernel<T, W, TPR, NV>), dim3(blocks), dim3(row_block<TPR>()), 0, s,
-                                   static_cast<const T *>(dy), static_cast<const T *>(h), static_cast<const W *>(weight), rstd,
-                                   static_cast<const T *>(dh), static_cast<T *>(dx),
+                const auto k = cols % 8 ? norm_grad_kernel<T, W, TPR, NV, false> : norm_grad_kernel<T, W, TPR, NV, true>;
+                hipLaunchKernelGGL(k, dim3(blocks), dim3(row_block<TPR>()), 0, s, static_cast<const T *>(dy), static_cast<const T *>(h),
+                                   static_cast<const W *>(weight), rstd, static_cast<const T *>(dh), static_cast<T *>(dx),
                                    dweight ? static_cast<float *>(scratch) : nullptr, p);
             });
         if (dweight)
-            hipLaunchKernelGGL(norm_grad_weight_kernel<W>, dim3(uint32_t((cols + 63) / 64)), dim3(256), 0, s,
+            hipLaunchKernelGGL(norm_grad_weight_kernel<W>, dim3(uint32_t((cols + 31) / 32)), dim3(1024), 0, s,
                                static_cast<const float *>(scratch), static_cast<W *>(dweight), rows > 0 ? parts : 0, int(cols));
     });
     return launched("ds_rms_norm_backward");
