@@ -10,6 +10,7 @@
 #include <type_traits>
 
 #include "conv_plan.hpp"
+#include "fastdiv.hpp"
 #include "fp8.hpp"
 
 namespace ds {
@@ -25,18 +26,42 @@ struct AppendParams {
     const int *table, *start, *count;
     int64_t ldt;
     int columns, pages, tokens, heads, dim, page;
+    FastDiv vecs;                      // of a token's vector, 8 elements each
     int64_t sb[2], st[2], sh[2];       // strides of k and v: sequence, token, head
 };
 
+// The 8 x 4 bytes of tokens t .. t + 7 and dimensions d .. d + 3 turned around: out[i] holds
+// dimension d + i of the 8 tokens, first to last.
+__device__ __forceinline__ void turn(const uint32_t (&in)[8], uint64_t (&out)[4])
+{
+    uint32_t half[2][4];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const uint32_t *q = in + 4 * k;
+        // Bytes 0, 1 of two tokens, then 2, 3; then two pairs of tokens together.
+        const uint32_t lo0 = __builtin_amdgcn_perm(q[1], q[0], 0x05010400u), lo1 = __builtin_amdgcn_perm(q[3], q[2], 0x05010400u);
+        const uint32_t hi0 = __builtin_amdgcn_perm(q[1], q[0], 0x07030602u), hi1 = __builtin_amdgcn_perm(q[3], q[2], 0x07030602u);
+        half[k][0] = __builtin_amdgcn_perm(lo1, lo0, 0x05040100u);
+        half[k][1] = __builtin_amdgcn_perm(lo1, lo0, 0x07060302u);
+        half[k][2] = __builtin_amdgcn_perm(hi1, hi0, 0x05040100u);
+        half[k][3] = __builtin_amdgcn_perm(hi1, hi0, 0x07060302u);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = uint64_t(half[1][i]) << 32 | half[0][i];
+}
+
 // One page's new tokens of one head: its scale, the rounding of what it holds already
-// to a larger scale, and the tokens. Every (page, head) is one block's alone.
-template <typename T>
+// to a larger scale, and the tokens. Every (page, head) is one block's alone. A thread keeps
+// its first HELD vectors of 8 elements from the search for the scale (of 8 a page of 128 x 128
+// or 64 x 256 elements; 4 or 1 where that is all, for more blocks a CU); values go through
+// LDS, where they change from tokens to dimensions.
+template <typename T, int HELD>
 __global__ void __launch_bounds__(256)
 append_kernel(const T *__restrict__ k, const T *__restrict__ v, uint8_t *__restrict__ kc, uint8_t *__restrict__ vc,
               uint8_t *__restrict__ ks, uint8_t *__restrict__ vs, const AppendParams p, int touched)
 {
     __shared__ float red[4];
-    extern __shared__ uint8_t tile[];       // values: [token][dim + 4]
+    extern __shared__ __align__(16) uint8_t tile[];       // values: [token, from a multiple of 8 on][dim + 4]
     const int b = int(blockIdx.x) / touched, j = int(blockIdx.x) - b * touched, h = int(blockIdx.y), which = int(blockIdx.z);
     const int start = p.start[b], n = p.count ? min(p.count[b], p.tokens) : p.tokens;
     if (start < 0 || n <= 0) return;
@@ -50,16 +75,28 @@ append_kernel(const T *__restrict__ k, const T *__restrict__ v, uint8_t *__restr
     const int64_t st = p.st[which], at = int64_t(pid) * p.heads + h;
     uint8_t *cache = (which ? vc : kc) + at * p.page * p.dim, *scale = (which ? vs : ks) + at;
     const int D = p.dim, vecs = D / 8, total = (hi - lo) * vecs;
+    const int before = min(max(int(*scale), kCacheLow), kCacheHigh);
+    Eight<T> held[HELD];
+    auto load = [&](int i) {
+        Eight<T> x;
+        const int tok = fdiv(i, p.vecs);
+        x.template load<true>(src + tok * st, uint32_t(i - tok * vecs) * 8, 8);
+        return x;
+    };
     float amax = 0.f;
-    for (int i = threadIdx.x; i < total; i += 256) {
-        float x[8];
-        load8(src + (i / vecs) * st + (i % vecs) * 8, 8, x);
+    auto look = [&](const Eight<T> &x) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) amax = fmaxf(amax, finite_abs(x[e]));
-    }
+        for (int e = 0; e < 8; ++e) amax = fmaxf(amax, finite_abs(x.at(e)));
+    };
+#pragma unroll
+    for (int q = 0; q < HELD; ++q)
+        if (int(threadIdx.x) + q * 256 < total) held[q] = load(int(threadIdx.x) + q * 256);
+#pragma unroll
+    for (int q = 0; q < HELD; ++q)
+        if (int(threadIdx.x) + q * 256 < total) look(held[q]);
+    for (int i = int(threadIdx.x) + HELD * 256; i < total; i += 256) look(load(i));
     amax = lanes_max<64>(amax);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = amax;
-    const int before = min(max(int(*scale), kCacheLow), kCacheHigh);
     __syncthreads();
     amax = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
     int e = amax == 0.f ? kCacheLow : min(max(scale_byte(amax), kCacheLow), kCacheHigh);
@@ -75,42 +112,45 @@ append_kernel(const T *__restrict__ k, const T *__restrict__ v, uint8_t *__restr
         }
     }
     // A finite element beyond the largest scale's range is held as the largest number.
-    auto held = [&](float x) { return fabsf(x) < __builtin_inff() ? fminf(fmaxf(x * s, -448.f), 448.f) : __builtin_nanf(""); };
-    const int pitch = D + 4;
-    for (int i = threadIdx.x; i < total; i += 256) {
-        const int tok = i / vecs, d = (i % vecs) * 8;
-        float x[8];
-        load8(src + tok * st + d, 8, x);
+    auto fit = [&](float x) { return fabsf(x) < __builtin_inff() ? fminf(fmaxf(x * s, -448.f), 448.f) : __builtin_nanf(""); };
+    const int pitch = D + 4, skew = lo & 7;
+    auto put = [&](int i, const Eight<T> &x) {
+        const int tok = fdiv(i, p.vecs), d = (i - tok * vecs) * 8;
         i32x2 q;
-        q[0] = to_fp8x4(held(x[0]), held(x[1]), held(x[2]), held(x[3]));
-        q[1] = to_fp8x4(held(x[4]), held(x[5]), held(x[6]), held(x[7]));
+        q[0] = to_fp8x4(fit(x.at(0)), fit(x.at(1)), fit(x.at(2)), fit(x.at(3)));
+        q[1] = to_fp8x4(fit(x.at(4)), fit(x.at(5)), fit(x.at(6)), fit(x.at(7)));
         if (which) {
-            *reinterpret_cast<int *>(tile + tok * pitch + d) = q[0];
-            *reinterpret_cast<int *>(tile + tok * pitch + d + 4) = q[1];
+            *reinterpret_cast<int *>(tile + (skew + tok) * pitch + d) = q[0];
+            *reinterpret_cast<int *>(tile + (skew + tok) * pitch + d + 4) = q[1];
         } else {
-            *reinterpret_cast<i32x2 *>(cache + int64_t(lo + tok) * D + d) = q;
+            *reinterpret_cast<i32x2 *>(cache + (lo + tok) * D + d) = q;
         }
-    }
+    };
+#pragma unroll
+    for (int q = 0; q < HELD; ++q)
+        if (int(threadIdx.x) + q * 256 < total) put(int(threadIdx.x) + q * 256, held[q]);
+    for (int i = int(threadIdx.x) + HELD * 256; i < total; i += 256) put(i, load(i));
     if (threadIdx.x == 0) *scale = uint8_t(e);
     if (!which) return;
     __syncthreads();
-    // Four tokens of one dimension a thread, from the tile's columns.
-    const int q0 = lo / 4, quads = (hi + 3) / 4 - q0;
-    for (int i = threadIdx.x; i < quads * D; i += 256) {
-        const int d = i / quads, q = q0 + i % quads;
-        uint8_t *o = cache + int64_t(d) * p.page + 4 * q;
-        uint32_t w = 0;
+    // Eight tokens (an eighth's: what lies before lo or from hi on is not written) of four
+    // dimensions a thread.
+    const int first = lo / 8, eighths = (hi + 7) / 8 - first;
+    for (int i = threadIdx.x; i < eighths * (D / 4); i += 256) {
+        const int dg = i / eighths, t = i - dg * eighths, from = (first + t) * 8;
+        uint32_t in[8];
+        uint64_t out[4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int tok = 4 * q + t - lo;
-            if (tok >= 0 && tok < hi - lo) w |= uint32_t(tile[tok * pitch + d]) << (8 * t);
-        }
-        if (4 * q >= lo && 4 * q + 4 <= hi) {
-            *reinterpret_cast<uint32_t *>(o) = w;
-        } else {
+        for (int q = 0; q < 8; ++q) in[q] = *reinterpret_cast<const uint32_t *>(tile + (t * 8 + q) * pitch + dg * 4);
+        turn(in, out);
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
-                if (4 * q + t >= lo && 4 * q + t < hi) o[t] = uint8_t(w >> (8 * t));
+        for (int q = 0; q < 4; ++q) {
+            uint8_t *o = cache + (dg * 4 + q) * p.page + from;
+            if (from >= lo && from + 8 <= hi) {
+                *reinterpret_cast<uint64_t *>(o) = out[q];
+            } else {
+                for (int x = max(lo - from, 0); x < min(hi - from, 8); ++x) o[x] = uint8_t(out[q] >> (8 * x));
+            }
         }
     }
 }
@@ -834,7 +874,7 @@ extern "C" ds_status ds_kv_cache_append(const void *k, const void *v, uint8_t *k
     const int64_t es = float_bytes(type);
     if (!es) return fail(DS_ERR_INVALID_ARG, "type must be DS_TYPE_F32, DS_TYPE_F16 or DS_TYPE_BF16");
     if (batch == 0 || tokens == 0) return ok();
-    AppendParams p{table, start, count, ldt, int(columns), int(pages), int(tokens), int(heads), int(dim), int(page), {}, {}, {}};
+    AppendParams p{table, start, count, ldt, int(columns), int(pages), int(tokens), int(heads), int(dim), int(page), make_fastdiv(uint32_t(dim / 8)), {}, {}, {}};
     int64_t bytes[2];
     for (int i = 0; i < 2; ++i) {
         const int64_t *s = i ? v_strides : k_strides;
@@ -853,11 +893,14 @@ extern "C" ds_status ds_kv_cache_append(const void *k, const void *v, uint8_t *k
                                       {k_scales, sb, "k_scales", true}, {v_scales, sb, "v_scales", true}}))
         return st;
     const dim3 grid(uint32_t(batch * touched), uint32_t(heads), 2);
-    const size_t lds = size_t(std::min(page, tokens)) * size_t(dim + 4);
+    // (Tokens from a multiple of 8 to a multiple of 8.)
+    const size_t lds = size_t(std::min(page, (tokens + 14) / 8 * 8)) * size_t(dim + 4);
     const auto s = static_cast<hipStream_t>(stream);
     const auto go = [&](auto t) {
         using T = decltype(t);
-        hipLaunchKernelGGL(append_kernel<T>, grid, dim3(256), lds, s, static_cast<const T *>(k), static_cast<const T *>(v),
+        const int64_t each = (std::min(page, tokens) * dim / 8 + 255) / 256;
+        const auto kernel = each <= 1 ? append_kernel<T, 1> : each <= 4 ? append_kernel<T, 4> : append_kernel<T, 8>;
+        hipLaunchKernelGGL(kernel, grid, dim3(256), lds, s, static_cast<const T *>(k), static_cast<const T *>(v),
                            k_cache, v_cache, k_scales, v_scales, p, touched);
     };
     if (type == DS_TYPE_F32) go(float{});

@@ -90,8 +90,8 @@ __device__ __forceinline__ int to_fp8x4(float a, float b, float c, float d)
     return __builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true);
 }
 
-// Eight consecutive elements as floats. Rows may begin anywhere (16-byte loads need
-// no alignment on this machine); `n` < 8 reads the first n, the others are 0.
+// Eight consecutive elements as floats. Rows may begin anywhere (16-byte loads need no
+// alignment on this machine); `n` < 8 reads the first n, the others are 0.
 template <typename T>
 __device__ __forceinline__ void load8(const T *p, int n, float (&v)[8])
 {
@@ -105,6 +105,41 @@ __device__ __forceinline__ void load8(const T *p, int n, float (&v)[8])
         for (int i = 0; i < 8; ++i) v[i] = i < n ? float(p[i]) : 0.f;
     }
 }
+
+// Eight consecutive elements as they are stored.
+template <typename T>
+struct Eight {
+    T v[8];
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = T(0.f);
+    }
+    __device__ __forceinline__ float at(int i) const { return float(v[i]); }
+    // The first n (or all, as always where WHOLE) of those at p + at.
+    template <bool WHOLE>
+    __device__ __forceinline__ void load(const T *p, uint32_t at, int n)
+    {
+        if (WHOLE || n >= 8) {
+            __builtin_memcpy(v, p + at, sizeof v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < n) v[i] = p[at + i];
+        }
+    }
+    template <bool WHOLE>
+    __device__ __forceinline__ void store(T *p, uint32_t at, int n) const
+    {
+        if (WHOLE || n >= 8) {
+            __builtin_memcpy(p + at, v, sizeof v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < n) p[at + i] = v[i];
+        }
+    }
+};
 
 template <typename T>
 __device__ __forceinline__ void store8(T *p, int n, const float (&v)[8])

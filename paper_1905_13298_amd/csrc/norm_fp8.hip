@@ -44,41 +44,6 @@ __device__ __forceinline__ float row_sum(float v, float *red)
     return v;
 }
 
-// Eight consecutive elements as they are stored.
-template <typename T>
-struct Eight {
-    T v[8];
-    __device__ __forceinline__ void clear()
-    {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = T(0.f);
-    }
-    __device__ __forceinline__ float at(int i) const { return float(v[i]); }
-    // The first n (or all, as always where WHOLE) of those at p + at.
-    template <bool WHOLE>
-    __device__ __forceinline__ void load(const T *p, uint32_t at, int n)
-    {
-        if (WHOLE || n >= 8) {
-            __builtin_memcpy(v, p + at, sizeof v);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < n) v[i] = p[at + i];
-        }
-    }
-    template <bool WHOLE>
-    __device__ __forceinline__ void store(T *p, uint32_t at, int n) const
-    {
-        if (WHOLE || n >= 8) {
-            __builtin_memcpy(p + at, v, sizeof v);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < n) p[at + i] = v[i];
-        }
-    }
-};
-
 template <int TPR>
 constexpr int row_block() { return TPR < 256 ? 256 : TPR; }
 
@@ -382,7 +347,7 @@ shift_to_fp8_kernel(const uint32_t *__restrict__ wp, uint8_t *__restrict__ y, in
 // ---------------------------------------------------------------------------
 
 // Threads and vectors per row: a wave holds rows of up to 1024 elements, four waves
-// up to 2048, eight up to 8192, sixteen up to 65536.
+// up to 2048, eight up to 16384, sixteen up to 65536.
 template <typename F>
 bool for_row_layout(int64_t cols, F &&f)
 {
@@ -393,7 +358,7 @@ bool for_row_layout(int64_t cols, F &&f)
     DS_TRY(256, 1);
     DS_TRY(512, 1);
     DS_TRY(512, 2);
-    DS_TRY(1024, 2);
+    DS_TRY(512, 4);
     DS_TRY(1024, 4);
     DS_TRY(1024, 8);
 #undef DS_TRY
