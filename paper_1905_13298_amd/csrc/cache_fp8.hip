@@ -30,26 +30,6 @@ struct AppendParams {
     int64_t sb[2], st[2], sh[2];       // strides of k and v: sequence, token, head
 };
 
-// The 8 x 4 bytes of tokens t .. t + 7 and dimensions d .. d + 3 turned around: out[i] holds
-// dimension d + i of the 8 tokens, first to last.
-__device__ __forceinline__ void turn(const uint32_t (&in)[8], uint64_t (&out)[4])
-{
-    uint32_t half[2][4];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const uint32_t *q = in + 4 * k;
-        // Bytes 0, 1 of two tokens, then 2, 3; then two pairs of tokens together.
-        const uint32_t lo0 = __builtin_amdgcn_perm(q[1], q[0], 0x05010400u), lo1 = __builtin_amdgcn_perm(q[3], q[2], 0x05010400u);
-        const uint32_t hi0 = __builtin_amdgcn_perm(q[1], q[0], 0x07030602u), hi1 = __builtin_amdgcn_perm(q[3], q[2], 0x07030602u);
-        half[k][0] = __builtin_amdgcn_perm(lo1, lo0, 0x05040100u);
-        half[k][1] = __builtin_amdgcn_perm(lo1, lo0, 0x07060302u);
-        half[k][2] = __builtin_amdgcn_perm(hi1, hi0, 0x05040100u);
-        half[k][3] = __builtin_amdgcn_perm(hi1, hi0, 0x07060302u);
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) out[i] = uint64_t(half[1][i]) << 32 | half[0][i];
-}
-
 // One page's new tokens of one head: its scale, the rounding of what it holds already
 // to a larger scale, and the tokens. Every (page, head) is one block's alone. A thread keeps
 // its first HELD vectors of 8 elements from the search for the scale (of 8 a page of 128 x 128

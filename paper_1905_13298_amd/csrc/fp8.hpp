@@ -90,6 +90,25 @@ __device__ __forceinline__ int to_fp8x4(float a, float b, float c, float d)
     return __builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true);
 }
 
+// 8 rows of 4 bytes turned around: out[i] holds byte i of the 8 rows, first to last.
+__device__ __forceinline__ void turn(const uint32_t (&in)[8], uint64_t (&out)[4])
+{
+    uint32_t half[2][4];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const uint32_t *q = in + 4 * k;
+            // Bytes 0, 1 of two rows, then 2, 3; then two pairs of rows together.
+        const uint32_t lo0 = __builtin_amdgcn_perm(q[1], q[0], 0x05010400u), lo1 = __builtin_amdgcn_perm(q[3], q[2], 0x05010400u);
+        const uint32_t hi0 = __builtin_amdgcn_perm(q[1], q[0], 0x07030602u), hi1 = __builtin_amdgcn_perm(q[3], q[2], 0x07030602u);
+        half[k][0] = __builtin_amdgcn_perm(lo1, lo0, 0x05040100u);
+        half[k][1] = __builtin_amdgcn_perm(lo1, lo0, 0x07060302u);
+        half[k][2] = __builtin_amdgcn_perm(hi1, hi0, 0x05040100u);
+        half[k][3] = __builtin_amdgcn_perm(hi1, hi0, 0x07060302u);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = uint64_t(half[1][i]) << 32 | half[0][i];
+}
+
 // Eight consecutive elements as floats. Rows may begin anywhere (16-byte loads need no
 // alignment on this machine); `n` < 8 reads the first n, the others are 0.
 template <typename T>
@@ -178,6 +197,16 @@ __device__ __forceinline__ void wait_all()
 {
     asm volatile("" : : : "memory");
     __builtin_amdgcn_s_waitcnt(0x0070);      // vmcnt(0) lgkmcnt(0)
+    asm volatile("" : : : "memory");
+}
+
+// The same but for its last N loads.
+template <int N>
+__device__ __forceinline__ void wait_but()
+{
+    static_assert(N < 64, "what the counter holds");
+    asm volatile("" : : : "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | (N >> 4) << 14);
     asm volatile("" : : : "memory");
 }
 

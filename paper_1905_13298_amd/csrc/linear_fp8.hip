@@ -10,6 +10,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "conv_plan.hpp"
 #include "fp8.hpp"
@@ -40,6 +41,12 @@ __device__ __forceinline__ i32x4 row16(const uint8_t *row, int k, int cols)
         }
     }
     return v;
+}
+
+__device__ __forceinline__ i32x8 whole32(const uint8_t *p)
+{
+    const i32x4 a = *reinterpret_cast<const i32x4 *>(p), b = *reinterpret_cast<const i32x4 *>(p + 16);
+    return i32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
 }
 
 __device__ __forceinline__ i32x8 row32(const uint8_t *row, int k, int cols)
@@ -94,7 +101,7 @@ __device__ __forceinline__ f32x4 mma(i32x8 w, i32x8 x, f32x4 c, int ws, int xs)
 // w and MT x 16 rows of x; its waves take every WAVES-th block of 128 of the reduction
 // and add their sums in LDS. The weights are the instruction's first operand, so that a
 // lane ends up with four consecutive outputs of one row of y.
-template <typename O, int WF, int MT, int WAVES>
+template <typename O, int WF, int MT, int WAVES, int UNROLL>
 __global__ void __launch_bounds__(64 * WAVES)
 linear_rows_kernel(const LinearParams p)
 {
@@ -112,7 +119,30 @@ linear_rows_kernel(const LinearParams p)
         xsrow[t] = p.xs + m * p.ldxs;
         acc[t] = f32x4{};
     }
-    for (int b = wave; b < p.kblocks; b += WAVES) {
+    // UNROLL whole blocks at a time, their loads before their products; the block that ends
+    // past the columns by itself.
+    const int full = p.k / kScaleBlock;
+    int b = wave;
+    for (; b + (UNROLL - 1) * WAVES < full; b += UNROLL * WAVES) {
+        i32x8 w[UNROLL], x[UNROLL][MT];
+        int ws[UNROLL], xs[UNROLL][MT];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const int at = b + u * WAVES, k = at * kScaleBlock + g * 32;
+            w[u] = whole32(wrow + k);
+            ws[u] = wsrow[at];
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                x[u][t] = whole32(xrow[t] + k);
+                xs[u][t] = xsrow[t][at];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u)
+#pragma unroll
+            for (int t = 0; t < MT; ++t) acc[t] = mma<WF, sizeof(O) == 4>(w[u], x[u][t], acc[t], ws[u], xs[u][t]);
+    }
+    for (; b < p.kblocks; b += WAVES) {
         const int k = b * kScaleBlock + g * 32;
         const i32x8 w = row32(wrow, k, p.k);
         const int ws = wsrow[b];
@@ -162,14 +192,16 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const uint8_t *p, in
 // at a time, which go from memory to LDS without registers, one step ahead of the
 // products. A row's eight 16-byte pieces are kept in an order of its own, so that the
 // lanes of a read find theirs in different banks.
-template <typename O, int WF, int BN, int BM, int WN, int WM>
+template <typename O, int WF, int BN, int BM, int WN, int WM, int STAGES>
 __global__ void __launch_bounds__(64 * WN * WM, 1)
 linear_tile_kernel(const LinearParams p, int tiles_n, int tiles_m)
 {
     constexpr int kWaves = WN * WM, NT = BN / WN / 16, MT = BM / WM / 16;
     constexpr int kStage = (BN + BM) * 128, kLoadsW = BN / 8 / kWaves, kLoadsX = BM / 8 / kWaves, kGroup = 8;
-    __shared__ __align__(16) uint8_t lds[2 * kStage];
-    __shared__ uint32_t scales[2][BM + BN / 128];
+    static_assert((kLoadsW + kLoadsX) % 8 == 0, "eight at a time");
+    constexpr int kGroups = 16;                  // of 4 steps, whose scales are in LDS together
+    __shared__ __align__(16) uint8_t lds[STAGES * kStage];
+    __shared__ uint32_t scales[kGroups][BM + BN / 128];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), r = lane & 15, g = lane >> 4;
     // Blocks are dealt to the 8 XCDs in turn: each takes a run of tiles, kGroup rows of
     // tiles at a time, so that those in flight share their inputs in its L2.
@@ -205,34 +237,28 @@ linear_tile_kernel(const LinearParams p, int tiles_n, int tiles_m)
     auto fetch_end = [&](int step, int buf) {
         const int k = step * 128 + piece;
 #pragma unroll 1
-        for (int i = 0; i < kLoadsW + kLoadsX; ++i) {
-            const bool w = i < kLoadsW;
-            const int row = ((w ? i : i - kLoadsW) * kWaves + wave) * 8 + (lane >> 3);
-            const uint8_t *src = w ? wbase + min(row, p.n - 1 - n0) * p.ldw : xbase + min(row, p.m - 1 - m0) * p.ldx;
-            *reinterpret_cast<i32x4 *>(lds + buf * kStage + (w ? 0 : BN * 128) + row * 128 + (lane & 7) * 16) = row16(src, k, p.k);
+        for (int i0 = 0; i0 < kLoadsW + kLoadsX; i0 += 8) {
+            i32x4 v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int i = i0 + j, row = ((i < kLoadsW ? i : i - kLoadsW) * kWaves + wave) * 8 + (lane >> 3);
+                const uint8_t *src = i < kLoadsW ? wbase + min(row, p.n - 1 - n0) * p.ldw : xbase + min(row, p.m - 1 - m0) * p.ldx;
+                v[j] = row16(src, k, p.k);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                *reinterpret_cast<i32x4 *>(lds + buf * kStage + ((i0 + j) * kWaves + wave) * 1024 + lane * 16) = v[j];
         }
     };
-    // The scales of four steps of the block's rows, a thread a row (of w's, by 128): read
-    // four steps ahead, in LDS from the step before their first.
-    constexpr int kScaleRows = BM + BN / 128;
-    static_assert(kScaleRows <= 2 * 64 * kWaves, "two rows a thread at most");
-    const uint8_t *srow[2];
-    uint32_t ahead4[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int row = int(threadIdx.x) + i * 64 * kWaves;
-        srow[i] = row < BM ? p.xs + min(m0 + row, p.m - 1) * p.ldxs : p.ws + min(n0 / 128 + row - BM, (p.n - 1) / 128) * p.ldws;
-    }
-    auto scale_row = [&](int i) { return i == 0 ? kScaleRows >= 64 * kWaves || int(threadIdx.x) < kScaleRows : int(threadIdx.x) + 64 * kWaves < kScaleRows; };
+    // The scales of the block's rows (of w's, by 128) for 64 steps from `step` on, four a word.
     auto fetch_scales = [&](int step) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-            if (scale_row(i)) ahead4[i] = load_scales4(srow[i], step, p.kblocks);
-    };
-    auto keep_scales = [&](int step) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-            if (scale_row(i)) scales[(step >> 2) & 1][threadIdx.x + i * 64 * kWaves] = place_scales4(ahead4[i], step, p.kblocks);
+        constexpr int kRows = BM + BN / 128;
+        const int groups = min(kGroups, (p.kblocks - step + 3) / 4);
+        for (int i = threadIdx.x; i < kRows * groups; i += 64 * kWaves) {
+            const int gr = i / kRows, row = i - gr * kRows, at = step + 4 * gr;
+            const uint8_t *src = row < BM ? p.xs + min(m0 + row, p.m - 1) * p.ldxs : p.ws + min(n0 / 128 + row - BM, (p.n - 1) / 128) * p.ldws;
+            scales[gr][row] = place_scales4(load_scales4(src, at, p.kblocks), at, p.kblocks);
+        }
     };
     uint32_t xs[MT], ws;
     f32x4 acc[NT][MT];
@@ -246,11 +272,9 @@ linear_tile_kernel(const LinearParams p, int tiles_n, int tiles_m)
         if (step < full) fetch(step, buf);
         else if (step < p.kblocks) fetch_end(step, buf);
     };
+#pragma unroll
+    for (int i = 0; i < STAGES; ++i) stage(i, i);
     fetch_scales(0);
-    stage(0, 0);
-    stage(1, 1);
-    keep_scales(0);
-    if (p.kblocks > 4) fetch_scales(4);
     wait_all();
     barrier();
     const int so = r * 128 + (g ^ (r >> 1)) * 16, s1 = so ^ 64;      // pieces g and g + 4
@@ -269,19 +293,20 @@ linear_tile_kernel(const LinearParams p, int tiles_n, int tiles_m)
     // sent for, and each of the last products is followed by the read of the next step's
     // weights into the registers that it leaves.
     for (int step = 0; step < p.kblocks; ++step) {
-        const int buf = step & 1;
+        const int buf = step % STAGES, following = buf + 1 < STAGES ? buf + 1 : 0;
         if ((step & 3) == 0) {
-            const uint32_t *from = scales[(step >> 2) & 1];
+            if ((step & (4 * kGroups - 1)) == 0 && step > 0) {
+                barrier();
+                fetch_scales(step);
+                wait_lds();
+                barrier();
+            }
+            const uint32_t *from = scales[(step >> 2) & (kGroups - 1)];
 #pragma unroll
             for (int t = 0; t < MT; ++t) xs[t] = from[(wm * MT + t) * 16 + r];
             ws = from[BM + wn * NT / 8];
         }
-        // The next four steps' before the barrier that precedes their first.
-        if ((step & 3) == 2 && step + 2 < p.kblocks) {
-            keep_scales(step + 2);
-            if (step + 6 < p.kblocks) fetch_scales(step + 6);
-        }
-        const uint8_t *const xb = xt + buf * kStage, *const wnext = wt + (buf ^ 1) * kStage;
+        const uint8_t *const xb = xt + buf * kStage, *const wnext = wt + following * kStage;
 #pragma unroll
         for (int b = 0; b + 1 < MT; ++b) {
             const i32x8 ahead = frag(xb, b + 1);
@@ -291,12 +316,16 @@ linear_tile_kernel(const LinearParams p, int tiles_n, int tiles_m)
             __builtin_amdgcn_sched_barrier(0);
         }
         if (step + 1 < p.kblocks) {
-            wait_all();
+            // The transfers of the steps behind the next one may be on their way.
+            const int behind = STAGES > 2 ? min(step + STAGES, full) - step - 2 : 0;
+            if (STAGES > 3 && behind >= 2) wait_but<2 * (kLoadsW + kLoadsX)>();
+            else if (STAGES > 2 && behind >= 1) wait_but<kLoadsW + kLoadsX>();
+            else wait_all();
             barrier();
-            stage(step + 2, buf);
+            stage(step + STAGES, buf);
         }
         // (After the last step these reads are of LDS that nothing uses any more.)
-        const i32x8 ahead = frag(xt + (buf ^ 1) * kStage, 0);
+        const i32x8 ahead = frag(xt + following * kStage, 0);
 #pragma unroll
         for (int a = 0; a < NT; ++a) {
             acc[a][MT - 1] = mma<WF, sizeof(O) == 4>(wf[a], x, acc[a][MT - 1], int(ws), int(xs[MT - 1]));
@@ -333,43 +362,39 @@ linear_tile_kernel(const LinearParams p, int tiles_n, int tiles_m)
     }
 }
 
-// w8 [n][k] to [k][n] (rows of ldt bytes, filled up with zeros): 64 x 64 bytes a block.
+// w8 [n][k] to [k][n] (rows of ldt bytes, filled up with zeros) and its scales [n / 128][k /
+// 128] to [k / 128][blocks of n]: 128 x 64 bytes a block, 8 x 4 of them a thread.
 __global__ void __launch_bounds__(256)
-transpose8_kernel(const uint8_t *__restrict__ w, uint8_t *__restrict__ t, int n, int k, int64_t ldw, int64_t ldt)
+transpose8_kernel(const uint8_t *__restrict__ w, const uint8_t *__restrict__ ws, uint8_t *__restrict__ t, uint8_t *__restrict__ ts, int n,
+                  int k, int64_t ldw, int64_t ldws, int64_t ldt)
 {
-    __shared__ uint8_t tile[64][68];
-    const int k0 = int(blockIdx.x) * 64, n0 = int(blockIdx.y) * 64;
-    const int row = int(threadIdx.x >> 2), piece = int(threadIdx.x & 3) * 16;
-    i32x4 v{};
-    if (n0 + row < n) v = row16(w + (n0 + row) * ldw, k0 + piece, k);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) *reinterpret_cast<int *>(&tile[row][piece + 4 * i]) = v[i];
-    __syncthreads();
-    if (k0 + row >= k || n0 + piece >= ldt) return;
-    i32x4 o;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        uint32_t word = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) word |= uint32_t(tile[piece + 4 * i + j][row]) << (8 * j);
-        o[i] = int(word);
+    __shared__ __align__(16) uint8_t tile[128][68];
+    const int k0 = int(blockIdx.x) * 64, n0 = int(blockIdx.y) * 128, row = int(threadIdx.x >> 1), piece = int(threadIdx.x & 1) * 32;
+    i32x4 v[2] = {};
+    if (n0 + row < n) {
+        v[0] = row16(w + (n0 + row) * ldw, k0 + piece, k);
+        v[1] = row16(w + (n0 + row) * ldw, k0 + piece + 16, k);
     }
-    *reinterpret_cast<i32x4 *>(t + (k0 + row) * ldt + n0 + piece) = o;
+    if (threadIdx.x == 0 && k0 % 128 == 0) ts[k0 / 128 * int64_t(gridDim.y) + blockIdx.y] = ws[blockIdx.y * ldws + k0 / 128];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) *reinterpret_cast<int *>(&tile[row][piece + 4 * i]) = v[i / 4][i % 4];
+    __syncthreads();
+    const int ng = int(threadIdx.x & 15) * 8, kg = int(threadIdx.x >> 4) * 4;
+    uint32_t in[8];
+    uint64_t out[4];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) in[i] = *reinterpret_cast<const uint32_t *>(&tile[ng + i][kg]);
+    turn(in, out);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (k0 + kg + i < k && n0 + ng < ldt) *reinterpret_cast<uint64_t *>(t + (k0 + kg + i) * ldt + n0 + ng) = out[i];
 }
 
-// The weights' scales [rows][cols] to [cols][rows].
-__global__ void __launch_bounds__(256)
-transpose_scales_kernel(const uint8_t *__restrict__ s, uint8_t *__restrict__ t, int rows, int cols, int64_t lds)
-{
-    const int i = int(blockIdx.x) * 256 + int(threadIdx.x);
-    if (i < rows * cols) t[(i % cols) * rows + i / cols] = s[(i / cols) * lds + i % cols];
-}
-
-template <typename O, int WF, int BN, int BM, int WN, int WM>
+template <typename O, int WF, int BN, int BM, int WN, int WM, int STAGES>
 void run_tiles(const LinearParams &p, hipStream_t s)
 {
     const int tn = (p.n + BN - 1) / BN, tm = (p.m + BM - 1) / BM;
-    hipLaunchKernelGGL((linear_tile_kernel<O, WF, BN, BM, WN, WM>), dim3(uint32_t((int64_t(tn) * tm + 7) / 8 * 8)), dim3(64 * WN * WM), 0, s, p, tn, tm);
+    hipLaunchKernelGGL((linear_tile_kernel<O, WF, BN, BM, WN, WM, STAGES>), dim3(uint32_t((int64_t(tn) * tm + 7) / 8 * 8)), dim3(64 * WN * WM), 0, s, p, tn, tm);
 }
 
 template <typename O, int WF>
@@ -378,16 +403,21 @@ void run_linear(const LinearParams &p, hipStream_t s)
     // The tiles' 32-bit offsets reach 256 rows.
     const bool reach = p.ldx <= (1 << 22) && p.ldw <= (1 << 22);
     if (p.m > 64 && reach) {
-        const int64_t t256 = int64_t((p.n + 255) / 256) * ((p.m + 255) / 256);
+        const int64_t t256 = int64_t((p.n + 255) / 256) * ((p.m + 255) / 256), t128 = int64_t((p.n + 127) / 128) * ((p.m + 127) / 128);
         if constexpr (sizeof(O) == 2) {
-            if (t256 >= 192) return run_tiles<O, WF, 256, 256, 2, 2>(p, s);
+            if (t256 >= 192) return run_tiles<O, WF, 256, 256, 2, 2, 2>(p, s);
         }
-        return run_tiles<O, WF, 128, 128, 2, 2>(p, s);
+        if (t128 <= 256) return run_tiles<O, WF, 128, 128, 2, 2, 4>(p, s);
+        return run_tiles<O, WF, 128, 128, 2, 2, 2>(p, s);
     }
-    const bool one = p.m <= 16;
-    const dim3 grid(uint32_t((p.n + 15) / 16), uint32_t((p.m + (one ? 15 : 63)) / (one ? 16 : 64)));
-    const auto k = one ? linear_rows_kernel<O, WF, 1, 8> : linear_rows_kernel<O, WF, 4, 8>;
-    hipLaunchKernelGGL(k, grid, dim3(512), 0, s, p);
+    const auto rows = [&](auto mt, auto waves, auto unroll) {
+        constexpr int MT = decltype(mt)::value, WAVES = decltype(waves)::value, UNROLL = decltype(unroll)::value;
+        const dim3 grid(uint32_t((p.n + 15) / 16), uint32_t((p.m + 16 * MT - 1) / (16 * MT)));
+        hipLaunchKernelGGL((linear_rows_kernel<O, WF, MT, WAVES, UNROLL>), grid, dim3(64 * WAVES), 0, s, p);
+    };
+    if (p.m <= 16) rows(std::integral_constant<int, 1>{}, std::integral_constant<int, 8>{}, std::integral_constant<int, 4>{});
+    else if (p.m <= 32) rows(std::integral_constant<int, 2>{}, std::integral_constant<int, 8>{}, std::integral_constant<int, 2>{});
+    else rows(std::integral_constant<int, 4>{}, std::integral_constant<int, 8>{}, std::integral_constant<int, 2>{});
 }
 
 template <typename O>
@@ -481,10 +511,10 @@ extern "C" ds_status ds_linear_fp8_backward_data(const uint8_t *dy8, const uint8
     const auto s = static_cast<hipStream_t>(stream);
     const int64_t ldt = up(n, 16);
     uint8_t *wt = static_cast<uint8_t *>(scratch), *wst = wt + up(k * ldt, 256);
-    const int nb = int(blocks_of(n)), kb = int(blocks_of(k));
-    hipLaunchKernelGGL(transpose8_kernel, dim3(uint32_t((k + 63) / 64), uint32_t((n + 63) / 64)), dim3(256), 0, s, w8, wt,
-                       int(n), int(k), ldw, ldt);
-    hipLaunchKernelGGL(transpose_scales_kernel, dim3(uint32_t((nb * kb + 255) / 256)), dim3(256), 0, s, w_scales, wst, nb, kb, ldws);
+    const int nb = int(blocks_of(n));
+    if (nb > 65535) return fail(DS_ERR_UNSUPPORTED, "more than 65535 x 128 rows of w8");
+    hipLaunchKernelGGL(transpose8_kernel, dim3(uint32_t((k + 63) / 64), uint32_t(nb)), dim3(256), 0, s, w8, w_scales, wt, wst, int(n), int(k),
+                       ldw, ldws, ldt);
     const LinearParams p{dy8, dy_scales, wt, wst, nullptr, dx, int(m), int(k), int(n), nb, lddy, lddys, ldt, int64_t(nb), lddx};
     launch(p, w_type, dx_type, s);
     return launched("ds_linear_fp8_backward_data");
