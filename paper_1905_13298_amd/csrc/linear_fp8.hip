@@ -82,7 +82,8 @@ __device__ __forceinline__ f16x8 widen(i32x8 v, int i)
 // the largest of them and drops what lies 2^-14 below it, which an output of 16 bits does
 // not show and one of 32 does: such an output (FULL) is formed from the same numbers as
 // 16-bit floats, whose products and sums keep 24 bits, the scales applied afterwards.
-template <int WF, bool FULL>
+// The scales are byte BYTE of ws and xs.
+template <int WF, bool FULL, int BYTE = 0>
 __device__ __forceinline__ f32x4 mma(i32x8 w, i32x8 x, f32x4 c, int ws, int xs)
 {
     if constexpr (FULL) {
@@ -90,78 +91,10 @@ __device__ __forceinline__ f32x4 mma(i32x8 w, i32x8 x, f32x4 c, int ws, int xs)
 #pragma unroll
         for (int i = 0; i < 4; ++i) part = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen<WF>(w, i), widen<0>(x, i), part, 0, 0, 0);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) c[i] += ldexpf(part[i], (ws & 255) + (xs & 255) - 254);
+        for (int i = 0; i < 4; ++i) c[i] += ldexpf(part[i], (ws >> (8 * BYTE) & 255) + (xs >> (8 * BYTE) & 255) - 254);
         return c;
     } else {
-        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, c, WF, 0, 0, ws, 0, xs);
-    }
-}
-
-// Few rows of x: the weights go from memory to registers, once. A block takes 16 rows of
-// w and MT x 16 rows of x; its waves take every WAVES-th block of 128 of the reduction
-// and add their sums in LDS. The weights are the instruction's first operand, so that a
-// lane ends up with four consecutive outputs of one row of y.
-template <typename O, int WF, int MT, int WAVES, int UNROLL>
-__global__ void __launch_bounds__(64 * WAVES)
-linear_rows_kernel(const LinearParams p)
-{
-    __shared__ f32x4 sums[WAVES][MT][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-    const int n0 = int(blockIdx.x) * 16, m0 = int(blockIdx.y) * 16 * MT;
-    const uint8_t *wrow = p.w + int64_t(min(n0 + r, p.n - 1)) * p.ldw;
-    const uint8_t *wsrow = p.ws + int64_t(n0 / kScaleBlock) * p.ldws;
-    const uint8_t *xrow[MT], *xsrow[MT];
-    f32x4 acc[MT];
-#pragma unroll
-    for (int t = 0; t < MT; ++t) {
-        const int64_t m = min(m0 + t * 16 + r, p.m - 1);
-        xrow[t] = p.x + m * p.ldx;
-        xsrow[t] = p.xs + m * p.ldxs;
-        acc[t] = f32x4{};
-    }
-    // UNROLL whole blocks at a time, their loads before their products; the block that ends
-    // past the columns by itself.
-    const int full = p.k / kScaleBlock;
-    int b = wave;
-    for (; b + (UNROLL - 1) * WAVES < full; b += UNROLL * WAVES) {
-        i32x8 w[UNROLL], x[UNROLL][MT];
-        int ws[UNROLL], xs[UNROLL][MT];
-#pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            const int at = b + u * WAVES, k = at * kScaleBlock + g * 32;
-            w[u] = whole32(wrow + k);
-            ws[u] = wsrow[at];
-#pragma unroll
-            for (int t = 0; t < MT; ++t) {
-                x[u][t] = whole32(xrow[t] + k);
-                xs[u][t] = xsrow[t][at];
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < UNROLL; ++u)
-#pragma unroll
-            for (int t = 0; t < MT; ++t) acc[t] = mma<WF, sizeof(O) == 4>(w[u], x[u][t], acc[t], ws[u], xs[u][t]);
-    }
-    for (; b < p.kblocks; b += WAVES) {
-        const int k = b * kScaleBlock + g * 32;
-        const i32x8 w = row32(wrow, k, p.k);
-        const int ws = wsrow[b];
-#pragma unroll
-        for (int t = 0; t < MT; ++t) acc[t] = mma<WF, sizeof(O) == 4>(w, row32(xrow[t], k, p.k), acc[t], ws, xsrow[t][b]);
-    }
-#pragma unroll
-    for (int t = 0; t < MT; ++t) sums[wave][t][lane] = acc[t];
-    __syncthreads();
-    for (int t = wave; t < MT; t += WAVES) {
-        f32x4 s = sums[0][t][lane];
-#pragma unroll
-        for (int i = 1; i < WAVES; ++i) s += sums[i][t][lane];
-        const int m = m0 + t * 16 + r, n = n0 + g * 4;
-        if (m >= p.m) continue;
-        O *y = static_cast<O *>(p.y) + m * p.ldy + n;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (n + i < p.n) y[i] = O(s[i] + (p.bias ? p.bias[n + i] : 0.f));
+        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, c, WF, 0, BYTE, ws, BYTE, xs);
     }
 }
 
@@ -183,6 +116,79 @@ __device__ __forceinline__ uint32_t place_scales4(uint32_t v, int b, int blocks)
     return blocks >= 4 ? v >> (8 * max(b - (blocks - 4), 0)) : v;
 }
 
+// Few rows of x: the weights go from memory to registers, once. A block takes 16 rows of
+// w and MT x 16 rows of x; each of its waves takes a share of the reduction, in blocks of 128,
+// and they add their sums in LDS. The weights are the instruction's first operand, so that a
+// lane ends up with four consecutive outputs of one row of y.
+template <typename O, int WF, int MT, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES)
+linear_rows_kernel(const LinearParams p)
+{
+    __shared__ f32x4 sums[WAVES][MT][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+    const int n0 = int(blockIdx.x) * 16, m0 = int(blockIdx.y) * 16 * MT;
+    const uint8_t *wrow = p.w + int64_t(min(n0 + r, p.n - 1)) * p.ldw;
+    const uint8_t *wsrow = p.ws + int64_t(n0 / kScaleBlock) * p.ldws;
+    const uint8_t *xrow[MT], *xsrow[MT];
+    f32x4 acc[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        const int64_t m = min(m0 + t * 16 + r, p.m - 1);
+        xrow[t] = p.x + m * p.ldx;
+        xsrow[t] = p.xs + m * p.ldxs;
+        acc[t] = f32x4{};
+    }
+    // Four whole blocks at a time, their loads before their products and their scales as one
+    // word (bytes by themselves took a fifth of the time at 64 rows); others one by one.
+    const int full = p.k / kScaleBlock, each = (p.kblocks + WAVES - 1) / WAVES, end = min(p.kblocks, (wave + 1) * each);
+    for (int b = wave * each; b < end;) {
+        if (b + 4 <= min(end, full)) {
+            i32x8 w[4], x[4][MT];
+            uint32_t ws = load_scales4(wsrow, b, p.kblocks), xs[MT];
+#pragma unroll
+            for (int t = 0; t < MT; ++t) xs[t] = load_scales4(xsrow[t], b, p.kblocks);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int k = (b + u) * kScaleBlock + g * 32;
+                w[u] = whole32(wrow + k);
+#pragma unroll
+                for (int t = 0; t < MT; ++t) x[u][t] = whole32(xrow[t] + k);
+            }
+            ws = place_scales4(ws, b, p.kblocks);
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                const uint32_t s = place_scales4(xs[t], b, p.kblocks);
+                acc[t] = mma<WF, sizeof(O) == 4, 0>(w[0], x[0][t], acc[t], int(ws), int(s));
+                acc[t] = mma<WF, sizeof(O) == 4, 1>(w[1], x[1][t], acc[t], int(ws), int(s));
+                acc[t] = mma<WF, sizeof(O) == 4, 2>(w[2], x[2][t], acc[t], int(ws), int(s));
+                acc[t] = mma<WF, sizeof(O) == 4, 3>(w[3], x[3][t], acc[t], int(ws), int(s));
+            }
+            b += 4;
+        } else {
+            const int k = b * kScaleBlock + g * 32;
+            const i32x8 w = row32(wrow, k, p.k);
+            const int ws = wsrow[b];
+#pragma unroll
+            for (int t = 0; t < MT; ++t) acc[t] = mma<WF, sizeof(O) == 4>(w, row32(xrow[t], k, p.k), acc[t], ws, xsrow[t][b]);
+            ++b;
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < MT; ++t) sums[wave][t][lane] = acc[t];
+    __syncthreads();
+    for (int t = wave; t < MT; t += WAVES) {
+        f32x4 s = sums[0][t][lane];
+#pragma unroll
+        for (int i = 1; i < WAVES; ++i) s += sums[i][t][lane];
+        const int m = m0 + t * 16 + r, n = n0 + g * 4;
+        if (m >= p.m) continue;
+        O *y = static_cast<O *>(p.y) + m * p.ldy + n;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (n + i < p.n) y[i] = O(s[i] + (p.bias ? p.bias[n + i] : 0.f));
+    }
+}
+
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const uint8_t *p, int64_t bytes)
 {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p), 0, int(bytes), 0x00020000);
@@ -198,7 +204,7 @@ linear_tile_kernel(const LinearParams p, int tiles_n, int tiles_m)
 {
     constexpr int kWaves = WN * WM, NT = BN / WN / 16, MT = BM / WM / 16;
     constexpr int kStage = (BN + BM) * 128, kLoadsW = BN / 8 / kWaves, kLoadsX = BM / 8 / kWaves, kGroup = 8;
-    static_assert((kLoadsW + kLoadsX) % 8 == 0, "eight at a time");
+    static_assert((kLoadsW + kLoadsX) % 4 == 0, "four at a time");
     constexpr int kGroups = 16;                  // of 4 steps, whose scales are in LDS together
     __shared__ __align__(16) uint8_t lds[STAGES * kStage];
     __shared__ uint32_t scales[kGroups][BM + BN / 128];
@@ -237,16 +243,16 @@ linear_tile_kernel(const LinearParams p, int tiles_n, int tiles_m)
     auto fetch_end = [&](int step, int buf) {
         const int k = step * 128 + piece;
 #pragma unroll 1
-        for (int i0 = 0; i0 < kLoadsW + kLoadsX; i0 += 8) {
-            i32x4 v[8];
+        for (int i0 = 0; i0 < kLoadsW + kLoadsX; i0 += 4) {
+            i32x4 v[4];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < 4; ++j) {
                 const int i = i0 + j, row = ((i < kLoadsW ? i : i - kLoadsW) * kWaves + wave) * 8 + (lane >> 3);
                 const uint8_t *src = i < kLoadsW ? wbase + min(row, p.n - 1 - n0) * p.ldw : xbase + min(row, p.m - 1 - m0) * p.ldx;
                 v[j] = row16(src, k, p.k);
             }
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
+            for (int j = 0; j < 4; ++j)
                 *reinterpret_cast<i32x4 *>(lds + buf * kStage + ((i0 + j) * kWaves + wave) * 1024 + lane * 16) = v[j];
         }
     };
@@ -254,6 +260,7 @@ linear_tile_kernel(const LinearParams p, int tiles_n, int tiles_m)
     auto fetch_scales = [&](int step) {
         constexpr int kRows = BM + BN / 128;
         const int groups = min(kGroups, (p.kblocks - step + 3) / 4);
+#pragma unroll 4
         for (int i = threadIdx.x; i < kRows * groups; i += 64 * kWaves) {
             const int gr = i / kRows, row = i - gr * kRows, at = step + 4 * gr;
             const uint8_t *src = row < BM ? p.xs + min(m0 + row, p.m - 1) * p.ldxs : p.ws + min(n0 / 128 + row - BM, (p.n - 1) / 128) * p.ldws;
@@ -407,17 +414,17 @@ void run_linear(const LinearParams &p, hipStream_t s)
         if constexpr (sizeof(O) == 2) {
             if (t256 >= 192) return run_tiles<O, WF, 256, 256, 2, 2, 2>(p, s);
         }
-        if (t128 <= 256) return run_tiles<O, WF, 128, 128, 2, 2, 4>(p, s);
+        if (t128 <= 256) return run_tiles<O, WF, 128, 128, 2, 4, 4>(p, s);
         return run_tiles<O, WF, 128, 128, 2, 2, 2>(p, s);
     }
-    const auto rows = [&](auto mt, auto waves, auto unroll) {
-        constexpr int MT = decltype(mt)::value, WAVES = decltype(waves)::value, UNROLL = decltype(unroll)::value;
+    const auto rows = [&](auto mt) {
+        constexpr int MT = decltype(mt)::value, WAVES = 8;
         const dim3 grid(uint32_t((p.n + 15) / 16), uint32_t((p.m + 16 * MT - 1) / (16 * MT)));
-        hipLaunchKernelGGL((linear_rows_kernel<O, WF, MT, WAVES, UNROLL>), grid, dim3(64 * WAVES), 0, s, p);
+        hipLaunchKernelGGL((linear_rows_kernel<O, WF, MT, WAVES>), grid, dim3(64 * WAVES), 0, s, p);
     };
-    if (p.m <= 16) rows(std::integral_constant<int, 1>{}, std::integral_constant<int, 8>{}, std::integral_constant<int, 4>{});
-    else if (p.m <= 32) rows(std::integral_constant<int, 2>{}, std::integral_constant<int, 8>{}, std::integral_constant<int, 2>{});
-    else rows(std::integral_constant<int, 4>{}, std::integral_constant<int, 8>{}, std::integral_constant<int, 2>{});
+    if (p.m <= 16) rows(std::integral_constant<int, 1>{});
+    else if (p.m <= 32) rows(std::integral_constant<int, 2>{});
+    else rows(std::integral_constant<int, 4>{});
 }
 
 template <typename O>
