@@ -15,7 +15,7 @@ import math
 import numpy as np
 import torch
 
-from ._native import DeepShiftError, call, lib
+from ._native import DeepShiftError, call, check, lib
 
 __all__ = ["DeepShiftError", "code_bits_flag", "describe_conv2d", "packed_row_words", "pack_shift_weights", "unpack_shift_weights",
            "linear_shift", "conv2d_shift", "linear_mul_i32", "conv2d_mul_i32", "out_size",
@@ -132,7 +132,8 @@ def _ptr(t):
 
 
 def _stream(dev: torch.device) -> int:
-    return torch.cuda.current_stream(dev).cuda_stream
+    # (What torch.cuda.current_stream(dev).cuda_stream returns, without an object: 0.1 us for 1.9.)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if dev.index is None else dev.index)
 
 
 class _on:
@@ -783,6 +784,23 @@ class JitConvMul(JitConv):
 _TYPE = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.float8_e4m3fn: 3, torch.float8_e5m2: 4}
 _FLOATS = (torch.bfloat16, torch.float16, torch.float32)
 _E4M3, _E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+_functions = {}
+
+
+def _launch(name: str, dev: torch.device, *args) -> None:
+    """Calls entry point `name` with the current stream of `dev` as its last argument. A decoded token's calls take
+    as long as the host does, so nothing is looked up twice and the device is set only where it is another."""
+    fn = _functions.get(name)
+    if fn is None:
+        fn = _functions[name] = getattr(lib(), name)
+    index = dev.index
+    if index == torch._C._cuda_getDevice():
+        status = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+    else:
+        with torch.cuda.device(dev):
+            status = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+    if status:
+        check(status)
 
 
 def _dev_as(t, name: str, dtypes, shape=None):
@@ -791,31 +809,37 @@ def _dev_as(t, name: str, dtypes, shape=None):
         raise TypeError(f"{name} must be a device tensor")
     if t.dtype not in dtypes:
         raise TypeError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     return t
 
 
 def _rows(t, name: str, dtypes, shape=None):
-    """t as a matrix whose rows' elements are consecutive, and its row stride."""
+    """The row stride of a matrix whose rows' elements are consecutive."""
     _dev_as(t, name, dtypes, shape)
     if t.dim() != 2:
         raise ValueError(f"{name} must have two dimensions")
-    if t.stride(1) != 1 and t.shape[1] > 1:
+    rows, cols = t.shape
+    ld, one = t.stride()
+    if one != 1 and cols > 1:
         raise ValueError(f"the elements of a row of {name} must be consecutive")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    return ld if rows > 1 or ld > cols else cols
+
+
+def _vector(t, name: str, dtypes, n: int):
+    """A contiguous vector of n elements."""
+    if not _dev_as(t, name, dtypes, (n,)).is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
 
 
 def _rows8(t, name: str, dtypes, shape=None):
     """An 8-bit matrix whose rows begin on 16 bytes, and its row stride: t, or a copy laid out so."""
     ld = _rows(t, name, dtypes, shape)
-    if ld % 16 or t.data_ptr() % 16 or ld < (t.shape[1] + 15) // 16 * 16:
-        if t.shape[0] == 1 and not t.data_ptr() % 16 and not t.shape[1] % 16:
-            return t, t.shape[1]
-        c = _empty8(t.shape[0], t.shape[1], t.dtype, t.device)
-        c.copy_(t)
-        return c, c.stride(0)
-    return t, ld
+    if not (ld | t.data_ptr()) & 15:
+        return t, ld
+    c = _empty8(t.shape[0], t.shape[1], t.dtype, t.device)
+    c.copy_(t)
+    return c, (t.shape[1] + 15) & -16
 
 
 def _empty8(rows: int, cols: int, dtype, dev):
@@ -829,10 +853,10 @@ def _blocks(n: int) -> int:
     return (n + 127) // 128
 
 
-def _same_device(dev, **tensors):
-    for name, t in tensors.items():
+def _same_device(dev, *tensors):
+    for t in tensors:
         if t is not None and t.device != dev:
-            raise ValueError(f"{name} is on {t.device}, not on {dev}")
+            raise ValueError(f"the tensors of a call are on {t.device} and on {dev}")
 
 
 def rms_norm(x, weight, residual=None, eps: float = 1e-6, quantize: bool = True):
@@ -843,22 +867,21 @@ def rms_norm(x, weight, residual=None, eps: float = 1e-6, quantize: bool = True)
     (float8_e8m0fnu), or x's type (scales None) with quantize=False. weight: x's type or float32."""
     ldx = _rows(x, "x", _FLOATS)
     rows, cols = x.shape
-    dev = x.device
-    _dev_as(weight, "weight", (x.dtype, torch.float32), (cols,))
-    if weight.stride(0) != 1 and cols > 1:
-        raise ValueError("weight must be contiguous")
+    dev, dtype = x.device, x.dtype
+    _vector(weight, "weight", (dtype, torch.float32), cols)
     ldr, h = 0, x
     if residual is not None:
-        ldr = _rows(residual, "residual", (x.dtype,), (rows, cols))
-        h = torch.empty((rows, cols), dtype=x.dtype, device=dev)
-    _same_device(dev, weight=weight, residual=residual)
-    scales = torch.empty((rows, _blocks(cols)), dtype=_E8M0, device=dev) if quantize else None
-    y = _empty8(rows, cols, _E4M3, dev) if quantize else torch.empty((rows, cols), dtype=x.dtype, device=dev)
+        ldr = _rows(residual, "residual", (dtype,), (rows, cols))
+        h = torch.empty_like(x) if x.is_contiguous() else torch.empty((rows, cols), dtype=dtype, device=dev)
+    _same_device(dev, weight, residual)
+    if quantize:
+        scales, y, ldy = torch.empty((rows, _blocks(cols)), dtype=_E8M0, device=dev), _empty8(rows, cols, _E4M3, dev), (cols + 15) & -16
+    else:
+        scales, y, ldy = None, torch.empty((rows, cols), dtype=dtype, device=dev), cols
     rstd = torch.empty(rows, dtype=torch.float32, device=dev)
-    with _on(dev):
-        call("ds_rms_norm", _ptr(x), _ptr(residual), _ptr(weight), _ptr(y), _ptr(scales),
-             None if residual is None else _ptr(h), _ptr(rstd), rows, cols, ldx, ldr, cols, (cols + 15) & -16 if quantize else cols, _blocks(cols),
-             eps, _TYPE[x.dtype], _TYPE[weight.dtype], _TYPE[y.dtype], _stream(dev))
+    _launch("ds_rms_norm", dev, x.data_ptr(), _ptr(residual), weight.data_ptr(), y.data_ptr(), _ptr(scales),
+            None if residual is None else h.data_ptr(), rstd.data_ptr(), rows, cols, ldx, ldr, cols, ldy, _blocks(cols), eps,
+            _TYPE[dtype], _TYPE[weight.dtype], _TYPE[y.dtype])
     return y, scales, h, rstd
 
 
@@ -871,17 +894,14 @@ def rms_norm_backward(dy, h, weight, rstd, dh=None):
     dev = dy.device
     ldh = _rows(h, "h", (dy.dtype,), (rows, cols))
     lddh = 0 if dh is None else _rows(dh, "dh", (dy.dtype,), (rows, cols))
-    _dev_as(weight, "weight", (dy.dtype, torch.float32), (cols,))
-    _dev_as(rstd, "rstd", (torch.float32,), (rows,))
-    if (weight.stride(0) != 1 and cols > 1) or (rstd.stride(0) != 1 and rows > 1):
-        raise ValueError("weight and rstd must be contiguous")
-    _same_device(dev, h=h, weight=weight, rstd=rstd, dh=dh)
+    _vector(weight, "weight", (dy.dtype, torch.float32), cols)
+    _vector(rstd, "rstd", (torch.float32,), rows)
+    _same_device(dev, h, weight, rstd, dh)
     dx = torch.empty((rows, cols), dtype=dy.dtype, device=dev)
     dw = torch.empty(cols, dtype=weight.dtype, device=dev)
-    with _on(dev):
-        scratch, size = _scratch8("ds_rms_norm_backward_scratch_bytes", (rows, cols), dev)
-        call("ds_rms_norm_backward", _ptr(dy), _ptr(h), _ptr(weight), _ptr(rstd), _ptr(dh), _ptr(dx), _ptr(dw), rows, cols,
-             ldy, ldh, lddh, cols, _TYPE[dy.dtype], _TYPE[weight.dtype], _ptr(scratch), size, _stream(dev))
+    scratch, size = _scratch8("ds_rms_norm_backward_scratch_bytes", (rows, cols), dev)
+    _launch("ds_rms_norm_backward", dev, dy.data_ptr(), h.data_ptr(), weight.data_ptr(), rstd.data_ptr(), _ptr(dh), dx.data_ptr(),
+            dw.data_ptr(), rows, cols, ldy, ldh, lddh, cols, _TYPE[dy.dtype], _TYPE[weight.dtype], _ptr(scratch), size)
     return dx, dw
 
 
@@ -898,12 +918,11 @@ def quantize_fp8(x, gate=None):
     rows, cols = x.shape
     dev = x.device
     ldg = 0 if gate is None else _rows(gate, "gate", (x.dtype,), (rows, cols))
-    _same_device(dev, gate=gate)
+    _same_device(dev, gate)
     y = _empty8(rows, cols, _E4M3, dev)
     scales = torch.empty((rows, _blocks(cols)), dtype=_E8M0, device=dev)
-    with _on(dev):
-        call("ds_quantize_fp8", _ptr(x), _ptr(gate), _ptr(y), _ptr(scales), rows, cols, ldx, ldg, (cols + 15) & -16,
-             _blocks(cols), _TYPE[x.dtype], _stream(dev))
+    _launch("ds_quantize_fp8", dev, x.data_ptr(), _ptr(gate), y.data_ptr(), scales.data_ptr(), rows, cols, ldx, ldg, (cols + 15) & -16,
+            _blocks(cols), _TYPE[x.dtype])
     return y, scales
 
 
@@ -915,9 +934,8 @@ def quantize_weights_fp8(w):
     dev = w.device
     w8 = _empty8(rows, cols, _E4M3, dev)
     scales = torch.empty((_blocks(rows), _blocks(cols)), dtype=_E8M0, device=dev)
-    with _on(dev):
-        call("ds_quantize_weights_fp8", _ptr(w), _ptr(w8), _ptr(scales), rows, cols, ldw, (cols + 15) & -16, _blocks(cols),
-             _TYPE[w.dtype], _stream(dev))
+    _launch("ds_quantize_weights_fp8", dev, w.data_ptr(), w8.data_ptr(), scales.data_ptr(), rows, cols, ldw, (cols + 15) & -16,
+            _blocks(cols), _TYPE[w.dtype])
     return w8, scales
 
 
@@ -930,9 +948,7 @@ def shift_weights_to_fp8(w_packed, cols: int, code_bits: int = 5):
         raise ValueError(f"w_packed must have {packed_row_words(cols, code_bits)} words a row, got {words}")
     dev = w_packed.device
     w8 = _empty8(rows, cols, torch.float8_e5m2, dev)
-    with _on(dev):
-        call("ds_shift_weights_to_fp8", _ptr(w_packed), _ptr(w8), rows, cols, (cols + 15) & -16, code_bits_flag(code_bits),
-             _stream(dev))
+    _launch("ds_shift_weights_to_fp8", dev, w_packed.data_ptr(), w8.data_ptr(), rows, cols, (cols + 15) & -16, code_bits_flag(code_bits))
     return w8, torch.full((_blocks(rows), _blocks(cols)), 127, dtype=torch.uint8, device=dev).view(_E8M0)
 
 
@@ -940,7 +956,7 @@ def _weights8(w8, w_scales, dev):
     w8, ldw = _rows8(w8, "w8", (_E4M3, torch.float8_e5m2))
     n, k = w8.shape
     ldws = _rows(w_scales, "w_scales", (_E8M0,), (_blocks(n), _blocks(k)))
-    _same_device(dev, w8=w8, w_scales=w_scales)
+    _same_device(dev, w8, w_scales)
     return w8, n, k, ldw, ldws
 
 
@@ -956,15 +972,14 @@ def linear_fp8(x8, x_scales, w8, w_scales, bias=None, out_dtype=torch.bfloat16):
     if x8.shape[1] != k:
         raise ValueError(f"x8 has {x8.shape[1]} columns, w8 {k}")
     ldxs = _rows(x_scales, "x_scales", (_E8M0,), (m, _blocks(k)))
-    if bias is not None and not _dev_as(bias, "bias", (torch.float32,), (n,)).is_contiguous():
-        raise ValueError("bias must be contiguous")
-    _same_device(dev, x_scales=x_scales, bias=bias)
+    if bias is not None:
+        _vector(bias, "bias", (torch.float32,), n)
+    _same_device(dev, x_scales, bias)
     if out_dtype not in _FLOATS:
         raise TypeError("out_dtype must be float32, float16 or bfloat16")
     y = torch.empty((m, n), dtype=out_dtype, device=dev)
-    with _on(dev):
-        call("ds_linear_fp8", _ptr(x8), _ptr(x_scales), _ptr(w8), _ptr(w_scales), _ptr(bias), _ptr(y), m, n, k, ldx, ldxs,
-             ldw, ldws, n, _TYPE[w8.dtype], _TYPE[out_dtype], _stream(dev))
+    _launch("ds_linear_fp8", dev, x8.data_ptr(), x_scales.data_ptr(), w8.data_ptr(), w_scales.data_ptr(), _ptr(bias), y.data_ptr(), m, n, k,
+            ldx, ldxs, ldw, ldws, n, _TYPE[w8.dtype], _TYPE[out_dtype])
     return y
 
 
@@ -978,14 +993,13 @@ def linear_fp8_backward_data(dy8, dy_scales, w8, w_scales, out_dtype=torch.bfloa
     if dy8.shape[1] != n:
         raise ValueError(f"dy8 has {dy8.shape[1]} columns, w8 {n} rows")
     ldys = _rows(dy_scales, "dy_scales", (_E8M0,), (m, _blocks(n)))
-    _same_device(dev, dy_scales=dy_scales)
+    _same_device(dev, dy_scales)
     if out_dtype not in _FLOATS:
         raise TypeError("out_dtype must be float32, float16 or bfloat16")
     dx = torch.empty((m, k), dtype=out_dtype, device=dev)
-    with _on(dev):
-        scratch, size = _scratch8("ds_linear_fp8_backward_data_scratch_bytes", (m, n, k), dev)
-        call("ds_linear_fp8_backward_data", _ptr(dy8), _ptr(dy_scales), _ptr(w8), _ptr(w_scales), _ptr(dx), m, n, k, lddy,
-             ldys, ldw, ldws, k, _TYPE[w8.dtype], _TYPE[out_dtype], _ptr(scratch), size, _stream(dev))
+    scratch, size = _scratch8("ds_linear_fp8_backward_data_scratch_bytes", (m, n, k), dev)
+    _launch("ds_linear_fp8_backward_data", dev, dy8.data_ptr(), dy_scales.data_ptr(), w8.data_ptr(), w_scales.data_ptr(), dx.data_ptr(),
+            m, n, k, lddy, ldys, ldw, ldws, k, _TYPE[w8.dtype], _TYPE[out_dtype], _ptr(scratch), size)
     return dx
 
 
@@ -1010,22 +1024,22 @@ def _check_cache(k_cache, v_cache, k_scales, v_scales, table, batch: int):
     _dev_as(v_scales, "v_scales", (_E8M0,), (pages, heads))
     if not (k_cache.is_contiguous() and v_cache.is_contiguous() and k_scales.is_contiguous() and v_scales.is_contiguous()):
         raise ValueError("a cache and its scales must be contiguous")
-    ldt = _rows(table, "table", (torch.int32,))
+    ldt = _rows(table, "table", _INT32)
     if table.shape[0] != batch:
         raise ValueError(f"table has {table.shape[0]} rows for {batch} sequences")
     return pages, heads, page, dim, ldt
 
 
-def _per_sequence(t, name: str, batch: int):
-    if t is not None and not _dev_as(t, name, (torch.int32,), (batch,)).is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
+_INT32 = (torch.int32,)
+_Strides = ctypes.c_int64 * 3
 
 
 def _vectors(t, name: str):
     """Element strides (sequence, token, head) of vectors [batch, tokens, heads, dim]."""
-    if t.stride(3) != 1:
+    b, n, h, one = t.stride()
+    if one != 1:
         raise ValueError(f"the elements of a vector of {name} must be consecutive")
-    return (ctypes.c_int64 * 3)(*t.stride()[:3])
+    return _Strides(b, n, h)
 
 
 def kv_cache_append(k, v, k_cache, v_cache, k_scales, v_scales, table, start, count=None):
@@ -1039,23 +1053,16 @@ def kv_cache_append(k, v, k_cache, v_cache, k_scales, v_scales, table, start, co
     _dev_as(v, "v", (k.dtype,), k.shape)
     batch, tokens = k.shape[:2]
     pages, heads, page, dim, ldt = _check_cache(k_cache, v_cache, k_scales, v_scales, table, batch)
-    if tuple(k.shape[2:]) != (heads, dim):
+    if k.shape[2] != heads or k.shape[3] != dim:
         raise ValueError(f"k has heads and dim {tuple(k.shape[2:])}, the cache {(heads, dim)}")
-    _per_sequence(_required(start, "start"), "start", batch)
-    _per_sequence(count, "count", batch)
+    _vector(start, "start", _INT32, batch)
+    if count is not None:
+        _vector(count, "count", _INT32, batch)
     dev = k.device
-    _same_device(dev, v=v, k_cache=k_cache, v_cache=v_cache, k_scales=k_scales, v_scales=v_scales, table=table,
-                 start=start, count=count)
-    with _on(dev):
-        call("ds_kv_cache_append", _ptr(k), _ptr(v), _ptr(k_cache), _ptr(v_cache), _ptr(k_scales), _ptr(v_scales), _ptr(table),
-             _ptr(start), _ptr(count), batch, tokens, heads, dim, page, pages, table.shape[1], ldt, _vectors(k, "k"),
-             _vectors(v, "v"), _TYPE[k.dtype], _stream(dev))
-
-
-def _required(t, name: str):
-    if t is None:
-        raise TypeError(f"{name} must be a device tensor")
-    return t
+    _same_device(dev, v, k_cache, v_cache, k_scales, v_scales, table, start, count)
+    _launch("ds_kv_cache_append", dev, k.data_ptr(), v.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), k_scales.data_ptr(),
+            v_scales.data_ptr(), table.data_ptr(), start.data_ptr(), _ptr(count), batch, tokens, heads, dim, page, pages,
+            table.shape[1], ldt, _vectors(k, "k"), _vectors(v, "v"), _TYPE[k.dtype])
 
 
 def attention_fp8(q, k_cache, v_cache, k_scales, v_scales, table, length, count=None, scale: float | None = None,
@@ -1072,16 +1079,15 @@ def attention_fp8(q, k_cache, v_cache, k_scales, v_scales, table, length, count=
     pages, heads, page, dim, ldt = _check_cache(k_cache, v_cache, k_scales, v_scales, table, batch)
     if qdim != dim or hq % heads:
         raise ValueError(f"q has {hq} heads of {qdim}, the cache {heads} of {dim}")
-    _per_sequence(_required(length, "length"), "length", batch)
-    _per_sequence(count, "count", batch)
+    _vector(length, "length", _INT32, batch)
+    if count is not None:
+        _vector(count, "count", _INT32, batch)
     dev = q.device
-    _same_device(dev, k_cache=k_cache, v_cache=v_cache, k_scales=k_scales, v_scales=v_scales, table=table, length=length,
-                 count=count)
+    _same_device(dev, k_cache, v_cache, k_scales, v_scales, table, length, count)
     o = torch.empty((batch, tokens, hq, dim), dtype=q.dtype, device=dev)
     shape = (batch, tokens, heads, hq // heads, dim, page, table.shape[1])
-    with _on(dev):
-        scratch, size = _scratch8("ds_attention_fp8_scratch_bytes", shape, dev)
-        call("ds_attention_fp8", _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(k_scales), _ptr(v_scales), _ptr(table),
-             _ptr(length), _ptr(count), _ptr(o), *shape[:6], pages, shape[6], ldt, _vectors(q, "q"), _vectors(o, "o"),
-             1 / math.sqrt(dim) if scale is None else scale, window, _TYPE[q.dtype], _ptr(scratch), size, _stream(dev))
+    scratch, size = _scratch8("ds_attention_fp8_scratch_bytes", shape, dev)
+    _launch("ds_attention_fp8", dev, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(),
+            table.data_ptr(), length.data_ptr(), _ptr(count), o.data_ptr(), *shape[:6], pages, shape[6], ldt, _vectors(q, "q"),
+            _vectors(o, "o"), 1 / math.sqrt(dim) if scale is None else scale, window, _TYPE[q.dtype], _ptr(scratch), size)
     return o
