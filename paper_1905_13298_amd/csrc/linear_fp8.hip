@@ -194,6 +194,43 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const uint8_t *p, in
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p), 0, int(bytes), 0x00020000);
 }
 
+// Where a lane's 16 bytes of a step are, or, past the reduction's end, an offset outside every
+// buffer: zeros are put there. A step is sent for in the same way whether it is whole, the last
+// or past it, since a branch in the loop would have the compiler move products behind it.
+__device__ __forceinline__ int inside(int offset, bool in) { return in ? offset : 0x7ffffff0; }
+
+// A reduction that ends inside a lane's 16 bytes: the bytes past its end, in LDS.
+__device__ __forceinline__ void clear_past(uint8_t *at, int left)
+{
+    if (left <= 0 || left >= 16) return;
+    i32x4 v = *reinterpret_cast<const i32x4 *>(at);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int n = left - 4 * i;
+        v[i] = n >= 4 ? v[i] : n <= 0 ? 0 : v[i] & int((1u << (8 * n)) - 1u);
+    }
+    *reinterpret_cast<i32x4 *>(at) = v;
+}
+
+// Four consecutive outputs of a row of y.
+template <typename O>
+__device__ __forceinline__ void store_outputs(const LinearParams &p, int m, int n, f32x4 v)
+{
+    O *y = static_cast<O *>(p.y) + m * p.ldy + n;
+    if (p.bias) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] += p.bias[min(n + i, p.n - 1)];
+    }
+    O o[4] = {O(v[0]), O(v[1]), O(v[2]), O(v[3])};
+    if (n + 4 <= p.n) {
+        __builtin_memcpy(y, o, sizeof o);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (n + i < p.n) y[i] = o[i];
+    }
+}
+
 // Many rows of x: a block forms BN outputs of BM rows of y, 128 elements of the reduction
 // at a time, which go from memory to LDS without registers, one step ahead of the
 // products. A row's eight 16-byte pieces are kept in an order of its own, so that the
@@ -229,32 +266,15 @@ linear_tile_kernel(const LinearParams p, int tiles_n, int tiles_m)
 #pragma unroll
     for (int i = 0; i < kLoadsX; ++i) xv[i] = min(i * kWaves * 8 + lrow, p.m - 1 - m0) * ldx + piece;
     const uint32_t base_lds = __builtin_amdgcn_readfirstlane(lds_address(lds));
-    auto fetch = [&](int step, int buf) {
+    auto stage = [&](int step, int buf) {
         const int k = step * 128;
+        const bool in = k + piece < p.k;
 #pragma unroll
         for (int i = 0; i < kLoadsW; ++i)
-            to_lds16(base_lds + buf * kStage + (i * kWaves + wave) * 1024, wr, wv[i], k);
+            to_lds16(base_lds + buf * kStage + (i * kWaves + wave) * 1024, wr, inside(wv[i], in), k);
 #pragma unroll
         for (int i = 0; i < kLoadsX; ++i)
-            to_lds16(base_lds + buf * kStage + (BN / 8 + i * kWaves + wave) * 1024, xr, xv[i], k);
-    };
-    // The last step of a reduction that ends inside a block of 128: through registers,
-    // with zeros past its end.
-    auto fetch_end = [&](int step, int buf) {
-        const int k = step * 128 + piece;
-#pragma unroll 1
-        for (int i0 = 0; i0 < kLoadsW + kLoadsX; i0 += 4) {
-            i32x4 v[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int i = i0 + j, row = ((i < kLoadsW ? i : i - kLoadsW) * kWaves + wave) * 8 + (lane >> 3);
-                const uint8_t *src = i < kLoadsW ? wbase + min(row, p.n - 1 - n0) * p.ldw : xbase + min(row, p.m - 1 - m0) * p.ldx;
-                v[j] = row16(src, k, p.k);
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                *reinterpret_cast<i32x4 *>(lds + buf * kStage + ((i0 + j) * kWaves + wave) * 1024 + lane * 16) = v[j];
-        }
+            to_lds16(base_lds + buf * kStage + (BN / 8 + i * kWaves + wave) * 1024, xr, inside(xv[i], in), k);
     };
     // The scales of the block's rows (of w's, by 128) for 64 steps from `step` on, four a word.
     auto fetch_scales = [&](int step) {
@@ -274,11 +294,6 @@ linear_tile_kernel(const LinearParams p, int tiles_n, int tiles_m)
 #pragma unroll
         for (int b = 0; b < MT; ++b) acc[a][b] = f32x4{};
 
-    const int full = p.k / 128;
-    auto stage = [&](int step, int buf) {
-        if (step < full) fetch(step, buf);
-        else if (step < p.kblocks) fetch_end(step, buf);
-    };
 #pragma unroll
     for (int i = 0; i < STAGES; ++i) stage(i, i);
     fetch_scales(0);
@@ -299,8 +314,19 @@ linear_tile_kernel(const LinearParams p, int tiles_n, int tiles_m)
     // says so and that the next step's have arrived. Behind it, the step after the next is
     // sent for, and each of the last products is followed by the read of the next step's
     // weights into the registers that it leaves.
+    const bool partial = p.k % 16 != 0;
     for (int step = 0; step < p.kblocks; ++step) {
         const int buf = step % STAGES, following = buf + 1 < STAGES ? buf + 1 : 0;
+        if (partial && step + 1 == p.kblocks) {
+#pragma unroll
+            for (int i = 0; i < kLoadsW + kLoadsX; ++i)
+                clear_past(lds + buf * kStage + (i * kWaves + wave) * 1024 + lane * 16, p.k - step * 128 - piece);
+            wait_lds();
+            barrier();
+#pragma unroll
+            for (int a = 0; a < NT; ++a) wf[a] = frag(wt + buf * kStage, a);
+            x = frag(xt + buf * kStage, 0);
+        }
         if ((step & 3) == 0) {
             if ((step & (4 * kGroups - 1)) == 0 && step > 0) {
                 barrier();
@@ -322,15 +348,10 @@ linear_tile_kernel(const LinearParams p, int tiles_n, int tiles_m)
             x = ahead;
             __builtin_amdgcn_sched_barrier(0);
         }
-        if (step + 1 < p.kblocks) {
-            // The transfers of the steps behind the next one may be on their way.
-            const int behind = STAGES > 2 ? min(step + STAGES, full) - step - 2 : 0;
-            if (STAGES > 3 && behind >= 2) wait_but<2 * (kLoadsW + kLoadsX)>();
-            else if (STAGES > 2 && behind >= 1) wait_but<kLoadsW + kLoadsX>();
-            else wait_all();
-            barrier();
-            stage(step + STAGES, buf);
-        }
+        // The transfers of the steps behind the next one may be on their way.
+        wait_but<(STAGES - 2) * (kLoadsW + kLoadsX)>();
+        barrier();
+        stage(step + STAGES, buf);
         // (After the last step these reads are of LDS that nothing uses any more.)
         const i32x8 ahead = frag(xt + following * kStage, 0);
 #pragma unroll
@@ -344,28 +365,170 @@ linear_tile_kernel(const LinearParams p, int tiles_n, int tiles_m)
 #pragma unroll
         for (int t = 0; t < MT; ++t) xs[t] >>= 8;
     }
+    wait_all();     // no transfer may outlive the block's LDS
 #pragma unroll
     for (int b = 0; b < MT; ++b) {
         const int m = m0 + (wm * MT + b) * 16 + r;
         if (m >= p.m) continue;
 #pragma unroll
-        for (int a = 0; a < NT; ++a) {
-            const int n = n0 + (wn * NT + a) * 16 + g * 4;
-            O *y = static_cast<O *>(p.y) + m * p.ldy + n;
-            f32x4 v = acc[a][b];
-            if (p.bias) {
+        for (int a = 0; a < NT; ++a) store_outputs<O>(p, m, n0 + (wn * NT + a) * 16 + g * 4, acc[a][b]);
+    }
+}
+
+// A large product: 256 x 256 outputs a block, 128 x 128 a wave, as linear_tile_kernel with
+// more of the reduction on its way. A step's elements of x come in two halves (the first
+// four tiles of 16 rows of every wave, and the last four), which go through five places in
+// turn; those of w go through two and into registers before their step. A half's place is
+// free when its last elements have been read, so there are two barriers a step: in front of
+// the last products of the first half the next but one step's second half and weights are
+// sent for, in front of those of the second half the first half of the step after that. What
+// a step waits for was sent for at least a step and a half before (a step takes 1.1 us at the
+// least here, memory behind the L2 answers after about 2).
+template <typename O, int WF>
+__global__ void __launch_bounds__(256, 1)
+linear_wide_kernel(const LinearParams p, int tiles_n, int tiles_m)
+{
+    constexpr int B = 256, NT = 8, MT = 8, kW = B * 128, kHalf = kW / 2, kPlaces = 5, kGroup = 4, kGroups = 8;
+    __shared__ __align__(16) uint8_t lds[2 * kW + kPlaces * kHalf];
+    __shared__ uint32_t scales[kGroups][B + 2];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), r = lane & 15, g = lane >> 4;
+    const int tiles = tiles_n * tiles_m, share = (tiles + 7) >> 3, at = (int(blockIdx.x) & 7) * share + (int(blockIdx.x) >> 3);
+    if ((int(blockIdx.x) >> 3) >= share || at >= tiles) return;
+    const int band = at / (kGroup * tiles_n), in = at - band * kGroup * tiles_n, deep = min(kGroup, tiles_m - band * kGroup);
+    const int n0 = in / deep * B, m0 = (band * kGroup + in % deep) * B;
+    const int wn = wave & 1, wm = wave >> 1;
+
+    const uint8_t *wbase = p.w + n0 * p.ldw, *xbase = p.x + m0 * p.ldx;
+    const int krow = (p.k + 15) & ~15, nlast = min(B, p.n - n0) - 1, mlast = min(B, p.m - m0) - 1;
+    const __amdgpu_buffer_rsrc_t wr = rows_rsrc(wbase, nlast * p.ldw + krow), xr = rows_rsrc(xbase, mlast * p.ldx + krow);
+    const int lrow = wave * 8 + (lane >> 3), piece = ((lane & 7) ^ ((lrow >> 1) & 7)) * 16;
+    // Load i of a wave: rows i * 32 + lrow of w; row i * 32 + lrow of a half of x is row 64 (i /
+    // 2) past it (a wave's half has 64 rows), and 64 more in the second half. Rows past the last
+    // read it instead.
+    auto xrow = [&](int half, int i) { return min(i / 2 * 128 + i % 2 * 32 + half * 64 + lrow, mlast); };
+    int wv[8], xv[2][4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] += p.bias[min(n + i, p.n - 1)];
-            }
-            O o[4] = {O(v[0]), O(v[1]), O(v[2]), O(v[3])};
-            if (n + 4 <= p.n) {
-                __builtin_memcpy(y, o, sizeof o);
-            } else {
+    for (int i = 0; i < 8; ++i) wv[i] = min(i * 32 + lrow, nlast) * int(p.ldw) + piece;
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (n + i < p.n) y[i] = o[i];
-            }
+    for (int i = 0; i < 8; ++i) xv[i / 4][i % 4] = xrow(i / 4, i % 4) * int(p.ldx) + piece;
+    const uint32_t base_lds = __builtin_amdgcn_readfirstlane(lds_address(lds));
+    // Load i of a step's weights, or of a half of its elements of x.
+    auto fetch_w = [&](int step, int i) {
+        to_lds16(base_lds + (step & 1) * kW + (i * 4 + wave) * 1024, wr, inside(wv[i], step * 128 + piece < p.k), step * 128);
+    };
+    auto fetch_x = [&](int step, int half, int place, int i) {
+        to_lds16(base_lds + 2 * kW + place * kHalf + (i * 4 + wave) * 1024, xr, inside(xv[half][i], step * 128 + piece < p.k), step * 128);
+    };
+    // The scales of the block's rows (of w's, by 128) for 32 steps from `step` on, four a word.
+    auto fetch_scales = [&](int step) {
+        const int groups = min(kGroups, (p.kblocks - step + 3) / 4);
+#pragma unroll 1
+        for (int i = threadIdx.x; i < (B + 2) * groups; i += 256) {
+            const int gr = i / (B + 2), row = i - gr * (B + 2), at = step + 4 * gr;
+            const uint8_t *src = row < B ? p.xs + min(m0 + row, p.m - 1) * p.ldxs : p.ws + min(n0 / 128 + row - B, (p.n - 1) / 128) * p.ldws;
+            scales[gr][row] = place_scales4(load_scales4(src, at, p.kblocks), at, p.kblocks);
         }
+    };
+    f32x4 acc[NT][MT];
+#pragma unroll
+    for (int a = 0; a < NT; ++a)
+#pragma unroll
+        for (int b = 0; b < MT; ++b) acc[a][b] = f32x4{};
+
+#pragma unroll
+    for (int i = 0; i < kPlaces * 4; ++i) fetch_x(i / 8, i / 4 % 2, i / 4, i % 4);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) fetch_w(i / 8, i % 8);
+    fetch_scales(0);
+    wait_all();
+    barrier();
+    const int so = r * 128 + (g ^ (r >> 1)) * 16, s1 = so ^ 64;      // pieces g and g + 4
+    auto frag = [&](const uint8_t *base, int t) {
+        const i32x4 a = *reinterpret_cast<const i32x4 *>(base + t * 2048 + so), b = *reinterpret_cast<const i32x4 *>(base + t * 2048 + s1);
+        return i32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    };
+    const uint8_t *const wt = lds + wn * NT * 2048, *const xt = lds + 2 * kW + wm * kHalf / 2;
+    i32x8 wf[NT], x;
+#pragma unroll
+    for (int a = 0; a < NT; ++a) wf[a] = frag(wt, a);
+    x = frag(xt, 0);
+    uint32_t xs[MT], ws;
+    int place = 0;                                  // of this step's first half
+    auto past = [&](int by) { const int q = place + by; return q >= kPlaces ? q - kPlaces : q; };
+    const bool partial = p.k % 16 != 0;
+    for (int step = 0; step < p.kblocks; ++step) {
+        if (partial && step + 1 == p.kblocks) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                clear_past(lds + (step & 1) * kW + (i * 4 + wave) * 1024 + lane * 16, p.k - step * 128 - piece);
+                clear_past(lds + 2 * kW + past(i / 4) * kHalf + (i % 4 * 4 + wave) * 1024 + lane * 16, p.k - step * 128 - piece);
+            }
+            wait_lds();
+            barrier();
+#pragma unroll
+            for (int a = 0; a < NT; ++a) wf[a] = frag(wt + (step & 1) * kW, a);
+            x = frag(xt + place * kHalf, 0);
+        }
+        if ((step & 3) == 0) {
+            if ((step & (4 * kGroups - 1)) == 0 && step > 0) {
+                barrier();
+                fetch_scales(step);
+                wait_lds();
+                barrier();
+            }
+            const uint32_t *from = scales[(step >> 2) & (kGroups - 1)];
+#pragma unroll
+            for (int t = 0; t < MT; ++t) xs[t] = from[(wm * MT + t) * 16 + r];
+            ws = from[B + wn];
+        }
+        const uint8_t *const x0 = xt + place * kHalf, *const x1 = xt + past(1) * kHalf, *const x2 = xt + past(2) * kHalf;
+#pragma unroll
+        for (int b = 0; b + 1 < MT; ++b) {
+            if (b == MT / 2 - 1) {
+                wait_lds();
+                barrier();
+            }
+            const i32x8 ahead = b + 1 < MT / 2 ? frag(x0, b + 1) : frag(x1, b + 1 - MT / 2);
+#pragma unroll
+            for (int a = 0; a < NT; ++a) {
+                acc[a][b] = mma<WF, false>(wf[a], x, acc[a][b], int(ws), int(xs[b]));
+                // A load behind each two or three products: 12 in the last four rows but one.
+                if (b >= MT / 2 - 1 && (a == 1 || a == 4 || a == 7)) {
+                    const int i = (b - (MT / 2 - 1)) * 3 + a / 3;
+                    if (i < 4) fetch_x(step + 2, 1, place, i);
+                    else fetch_w(step + 2, i - 4);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            x = ahead;
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        // Behind the next step's weights: the first half of step + 2, its second half and weights.
+        wait_but<16>();
+        barrier();
+        // (After the last step these reads are of LDS that nothing uses any more.)
+        const i32x8 ahead = frag(x2, 0);
+        const uint8_t *const wnext = wt + ((step + 1) & 1) * kW;
+#pragma unroll
+        for (int a = 0; a < NT; ++a) {
+            acc[a][MT - 1] = mma<WF, false>(wf[a], x, acc[a][MT - 1], int(ws), int(xs[MT - 1]));
+            wf[a] = frag(wnext, a);
+            if (a % 2) fetch_x(step + 3, 0, past(1), a / 2);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        x = ahead;
+        ws >>= 8;
+#pragma unroll
+        for (int t = 0; t < MT; ++t) xs[t] >>= 8;
+        place = past(2);
+    }
+    wait_all();     // no transfer may outlive the block's LDS
+#pragma unroll
+    for (int b = 0; b < MT; ++b) {
+        const int m = m0 + (wm * MT + b) * 16 + r;
+        if (m >= p.m) continue;
+#pragma unroll
+        for (int a = 0; a < NT; ++a) store_outputs<O>(p, m, n0 + (wn * NT + a) * 16 + g * 4, acc[a][b]);
     }
 }
 
@@ -412,7 +575,11 @@ void run_linear(const LinearParams &p, hipStream_t s)
     if (p.m > 64 && reach) {
         const int64_t t256 = int64_t((p.n + 255) / 256) * ((p.m + 255) / 256), t128 = int64_t((p.n + 127) / 128) * ((p.m + 127) / 128);
         if constexpr (sizeof(O) == 2) {
-            if (t256 >= 192) return run_tiles<O, WF, 256, 256, 2, 2, 2>(p, s);
+            if (t256 >= 192) {
+                const int tn = (p.n + 255) / 256, tm = (p.m + 255) / 256;
+                hipLaunchKernelGGL((linear_wide_kernel<O, WF>), dim3(uint32_t((t256 + 7) / 8 * 8)), dim3(256), 0, s, p, tn, tm);
+                return;
+            }
         }
         if (t128 <= 256) return run_tiles<O, WF, 128, 128, 2, 4, 4>(p, s);
         return run_tiles<O, WF, 128, 128, 2, 2, 2>(p, s);
