@@ -572,15 +572,23 @@ void run_linear(const LinearParams &p, hipStream_t s)
 {
     // The tiles' 32-bit offsets reach 256 rows.
     const bool reach = p.ldx <= (1 << 22) && p.ldw <= (1 << 22);
+    // Up to 64 rows the weights are read once without LDS (linear_rows_kernel).
     if (p.m > 64 && reach) {
         const int64_t t256 = int64_t((p.n + 255) / 256) * ((p.m + 255) / 256), t128 = int64_t((p.n + 127) / 128) * ((p.m + 127) / 128);
         if constexpr (sizeof(O) == 2) {
-            if (t256 >= 192) {
+            // Tiles of 256 where their rounds over the 256 CUs cost less: a round takes 50 to 57 us at
+            // k = 4096, so much as 640 tiles of 128 (54 us). 2500 x 4096 outputs (160 and 640 tiles):
+            // 52 and 54 us; 2048 x 4096: 52 and 40; 2900 x 6000 (288 and 1081): 102 and 82; 5000 x
+            // 5000: 105 and 117; 4096 x 4096: 58 and 70.
+            if (t128 >= 640 * ((t256 + 255) / 256)) {
                 const int tn = (p.n + 255) / 256, tm = (p.m + 255) / 256;
                 hipLaunchKernelGGL((linear_wide_kernel<O, WF>), dim3(uint32_t((t256 + 7) / 8 * 8)), dim3(256), 0, s, p, tn, tm);
                 return;
             }
         }
+        // One block a CU at most: eight waves, four steps in LDS (2005 x 2048 outputs of 1000: 16.4 us,
+        // 4 waves with two steps 18.5). More: two blocks of four waves share a CU (5000 x 5000 outputs of
+        // 4096: 117 us, eight waves and four steps 140).
         if (t128 <= 256) return run_tiles<O, WF, 128, 128, 2, 4, 4>(p, s);
         return run_tiles<O, WF, 128, 128, 2, 2, 2>(p, s);
     }
