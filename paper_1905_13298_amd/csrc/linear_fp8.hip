@@ -572,8 +572,12 @@ void run_linear(const LinearParams &p, hipStream_t s)
 {
     // The tiles' 32-bit offsets reach 256 rows.
     const bool reach = p.ldx <= (1 << 22) && p.ldw <= (1 << 22);
-    // Up to 64 rows the weights are read once without LDS (linear_rows_kernel).
-    if (p.m > 64 && reach) {
+    // Up to 64 rows linear_rows_kernel, whose time goes with its groups of 16 outputs times 16 rows,
+    // where those are few: 64 x 4096 outputs of 4096 (1024 groups) 12.9 us, tiles 17.8; 32 x 8192 (1024)
+    // 14.7 and 17.5; 32 x 11000 (1376) 20.4 and 17.6; 64 x 11000 (2752) 41 and 18. Up to 16 rows always:
+    // 8 x 32768 30.5 and 34.5, 16 x 16384 18.2 and 17.3.
+    const int64_t groups = int64_t((p.n + 15) / 16) * (p.m <= 16 ? 1 : p.m <= 32 ? 2 : 4);
+    if ((p.m > 64 || (p.m > 16 && groups > 1200)) && reach) {
         const int64_t t256 = int64_t((p.n + 255) / 256) * ((p.m + 255) / 256), t128 = int64_t((p.n + 127) / 128) * ((p.m + 127) / 128);
         if constexpr (sizeof(O) == 2) {
             // Tiles of 256 where their rounds over the 256 CUs cost less: a round takes 50 to 57 us at
@@ -586,8 +590,8 @@ void run_linear(const LinearParams &p, hipStream_t s)
                 return;
             }
         }
-        // One block a CU at most: eight waves, four steps in LDS (2005 x 2048 outputs of 1000: 16.4 us,
-        // 4 waves with two steps 18.5). More: two blocks of four waves share a CU (5000 x 5000 outputs of
+        // One block a CU at most: eight waves, four steps in LDS (1024 x 4096 outputs of 4096: 22.8 us,
+        // four waves with two steps 26.2). More: two blocks of four waves share a CU (5000 x 5000 outputs of
         // 4096: 117 us, eight waves and four steps 140).
         if (t128 <= 256) return run_tiles<O, WF, 128, 128, 2, 4, 4>(p, s);
         return run_tiles<O, WF, 128, 128, 2, 2, 2>(p, s);

@@ -314,6 +314,18 @@ def test_product_input_gradient(ops, m, n, k, wtype, out):
     near(dx, dy @ w, product_terms(dy, w.T.contiguous(), n, out == F32))
 
 
+@pytest.mark.parametrize("m,n,k", [(20, 11000, 130), (50, 5501, 272), (2561, 4100, 1), (2561, 4100, 136), (4100, 2700, 250), (2561, 4100, 384),
+                                   (2817, 3900, 655), (2561, 4100, 4230), (5000, 4400, 1000)])
+@pytest.mark.parametrize("wtype,out", [(E4M3, BF16), (E5M2, F16)])
+def test_product_of_many_tiles(ops, m, n, k, wtype, out):
+    """Every tile's edges in the columns, the first and last rows and some between."""
+    x8, xs, w8, ws = operands(ops, m, n, k, wtype, m + k)
+    y = ops.linear_fp8(x8, xs, w8, ws, out_dtype=out).cpu()
+    rows = torch.unique(torch.cat([torch.arange(min(m, 20)), torch.arange(max(m - 20, 0), m), torch.arange(0, m, 37)]))
+    x, w = value(x8, xs)[rows], value(w8, ws, 128)
+    near(y[rows], x @ w.T, product_terms(x, w, k, False))
+
+
 def test_product_is_exact_on_small_integers_and_equals_linear_shift(ops):
     """Integers times signed powers of two: every sum is exact, so the 8-bit product equals LinearShift on inputs whose
     shifts lose nothing."""
