@@ -33,8 +33,10 @@ struct AppendParams {
 // One page's new tokens of one head: its scale, the rounding of what it holds already
 // to a larger scale, and the tokens. Every (page, head) is one block's alone. A thread keeps
 // its first HELD vectors of 8 elements from the search for the scale (of 8 a page of 128 x 128
-// or 64 x 256 elements; 4 or 1 where that is all, for more blocks a CU); values go through
-// LDS, where they change from tokens to dimensions.
+// or 64 x 256 elements; 4 or 1 where that is all, for more blocks a CU: 16 x 2001 tokens, 8 heads
+// of 128, pages of 32 take 48 us with 4, 62 with 8, 51 with 1; single tokens 5.4 with 1, 5.9 with 8);
+// values go through LDS, where they change from tokens to dimensions. Bound by bandwidth: 4 x 2001 tokens
+// in 16 bits, 49 MB, 14.2 us (3.5 TB/s, the launch's 2 us among them).
 template <typename T, int HELD>
 __global__ void __launch_bounds__(256)
 append_kernel(const T *__restrict__ k, const T *__restrict__ v, uint8_t *__restrict__ kc, uint8_t *__restrict__ vc,
@@ -333,8 +335,9 @@ __device__ __forceinline__ void store_row(const AttentionParams &p, int b, int h
 __device__ __forceinline__ float inverse(float total) { return total > 0.f ? 1.f / total : total == 0.f ? 0.f : total; }
 
 // Up to 16 queries of a kv head (tokens being decoded): a block of 4 waves takes a share of
-// the keys, each wave every fourth 64 of it straight from memory to registers, and joins
-// them at its end.
+// the keys, each wave every fourth 64 of it straight from memory to registers (no two waves
+// share any, so LDS would only add a trip), and joins them at its end. Bound by reading the
+// cache once: 131072 keys of 8 heads of 128, 268 MB, 57 us with the join (4.7 TB/s).
 template <typename T, int DP>
 __global__ void __launch_bounds__(256)
 attention_few_kernel(const AttentionParams p)
@@ -468,12 +471,16 @@ attention_few_kernel(const AttentionParams p)
 // x 32 in 32 clocks where two waves reach one in 16). Row 8 w + 4 hf + e of tile tt is key
 // 32 tt + 16 (w / 2) + 8 hf + 4 (w % 2) + e: lane half hf then holds the keys that it
 // contracts in the second product.
-// ONE: a page holds whole steps (64 or 128 tokens), so that a step has one scale.
-template <typename T, int DP, int WAVES, bool ONE>
+//
+// Bound by the matrix instructions and the exponentials between them, which do not overlap in one
+// wave: 2 x 1000 queries of 32 heads over up to 8000 keys of 8 heads of 128 take 232 us, pages of
+// 16 tokens as long as those of 64 (the products alone take 203 us at the rate of a large 16-bit
+// product).
+template <typename T, int DP, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES, DP <= 128 ? 2 : 1)
 attention_many_kernel(const AttentionParams p, int bhs)
 {
-    constexpr int QC = DP / 16, DT = DP / 32, kLoads = DP / 64, kRuns = 4 / WAVES, kScales = ONE ? 1 : 4;
+    constexpr int QC = DP / 16, DT = DP / 32, kLoads = DP / 64, kRuns = 4 / WAVES, kScales = 4;
     constexpr int kKeys = kStep * DP * 2;      // bytes of a step's keys, or values
     typedef typename Vec8<T>::type v8;
     __shared__ __align__(16) uint8_t lds[2][2 * kKeys];
@@ -508,11 +515,11 @@ attention_many_kernel(const AttentionParams p, int bhs)
     // The table's entry of the g-th 16 keys of a step; a page of the cache or -1.
     const int *const table = p.table + b * p.ldt;
     auto entry = [&](int step) {
-        const int key = step * kStep + (ONE ? 0 : g * 16);
+        const int key = step * kStep + g * 16;
         return step < to && key < thi ? table[key >> p.page_shift] : -1;
     };
     auto on_page = [&](int pid) { return unsigned(pid) < unsigned(p.pages) ? pid : -1; };
-    auto on_pages = [&](int pids) { return ONE ? __builtin_amdgcn_readfirstlane(pids) >= 0 : bool(__all(pids >= 0)); };
+    auto on_pages = [&](int pids) { return bool(__all(pids >= 0)); };
     i32x4 kraw[kRuns][kLoads], vraw[kRuns][kLoads];
     // This wave's runs of 16 keys of a step: of the values dimension `lane`, of the keys a
     // piece of 16 dimensions of one key (what lies past `dim` is read somewhere inside). Where
@@ -528,7 +535,7 @@ attention_many_kernel(const AttentionParams p, int bhs)
     auto fetch = [&](int step, int pids) {
 #pragma unroll
         for (int q = 0; q < kRuns; ++q) {
-            const int which = wave * kRuns + q, pid = ONE ? __builtin_amdgcn_readfirstlane(pids) : __builtin_amdgcn_readlane(pids, which * 16);
+            const int which = wave * kRuns + q, pid = __builtin_amdgcn_readlane(pids, which * 16);
             const int slot = (step * kStep + which * 16) & (page - 1);
             const int64_t at = max(pid, 0) * page_bytes;
             const uint8_t *k = kh + at + slot * D, *v = vh + at + slot;
@@ -656,7 +663,7 @@ attention_many_kernel(const AttentionParams p, int bhs)
         const float sub = or_zero(m);
 #pragma unroll
         for (int j = 0; j < kScales; ++j) {
-            auto of = [&](float v) { return ONE ? v : __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), j * 16)); };
+            auto of = [&](float v) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), j * 16)); };
             sk[j] = of(ps.sk);
             lv[j] = of(ps.lv);
             iv[j] = of(ps.iv);
@@ -732,7 +739,8 @@ attention_many_kernel(const AttentionParams p, int bhs)
 }
 
 // The splits of a row together: a block of 4 waves per row, LANES lanes (4 dimensions each)
-// per split, so that 16 or 8 or 4 splits are read at once.
+// per split, so that 16 or 8 or 4 splits are read at once. A few us (64 splits of 32 rows: 3), behind
+// the launch that writes them.
 template <typename T, int LANES>
 __global__ void __launch_bounds__(256)
 attention_join_kernel(const AttentionParams p)
@@ -793,8 +801,13 @@ struct Plan {
     int64_t rows;
 };
 
-// How a call is split: over the rows first, then over the keys until there are about 512
-// blocks (1024 of few queries) of at least 8 steps of 64 keys.
+// How a call is split: over the rows first, then over the keys until 512 blocks (two a CU) have at
+// least 8 steps of 64 keys each. Measured (8 heads of 128, 4 query heads each): one query over
+// 131072 keys 57 us, with 1024 blocks 60, unsplit 1209; 16 x 1 over up to 8192 40, 42 and, with 2048, 46;
+// 48 x 1 (384 blocks, two splits each, since lengths differ) 93 and unsplit 108; 100 queries over 32768
+// keys 85, with 256 blocks 97, with 1024 94. Up to 16 rows run attention_few_kernel (48 x 1: 93 us,
+// the other 230). From 17 to 64 rows blocks of two waves: 32 x 16 queries over 4096 keys 83 us, of
+// four 90; above, of four: 2 x 1000 queries 232, of two 371.
 Plan plan_attention(int64_t batch, int64_t tokens, int64_t heads, int64_t group, int64_t columns, int64_t page)
 {
     Plan a;
@@ -802,7 +815,7 @@ Plan plan_attention(int64_t batch, int64_t tokens, int64_t heads, int64_t group,
     a.waves = a.rows <= 16 ? 0 : a.rows <= 64 ? 2 : 4;
     a.row_tiles = a.waves ? int((a.rows + 32 * a.waves - 1) / (32 * a.waves)) : 1;
     const int64_t blocks = std::max<int64_t>(batch * heads * a.row_tiles, 1), steps = (columns * page + kStep - 1) / kStep;
-    a.splits = int(std::max<int64_t>(1, std::min<int64_t>({(a.waves ? 512 : 1024) / blocks, (steps + 7) / 8, 256})));
+    a.splits = int(std::max<int64_t>(1, std::min<int64_t>({a.waves ? 512 / blocks : (511 + blocks) / blocks, (steps + 7) / 8, 256})));
     return a;
 }
 
@@ -818,10 +831,7 @@ void run_attention(const AttentionParams &p, const Plan &a, int64_t batch, hipSt
     const dim3 many(uint32_t((int64_t(bhs) * a.row_tiles * a.splits + 7) / 8 * 8));
     if (a.waves == 0) hipLaunchKernelGGL((attention_few_kernel<T, DP>), dim3(a.splits, bhs), dim3(256), 0, s, p);
     else {
-        const bool one = (1 << p.page_shift) % kStep == 0;
-        const auto k = a.waves == 2 ? (one ? attention_many_kernel<T, DP, 2, true> : attention_many_kernel<T, DP, 2, false>)
-                                    : (one ? attention_many_kernel<T, DP, 4, true> : attention_many_kernel<T, DP, 4, false>);
-        hipLaunchKernelGGL(k, many, dim3(64 * a.waves), 0, s, p, bhs);
+        hipLaunchKernelGGL((a.waves == 2 ? attention_many_kernel<T, DP, 2> : attention_many_kernel<T, DP, 4>), many, dim3(64 * a.waves), 0, s, p, bhs);
     }
     if (a.splits > 1)
         hipLaunchKernelGGL((attention_join_kernel<T, DP / 4>), dim3(uint32_t(bhs * a.rows)), dim3(256), 0, s, p);
