@@ -121,7 +121,7 @@ __device__ __forceinline__ uint32_t place_scales4(uint32_t v, int b, int blocks)
 // and they add their sums in LDS. The weights are the instruction's first operand, so that a
 // lane ends up with four consecutive outputs of one row of y. Bound by the latency of reading
 // w: 8 x 4096 outputs of 4096, 17 MB, 6.4 us (2.6 TB/s; the launch and the sums' exchange are about 3
-// of them); from 32 rows on by the loads of x, which every block repeats.
+// of them); with more rows by the loads of x, which every block repeats.
 template <typename O, int WF, int MT, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES)
 linear_rows_kernel(const LinearParams p)
@@ -234,21 +234,21 @@ __device__ __forceinline__ void store_outputs(const LinearParams &p, int m, int 
 }
 
 // Many rows of x: a block forms BN outputs of BM rows of y, 128 elements of the reduction
-// at a time, which go from memory to LDS without registers, one step ahead of the
+// at a time, which go from memory to LDS without registers, STAGES - 1 steps ahead of the
 // products. A row's eight 16-byte pieces are kept in an order of its own, so that the
 // lanes of a read find theirs in different banks. Bound by the transfers' latency where
-// there is one round of blocks (128 x 4096 outputs of 4096: 19 us for 32 steps), by LDS reads where there
-// are more (5000 x 5000: 117 us, 1.75 PFLOP/s).
+// there is one round of blocks (128 x 4096 outputs of 4096, tiles of 64: 11.8 us for 32 steps), by LDS reads
+// where there are more (tiles of 128, 2900 x 6000 outputs of 4096: 82 us, 1.7 PFLOP/s).
 template <typename O, int WF, int BN, int BM, int WN, int WM, int STAGES>
 __global__ void __launch_bounds__(64 * WN * WM, 1)
 linear_tile_kernel(const LinearParams p, int tiles_n, int tiles_m)
 {
     constexpr int kWaves = WN * WM, NT = BN / WN / 16, MT = BM / WM / 16;
     constexpr int kStage = (BN + BM) * 128, kLoadsW = BN / 8 / kWaves, kLoadsX = BM / 8 / kWaves, kGroup = 8;
-    static_assert((kLoadsW + kLoadsX) % 4 == 0, "four at a time");
     constexpr int kGroups = 16;                  // of 4 steps, whose scales are in LDS together
+    constexpr int kWeights = (BN + 127) / 128;    // scales of w a step
     __shared__ __align__(16) uint8_t lds[STAGES * kStage];
-    __shared__ uint32_t scales[kGroups][BM + BN / 128];
+    __shared__ uint32_t scales[kGroups][BM + kWeights];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), r = lane & 15, g = lane >> 4;
     // Blocks are dealt to the 8 XCDs in turn: each takes a run of tiles, kGroup rows of
     // tiles at a time, so that those in flight share their inputs in its L2.
@@ -282,7 +282,7 @@ linear_tile_kernel(const LinearParams p, int tiles_n, int tiles_m)
     };
     // The scales of the block's rows (of w's, by 128) for 64 steps from `step` on, four a word.
     auto fetch_scales = [&](int step) {
-        constexpr int kRows = BM + BN / 128;
+        constexpr int kRows = BM + kWeights;
         const int groups = min(kGroups, (p.kblocks - step + 3) / 4);
 #pragma unroll 4
         for (int i = threadIdx.x; i < kRows * groups; i += 64 * kWaves) {
@@ -576,32 +576,42 @@ void run_tiles(const LinearParams &p, hipStream_t s)
     hipLaunchKernelGGL((linear_tile_kernel<O, WF, BN, BM, WN, WM, STAGES>), dim3(uint32_t((int64_t(tn) * tm + 7) / 8 * 8)), dim3(64 * WN * WM), 0, s, p, tn, tm);
 }
 
+// Which kernel a product runs on. (Up to 32 bits' offsets only: further apart, rows go through
+// linear_rows_kernel.)
 template <typename O, int WF>
 void run_linear(const LinearParams &p, hipStream_t s)
 {
     // The tiles' 32-bit offsets reach 256 rows.
     const bool reach = p.ldx <= (1 << 22) && p.ldw <= (1 << 22);
-    // Up to 64 rows linear_rows_kernel, whose time goes with its groups of 16 outputs times 16 rows,
-    // where those are few: 64 x 4096 outputs of 4096 (1024 groups) 12.9 us, tiles 17.8; 32 x 8192 (1024)
-    // 14.7 and 17.5; 32 x 11000 (1376) 20.4 and 17.6; 64 x 11000 (2752) 41 and 18. Up to 16 rows always:
-    // 8 x 32768 30.5 and 34.5, 16 x 16384 18.2 and 17.3.
+    // Few rows: linear_rows_kernel, whose time goes with its groups of 16 outputs times 16 rows, where those
+    // are few. k = 4096, us, tiles behind: 8 x 8192 outputs (512 groups) 9.5 and 11.2, 8 x 11000 (688) 12.4 and
+    // 11.5; 32 x 4096 (512) 8.8 and 11.4, 32 x 5504 (688) 14.6 and 11.5; 64 x 2048 (512) 12.6 and 11.6.
+    // Outputs in 32 bits, whose products are more instructions in either: 8 x 11000 12.6 and 20.8.
     const int64_t groups = int64_t((p.n + 15) / 16) * (p.m <= 16 ? 1 : p.m <= 32 ? 2 : 4);
-    if ((p.m > 64 || (p.m > 16 && groups > 1200)) && reach) {
+    constexpr bool wide_sums = sizeof(O) == 4;
+    if ((p.m > (wide_sums ? 64 : 32) || groups > (wide_sums ? 1200 : 512)) && reach) {
         const int64_t t256 = int64_t((p.n + 255) / 256) * ((p.m + 255) / 256), t128 = int64_t((p.n + 127) / 128) * ((p.m + 127) / 128);
         if constexpr (sizeof(O) == 2) {
-            // Tiles of 256 where their rounds over the 256 CUs cost less: a round takes 50 to 57 us at
-            // k = 4096, so much as 640 tiles of 128 (54 us). 2500 x 4096 outputs (160 and 640 tiles):
-            // 52 and 54 us; 2048 x 4096: 52 and 40; 2900 x 6000 (288 and 1081): 102 and 82; 5000 x
-            // 5000: 105 and 117; 4096 x 4096: 58 and 70.
-            if (t128 >= 640 * ((t256 + 255) / 256)) {
+            // Whichever takes less by what its rounds take (in 10 ns): of 256 tiles of 256, or, two a CU,
+            // of half as many CUs' tiles of 128. Measured (tiles of 256 and of 128, us): k = 4096, 2500 x 4096
+            // outputs 52 and 54; 2048 x 4096 52 and 40; 2900 x 6000 102 and 82; 5000 x 5000 105 and 117;
+            // 4096 x 4096 58 and 70; 8192 x 8192 231 and 300; k = 128, 5698 x 4352 30 and 24, 4096 x 4096 17 and
+            // 17; k = 1024, 5698 x 4352 46 and 39, 8192 x 8192 88 and 94.
+            const int64_t wide = (t256 + 255) / 256 * (1300 + 120 * p.kblocks), two = (t128 + 255) / 256 * (350 + 43 * p.kblocks);
+            if (t128 > 256 && wide <= two) {
                 const int tn = (p.n + 255) / 256, tm = (p.m + 255) / 256;
                 hipLaunchKernelGGL((linear_wide_kernel<O, WF>), dim3(uint32_t((t256 + 7) / 8 * 8)), dim3(256), 0, s, p, tn, tm);
                 return;
             }
         }
-        // One block a CU at most: eight waves, four steps in LDS (1024 x 4096 outputs of 4096: 22.8 us,
-        // four waves with two steps 26.2). More: two blocks of four waves share a CU (5000 x 5000 outputs of
-        // 4096: 117 us, eight waves and four steps 140).
+        // Up to two blocks a CU of 64 x 64: a step's products and reads are a quarter as many, and it is
+        // their time that a lone block waits for (128 x 4096 outputs of 4096: 11.8 us, tiles of 128 19.1; 6383
+        // x 80 of 2822: 11.3 and 16.7; 512 x 4096 of 4096: 17.3 and 19.5; 1024 x 4096: 32 and 23).
+        const int64_t t64 = int64_t((p.n + 63) / 64) * ((p.m + 63) / 64);
+        if (t64 <= 512) return run_tiles<O, WF, 64, 64, 2, 2, 4>(p, s);
+        // One block of 128 x 128 a CU at most: eight waves, four steps in LDS (1024 x 4096 outputs of 4096:
+        // 22.8 us, four waves with two steps 26.2). More: two blocks of four waves share a CU (5000 x 5000
+        // outputs of 4096: 117 us, eight waves and four steps 140).
         if (t128 <= 256) return run_tiles<O, WF, 128, 128, 2, 4, 4>(p, s);
         return run_tiles<O, WF, 128, 128, 2, 2, 2>(p, s);
     }

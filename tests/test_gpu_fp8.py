@@ -314,7 +314,7 @@ def test_product_input_gradient(ops, m, n, k, wtype, out):
     near(dx, dy @ w, product_terms(dy, w.T.contiguous(), n, out == F32))
 
 
-@pytest.mark.parametrize("m,n,k", [(20, 11000, 130), (50, 5501, 272), (2561, 4100, 1), (2561, 4100, 136), (4100, 2700, 250), (2561, 4100, 384),
+@pytest.mark.parametrize("m,n,k", [(20, 11000, 130), (50, 5501, 272), (1, 9000, 1100), (40, 130, 700), (700, 300, 640), (1000, 3000, 333), (2561, 4100, 1), (2561, 4100, 136), (4100, 2700, 250), (2561, 4100, 384),
                                    (2817, 3900, 655), (2561, 4100, 4230), (5000, 4400, 1000)])
 @pytest.mark.parametrize("wtype,out", [(E4M3, BF16), (E5M2, F16)])
 def test_product_of_many_tiles(ops, m, n, k, wtype, out):
