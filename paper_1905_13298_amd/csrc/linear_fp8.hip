@@ -383,11 +383,12 @@ linear_tile_kernel(const LinearParams p, int tiles_n, int tiles_m)
 // more of the reduction on its way. A step's elements of x come in two halves (the first
 // four tiles of 16 rows of every wave, and the last four), which go through five places in
 // turn; those of w go through two and into registers before their step. A half's place is
-// free when its last elements have been read, so there are two barriers a step: in front of
-// the last products of the first half the next but one step's second half and weights are
-// sent for, in front of those of the second half the first half of the step after that. What
-// a step waits for was sent for at least a step and a half before (a step takes 1.1 us at the
-// least here, memory behind the L2 answers after about 2). Bound by the matrix instructions, at
+// free when its last elements have been read, so there are two barriers a step: from the last
+// products of the first half on, the next but one step's second half and weights are sent
+// for, among those of the second half's last row the first half of the step after that, a transfer
+// behind every two or three products (all at once: 247 us for 233). What a step waits for was
+// sent for about a step before (a step takes 1.1 us at the least, memory behind the L2 answers
+// after up to 2). Bound by the matrix instructions, at
 // the clock that the card holds while they run, and by a block's start and end, which nothing
 // overlaps: 8192 x 8192 outputs of 4096 in 231 us (2.4 PFLOP/s).
 template <typename O, int WF>
