@@ -201,6 +201,10 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const uint8_t *p, in
 // or past it, since a branch in the loop would have the compiler move products behind it.
 __device__ __forceinline__ int inside(int offset, bool in) { return in ? offset : 0x7ffffff0; }
 
+// The scalar offset of a step: the last step's for those past it. The range check takes it off the
+// buffer's size, which may be as little as one row, so it has to stay within that.
+__device__ __forceinline__ int step_offset(int step, int steps) { return min(step, steps - 1) * 128; }
+
 // A reduction that ends inside a lane's 16 bytes: the bytes past its end, in LDS.
 __device__ __forceinline__ void clear_past(uint8_t *at, int left)
 {
@@ -271,8 +275,8 @@ linear_tile_kernel(const LinearParams p, int tiles_n, int tiles_m)
     for (int i = 0; i < kLoadsX; ++i) xv[i] = min(i * kWaves * 8 + lrow, p.m - 1 - m0) * ldx + piece;
     const uint32_t base_lds = __builtin_amdgcn_readfirstlane(lds_address(lds));
     auto stage = [&](int step, int buf) {
-        const int k = step * 128;
-        const bool in = k + piece < p.k;
+        const int k = step_offset(step, p.kblocks);
+        const bool in = step * 128 + piece < p.k;
 #pragma unroll
         for (int i = 0; i < kLoadsW; ++i)
             to_lds16(base_lds + buf * kStage + (i * kWaves + wave) * 1024, wr, inside(wv[i], in), k);
@@ -421,10 +425,12 @@ linear_wide_kernel(const LinearParams p, int tiles_n, int tiles_m)
     const uint32_t base_lds = __builtin_amdgcn_readfirstlane(lds_address(lds));
     // Load i of a step's weights, or of a half of its elements of x.
     auto fetch_w = [&](int step, int i) {
-        to_lds16(base_lds + (step & 1) * kW + (i * 4 + wave) * 1024, wr, inside(wv[i], step * 128 + piece < p.k), step * 128);
+        to_lds16(base_lds + (step & 1) * kW + (i * 4 + wave) * 1024, wr, inside(wv[i], step * 128 + piece < p.k),
+                 step_offset(step, p.kblocks));
     };
     auto fetch_x = [&](int step, int half, int place, int i) {
-        to_lds16(base_lds + 2 * kW + place * kHalf + (i * 4 + wave) * 1024, xr, inside(xv[half][i], step * 128 + piece < p.k), step * 128);
+        to_lds16(base_lds + 2 * kW + place * kHalf + (i * 4 + wave) * 1024, xr, inside(xv[half][i], step * 128 + piece < p.k),
+                 step_offset(step, p.kblocks));
     };
     // The scales of the block's rows (of w's, by 128) for 32 steps from `step` on, four a word.
     auto fetch_scales = [&](int step) {
