@@ -663,8 +663,9 @@ int64_t ds_linear_fp8_backward_data_scratch_bytes(int64_t m, int64_t n, int64_t 
  * tokens; dim: a multiple of 16, at most 256. Row b of `table` [batch][columns] (ldt
  * elements apart) lists the pages of sequence b in order.
  *
- * ds_kv_cache_append writes tokens 0 .. count[b] - 1 (count NULL: all) of k and v
- * [batch][tokens][heads][dim] at positions start[b], start[b] + 1, .. of sequence b. A
+ * ds_kv_cache_append writes tokens 0 .. count[b] - 1 (count NULL or above tokens: all) of k and
+ * v [batch][tokens][heads][dim] at positions start[b], start[b] + 1, .. of sequence b (none where
+ * start[b] is negative). A
  * page's scale is the one its new tokens need; where it already holds tokens before
  * start[b], the larger of that and its own, and what it holds is rounded again where the
  * scale grows. Values past the scales' range are held as the largest number. Tokens of a
@@ -681,11 +682,12 @@ ds_status ds_kv_cache_append(const void *k, const void *v, uint8_t *k_cache, uin
 
 /* Causal attention of q [batch][tokens][heads * group][dim] (type DS_TYPE_F16 or
  * DS_TYPE_BF16; query head h reads head h / group of the cache) over sequences of
- * length[b] tokens in the cache, the last count[b] of which (count NULL: tokens) are the
- * queries': query i < count[b] is at position length[b] - count[b] + i and sees the keys
- * up to its own, the last `window` of them where window > 0. o (q's shape and type) =
- * softmax(scale * q k) v; a query that sees no key, or i >= count[b], gets zeros. Keys on
- * a page outside 0 .. pages - 1 are not seen (a page may leave a sequence that way). What
+ * length[b] tokens, the last count[b] of which (count NULL: tokens) are the queries': query
+ * i < count[b] is at position length[b] - count[b] + i and sees the keys up to its own, the
+ * last `window` of them where window > 0. o (q's shape and type) = softmax(scale * q k) v; a
+ * query that sees no key, or i >= count[b], gets zeros. Keys past the table's columns, or on a
+ * page outside 0 .. pages - 1, are not seen (a page may leave a sequence that way) and move no
+ * position. A length below 0 is taken as 0, a count outside 0 .. tokens as the nearest of those. What
  * pages hold past a sequence's end does not matter; a NaN among the values of a token
  * that one query of a call sees reaches the queries of the same call and head that do not.
  * scratch: ds_attention_fp8_scratch_bytes (0: none needed). */

@@ -286,27 +286,31 @@ __device__ __forceinline__ int key_mask(int key, int low, int high)
     return int(mask);
 }
 
-// What the queries of 16 rows of a kv head see.
+// A sequence's queries and the position of the first, which a length beyond the table does not
+// move (and which is negative where there are more queries than tokens); the keys that have a column.
 struct Sequence {
-    int length, count, first;
+    int count, first, keys;
     __device__ __forceinline__ Sequence(const AttentionParams &p, int b)
     {
-        length = int(min(int64_t(max(p.length[b], 0)), int64_t(p.columns) << p.page_shift));
-        count = min(p.count ? max(p.count[b], 0) : p.tokens, min(p.tokens, length));
-        first = length - count;            // position of the first query
+        const int length = max(p.length[b], 0);
+        count = p.count ? min(max(p.count[b], 0), p.tokens) : p.tokens;
+        first = length - count;
+        keys = int(min(int64_t(length), int64_t(p.columns) << p.page_shift));
     }
 };
 
-// A lane's query: row `row` of head h, its keys [low, high), its elements as the first
-// product's second operand (chunk c: elements c * CHUNK + g * GROUP .. + 7).
+// A lane's query: row `row` of head h, its keys [low, high) (0, 0 where it sees none), its elements as
+// the first product's second operand (chunk c: elements c * CHUNK + g * GROUP .. + 7).
 template <typename T, int DP, int CHUNK, int GROUP, int N>
 __device__ __forceinline__ bool load_query(const AttentionParams &p, const Sequence &seq, int b, int h, int row, int g, int &low, int &high,
                                            typename Vec8<T>::type (&qf)[N])
 {
     const int t = row / p.group, hq = h * p.group + row - t * p.group;
     const bool live = row < p.rows && t < seq.count;
-    high = live ? seq.first + t + 1 : 0;
-    low = live && p.window ? max(high - p.window, 0) : 0;
+    const int upto = live ? seq.first + t + 1 : 0;
+    high = min(max(upto, 0), seq.keys);
+    low = p.window ? max(max(upto, 0) - p.window, 0) : 0;
+    if (low >= high) low = high = 0;
     const T *src = static_cast<const T *>(p.q) + b * p.qb + (live ? t * p.qt + hq * p.qh : 0);
 #pragma unroll
     for (int c = 0; c < N; ++c) {
@@ -355,8 +359,8 @@ attention_few_kernel(const AttentionParams p)
     const Sequence seq(p, b);
     v8 qf[QC];
     int low, high;
-    const bool live = load_query<T, DP, 8, DP / 4, QC>(p, seq, b, h, r, g, low, high, qf);
-    int tlo = live ? low : 0x7fffffff, thi = high;
+    load_query<T, DP, 8, DP / 4, QC>(p, seq, b, h, r, g, low, high, qf);
+    int tlo = high > 0 ? low : 0x7fffffff, thi = high;
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) {
         tlo = min(tlo, __shfl_xor(tlo, o));
@@ -503,8 +507,9 @@ attention_many_kernel(const AttentionParams p, int bhs)
     if (!live) high = 0x7fffffff;
     // The block's keys: from the first that its first query sees to its last query's own.
     const int t0 = tile * WAVES * 32 / p.group, t1 = min(((tile + 1) * WAVES * 32 - 1) / p.group, seq.count - 1);
-    const int thi = t0 < seq.count ? seq.first + t1 + 1 : 0, tlo = p.window ? max(seq.first + t0 + 1 - p.window, 0) : 0;
-    const int s0 = thi > 0 ? tlo / kStep : 0, s1 = (thi + kStep - 1) / kStep;
+    const int thi = t0 < seq.count ? min(max(seq.first + t1 + 1, 0), seq.keys) : 0;
+    const int tlo = p.window ? max(max(seq.first + t0 + 1, 0) - p.window, 0) : 0;
+    const int s0 = thi > tlo ? tlo / kStep : 0, s1 = thi > tlo ? (thi + kStep - 1) / kStep : 0;
     const int each = (s1 - s0 + p.splits - 1) / p.splits;
     const int from = s0 + split * each, to = min(s1, from + each);
 

@@ -94,10 +94,11 @@ class Decoder:
 
     def __call__(self, x, count=None):
         """x [batch, tokens, hidden] of the next tokens, the first count[b] of them (all without count) those
-        of sequence b -> the last norm's output. A prompt and single tokens alike; with one shape a
-        call it can be captured into a graph. Tokens past the capacity are dropped."""
+        of sequence b (all where it is more) -> the last norm's output. A prompt and single tokens alike; with one
+        shape a call it can be captured into a graph. Tokens past the capacity are not kept: they count in `length`,
+        come out as tokens that see what was kept, and are seen by none."""
         start = self.length.clone()
-        self.length += x.shape[1] if count is None else count
+        self.length += x.shape[1] if count is None else count.clamp(0, x.shape[1])
         residual = None
         for layer, cache in zip(self.layers, self.caches):
             x, residual = layer(x, residual, cache, self.table, start, self.length, count)

@@ -1044,8 +1044,8 @@ def _vectors(t, name: str):
 
 def kv_cache_append(k, v, k_cache, v_cache, k_scales, v_scales, table, start, count=None):
     """Writes k and v [batch, tokens, heads, dim] into a paged 8-bit cache, in place: tokens 0 .. count[b] - 1
-    (all without count) at positions start[b], start[b] + 1, .. of sequence b, whose pages row b of `table`
-    [batch, columns] lists (all int32 device tensors). A page's scale grows where its new tokens need it, and
+    (all without count, or where it is more) at positions start[b], start[b] + 1, .. of sequence b, whose pages row b
+    of `table` [batch, columns] lists (all int32 device tensors). A page's scale grows where its new tokens need it, and
     what it holds is rounded again. Tokens past the table, or on a page outside the cache, are dropped."""
     _dev_as(k, "k", _FLOATS)
     if k.dim() != 4:
@@ -1068,10 +1068,11 @@ def kv_cache_append(k, v, k_cache, v_cache, k_scales, v_scales, table, start, co
 def attention_fp8(q, k_cache, v_cache, k_scales, v_scales, table, length, count=None, scale: float | None = None,
                   window: int = 0):
     """Causal attention of q [batch, tokens, query heads, dim] (float16 or bfloat16) over a paged 8-bit cache: o, of
-    q's shape and type. Sequence b has length[b] tokens in the cache, the last count[b] of them (all `tokens`
-    without count) the queries'; query head h reads head h // (query heads / heads). A query sees the keys up to
-    its own position, the last `window` of them where window > 0; one that sees none gets zeros. scale: 1 / sqrt(dim)
-    without one. table, length, count: int32 device tensors."""
+    q's shape and type. Sequence b has length[b] tokens, the last count[b] of them (all `tokens` without count, or
+    where it is more) the queries'; query head h reads head h // (query heads / heads). A query sees the keys up to
+    its own position, the last `window` of them where window > 0; one that sees none gets zeros. Tokens past the
+    table, which an append drops, count for positions and are not seen. scale: 1 / sqrt(dim) without one. table, length,
+    count: int32 device tensors."""
     _dev_as(q, "q", (torch.bfloat16, torch.float16))
     if q.dim() != 4:
         raise ValueError("q must be [batch, tokens, heads, dim]")

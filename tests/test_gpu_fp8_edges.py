@@ -4,11 +4,12 @@ numbers. Definitions in 64 bits and tolerances as in test_gpu_fp8.
 """
 import math
 
+import numpy as np  # noqa: F401
 import pytest
 import torch
 
-from .test_gpu_fp8 import (BF16, DEV, E4M3, E5M2, E8M0, F16, F32, filled_cache, near, normal, operands, product_terms,  # noqa: F401
-                           value)
+from .test_gpu_decoder import build as build_decoder
+from .test_gpu_fp8 import BF16, DEV, E4M3, F16, F32, filled_cache, near, normal, operands, product_terms, value  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -32,3 +33,105 @@ def test_product_tiles_of_one_row(ops, m, n, k):
     rows = torch.tensor([0, 1, m // 2, m - 2, m - 1])
     x, w = value(x8, xs)[rows], value(w8, ws, 128)
     near(y[rows], x @ w.T, product_terms(x, w, k, False))
+
+
+# ---------------------------------------------------------------------------
+# Attention.
+
+def definition(q, cache, table, length, count, window, scale):
+    """(o, what it may be off by) of the definition in 64 bits: query i < count of a sequence is at position
+    length - count + i and sees the keys up to there, the last `window` of them, that the table has a page for."""
+    k8, v8, ks, vs = (t.cpu() for t in cache)
+    pages, heads, page, dim = k8.shape
+    batch, tokens, hq, _ = q.shape
+    o, off = torch.zeros(batch, tokens, hq, dim, dtype=torch.float64), torch.zeros(batch, tokens, hq, dim, dtype=torch.float64)
+    for b in range(batch):
+        c, n = min(max(int(count[b]), 0), tokens), min(max(int(length[b]), 0), table.shape[1] * page)
+        if c == 0 or n == 0:
+            continue
+        pid = table[b, :(n + page - 1) // page].long()
+        good = ((pid >= 0) & (pid < pages)).repeat_interleave(page)[:n]
+        pid = torch.where((pid >= 0) & (pid < pages), pid, 0)
+        pos = (max(int(length[b]), 0) - c + torch.arange(c))[:, None]
+        j = torch.arange(n)[None, :]
+        seen = (j <= pos) & good[None, :]
+        if window:
+            seen &= j > pos - window
+        some = seen.any(1, keepdim=True)
+        for h in range(heads):
+            key = torch.exp2(ks.view(torch.uint8)[pid, h].double() - 127).repeat_interleave(page)[:n]
+            val = torch.exp2(vs.view(torch.uint8)[pid, h].double() - 127).repeat_interleave(page)[:n]
+            k = torch.where(seen.any(0)[:, None], k8[pid, h].double().reshape(-1, dim)[:n] * key[:, None], 0.0)
+            v = torch.where(seen.any(0)[:, None], v8[pid, h].double().transpose(1, 2).reshape(-1, dim)[:n], 0.0)     # without the scale
+            nan = v.isnan()
+            v = v.nan_to_num(0.0)
+            for g in range(hq // heads):
+                x = q[b, :c, h * (hq // heads) + g].double()
+                s = torch.where(seen, scale * (x @ k.T), -math.inf)
+                p = torch.exp(s - torch.where(some, s.amax(1, keepdim=True), 0.0))
+                total = p.sum(1, keepdim=True).clamp(min=1e-300)
+                p = p * val
+                out = torch.where(some, p @ v / total, 0.0)
+                o[b, :c, h * (hq // heads) + g] = torch.where(seen.double() @ nan.double() > 0, math.nan, out)
+                # Scores in 32 bits; weights rounded to 2^-11 each for itself (their errors add up as squares do: 6
+                # deviations of a uniform error); below 2^-25 of the largest one, to 2^-36 of it.
+                ds = ((dim + 4) * 2.0 ** -23 * scale * (x.abs() @ k.abs().T) + s.abs().nan_to_num(posinf=0) * 2.0 ** -22).nan_to_num()
+                rel = 2 * (ds * seen).amax(1, keepdim=True) + 2.0 ** -20
+                squares = 6 / math.sqrt(3) * (torch.maximum(p * 2.0 ** -11, p.amax(1, keepdim=True) * 2.0 ** -36 * seen).square() @ v.square()).sqrt()
+                off[b, :c, h * (hq // heads) + g] = torch.where(some, (rel * (p @ v.abs()) + squares) / total, 0.0)
+    return o, off
+
+
+def agree(o, want, off):
+    nan = want.isnan()
+    assert torch.equal(o.cpu().isnan(), nan)
+    near(o.cpu().nan_to_num(0.0), want.nan_to_num(0.0), off)
+
+
+def pages_of(ops, batch, columns, heads, page, dim, seed=0):
+    cache = filled_cache(ops, batch * columns + 2, heads, page, dim, seed)
+    table = torch.randperm(batch * columns + 2, generator=torch.Generator().manual_seed(seed))[:batch * columns].reshape(batch, columns)
+    return cache, table.to(torch.int32)
+
+
+def attend(ops, q, cache, table, length, count=None, window=0):
+    length = torch.tensor(length, dtype=torch.int32)
+    c = torch.tensor([q.shape[1]] * len(length) if count is None else count, dtype=torch.int32)
+    o = ops.attention_fp8(q.to(DEV), *cache, table.to(DEV), length.to(DEV), None if count is None else c.to(DEV), window=window)
+    return o, *definition(q, cache, table, length, c, window, 1 / math.sqrt(q.shape[3]))
+
+
+@pytest.mark.parametrize("tokens,group", [(1, 2), (5, 2), (10, 4), (150, 2)])
+@pytest.mark.parametrize("window", [0, 7, 40])
+def test_attention_of_sequences_past_their_table(ops, tokens, group, window):
+    """Queries keep their positions where their own keys found no room, where counts are over the tokens or the length, and
+    where lengths are negative."""
+    columns, page, dim = 4, 16, 64
+    cap = columns * page
+    length = [cap + tokens - 1, cap + 1, cap + 6, cap, 3, 0, -9, cap + 500, 30]
+    count = [tokens, tokens, tokens, tokens + 3, 5, tokens, 1, tokens, -2]
+    cache, table = pages_of(ops, len(length), columns, 2, page, dim)
+    q = normal(3, len(length), tokens, 2 * group, dim).to(BF16)
+    agree(*attend(ops, q, cache, table, length, count, window))
+
+
+# ---------------------------------------------------------------------------
+# Decoder.
+
+def test_decoder_past_its_capacity():
+    """A ragged prompt that crosses the capacity: the tokens that found room come out as from a decoder with more of it."""
+    make, ps, norm, rng = build_decoder(5, 2, 256, 8, 2, 32, 512, BF16, 3, 64, 16, 0)
+    room, ps, norm, rng = build_decoder(5, 2, 256, 8, 2, 32, 512, BF16, 3, 96, 16, 0)
+    small, large = make(), room()
+    assert (small.capacity, large.capacity) == (64, 96)
+    x = torch.from_numpy(rng.standard_normal((3, 80, 256))).to(DEV, BF16)
+    first = torch.tensor([60, 10, 33], dtype=torch.int32, device=DEV)
+    assert torch.equal(small(x[:, :60], first), large(x[:, :60], first))
+    got, want = small(x[:, 60:72]), large(x[:, 60:72])
+    for b, n in enumerate((4, 12, 12)):
+        assert torch.equal(got[b, :n], want[b, :n])
+    assert small.length.tolist() == large.length.tolist() == [72, 22, 45]
+    # A count above the tokens means all of them.
+    many = torch.full((3,), 9, dtype=torch.int32, device=DEV)
+    got, want = small(x[:, 72:74], many), large(x[:, 72:74])
+    assert torch.equal(got[1:], want[1:]) and small.length.tolist() == [74, 24, 47]
