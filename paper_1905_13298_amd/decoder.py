@@ -97,11 +97,26 @@ class Decoder:
         of sequence b (all where it is more) -> the last norm's output. A prompt and single tokens alike; with one
         shape a call it can be captured into a graph. Tokens past the capacity are not kept: they count in `length`,
         come out as tokens that see what was kept, and are seen by none."""
-        start = self.length.clone()
-        self.length += x.shape[1] if count is None else count.clamp(0, x.shape[1])
+        self._check(x, count)
+        length = self.length + (x.shape[1] if count is None else count.clamp(0, x.shape[1]))
         residual = None
         for layer, cache in zip(self.layers, self.caches):
-            x, residual = layer(x, residual, cache, self.table, start, self.length, count)
+            x, residual = layer(x, residual, cache, self.table, self.length, length, count)
         hidden = x.shape[2]
         y, _, _, _ = ops.rms_norm(x.reshape(-1, hidden), self.norm, residual.reshape(-1, hidden), quantize=False)
+        self.length.copy_(length)      # (once nothing can be refused any more)
         return y.view(x.shape)
+
+    def _check(self, x, count):
+        """Refuses a call before any cache is written: a decoder is as it was behind an error."""
+        ops._dev_as(x, "x", (torch.bfloat16, torch.float16))
+        batch, hidden = self.length.shape[0], self.norm.shape[0]
+        if x.dim() != 3 or x.shape[0] != batch or x.shape[2] != hidden:
+            raise ValueError(f"x must be [{batch}, tokens, {hidden}], got {tuple(x.shape)}")
+        norms = [self.norm] + [n.norm for layer in self.layers for n in (layer.qkv, layer.gate_up)]
+        for norm in norms:
+            if norm.dtype not in (x.dtype, torch.float32):
+                raise TypeError(f"x is {x.dtype}, a norm's weight {norm.dtype}")
+        if count is not None:
+            ops._vector(count, "count", (torch.int32,), batch)
+        ops._same_device(x.device, count, self.length, *norms)

@@ -135,3 +135,20 @@ def test_decoder_past_its_capacity():
     many = torch.full((3,), 9, dtype=torch.int32, device=DEV)
     got, want = small(x[:, 72:74], many), large(x[:, 72:74])
     assert torch.equal(got[1:], want[1:]) and small.length.tolist() == [74, 24, 47]
+
+
+def test_decoder_is_unchanged_by_a_refused_call():
+    make, ps, norm, rng = build_decoder(6, 1, 256, 8, 2, 32, 512, BF16, 2, 64, 16, 0)
+    model, other = make(), make()
+    x = torch.from_numpy(rng.standard_normal((2, 4, 256))).to(DEV, BF16)
+    two = torch.full((2,), 2, dtype=torch.int32, device=DEV)
+    bad = [lambda: model(x.float()), lambda: model(x.half()), lambda: model(x.cpu()), lambda: model(x[:1]), lambda: model(x[0]), lambda: model(x[..., :128]),
+           lambda: model(x, two.long()), lambda: model(x, two[:1]), lambda: model(x, two.cpu()), lambda: model(x, two[:, None]), lambda: model(x, 2)]
+    for i, call in enumerate(bad):
+        with pytest.raises((TypeError, ValueError)):
+            call()
+            pytest.fail(f"case {i} was accepted")
+        assert model.length.tolist() == [0, 0], i
+    for a, b in zip(model.caches[0], other.caches[0]):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    assert torch.equal(model(x, two), other(x, two)) and model.length.tolist() == [2, 2]
