@@ -65,10 +65,11 @@ class DecoderLayer:
         next layer; the layer's output is their sum. The tokens are appended at `start` (length = start + count)."""
         batch, tokens, hidden = x.shape
         qkv, h, _ = self.qkv(x.reshape(-1, hidden), None if residual is None else residual.reshape(-1, hidden))
-        q, k, v = qkv.view(batch, tokens, -1, self.dim).split([self.heads, self.kv_heads, self.kv_heads], dim=2)
+        heads = [self.heads, self.kv_heads, self.kv_heads]
+        q, k, v = qkv.view(batch, tokens, sum(heads), self.dim).split(heads, dim=2)
         ops.kv_cache_append(k, v, *cache, table, start, count)
         o = ops.attention_fp8(q, *cache, table, length, count, window=self.window)
-        a = ops.linear_fp8(*ops.quantize_fp8(o.view(batch * tokens, -1)), *self.out, out_dtype=x.dtype)
+        a = ops.linear_fp8(*ops.quantize_fp8(o.view(batch * tokens, self.heads * self.dim)), *self.out, out_dtype=x.dtype)
         gu, h, _ = self.gate_up(a, h)
         gate, up = gu.chunk(2, dim=1)
         y = ops.linear_fp8(*ops.quantize_fp8(up, gate), *self.down, out_dtype=x.dtype)

@@ -152,3 +152,15 @@ def test_decoder_is_unchanged_by_a_refused_call():
     for a, b in zip(model.caches[0], other.caches[0]):
         assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
     assert torch.equal(model(x, two), other(x, two)) and model.length.tolist() == [2, 2]
+
+
+def test_decoder_without_tokens():
+    """No tokens: no rows come out and nothing changes."""
+    make, ps, norm, rng = build_decoder(6, 2, 256, 8, 2, 32, 512, BF16, 2, 64, 16, 0)
+    model = make()
+    x = torch.from_numpy(rng.standard_normal((2, 4, 256))).to(DEV, BF16)
+    want = make()(x)
+    assert model(x[:, :0]).shape == (2, 0, 256) and model.length.tolist() == [0, 0]
+    none = model(x, torch.zeros(2, dtype=torch.int32, device=DEV))
+    assert none.shape == x.shape and model.length.tolist() == [0, 0]
+    assert torch.equal(model(x), want)
