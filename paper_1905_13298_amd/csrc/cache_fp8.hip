@@ -144,16 +144,20 @@ append_kernel(const T *__restrict__ k, const T *__restrict__ v, uint8_t *__restr
 //   S^T = K Q^T (the matrix instruction's rows are keys, its columns queries), so that a
 //   lane holds 16 consecutive keys of one query;
 //   t = S * 2^ek * scale * log2(e) + log2(2^ev): the value scale ev of the keys' page goes
-//   into the exponent, so p = 2^(t - m), m the running maximum of t, is at most 1 and
-//   weighs the 8-bit values themselves;
+//   into the exponent, so that p = 2^(t - m) weighs the 8-bit values themselves; m is such that
+//   the largest p of a row is from 2^9 to 2^15;
 //   O^T += V^T P (rows: dimensions, columns: queries), l += p * 2^-ev.
 //
 // The two layouts agree, so that p goes from the first product to the second in place:
 // the key of row r of a 16-key tile t is chosen as (r / 4) * 16 + t * 4 + r % 4, which
 // leaves lane group g (lane / 16) with keys 16 g .. 16 g + 15, and those are the ones that
 // it contracts in the second product, 8 at a time. Keys become numbers of the queries'
-// type exactly; p and the values are 16-bit floats with 10 bits of mantissa (values
-// exactly, p rounded once to 2^-11).
+// type exactly; p and the values are 16-bit floats with 10 bits of mantissa: values exactly, p
+// rounded once, to 2^-11 of itself down to 2^-23 of the row's largest and to 2^-34 of that one
+// below (l has all of it in 32 bits). The largest is of t, thus of weights times their page's value
+// scale: where pages' scales are 2^d apart, weights on the smaller one keep their bits down to
+// 2^(d - 23) of the largest, and what 10^4 of them lose below that is less than the larger page's
+// values were rounded by when they became 8 bits (unless those are exactly 0).
 
 constexpr int kStep = 64;       // keys of a step
 
@@ -210,22 +214,24 @@ __device__ __forceinline__ PageScale page_scale(int ek, int ev, float scale)
     return PageScale{fmaxf(power_of_two(uint32_t(ek)) * scale, 0x1p-126f), float(ev - 127), power_of_two(uint32_t(254 - ev))};
 }
 
-// The running maximum m of a row moves only when it is passed by more than 2^8, so that the
-// sums are hardly ever rescaled: weights reach 2^8 at most, far inside the range of a 16-bit
-// float. So the exponents are formed with the old maximum, and where none is above 8 they
-// stay.
-constexpr float kSlack = 8.f;
+// A row's reference m lies kBias below the largest exponent that it was set by and moves only when
+// it is passed by more than kBias + kSlack, so that the sums are hardly ever rescaled: the exponents
+// are formed with the old one, and where none is above that they stay. Weights reach 2^15 at
+// most, the upper end of a 16-bit float's range (65504), and have the rest of it below them. What the
+// bias gains there the slack loses in time: 2 x 1000 queries over up to 8000 keys take 256.8 us, with
+// 7 and 8 255.2, with 11 and 4 260.7 (heads of 64, 4000 keys: 94.4, 93.6 and 97.9).
+constexpr float kBias = 9.f, kSlack = 6.f;
 
-// `top`: the largest of a row's new exponents, relative to the maximum (0 in its place where
-// there is none yet). Moves the maximum where it has to, in a branch that is rarely taken: then
+// `top`: the largest of a row's new exponents, relative to the reference (0 in its place where
+// there is none yet). Moves the reference where it has to, in a branch that is rarely taken: then
 // shift(by) takes `by` off the exponents and rescale(alpha) multiplies the sums.
 template <typename Shift, typename Rescale>
 __device__ __forceinline__ void raise(float &m, float &l, float top, Shift &&shift, Rescale &&rescale)
 {
-    const bool none = m == -__builtin_inff(), grown = none ? top > m : top > kSlack;
+    const bool none = m == -__builtin_inff(), grown = none ? top > m : top > kBias + kSlack;
     if (__any(grown)) {
-        const float by = grown ? top : 0.f, alpha = grown ? (none ? 0.f : __builtin_amdgcn_exp2f(-top)) : 1.f;
-        m = none ? (grown ? top : m) : m + by;
+        const float by = grown ? top - kBias : 0.f, alpha = grown ? (none ? 0.f : __builtin_amdgcn_exp2f(-by)) : 1.f;
+        m = none ? (grown ? by : m) : m + by;
         l *= alpha;
         shift(by);
         rescale(alpha);
@@ -689,7 +695,7 @@ attention_many_kernel(const AttentionParams p, int bhs)
                   for (int d = 0; d < DT; ++d) acc[d] *= alpha;
               });
         // (The sum is of the 32-bit weights: of a page whose scale is far below the largest one's
-        // nothing may be left in 16 bits, where its values do not count but its weights do.)
+        // nothing may be left in 16 bits, but its weights count all the same.)
         f16x8 pf[4];
         float sum[4] = {};
         auto weigh = [&](int q, int i) {

@@ -74,10 +74,10 @@ def definition(q, cache, table, length, count, window, scale):
                 out = torch.where(some, p @ v / total, 0.0)
                 o[b, :c, h * (hq // heads) + g] = torch.where(seen.double() @ nan.double() > 0, math.nan, out)
                 # Scores in 32 bits; weights rounded to 2^-11 each for itself (their errors add up as squares do: 6
-                # deviations of a uniform error); below 2^-25 of the largest one, to 2^-36 of it.
+                # deviations of a uniform error); below 2^-23 of the largest one, to 2^-34 of it.
                 ds = ((dim + 4) * 2.0 ** -23 * scale * (x.abs() @ k.abs().T) + s.abs().nan_to_num(posinf=0) * 2.0 ** -22).nan_to_num()
                 rel = 2 * (ds * seen).amax(1, keepdim=True) + 2.0 ** -20
-                squares = 6 / math.sqrt(3) * (torch.maximum(p * 2.0 ** -11, p.amax(1, keepdim=True) * 2.0 ** -36 * seen).square() @ v.square()).sqrt()
+                squares = 6 / math.sqrt(3) * (torch.maximum(p * 2.0 ** -11, p.amax(1, keepdim=True) * 2.0 ** -34 * seen).square() @ v.square()).sqrt()
                 off[b, :c, h * (hq // heads) + g] = torch.where(some, (rel * (p @ v.abs()) + squares) / total, 0.0)
     return o, off
 
@@ -113,6 +113,55 @@ def test_attention_of_sequences_past_their_table(ops, tokens, group, window):
     cache, table = pages_of(ops, len(length), columns, 2, page, dim)
     q = normal(3, len(length), tokens, 2 * group, dim).to(BF16)
     agree(*attend(ops, q, cache, table, length, count, window))
+
+def shared_pages(ops, k, v, page, batch):
+    """A cache of one sequence [n, dim] that `batch` sequences share, enough that no sequence is split."""
+    n, dim = k.shape
+    cache = ops.kv_cache((n + page - 1) // page, 1, page, dim, DEV)
+    table = torch.arange(cache[0].shape[0], dtype=torch.int32)[None]
+    ops.kv_cache_append(k[None, :, None].to(DEV), v[None, :, None].to(DEV), *cache, table.to(DEV), torch.zeros(1, dtype=torch.int32, device=DEV))
+    return cache, table.repeat(batch, 1)
+
+
+def one_of_many(ops, q, cache, table, n, window=0):
+    """The first of many equal sequences, against the definition."""
+    batch = table.shape[0]
+    length = torch.full((batch,), n, dtype=torch.int32)
+    o = ops.attention_fp8(q.to(DEV).expand(batch, *q.shape[1:]), *cache, table.to(DEV), length.to(DEV), window=window)
+    assert bool((o == o[:1]).all())
+    agree(o[:1], *definition(q, cache, table[:1], length[:1], torch.tensor([q.shape[1]]), window, 1 / math.sqrt(q.shape[3])))
+
+
+@pytest.mark.parametrize("low,high", [(-18, -20), (-20, -24), (-23, -27)])
+@pytest.mark.parametrize("tokens,group", [(1, 4), (8, 4), (40, 4)])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_attention_of_a_sink_and_many_small_weights(ops, low, high, tokens, group, dim):
+    """A dominant key without a value; all that comes out is of keys with 2^low .. 2^high of its weight."""
+    n = 16384
+    k = torch.zeros(n, dim)
+    k[:, 0] = (torch.rand(n, generator=torch.Generator().manual_seed(1)) * (high - low) + low) * math.log(2) + 8
+    k[:, 1] = normal(2, n)
+    k[0, 0], k[0, 1] = 8, 0
+    v = normal(3, n, dim) * 1024
+    v[0] = 0
+    cache, table = shared_pages(ops, k, v, 64, 512)
+    q = torch.zeros(1, tokens, group, dim, dtype=F16)
+    q[..., 0], q[..., 1] = math.sqrt(dim), 0.25
+    one_of_many(ops, q, cache, table, n)
+
+
+@pytest.mark.parametrize("times", [12, 16])
+@pytest.mark.parametrize("tokens,group", [(1, 4), (8, 4), (40, 4)])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_attention_beside_a_large_value_that_no_query_sees(ops, times, tokens, group, dim):
+    """A value before the window that is 2^times as large as the others sets its page's scale."""
+    n, page = 8192, 64
+    window = n - tokens - 30
+    k, v = normal(4, n, dim), normal(5, n, dim) * 16
+    v[3] *= 2.0 ** times
+    cache, table = shared_pages(ops, k, v, page, 512)
+    q = (normal(6, 1, tokens, group, dim)).to(F16)
+    one_of_many(ops, q, cache, table, n, window)
 
 
 # ---------------------------------------------------------------------------
