@@ -634,7 +634,8 @@ ds_status ds_quantize_weights_fp8(const void *w, uint8_t *w8, uint8_t *scales, i
                                   int32_t type, void *stream);
 
 /* Packed shift codes (flags: DS_CODE_BITS) as E5M2 numbers +-2^-shift and 0, exactly;
- * every scale of such a matrix is 2^0, the byte 127. */
+ * every scale of such a matrix is 2^0, the byte 127. Up to 65535 rows a call (a larger
+ * matrix is several calls' rows). */
 ds_status ds_shift_weights_to_fp8(const uint32_t *w_packed, uint8_t *w8, int64_t rows,
                                   int64_t cols, int64_t ldw8, uint32_t flags, void *stream);
 

@@ -948,7 +948,10 @@ def shift_weights_to_fp8(w_packed, cols: int, code_bits: int = 5):
         raise ValueError(f"w_packed must have {packed_row_words(cols, code_bits)} words a row, got {words}")
     dev = w_packed.device
     w8 = _empty8(rows, cols, torch.float8_e5m2, dev)
-    _launch("ds_shift_weights_to_fp8", dev, w_packed.data_ptr(), w8.data_ptr(), rows, cols, (cols + 15) & -16, code_bits_flag(code_bits))
+    pitch = (cols + 15) & -16
+    for r in range(0, max(rows, 1), 65535):     # what a call takes
+        _launch("ds_shift_weights_to_fp8", dev, w_packed.data_ptr() + r * words * 4, w8.data_ptr() + r * pitch, min(rows - r, 65535), cols, pitch,
+                code_bits_flag(code_bits))
     return w8, torch.full((_blocks(rows), _blocks(cols)), 127, dtype=torch.uint8, device=dev).view(_E8M0)
 
 

@@ -213,3 +213,17 @@ def test_decoder_without_tokens():
     none = model(x, torch.zeros(2, dtype=torch.int32, device=DEV))
     assert none.shape == x.shape and model.length.tolist() == [0, 0]
     assert torch.equal(model(x), want)
+
+
+# ---------------------------------------------------------------------------
+# Weights.
+
+@pytest.mark.parametrize("rows,cols,bits", [(65536, 5, 5), (131100, 20, 4)])
+def test_shift_weights_of_many_rows(ops, rows, cols, bits):
+    rng = np.random.default_rng(rows)
+    codes = (rng.integers(0, 2 ** (bits - 1) - 1, (rows, cols)) + 16 * rng.integers(0, 2, (rows, cols))).astype(np.uint8)
+    w8, s = ops.shift_weights_to_fp8(torch.from_numpy(ops.pack_shift_weights(codes, bits).view(np.int32)).to(DEV), cols, bits)
+    want = np.where(codes & 16, -1.0, 1.0) * 2.0 ** -(codes & 15).astype(float)
+    assert np.array_equal(w8.cpu().double().numpy(), want) and s.shape == ((rows + 127) // 128, 1)
+    with pytest.raises(ops.DeepShiftError):
+        ops.shift_weights_to_fp8(torch.zeros(0, 2, dtype=torch.int32, device=DEV), 12, 5)
