@@ -581,7 +581,8 @@ ds_status ds_get_tuning(const char *name, int32_t *value);
  * for each page of tokens and head. A quantiser takes the least power of two that
  * brings the block's largest finite magnitude to at most 448 (2^0 for a block of
  * zeros, 2^-48 in a cache), rounds to nearest even, and holds an element that is
- * not finite as NaN, which has no say in its block's scale.
+ * not finite as NaN, which has no say in its block's scale. The byte 255 is a scale that is
+ * no number (no quantiser writes it): its block's products are NaN.
  *
  * Element types of the other tensors: ds_dtype. Strides (ld*) count elements from
  * one row to the next; an 8-bit matrix's rows begin on 16 bytes, a multiple of 16

@@ -35,6 +35,21 @@ def test_product_tiles_of_one_row(ops, m, n, k):
     near(y[rows], x @ w.T, product_terms(x, w, k, False))
 
 
+@pytest.mark.parametrize("m", [5, 70, 1100])
+@pytest.mark.parametrize("out", [BF16, F16, F32])
+def test_product_nan_scales(ops, m, out):
+    """A scale of NaN makes its block's products NaN: one row (x) or 128 columns (w) of y, in every output type."""
+    n, k = 400, 700
+    x8, xs, w8, ws = operands(ops, m, n, k, E4M3)
+    want = ops.linear_fp8(x8, xs, w8, ws, out_dtype=out)
+    xs.view(torch.uint8)[m // 2, 3] = 255
+    ws.view(torch.uint8)[1, 5] = 255
+    got = ops.linear_fp8(x8, xs, w8, ws, out_dtype=out)
+    nan = torch.zeros(m, n, dtype=torch.bool, device=DEV)
+    nan[m // 2], nan[:, 128:256] = True, True
+    assert torch.equal(got.isnan(), nan) and torch.equal(got[~nan], want[~nan])
+
+
 # ---------------------------------------------------------------------------
 # Attention.
 
