@@ -97,7 +97,7 @@ norm_kernel(const T *__restrict__ x, const T *__restrict__ residual, const W *__
         float o[8], amax = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            o[e] = v[i].at(e) * r * w[i].at(e);
+            o[e] = WHOLE || e < n ? v[i].at(e) * r * w[i].at(e) : 0.f;      // (r may be no number)
             amax = fmaxf(amax, finite_abs(o[e]));
         }
         if constexpr (QUANT) {

@@ -242,3 +242,17 @@ def test_shift_weights_of_many_rows(ops, rows, cols, bits):
     assert np.array_equal(w8.cpu().double().numpy(), want) and s.shape == ((rows + 127) // 128, 1)
     with pytest.raises(ops.DeepShiftError):
         ops.shift_weights_to_fp8(torch.zeros(0, 2, dtype=torch.int32, device=DEV), 12, 5)
+
+
+# ---------------------------------------------------------------------------
+# Norm.
+
+@pytest.mark.parametrize("cols", [1, 300, 1001, 3002])
+def test_norm_writes_zeros_behind_a_row_without_numbers(ops, cols):
+    x = normal(4, 3, cols).to(BF16)
+    x[1, 0] = float("nan")
+    x[2] = 0
+    y, s, _, _ = ops.rms_norm(x.to(DEV), torch.ones(cols, device=DEV), eps=0.0)
+    whole = y.view(torch.uint8).as_strided((3, (cols + 7) // 8 * 8), (y.stride(0), 1)).cpu()
+    assert torch.all(whole[:, cols:] == 0)
+    assert torch.all(whole[1:, :cols] & 0x7F == 0x7F)
