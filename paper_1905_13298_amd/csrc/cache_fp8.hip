@@ -887,7 +887,7 @@ extern "C" ds_status ds_kv_cache_append(const void *k, const void *v, uint8_t *k
     }
     const int64_t cb = pages * heads * page * dim, sb = pages * heads;
     const int touched = int((tokens + page - 2) / page + 1);
-    if (batch * touched > kMaxElems) return fail(DS_ERR_UNSUPPORTED, "too many pages in one call");
+    if (!grid_fits(batch * touched, 256)) return fail(DS_ERR_UNSUPPORTED, "too many pages in one call");
     if (ds_status st = check_tensors({{k, bytes[0], "k", false}, {v, bytes[1], "v", false}, {table, span(batch, ldt, columns) * 4, "table", false},
                                       {start, batch * 4, "start", false}, {count, batch * 4, "count", false},
                                       {k_cache, cb, "k_cache", true}, {v_cache, cb, "v_cache", true},

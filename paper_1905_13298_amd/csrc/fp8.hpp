@@ -27,6 +27,9 @@ inline ds_status launched(const char *what)
     return fail(DS_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
+// Whether a launch can have that many blocks: a grid's first axis has fewer than 2^32 threads.
+inline bool grid_fits(int64_t blocks, int64_t threads) { return blocks <= int64_t(0xffffffff) / threads; }
+
 // Bytes that `rows` rows of `row` bytes span when they begin `pitch` bytes apart.
 inline int64_t span(int64_t rows, int64_t pitch, int64_t row) { return rows <= 0 ? 0 : (rows - 1) * pitch + row; }
 

@@ -610,13 +610,15 @@ void run_tiles(const LinearParams &p, hipStream_t s)
     hipLaunchKernelGGL((linear_tile_kernel<O, WF, BN, BM, WN, WM, STAGES>), dim3(uint32_t((int64_t(tn) * tm + 7) / 8 * 8)), dim3(64 * WN * WM), 0, s, p, tn, tm);
 }
 
+// Rows further apart are out of the tiles' reach, whose 32-bit offsets span 256 of them.
+constexpr int64_t kReach = 1 << 22;
+
 // Which kernel a product runs on. (Up to 32 bits' offsets only: further apart, rows go through
 // linear_rows_kernel.)
 template <typename O, int WF>
 void run_linear(const LinearParams &p, hipStream_t s)
 {
-    // The tiles' 32-bit offsets reach 256 rows.
-    const bool reach = p.ldx <= (1 << 22) && p.ldw <= (1 << 22);
+    const bool reach = p.ldx <= kReach && p.ldw <= kReach;
     // Few rows: linear_rows_kernel, whose time goes with its groups of 16 outputs times 16 rows, where those
     // are few. k = 4096, us, tiles behind: 8 x 8192 outputs (512 groups) 9.5 and 11.2, 8 x 11000 (688) 12.4 and
     // 11.5; 32 x 4096 (512) 8.8 and 11.4, 32 x 5504 (688) 14.6 and 11.5; 64 x 2048 (512) 12.6 and 11.6.
@@ -666,6 +668,9 @@ void run_linear(const LinearParams &p, bool e5m2, hipStream_t s)
     else run_linear<O, 0>(p, s);
 }
 
+// Whether rows of x too far apart for the tiles, or of w, are few enough for linear_rows_kernel's grid.
+bool rows_fit(int64_t m, int64_t ldx, int64_t ldw) { return (ldx <= kReach && ldw <= kReach) || m <= 64 * 65535; }
+
 int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 int64_t blocks_of(int64_t v) { return (v + kScaleBlock - 1) / kScaleBlock; }
 
@@ -706,6 +711,7 @@ extern "C" ds_status ds_linear_fp8(const uint8_t *x8, const uint8_t *x_scales, c
     if (m != 0 && (!x8 || !x_scales || !w8 || !w_scales || !y))
         return fail(DS_ERR_NULL_POINTER, "x8, w8, their scales and y must not be NULL");
     if (ds_status st = check_linear("y", m, n, k, k, n, x8, w8, ldx, ldxs, ldw, ldws, ldy, w_type, y_type)) return st;
+    if (!rows_fit(m, ldx, ldw)) return fail(DS_ERR_UNSUPPORTED, "more than 64 x 65535 rows, some more than 4 MiB apart");
     if (m == 0) return ok();
     const int64_t es = float_bytes(y_type);
     if (ds_status st = check_tensors({{x8, span(m, ldx, up(k, 16)), "x8", false},
@@ -735,6 +741,7 @@ extern "C" ds_status ds_linear_fp8_backward_data(const uint8_t *dy8, const uint8
     if (m != 0 && (!dy8 || !dy_scales || !w8 || !w_scales || !dx))
         return fail(DS_ERR_NULL_POINTER, "dy8, w8, their scales and dx must not be NULL");
     if (ds_status st = check_linear("dx", m, n, k, n, k, dy8, w8, lddy, lddys, ldw, ldws, lddx, w_type, dx_type)) return st;
+    if (!rows_fit(m, lddy, up(n, 16))) return fail(DS_ERR_UNSUPPORTED, "more than 64 x 65535 rows, some more than 4 MiB apart");
     if (m == 0) return ok();
     const int64_t need = ds_linear_fp8_backward_data_scratch_bytes(m, n, k), es = float_bytes(dx_type);
     if (!scratch) return fail(DS_ERR_NULL_POINTER, "scratch must not be NULL");

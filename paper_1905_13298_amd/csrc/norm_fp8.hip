@@ -446,6 +446,12 @@ extern "C" ds_status ds_rms_norm(const void *x, const void *residual, const void
         if (rows != 0 && !scales) return fail(DS_ERR_NULL_POINTER, "an 8-bit y needs scales");
         if (ds_status st = check_rows8(y, cols, ldy, lds, blocks_of(cols))) return st;
     }
+    bool fits = true;
+    for_row_layout(cols, [&](auto tpr, auto) {
+        constexpr int block = row_block<decltype(tpr)::value>(), per = block / decltype(tpr)::value;
+        fits = grid_fits((rows + per - 1) / per, block);
+    });
+    if (!fits) return fail(DS_ERR_UNSUPPORTED, "too many rows for a launch");
     if (rows == 0) return ok();
     const int64_t es = float_bytes(type), row = cols * es;
     if (ds_status st = check_tensors({{x, span(rows, ldx * es, row), "x", false},
@@ -533,7 +539,7 @@ extern "C" ds_status ds_quantize_fp8(const void *x, const void *gate, uint8_t *y
     if (ldx < cols || (gate && ldg < cols)) return fail(DS_ERR_INVALID_ARG, "a row's stride is shorter than the row");
     const int64_t nb = blocks_of(cols);
     if (ds_status st = check_rows8(y, cols, ldy, lds, nb)) return st;
-    if (prod({std::max<int64_t>(rows, 1), nb}) > kMaxElems) return fail(DS_ERR_UNSUPPORTED, "2^31 or more scales");
+    if (!grid_fits((rows * nb + 15) / 16, 256)) return fail(DS_ERR_UNSUPPORTED, "2^28 or more scales");
     if (rows == 0) return ok();
     const int64_t es = float_bytes(type), row = cols * es;
     if (ds_status st = check_tensors({{x, span(rows, ldx * es, row), "x", false},
@@ -560,7 +566,7 @@ extern "C" ds_status ds_quantize_weights_fp8(const void *w, uint8_t *w8, uint8_t
     if (ldw < cols) return fail(DS_ERR_INVALID_ARG, "a row's stride is shorter than the row");
     const int64_t nb = blocks_of(cols), rb = blocks_of(rows);
     if (ds_status st = check_rows8(w8, cols, ldw8, lds, nb)) return st;
-    if (rb > 65535) return fail(DS_ERR_UNSUPPORTED, "more than 65535 x 128 rows");
+    if (rb > 65535 || !grid_fits(nb, 256)) return fail(DS_ERR_UNSUPPORTED, "more than 65535 x 128 rows, or 2^24 or more x 128 columns");
     const int64_t es = float_bytes(type);
     if (ds_status st = check_tensors({{w, span(rows, ldw * es, cols * es), "w", false},
                                       {w8, span(rows, ldw8, (cols + 7) / 8 * 8), "w8", true},
