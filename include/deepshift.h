@@ -663,7 +663,7 @@ int64_t ds_linear_fp8_backward_data_scratch_bytes(int64_t m, int64_t n, int64_t 
  * v_cache [pages][heads][dim][page], scales [pages][heads] each, within 2^-48 .. 2^48 (an
  * attention reads a scale outside as the nearest one inside). page: 16, 32, 64 or 128
  * tokens; dim: a multiple of 16, at most 256. Row b of `table` [batch][columns] (ldt
- * elements apart) lists the pages of sequence b in order.
+ * elements apart) lists the pages of sequence b in order; columns x page is at most 2^31 - 4096.
  *
  * ds_kv_cache_append writes tokens 0 .. count[b] - 1 (count NULL or above tokens: all) of k and
  * v [batch][tokens][heads][dim] at positions start[b], start[b] + 1, .. of sequence b (none where

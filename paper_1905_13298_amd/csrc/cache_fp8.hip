@@ -161,6 +161,9 @@ append_kernel(const T *__restrict__ k, const T *__restrict__ v, uint8_t *__restr
 
 constexpr int kStep = 64;       // keys of a step
 
+// Key positions are 32-bit numbers, those of some steps past a table's last one among them.
+constexpr int64_t kMaxKeys = (int64_t(1) << 31) - 4096;
+
 struct AttentionParams {
     const void *q;
     const uint8_t *kc, *vc, *ks, *vs;
@@ -802,7 +805,7 @@ ds_status check_cache(int64_t batch, int64_t tokens, int64_t heads, int64_t dim,
     if (dim % 16 || dim > 256) return fail(DS_ERR_UNSUPPORTED, "dim must be a multiple of 16, at most 256");
     if (!page_ok(page)) return fail(DS_ERR_UNSUPPORTED, "a page must have 16, 32, 64 or 128 tokens");
     if (ldt < columns) return fail(DS_ERR_INVALID_ARG, "a row of the table is shorter than its columns");
-    if (heads > 65535 || batch > (1 << 20) || tokens > (1 << 24) || pages > kMaxElems || columns * page > kMaxElems)
+    if (heads > 65535 || batch > (1 << 20) || tokens > (1 << 24) || pages > kMaxElems || columns > kMaxKeys / page)
         return fail(DS_ERR_UNSUPPORTED, "too many heads, sequences, tokens or pages");
     return DS_SUCCESS;
 }

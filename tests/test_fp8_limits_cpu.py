@@ -36,3 +36,12 @@ def test_product_rows_out_of_the_tiles_reach():
 
 def test_append_pages_of_a_launch():
     assert append(batch=2 ** 20, tokens=16 * 14) == ARG and append(batch=2 ** 20, tokens=16 * 15 + 2) == UNSUP
+
+
+def test_columns_times_page_of_a_table():
+    """Key positions are 32-bit numbers, some steps past the last one."""
+    for call in (append, attention):
+        assert call(columns=(2 ** 31 - 4096) // 16, ldt=2 ** 30) != UNSUP
+        assert call(columns=2 ** 27 - 1, ldt=2 ** 30) == UNSUP         # 2^31 - 16 keys
+        assert call(columns=2 ** 60, ldt=2 ** 60) == UNSUP             # 2^64 keys
+        assert call(columns=2 ** 62, ldt=2 ** 62, page=128) == UNSUP
