@@ -886,12 +886,12 @@ extern "C" ds_status ds_kv_cache_append(const void *k, const void *v, uint8_t *k
         p.sb[i] = s[0];
         p.st[i] = s[1];
         p.sh[i] = s[2];
-        bytes[i] = ((batch - 1) * s[0] + (tokens - 1) * s[1] + (heads - 1) * s[2] + dim) * es;
+        bytes[i] = span(batch, tokens, heads, s, dim, es);
     }
     const int64_t cb = pages * heads * page * dim, sb = pages * heads;
     const int touched = int((tokens + page - 2) / page + 1);
     if (!grid_fits(batch * touched, 256)) return fail(DS_ERR_UNSUPPORTED, "too many pages in one call");
-    if (ds_status st = check_tensors({{k, bytes[0], "k", false}, {v, bytes[1], "v", false}, {table, span(batch, ldt, columns) * 4, "table", false},
+    if (ds_status st = check_tensors({{k, bytes[0], "k", false}, {v, bytes[1], "v", false}, {table, span(batch, ldt, columns, 4), "table", false},
                                       {start, batch * 4, "start", false}, {count, batch * 4, "count", false},
                                       {k_cache, cb, "k_cache", true}, {v_cache, cb, "v_cache", true},
                                       {k_scales, sb, "k_scales", true}, {v_scales, sb, "v_scales", true}}))
@@ -944,14 +944,14 @@ extern "C" ds_status ds_attention_fp8(const void *q, const uint8_t *k_cache, con
     for (int i = 0; i < 2; ++i) {
         const int64_t *s = i ? o_strides : q_strides;
         if (s[0] < 0 || s[1] < 0 || s[2] < 0) return fail(DS_ERR_INVALID_ARG, "strides must be >= 0");
-        bytes[i] = ((batch - 1) * s[0] + (tokens - 1) * s[1] + (heads * group - 1) * s[2] + dim) * 2;
+        bytes[i] = span(batch, tokens, heads * group, s, dim, 2);
     }
     const int64_t cb = pages * heads * page * dim, sb = pages * heads, need = 4 * part_floats(a, batch, heads, dim);
     if (need > 0 && !scratch) return fail(DS_ERR_NULL_POINTER, "scratch must not be NULL");
     if (need > scratch_bytes) return fail(DS_ERR_BUFFER_TOO_SMALL, "scratch has %lld bytes, %lld are needed", (long long)scratch_bytes, (long long)need);
     if (ds_status st = check_tensors({{q, bytes[0], "q", false}, {k_cache, cb, "k_cache", false}, {v_cache, cb, "v_cache", false},
                                       {k_scales, sb, "k_scales", false}, {v_scales, sb, "v_scales", false},
-                                      {table, span(batch, ldt, columns) * 4, "table", false}, {length, batch * 4, "length", false},
+                                      {table, span(batch, ldt, columns, 4), "table", false}, {length, batch * 4, "length", false},
                                       {count, batch * 4, "count", false}, {o, bytes[1], "o", true},
                                       {need ? scratch : nullptr, need, "scratch", true}}))
         return st;

@@ -30,8 +30,24 @@ inline ds_status launched(const char *what)
 // Whether a launch can have that many blocks: a grid's first axis has fewer than 2^32 threads.
 inline bool grid_fits(int64_t blocks, int64_t threads) { return blocks <= int64_t(0xffffffff) / threads; }
 
-// Bytes that `rows` rows of `row` bytes span when they begin `pitch` bytes apart.
-inline int64_t span(int64_t rows, int64_t pitch, int64_t row) { return rows <= 0 ? 0 : (rows - 1) * pitch + row; }
+// Bytes of so many elements, -1 for more than 2^62.
+inline int64_t bytes_of(__int128 elements, int64_t size)
+{
+    const __int128 bytes = elements * size;
+    return bytes > __int128(1) << 62 ? -1 : int64_t(bytes);
+}
+
+// Bytes that `rows` rows of `row` elements span when they begin `ld` elements apart.
+inline int64_t span(int64_t rows, int64_t ld, int64_t row, int64_t size = 1)
+{
+    return rows <= 0 ? 0 : bytes_of(__int128(rows - 1) * ld + row, size);
+}
+
+// Bytes that vectors [a][b][c][row] of the given strides span.
+inline int64_t span(int64_t a, int64_t b, int64_t c, const int64_t *strides, int64_t row, int64_t size)
+{
+    return bytes_of(__int128(a - 1) * strides[0] + __int128(b - 1) * strides[1] + __int128(c - 1) * strides[2] + row, size);
+}
 
 // A tensor of a call: checked to lie in device memory; an output overlaps no other.
 struct Tensor {
@@ -43,6 +59,8 @@ struct Tensor {
 
 inline ds_status check_tensors(std::initializer_list<Tensor> list)
 {
+    for (const Tensor &t : list)
+        if (t.p && t.bytes < 0) return fail(DS_ERR_UNSUPPORTED, "%s spans more than 2^62 bytes", t.name);
     for (const Tensor &t : list) {
         if (!t.out || !t.p) continue;
         for (const Tensor &o : list)

@@ -719,7 +719,7 @@ extern "C" ds_status ds_linear_fp8(const uint8_t *x8, const uint8_t *x_scales, c
                                       {w8, span(n, ldw, up(k, 16)), "w8", false},
                                       {w_scales, span(blocks_of(n), ldws, blocks_of(k)), "w_scales", false},
                                       {bias, n * 4, "bias", false},
-                                      {y, span(m, ldy * es, n * es), "y", true}}))
+                                      {y, span(m, ldy, n, es), "y", true}}))
         return st;
     const LinearParams p{x8, x_scales, w8, w_scales, bias, y, int(m), int(n), int(k), int(blocks_of(k)), ldx, ldxs, ldw, ldws, ldy};
     launch(p, w_type, y_type, static_cast<hipStream_t>(stream));
@@ -751,7 +751,7 @@ extern "C" ds_status ds_linear_fp8_backward_data(const uint8_t *dy8, const uint8
                                       {dy_scales, span(m, lddys, blocks_of(n)), "dy_scales", false},
                                       {w8, span(n, ldw, up(k, 16)), "w8", false},
                                       {w_scales, span(blocks_of(n), ldws, blocks_of(k)), "w_scales", false},
-                                      {dx, span(m, lddx * es, k * es), "dx", true},
+                                      {dx, span(m, lddx, k, es), "dx", true},
                                       {scratch, need, "scratch", true}}))
         return st;
     const auto s = static_cast<hipStream_t>(stream);

@@ -453,13 +453,13 @@ extern "C" ds_status ds_rms_norm(const void *x, const void *residual, const void
     });
     if (!fits) return fail(DS_ERR_UNSUPPORTED, "too many rows for a launch");
     if (rows == 0) return ok();
-    const int64_t es = float_bytes(type), row = cols * es;
-    if (ds_status st = check_tensors({{x, span(rows, ldx * es, row), "x", false},
-                                      {residual, span(rows, ldr * es, row), "residual", false},
+    const int64_t es = float_bytes(type);
+    if (ds_status st = check_tensors({{x, span(rows, ldx, cols, es), "x", false},
+                                      {residual, span(rows, ldr, cols, es), "residual", false},
                                       {weight, cols * float_bytes(weight_type), "weight", false},
-                                      {y, quant ? span(rows, ldy, (cols + 7) / 8 * 8) : span(rows, ldy * es, row), "y", true},
+                                      {y, quant ? span(rows, ldy, (cols + 7) / 8 * 8) : span(rows, ldy, cols, es), "y", true},
                                       {quant ? scales : nullptr, span(rows, lds, blocks_of(cols)), "scales", true},
-                                      {h, span(rows, ldh * es, row), "h", true},
+                                      {h, span(rows, ldh, cols, es), "h", true},
                                       {rstd, rows * 4, "rstd", true}}))
         return st;
     const NormParams p{rows, ldx, ldr, ldh, ldy, lds, int(cols), eps};
@@ -500,13 +500,13 @@ extern "C" ds_status ds_rms_norm_backward(const void *dy, const void *h, const v
     const int64_t need = dweight ? ds_rms_norm_backward_scratch_bytes(rows, cols) : 0;
     if (need > 0 && !scratch) return fail(DS_ERR_NULL_POINTER, "dweight needs scratch");
     if (need > scratch_bytes) return fail(DS_ERR_BUFFER_TOO_SMALL, "scratch has %lld bytes, %lld are needed", (long long)scratch_bytes, (long long)need);
-    const int64_t es = float_bytes(type), row = cols * es;
-    if (ds_status st = check_tensors({{dy, span(rows, lddy * es, row), "dy", false},
-                                      {h, span(rows, ldh * es, row), "h", false},
+    const int64_t es = float_bytes(type);
+    if (ds_status st = check_tensors({{dy, span(rows, lddy, cols, es), "dy", false},
+                                      {h, span(rows, ldh, cols, es), "h", false},
                                       {weight, cols * float_bytes(weight_type), "weight", false},
                                       {rstd, rows * 4, "rstd", false},
-                                      {dh, span(rows, lddh * es, row), "dh", false},
-                                      {dx, span(rows, lddx * es, row), "dx", true},
+                                      {dh, span(rows, lddh, cols, es), "dh", false},
+                                      {dx, span(rows, lddx, cols, es), "dx", true},
                                       {dweight, cols * float_bytes(weight_type), "dweight", true},
                                       {need ? scratch : nullptr, need, "scratch", true}}))
         return st;
@@ -541,9 +541,9 @@ extern "C" ds_status ds_quantize_fp8(const void *x, const void *gate, uint8_t *y
     if (ds_status st = check_rows8(y, cols, ldy, lds, nb)) return st;
     if (!grid_fits((rows * nb + 15) / 16, 256)) return fail(DS_ERR_UNSUPPORTED, "2^28 or more scales");
     if (rows == 0) return ok();
-    const int64_t es = float_bytes(type), row = cols * es;
-    if (ds_status st = check_tensors({{x, span(rows, ldx * es, row), "x", false},
-                                      {gate, span(rows, ldg * es, row), "gate", false},
+    const int64_t es = float_bytes(type);
+    if (ds_status st = check_tensors({{x, span(rows, ldx, cols, es), "x", false},
+                                      {gate, span(rows, ldg, cols, es), "gate", false},
                                       {y, span(rows, ldy, (cols + 7) / 8 * 8), "y", true},
                                       {scales, span(rows, lds, nb), "scales", true}}))
         return st;
@@ -568,7 +568,7 @@ extern "C" ds_status ds_quantize_weights_fp8(const void *w, uint8_t *w8, uint8_t
     if (ds_status st = check_rows8(w8, cols, ldw8, lds, nb)) return st;
     if (rb > 65535 || !grid_fits(nb, 256)) return fail(DS_ERR_UNSUPPORTED, "more than 65535 x 128 rows, or 2^24 or more x 128 columns");
     const int64_t es = float_bytes(type);
-    if (ds_status st = check_tensors({{w, span(rows, ldw * es, cols * es), "w", false},
+    if (ds_status st = check_tensors({{w, span(rows, ldw, cols, es), "w", false},
                                       {w8, span(rows, ldw8, (cols + 7) / 8 * 8), "w8", true},
                                       {scales, span(rb, lds, nb), "scales", true}}))
         return st;

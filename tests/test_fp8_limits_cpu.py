@@ -45,3 +45,28 @@ def test_columns_times_page_of_a_table():
         assert call(columns=2 ** 27 - 1, ldt=2 ** 30) == UNSUP         # 2^31 - 16 keys
         assert call(columns=2 ** 60, ldt=2 ** 60) == UNSUP             # 2^64 keys
         assert call(columns=2 ** 62, ldt=2 ** 62, page=128) == UNSUP
+
+
+FAR = 2 ** 61      # elements between rows: two rows of 16-bit elements are 2^62 bytes apart
+
+
+@pytest.mark.parametrize("by", ["ldx", "ldr", "ldh", "ldy", "lds"])
+def test_norm_strides_past_what_bytes_count(by):
+    assert norm(**{by: FAR * 2 if by in ("ldy", "lds") else FAR}) == UNSUP
+    assert norm(rows=1, **{by: FAR}) == ARG        # a single row goes nowhere
+
+
+def test_other_strides_past_what_bytes_count():
+    assert status("ds_rms_norm_backward", *P[:7], 4, 256, 256, FAR, 256, 256, 2, 2, P[8], 1 << 20, None) == UNSUP
+    assert status("ds_quantize_fp8", P[0], None, P[1], P[2], 4, 256, FAR, 0, 256, 2, 2, None) == UNSUP
+    assert status("ds_quantize_weights_fp8", P[0], P[1], P[2], 4, 256, 256, FAR * 2, 2, 2, None) == UNSUP
+    assert status("ds_shift_weights_to_fp8", P[0], P[1], 4, 256, FAR * 2, 0, None) == UNSUP
+    assert linear(ldy=FAR) == UNSUP and linear(ldw=FAR) == UNSUP and linear(ldxs=FAR * 3) == UNSUP
+    assert grad(lddx=FAR) == UNSUP and grad(ldws=FAR * 2) == ARG       # (one row of scales)
+    for where in range(3):
+        size = [1024, 128, 64]
+        size[where] = FAR
+        kept = (ctypes.c_int64 * 3)(*size)
+        st = ctypes.cast(kept, ctypes.c_void_p)
+        assert append(st=st, batch=2) == UNSUP and attention(st=st, batch=2) == UNSUP
+    assert append(batch=2, ldt=FAR) == UNSUP and attention(batch=2, ldt=FAR) == UNSUP
