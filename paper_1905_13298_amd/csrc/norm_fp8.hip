@@ -336,12 +336,12 @@ __global__ void __launch_bounds__(256)
 shift_to_fp8_kernel(const uint32_t *__restrict__ wp, uint8_t *__restrict__ y, int cols, int wpr, int64_t ldy, const CodeFmt fmt)
 {
     const int64_t row = blockIdx.y;
-    const int c = (int(blockIdx.x) * 256 + int(threadIdx.x)) * 8;
-    if (c >= cols) return;
+    const uint32_t c = (blockIdx.x * 256 + threadIdx.x) * 8, n = uint32_t(cols);      // (c: up to 2^31)
+    if (c >= n) return;
     uint32_t q[2] = {};
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const uint32_t code = c + i < cols ? fmt.at(wp + row * wpr, c + i) : 15u, sh = code & 15u;
+        const uint32_t code = c + i < n ? fmt.at(wp + row * wpr, int(c + i)) : 15u, sh = code & 15u;
         const uint32_t byte = sh == 15u ? 0u : (code >> 4) << 7 | (15u - sh) << 2;
         q[i >> 2] |= byte << (8 * (i & 3));
     }

@@ -9,7 +9,7 @@ import pytest
 import torch
 
 from .test_gpu_decoder import build as build_decoder
-from .test_gpu_fp8 import BF16, DEV, E4M3, F16, F32, filled_cache, near, normal, operands, product_terms, value  # noqa: F401
+from .test_gpu_fp8 import BF16, DEV, E4M3, E5M2, F16, F32, filled_cache, near, normal, operands, product_terms, value  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -242,6 +242,23 @@ def test_shift_weights_of_many_rows(ops, rows, cols, bits):
     assert np.array_equal(w8.cpu().double().numpy(), want) and s.shape == ((rows + 127) // 128, 1)
     with pytest.raises(ops.DeepShiftError):
         ops.shift_weights_to_fp8(torch.zeros(0, 2, dtype=torch.int32, device=DEV), 12, 5)
+
+
+def test_shift_weights_of_one_row_of_2_to_the_31(ops):
+    """The last block's columns pass 31 bits: they are written up to a multiple of 8 and no further."""
+    cols = 2 ** 31 - 1
+    words = ops.packed_row_words(cols, 5)
+    wp = torch.full((1, words), 0x01084210, dtype=torch.int32, device=DEV)
+    last = torch.randint(0, 2 ** 30, (100,), generator=torch.Generator().manual_seed(1)).int()
+    wp[0, -100:] = last.to(DEV)
+    buffer = torch.full((2 ** 31 + 8192,), 0xAA, dtype=torch.uint8, device=DEV)
+    ops.call("ds_shift_weights_to_fp8", wp.data_ptr(), buffer.data_ptr() + 4096, 1, cols, 2 ** 31, 0, torch.cuda.current_stream().cuda_stream)
+    assert torch.all(buffer[:4096] == 0xAA) and torch.all(buffer[4096 + 2 ** 31:] == 0xAA)
+    n = cols - (words - 100) * 6
+    codes = torch.stack([(last >> (5 * j)) & 31 for j in range(6)], 1).reshape(-1)[:n]
+    want = torch.where((codes & 15) == 15, 0.0, torch.where(codes >= 16, -1.0, 1.0) * torch.exp2(-(codes & 15).float()))
+    got = buffer[4096 + cols - n:4096 + cols].cpu().view(E5M2).float()
+    assert torch.equal(got, want) and int(buffer[4096 + cols]) == 0
 
 
 # ---------------------------------------------------------------------------
