@@ -690,8 +690,8 @@ ds_status ds_kv_cache_append(const void *k, const void *v, uint8_t *k_cache, uin
  * query that sees no key, or i >= count[b], gets zeros. Keys past the table's columns, or on a
  * page outside 0 .. pages - 1, are not seen (a page may leave a sequence that way) and move no
  * position. A length below 0 is taken as 0, a count outside 0 .. tokens as the nearest of those. What
- * pages hold past a sequence's end does not matter; a NaN among the values of a token
- * that one query of a call sees reaches the queries of the same call and head that do not.
+ * pages hold past a sequence's end does not matter; a NaN among the values of a token makes
+ * NaN of its element in the results of the queries that see the token, and of no others.
  * scratch: ds_attention_fp8_scratch_bytes (0: none needed). */
 ds_status ds_attention_fp8(const void *q, const uint8_t *k_cache, const uint8_t *v_cache,
                            const uint8_t *k_scales, const uint8_t *v_scales, const int32_t *table,

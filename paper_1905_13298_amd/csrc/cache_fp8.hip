@@ -295,6 +295,11 @@ __device__ __forceinline__ int key_mask(int key, int low, int high)
     return int(mask);
 }
 
+// 0x80 in each byte of x that is an E4M3 NaN. A weight of 0 does not keep a NaN out of a sum: where
+// some queries see a step's keys and others do not, values that are NaN are taken out, and come back
+// as NaN in the results of the queries that see them (a product of where they are with what is seen).
+__device__ __forceinline__ uint32_t nan_bytes(int x) { return ((uint32_t(x) & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+
 // A sequence's queries and the position of the first, which a length beyond the table does not
 // move (and which is negative where there are more queries than tokens); the keys that have a column.
 struct Sequence {
@@ -350,8 +355,10 @@ __device__ __forceinline__ float inverse(float total) { return total > 0.f ? 1.f
 // Up to 16 queries of a kv head (tokens being decoded): a block of 4 waves takes a share of
 // the keys, each wave every fourth 64 of it straight from memory to registers (no two waves
 // share any, so LDS would only add a trip), and joins them at its end. Bound by reading the
-// cache once: 131072 keys of 8 heads of 128, 268 MB, 57 us with the join (4.7 TB/s).
-template <typename T, int DP>
+// cache once: 131072 keys of 8 heads of 128, 268 MB, 57 us with the join (4.7 TB/s). ONE: of one token,
+// whose query heads all see the same keys (16 x 1 over up to 8192: 40.5 us, with the code for values
+// that are NaN 41.3).
+template <typename T, int DP, bool ONE>
 __global__ void __launch_bounds__(256)
 attention_few_kernel(const AttentionParams p)
 {
@@ -377,6 +384,9 @@ attention_few_kernel(const AttentionParams p)
     }
     tlo = __builtin_amdgcn_readfirstlane(tlo);
     thi = __builtin_amdgcn_readfirstlane(thi);
+    // Keys that some query sees: [tlo, thi), others are masked in the values themselves; that every one
+    // sees: [alo, ahi).
+    const int alo = p.window ? max(max(seq.first + seq.count, 0) - p.window, 0) : 0, ahi = min(max(seq.first + 1, 0), seq.keys);
     const int s0 = thi > 0 ? tlo / kStep : 0, s1 = (thi + kStep - 1) / kStep;
     const int each = (s1 - s0 + p.splits - 1) / p.splits;
     const int from = s0 + split * each, to = min(s1, from + each);
@@ -434,10 +444,43 @@ attention_few_kernel(const AttentionParams p)
                 for (int d = 0; d < DT; ++d) vraw[d][w] &= mask;
             }
         }
+        if (!ONE && (base + kStep > ahi || base < alo)) {
+            uint32_t nan = 0;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) nan |= nan_bytes(vraw[d][w]);
+            if (__any(nan != 0)) {
+                f16x8 seen[2];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) seen[i >> 3][i & 7] = _Float16(held && vrun + i >= low && vrun + i < high ? 1.f : 0.f);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    i32x4 where;                  // 1 for NaN
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        asm("" : "+v"(vraw[d][w]));     // (not kept from above: registers)
+                        const uint32_t z = nan_bytes(vraw[d][w]) >> 7;
+                        where[w] = int(z * 0x38u);
+                        vraw[d][w] &= int(~(z * 0xffu));
+                    }
+                    f32x4 n{};
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) n = mma(widen<_Float16>(where[2 * c], where[2 * c + 1]), seen[c], n);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[d][i] += n[i] > 0.f ? __builtin_nanf("") : 0.f;
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        }
 #pragma unroll
         for (int c = 0; c < 2; ++c)
 #pragma unroll
             for (int d = 0; d < DT; ++d) acc[d] = mma(widen<_Float16>(vraw[d][2 * c], vraw[d][2 * c + 1]), pf[c], acc[d]);
+    }
+    if (high == 0) {      // a row that sees no key, whatever the others see
+#pragma unroll
+        for (int d = 0; d < DT; ++d) acc[d] = f32x4{};
     }
     // The waves' sums together: a lane's l is its own keys'.
     l += __shfl_xor(l, 16);
@@ -497,6 +540,7 @@ attention_many_kernel(const AttentionParams p, int bhs)
     constexpr int kKeys = kStep * DP * 2;      // bytes of a step's keys, or values
     typedef typename Vec8<T>::type v8;
     __shared__ __align__(16) uint8_t lds[2][2 * kKeys];
+    __shared__ int nans[2][WAVES];             // whether a wave's part of the values has any
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), r = lane & 31, hf = lane >> 5, g = lane >> 4;
     // An eighth of the work to each XCD, a head's blocks together, so that they read its
     // keys through one L2, the same head of every sequence next, whose lengths may differ; the
@@ -518,6 +562,9 @@ attention_many_kernel(const AttentionParams p, int bhs)
     const int t0 = tile * WAVES * 32 / p.group, t1 = min(((tile + 1) * WAVES * 32 - 1) / p.group, seq.count - 1);
     const int thi = t0 < seq.count ? min(max(seq.first + t1 + 1, 0), seq.keys) : 0;
     const int tlo = p.window ? max(max(seq.first + t0 + 1, 0) - p.window, 0) : 0;
+    // Steps of which one of its queries does not see every key.
+    const int alo = p.window ? max(max(seq.first + t1 + 1, 0) - p.window, 0) : 0, ahi = min(max(seq.first + t0 + 1, 0), seq.keys);
+    auto mixed = [&](int step) { return step * kStep < alo || step * kStep + kStep > ahi; };
     const int s0 = thi > tlo ? tlo / kStep : 0, s1 = thi > tlo ? (thi + kStep - 1) / kStep : 0;
     const int each = (s1 - s0 + p.splits - 1) / p.splits;
     const int from = s0 + split * each, to = min(s1, from + each);
@@ -582,6 +629,17 @@ attention_many_kernel(const AttentionParams p, int bhs)
             }
         }
     };
+    auto note_nans = [&](int step, int buf) {
+        if (!mixed(step)) return;
+        uint32_t nan = 0;
+#pragma unroll
+        for (int q = 0; q < kRuns; ++q)
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) nan |= nan_bytes(vraw[q][i][w]);
+        nans[buf][wave] = __any(nan != 0);
+    };
     // Part u of what fetch() read, to LDS: 8 keys or values a lane.
     constexpr int kParts = kRuns * kLoads * 4;
     auto put = [&](int u, int buf) {
@@ -611,6 +669,7 @@ attention_many_kernel(const AttentionParams p, int bhs)
         fetch(from, pid1);
         look_ahead(from + 1);
         clear(from, pid1);
+        note_nans(from, 0);
 #pragma unroll
         for (int u = 0; u < kParts; ++u) put(u, 0);
         pid0 = pid1;
@@ -634,13 +693,55 @@ attention_many_kernel(const AttentionParams p, int bhs)
         auto value_part = [&](int n) {
             return *reinterpret_cast<const f16x8 *>(vt + n % DT * 32 * 128 + ((n / DT * 2 + hf) ^ ((r >> 1) & 7)) * 16);
         };
+        if (mixed(step)) {
+            int nan = 0;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) nan |= nans[buf][w];
+            if (__builtin_amdgcn_readfirstlane(nan)) {      // the same in every wave
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    f32x16 n{};
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const bool there = __builtin_amdgcn_readlane(pid0, q * 16) >= 0;
+                        const f16x8 v = value_part(q * DT + d);
+                        f16x8 where, seen;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int key = base + q * 16 + hf * 8 + i;
+                            where[i] = _Float16(v[i] != v[i] ? 1.f : 0.f);
+                            seen[i] = _Float16(there && key >= low && key < high ? 1.f : 0.f);
+                        }
+                        n = mma32(where, seen, n);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[d][i] += n[i] > 0.f ? __builtin_nanf("") : 0.f;
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                wait_lds();
+                barrier();
+                for (int i = int(threadIdx.x); i < kKeys / 16; i += 64 * WAVES) {
+                    f16x8 *const at = reinterpret_cast<f16x8 *>(lds[buf] + kKeys + i * 16);
+                    f16x8 v = *at;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = v[e] != v[e] ? _Float16(0.f) : v[e];
+                    *at = v;
+                }
+                wait_lds();
+                barrier();
+            }
+        }
         v8 kf[kAhead];
 #pragma unroll
         for (int n = 0; n < kAhead; ++n) kf[n] = key_part(n);
         const PageScale ps = page_scale(ek, ev, p.scale);
         const bool held = on_pages(pid0);
         const int now = pid0;
-        if (step + 1 < to) clear(step + 1, pid1);
+        if (step + 1 < to) {
+            clear(step + 1, pid1);
+            note_nans(step + 1, buf ^ 1);
+        }
         f32x16 s[2];
 #pragma unroll
         for (int n = 0; n < kFirst; ++n) {
@@ -843,8 +944,9 @@ void run_attention(const AttentionParams &p, const Plan &a, int64_t batch, hipSt
 {
     const int bhs = int(batch * p.heads);
     const dim3 many(uint32_t((int64_t(bhs) * a.row_tiles * a.splits + 7) / 8 * 8));
-    if (a.waves == 0) hipLaunchKernelGGL((attention_few_kernel<T, DP>), dim3(a.splits, bhs), dim3(256), 0, s, p);
-    else {
+    if (a.waves == 0) {
+        hipLaunchKernelGGL((p.tokens == 1 ? attention_few_kernel<T, DP, true> : attention_few_kernel<T, DP, false>), dim3(a.splits, bhs), dim3(256), 0, s, p);
+    } else {
         hipLaunchKernelGGL((a.waves == 2 ? attention_many_kernel<T, DP, 2> : attention_many_kernel<T, DP, 4>), many, dim3(64 * a.waves), 0, s, p, bhs);
     }
     if (a.splits > 1)

@@ -179,6 +179,28 @@ def test_attention_beside_a_large_value_that_no_query_sees(ops, times, tokens, g
     one_of_many(ops, q, cache, table, n, window)
 
 
+@pytest.mark.parametrize("dim,tokens,group,page,length", [(64, 1, 4, 16, 40), (256, 1, 3, 64, 300), (64, 5, 2, 16, 40), (128, 3, 5, 64, 300), (256, 2, 1, 32, 33), (64, 70, 2, 16, 90), (128, 200, 3, 64, 700),
+                                                          (256, 40, 1, 128, 250), (80, 33, 2, 32, 33), (128, 9, 1, 64, 9000), (128, 30, 2, 64, 9000)])
+@pytest.mark.parametrize("window", [0, 20])
+def test_attention_nan_values_reach_the_queries_that_see_them(ops, dim, tokens, group, page, length, window):
+    heads, columns = 2, (length + page - 1) // page
+    cache, table = pages_of(ops, 2, columns, heads, page, dim, seed=7)
+    lengths, counts = [length, length - 3], [tokens, tokens - 1]
+    v8 = cache[1].view(torch.uint8)
+    for b, n in enumerate(lengths):
+        # In the last tokens, in the first ones that a window hides from some, and one before all of those.
+        for i, t in enumerate(sorted({max(n - tokens - 30, 0), max(n - tokens - 12, 0), n - tokens, n - tokens // 2 - 1, n - 1})):
+            v8[int(table[b, t // page]), i % heads, (5 * i + 3) % dim, t % page] = 0x7F if i % 2 else 0xFF
+    q = normal(8, 2, tokens, heads * group, dim).to(BF16)
+    o, want, off = attend(ops, q, cache, table, lengths, counts, window)
+    agree(o, want, off)
+    assert bool(want.isnan().any()) and not bool(want.isnan().all())
+    v8.copy_(torch.where((v8 & 0x7F) == 0x7F, torch.zeros_like(v8), v8))
+    clean, _, _ = attend(ops, q, cache, table, lengths, counts, window)
+    nan = o.isnan()
+    assert torch.equal(o[~nan], clean[~nan])
+
+
 # ---------------------------------------------------------------------------
 # Decoder.
 
