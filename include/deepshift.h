@@ -642,7 +642,9 @@ ds_status ds_shift_weights_to_fp8(const uint32_t *w_packed, uint8_t *w8, int64_t
 
 /* y[m][n] = bias[n] + sum_k x8[m][k] * w8[n][k] of the scaled values: x8 E4M3 with
  * scales [m][ceil(k / 128)], w8 of w_type (DS_TYPE_F8E4M3 or DS_TYPE_F8E5M2) with
- * scales [ceil(n / 128)][ceil(k / 128)], bias float32 or NULL, y of y_type. */
+ * scales [ceil(n / 128)][ceil(k / 128)], bias float32 or NULL, y of y_type. A y of 16
+ * bits comes of the 8-bit matrix instruction, which drops what lies 2^-14 below the
+ * largest of eight products; one of 32 bits keeps 24 bits of each. */
 ds_status ds_linear_fp8(const uint8_t *x8, const uint8_t *x_scales, const uint8_t *w8,
                         const uint8_t *w_scales, const float *bias, void *y, int64_t m, int64_t n,
                         int64_t k, int64_t ldx, int64_t ldxs, int64_t ldw, int64_t ldws,
@@ -692,7 +694,7 @@ ds_status ds_kv_cache_append(const void *k, const void *v, uint8_t *k_cache, uin
  * position. A length below 0 is taken as 0, a count outside 0 .. tokens as the nearest of those. What
  * pages hold past a sequence's end does not matter; a NaN among the values of a token makes
  * NaN of its element in the results of the queries that see the token, and of no others.
- * scratch: ds_attention_fp8_scratch_bytes (0: none needed). */
+ * Up to 65535 sequences times heads. scratch: ds_attention_fp8_scratch_bytes (0: none needed). */
 ds_status ds_attention_fp8(const void *q, const uint8_t *k_cache, const uint8_t *v_cache,
                            const uint8_t *k_scales, const uint8_t *v_scales, const int32_t *table,
                            const int32_t *length, const int32_t *count, void *o, int64_t batch,

@@ -529,8 +529,8 @@ attention_few_kernel(const AttentionParams p)
 // contracts in the second product.
 //
 // Bound by the matrix instructions and the exponentials between them, which do not overlap in one
-// wave: 2 x 1000 queries of 32 heads over up to 8000 keys of 8 heads of 128 take 232 us, pages of
-// 16 tokens as long as those of 64 (the products alone take 203 us at the rate of a large 16-bit
+// wave: 2 x 1000 queries of 32 heads over up to 8000 keys of 8 heads of 128 take 254 to 270 us, pages
+// of 16 tokens as long as those of 64 (the products alone take 203 us at the rate of a large 16-bit
 // product).
 template <typename T, int DP, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES, DP <= 128 ? 2 : 1)
@@ -917,12 +917,14 @@ struct Plan {
 };
 
 // How a call is split: over the rows first, then over the keys until 512 blocks (two a CU) have at
-// least 8 steps of 64 keys each. Measured (8 heads of 128, 4 query heads each): one query over
-// 131072 keys 57 us, with 1024 blocks 60, unsplit 1209; 16 x 1 over up to 8192 40, 42 and, with 2048, 46;
-// 48 x 1 (384 blocks, two splits each, since lengths differ) 93 and unsplit 108; 100 queries over 32768
-// keys 85, with 256 blocks 97, with 1024 94. Up to 16 rows run attention_few_kernel (48 x 1: 93 us,
-// the other 230). From 17 to 64 rows blocks of two waves: 32 x 16 queries over 4096 keys 83 us, of
-// four 90; above, of four: 2 x 1000 queries 232, of two 371.
+// least 8 steps of 64 keys each. Measured (8 heads of 128, 4 query heads each; us): one query over 131072
+// keys 57, with 256 blocks 61, with 1024 61, unsplit 1202; 16 x 1 over up to 8192 40, 55, 43 and, with 2048,
+// 48; 48 x 1 (384 blocks, two splits each, since lengths differ) 94, with 1024 91, unsplit 108; 100 queries
+// over 32768 keys 95, with 256 blocks 116, with 1024 115. Up to 16 rows run attention_few_kernel (48 x 1: 94,
+// the other 238; 32 x 16 of 1 query head over 4096 keys 56 and 79). From 17 to 64 rows blocks of two waves:
+// 32 x 16 queries over 4096 keys 90, of four 98, of 2 query heads 81 and 88; above, of four: 2 x 1000
+// queries 270, of two 410. (Splits go by the table's width, not by lengths: 64 sequences of 8 heads are
+// not split, and one of them that is much longer than the others is what a call waits for.)
 Plan plan_attention(int64_t batch, int64_t tokens, int64_t heads, int64_t group, int64_t columns, int64_t page)
 {
     Plan a;

@@ -79,9 +79,11 @@ __device__ __forceinline__ f16x8 widen(i32x8 v, int i)
 }
 
 // c + one block's products. The 8-bit instruction aligns the products of each 8 elements with
-// the largest of them and drops what lies 2^-14 below it, which an output of 16 bits does
-// not show and one of 32 does: such an output (FULL) is formed from the same numbers as
-// 16-bit floats, whose products and sums keep 24 bits, the scales applied afterwards.
+// the largest of them and drops what lies 2^-14 below it. For normal inputs, 128 to 11008 elements
+// of them, that is 2.8e-5 of the outputs' root mean square (E4M3 weights) or 6.5e-5 (E5M2) without a
+// bias: a 60th or a 25th of what rounding to bfloat16 costs, an 8th or a third for a 16-bit float. An
+// output of 32 bits would show it: it (FULL) is formed from the same numbers as 16-bit floats, whose
+// products and sums keep 24 bits, the scales applied afterwards.
 // The scales are byte BYTE of ws and xs.
 template <int WF, bool FULL, int BYTE = 0>
 __device__ __forceinline__ f32x4 mma(i32x8 w, i32x8 x, f32x4 c, int ws, int xs)
@@ -129,7 +131,7 @@ __device__ __forceinline__ bool no_number(uint32_t word, int n)
 // w and MT x 16 rows of x; each of its waves takes a share of the reduction, in blocks of 128,
 // and they add their sums in LDS. The weights are the instruction's first operand, so that a
 // lane ends up with four consecutive outputs of one row of y. Bound by the latency of reading
-// w: 8 x 4096 outputs of 4096, 17 MB, 6.4 us (2.6 TB/s; the launch and the sums' exchange are about 3
+// w: 8 x 4096 outputs of 4096, 17 MB, 6.6 us (2.6 TB/s; the launch and the sums' exchange are about 3
 // of them); with more rows by the loads of x, which every block repeats.
 template <typename O, int WF, int MT, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES)
@@ -255,8 +257,8 @@ __device__ __forceinline__ void store_outputs(const LinearParams &p, int m, int 
 // at a time, which go from memory to LDS without registers, STAGES - 1 steps ahead of the
 // products. A row's eight 16-byte pieces are kept in an order of its own, so that the
 // lanes of a read find theirs in different banks. Bound by the transfers' latency where
-// there is one round of blocks (128 x 4096 outputs of 4096, tiles of 64: 11.8 us for 32 steps), by LDS reads
-// where there are more (tiles of 128, 2900 x 6000 outputs of 4096: 82 us, 1.7 PFLOP/s).
+// there is one round of blocks (128 x 4096 outputs of 4096, tiles of 64: 12.8 us for 32 steps), by LDS reads
+// where there are more (tiles of 128, 2900 x 6000 outputs of 4096: 84 us, 1.7 PFLOP/s).
 template <typename O, int WF, int BN, int BM, int WN, int WM, int STAGES>
 __global__ void __launch_bounds__(64 * WN * WM, 1)
 linear_tile_kernel(const LinearParams p, int tiles_n, int tiles_m)
@@ -421,7 +423,7 @@ linear_tile_kernel(const LinearParams p, int tiles_n, int tiles_m)
 // sent for about a step before (a step takes 1.1 us at the least, memory behind the L2 answers
 // after up to 2). Bound by the matrix instructions, at
 // the clock that the card holds while they run, and by a block's start and end, which nothing
-// overlaps: 8192 x 8192 outputs of 4096 in 231 us (2.4 PFLOP/s).
+// overlaps: 8192 x 8192 outputs of 4096 in 229 to 236 us (2.4 PFLOP/s).
 template <typename O, int WF>
 __global__ void __launch_bounds__(256, 1)
 linear_wide_kernel(const LinearParams p, int tiles_n, int tiles_m)
@@ -576,7 +578,7 @@ linear_wide_kernel(const LinearParams p, int tiles_n, int tiles_m)
 // 128] to [k / 128][blocks of n]: 128 x 64 bytes a block, 8 x 4 of them a thread. The gradient
 // contracts over w's rows and the matrix instruction wants them consecutive in a lane; turned
 // around once in scratch they go through the forward product's kernels (2048 columns by 1000
-// rows: 3 of the gradient's 16 us).
+// rows: 4.2 of the gradient's 16 us).
 __global__ void __launch_bounds__(256)
 transpose8_kernel(const uint8_t *__restrict__ w, const uint8_t *__restrict__ ws, uint8_t *__restrict__ t, uint8_t *__restrict__ ts, int n,
                   int k, int64_t ldw, int64_t ldws, int64_t ldt)
@@ -620,9 +622,10 @@ void run_linear(const LinearParams &p, hipStream_t s)
 {
     const bool reach = p.ldx <= kReach && p.ldw <= kReach;
     // Few rows: linear_rows_kernel, whose time goes with its groups of 16 outputs times 16 rows, where those
-    // are few. k = 4096, us, tiles behind: 8 x 8192 outputs (512 groups) 9.5 and 11.2, 8 x 11000 (688) 12.4 and
-    // 11.5; 32 x 4096 (512) 8.8 and 11.4, 32 x 5504 (688) 14.6 and 11.5; 64 x 2048 (512) 12.6 and 11.6.
-    // Outputs in 32 bits, whose products are more instructions in either: 8 x 11000 12.6 and 20.8.
+    // are few. k = 4096, us, tiles behind: 8 x 8192 outputs (512 groups) 9.7 and 12.1, 8 x 11000 (688) 12.6 and
+    // 12.4; 32 x 4096 (512) 9.1 and 12.2, 32 x 5504 (688) 14.9 and 12.3; 64 x 2048 (512) 12.9 and 12.0.
+    // Outputs in 32 bits, whose products are more instructions in either: 8 x 11000 13.0 and 22.1, 64 x 4096
+    // 14.3 and 22.3, 128 x 4096 26.1 and 22.6.
     const int64_t groups = int64_t((p.n + 15) / 16) * (p.m <= 16 ? 1 : p.m <= 32 ? 2 : 4);
     constexpr bool wide_sums = sizeof(O) == 4;
     if ((p.m > (wide_sums ? 64 : 32) || groups > (wide_sums ? 1200 : 512)) && reach) {
@@ -630,9 +633,9 @@ void run_linear(const LinearParams &p, hipStream_t s)
         if constexpr (sizeof(O) == 2) {
             // Whichever takes less by what its rounds take (in 10 ns): of 256 tiles of 256, or, two a CU,
             // of half as many CUs' tiles of 128. Measured (tiles of 256 and of 128, us): k = 4096, 2500 x 4096
-            // outputs 52 and 54; 2048 x 4096 52 and 40; 2900 x 6000 102 and 82; 5000 x 5000 105 and 117;
-            // 4096 x 4096 58 and 70; 8192 x 8192 231 and 300; k = 128, 5698 x 4352 30 and 24, 4096 x 4096 17 and
-            // 17; k = 1024, 5698 x 4352 46 and 39, 8192 x 8192 88 and 94.
+            // outputs 52 and 55; 2048 x 4096 52 and 38; 2900 x 6000 105 and 84; 5000 x 5000 108 and 116;
+            // 4096 x 4096 60 and 70; 8192 x 8192 236 and 311; k = 128, 5698 x 4352 31 and 24, 4096 x 4096 17 and
+            // 17; k = 1024, 5698 x 4352 48 and 39, 8192 x 8192 92 and 101.
             const int64_t wide = (t256 + 255) / 256 * (1300 + 120 * p.kblocks), two = (t128 + 255) / 256 * (350 + 43 * p.kblocks);
             if (t128 > 256 && wide <= two) {
                 const int tn = (p.n + 255) / 256, tm = (p.m + 255) / 256;
@@ -641,13 +644,15 @@ void run_linear(const LinearParams &p, hipStream_t s)
             }
         }
         // Up to two blocks a CU of 64 x 64: a step's products and reads are a quarter as many, and it is
-        // their time that a lone block waits for (128 x 4096 outputs of 4096: 11.8 us, tiles of 128 19.1; 6383
-        // x 80 of 2822: 11.3 and 16.7; 512 x 4096 of 4096: 17.3 and 19.5; 1024 x 4096: 32 and 23).
+        // their time that a lone block waits for (us, tiles of 128 behind; 128 x 4096 outputs of 4096: 12.8 and
+        // 19.5; 6383 x 80 of 2822: 11.7 and 17.0; 512 x 4096 of 128, 1024, 4096, 11008: 5.3 and 6.0, 7.7 and 9.1,
+        // 16.9 and 19.9, 38.9 and 42.4. More blocks, 1024 x 4096 of the first three: 8.7 and 6.7, 13.5 and 10.6,
+        // 30 and 21; 2005 x 2048 of 1000: 17.0 and 12.3).
         const int64_t t64 = int64_t((p.n + 63) / 64) * ((p.m + 63) / 64);
         if (t64 <= 512) return run_tiles<O, WF, 64, 64, 2, 2, 4>(p, s);
         // One block of 128 x 128 a CU at most: eight waves, four steps in LDS (1024 x 4096 outputs of 4096:
-        // 22.8 us, four waves with two steps 26.2). More: two blocks of four waves share a CU (5000 x 5000
-        // outputs of 4096: 117 us, eight waves and four steps 140).
+        // 21.5 us, four waves with two steps 26.3; 2005 x 2048 of 1000: 12.3 and 13.4). More: two blocks of four
+        // waves share a CU (5000 x 5000 outputs of 4096: 113 us, eight waves and four steps 130).
         if (t128 <= 256) return run_tiles<O, WF, 128, 128, 2, 4, 4>(p, s);
         return run_tiles<O, WF, 128, 128, 2, 2, 2>(p, s);
     }
