@@ -667,12 +667,11 @@ int64_t ds_linear_fp8_backward_data_scratch_bytes(int64_t m, int64_t n, int64_t 
  * tokens; dim: a multiple of 16, at most 256. Row b of `table` [batch][columns] (ldt
  * elements apart) lists the pages of sequence b in order; columns x page is at most 2^31 - 4096.
  *
- * ds_kv_cache_append writes tokens 0 .. count[b] - 1 (count NULL or above tokens: all) of k and
- * v [batch][tokens][heads][dim] at positions start[b], start[b] + 1, .. of sequence b (none where
- * start[b] is negative). A
- * page's scale is the one its new tokens need; where it already holds tokens before
- * start[b], the larger of that and its own, and what it holds is rounded again where the
- * scale grows. Values past the scales' range are held as the largest number. Tokens of a
+ * ds_kv_cache_append writes tokens 0 .. count[b] - 1 (count NULL or above tokens: all) of
+ * k and v [batch][tokens][heads][dim] at positions start[b], start[b] + 1, .. of sequence b
+ * (none where start[b] is negative). A page's scale is the one its new tokens need; where it
+ * already holds tokens before start[b], the larger of that and its own, and what it holds is
+ * rounded again where the scale grows. Values past the scales' range are held as the largest number. Tokens of a
  * column past the table, or of a page outside 0 .. pages - 1, are dropped. The pages that
  * a call writes must be distinct. strides: of k and v in elements (sequence, token,
  * head; host memory, read before the call returns); a vector's elements are consecutive. */
@@ -690,11 +689,12 @@ ds_status ds_kv_cache_append(const void *k, const void *v, uint8_t *k_cache, uin
  * i < count[b] is at position length[b] - count[b] + i and sees the keys up to its own, the
  * last `window` of them where window > 0. o (q's shape and type) = softmax(scale * q k) v; a
  * query that sees no key, or i >= count[b], gets zeros. Keys past the table's columns, or on a
- * page outside 0 .. pages - 1, are not seen (a page may leave a sequence that way) and move no
- * position. A length below 0 is taken as 0, a count outside 0 .. tokens as the nearest of those. What
- * pages hold past a sequence's end does not matter; a NaN among the values of a token makes
- * NaN of its element in the results of the queries that see the token, and of no others.
- * Up to 65535 sequences times heads. scratch: ds_attention_fp8_scratch_bytes (0: none needed). */
+ * page outside 0 .. pages - 1, are not seen (a page may leave a sequence that way) and move
+ * no position. A length below 0 is taken as 0, a count outside 0 .. tokens as the nearest of
+ * those. What pages hold past a sequence's end does not matter; a NaN among the values of a
+ * token makes NaN of its element in the results of the queries that see the token, and of no
+ * others. Up to 65535 sequences times heads. scratch: ds_attention_fp8_scratch_bytes (0:
+ * none needed). */
 ds_status ds_attention_fp8(const void *q, const uint8_t *k_cache, const uint8_t *v_cache,
                            const uint8_t *k_scales, const uint8_t *v_scales, const int32_t *table,
                            const int32_t *length, const int32_t *count, void *o, int64_t batch,

@@ -947,7 +947,8 @@ void run_attention(const AttentionParams &p, const Plan &a, int64_t batch, hipSt
     const int bhs = int(batch * p.heads);
     const dim3 many(uint32_t((int64_t(bhs) * a.row_tiles * a.splits + 7) / 8 * 8));
     if (a.waves == 0) {
-        hipLaunchKernelGGL((p.tokens == 1 ? attention_few_kernel<T, DP, true> : attention_few_kernel<T, DP, false>), dim3(a.splits, bhs), dim3(256), 0, s, p);
+        hipLaunchKernelGGL((p.tokens == 1 ? attention_few_kernel<T, DP, true> : attention_few_kernel<T, DP, false>), dim3(a.splits, bhs),
+                           dim3(256), 0, s, p);
     } else {
         hipLaunchKernelGGL((a.waves == 2 ? attention_many_kernel<T, DP, 2> : attention_many_kernel<T, DP, 4>), many, dim3(64 * a.waves), 0, s, p, bhs);
     }

@@ -673,7 +673,8 @@ void run_linear(const LinearParams &p, bool e5m2, hipStream_t s)
     else run_linear<O, 0>(p, s);
 }
 
-// Whether rows of x too far apart for the tiles, or of w, are few enough for linear_rows_kernel's grid.
+// Whether a product whose rows are too far apart for the tiles has few enough for linear_rows_kernel's
+// grid, whose second axis takes 65535 times 64 of them.
 bool rows_fit(int64_t m, int64_t ldx, int64_t ldw) { return (ldx <= kReach && ldw <= kReach) || m <= 64 * 65535; }
 
 int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
