@@ -597,7 +597,8 @@ typedef enum ds_dtype {
     DS_TYPE_F16 = 1,
     DS_TYPE_BF16 = 2,
     DS_TYPE_F8E4M3 = 3,
-    DS_TYPE_F8E5M2 = 4
+    DS_TYPE_F8E5M2 = 4,
+    DS_TYPE_F64 = 5              /* frequencies of positions only */
 } ds_dtype;
 
 /* Root-mean-square norm. h = x + residual, rounded to `type` and stored (residual
@@ -704,6 +705,92 @@ ds_status ds_attention_fp8(const void *q, const uint8_t *k_cache, const uint8_t 
                            int64_t window, int32_t type, void *scratch, int64_t scratch_bytes,
                            void *stream);
 int64_t ds_attention_fp8_scratch_bytes(int64_t batch, int64_t tokens, int64_t heads,
+                                       int64_t group, int64_t dim, int64_t page,
+                                       int64_t columns);
+
+/* Query and key heads, normed and turned by their tokens' positions in one pass. For each vector x of
+ * q [batch][tokens][heads][dim] and k [batch][tokens][kv_heads][dim] (type; k NULL with kv_heads 0):
+ * u = x / sqrt(mean(x^2) + eps) * weight (q_weight, k_weight [dim], `type` or float32 as weight_type says;
+ * NULL: u = x), then each pair (a, b) of u becomes (a cos - b sin, b cos + a sin) of the angle
+ * position * frequency, and elements past the pairs stay. Pair i < pairs <= dim / 2 is elements i and
+ * i + pairs, or 2 i and 2 i + 1 where `interleaved` is not 0. positions [axes][batch][tokens] int32 (any
+ * value; strides: axis, sequence, token); frequencies [pairs] in radians a position, DS_TYPE_F32 or
+ * DS_TYPE_F64; the angle is taken in 64 bits and rounded once it lies within a turn. axes: 1, or up to 4 with sections
+ * [axes] (host memory): the first sections[0] pairs go by the first axis, and so on; they add up to pairs.
+ * dim: even, at most 256. strides: of the vectors in elements (sequence, token, head); a vector's
+ * elements are consecutive. The strides and sections are read before the call returns. */
+ds_status ds_rotary_norm(const void *q, const void *k, const int32_t *positions,
+                         const void *frequencies, const void *q_weight, const void *k_weight,
+                         void *q_out, void *k_out, int64_t batch, int64_t tokens, int64_t heads,
+                         int64_t kv_heads, int64_t dim, int64_t pairs, int64_t axes,
+                         const int32_t *sections, const int64_t *q_strides,
+                         const int64_t *k_strides, const int64_t *position_strides,
+                         const int64_t *q_out_strides, const int64_t *k_out_strides,
+                         int32_t interleaved, float eps, int32_t type, int32_t weight_type,
+                         int32_t frequency_type, void *stream);
+
+/* Its gradient: dq, dk (of q and k) from dq_out, dk_out (of the results) and the call's inputs, and
+ * dq_weight, dk_weight in the weights' type (NULL: not wanted; with one of them scratch of
+ * ds_rotary_norm_backward_scratch_bytes is). q and k may be NULL where they have no weight. The
+ * sums are taken in the same order in every run. Without tokens the weights' gradients are 0. */
+ds_status ds_rotary_norm_backward(const void *dq_out, const void *dk_out, const void *q,
+                                  const void *k, const int32_t *positions,
+                                  const void *frequencies, const void *q_weight,
+                                  const void *k_weight, void *dq, void *dk, void *dq_weight,
+                                  void *dk_weight, int64_t batch, int64_t tokens, int64_t heads,
+                                  int64_t kv_heads, int64_t dim, int64_t pairs, int64_t axes,
+                                  const int32_t *sections, const int64_t *dq_out_strides,
+                                  const int64_t *dk_out_strides, const int64_t *q_strides,
+                                  const int64_t *k_strides, const int64_t *position_strides,
+                                  const int64_t *dq_strides, const int64_t *dk_strides,
+                                  int32_t interleaved, float eps, int32_t type,
+                                  int32_t weight_type, int32_t frequency_type, void *scratch,
+                                  int64_t scratch_bytes, void *stream);
+int64_t ds_rotary_norm_backward_scratch_bytes(int64_t batch, int64_t tokens, int64_t dim);
+
+/* A paged cache of keys and values in 4 bits: E2M1 numbers (0, 0.5, 1, 1.5, 2, 3, 4, 6 with codes 0 .. 7,
+ * and 8 for the sign), two a byte, the first in the low half, and an E8M0 scale for each token, head and
+ * 32 elements (of the last block, what dim leaves). k_cache [pages][heads][page][dim / 2]; v_cache
+ * [pages][heads][page / 4][dim / 8][4 tokens][4 bytes of 8 elements]; k_scales, v_scales
+ * [pages][heads][ceil(dim / 32)][page]; each begins on 16 bytes. page, dim and table as above.
+ *
+ * ds_kv_cache_fp4_append writes tokens as ds_kv_cache_append does, each for itself: what a page
+ * holds of other tokens stays as it is. A scale is the least power of two within 2^-23 .. 2^13 that brings its
+ * elements to at most 6, so that every number held is a 16-bit float exactly; elements are rounded to
+ * nearest even, those beyond +-49152 are held as that. A block with an element that is infinite or NaN is
+ * NaN as a whole (scale byte 255). The slots that a call writes must be distinct. */
+ds_status ds_kv_cache_fp4_append(const void *k, const void *v, uint8_t *k_cache, uint8_t *v_cache,
+                                 uint8_t *k_scales, uint8_t *v_scales, const int32_t *table,
+                                 const int32_t *start, const int32_t *count, int64_t batch,
+                                 int64_t tokens, int64_t heads, int64_t dim, int64_t page,
+                                 int64_t pages, int64_t columns, int64_t ldt,
+                                 const int64_t *k_strides, const int64_t *v_strides, int32_t type,
+                                 void *stream);
+
+/* The way back: k and v [batch][tokens][heads][dim] (type) of positions start[b] .. of sequence b,
+ * exactly (in DS_TYPE_F16 too). Tokens from count[b] on (count NULL: tokens), of a sequence whose start is negative, of
+ * a column past the table or of a page outside 0 .. pages - 1 are 0. */
+ds_status ds_kv_cache_fp4_read(const uint8_t *k_cache, const uint8_t *v_cache,
+                               const uint8_t *k_scales, const uint8_t *v_scales,
+                               const int32_t *table, const int32_t *start, const int32_t *count,
+                               void *k, void *v, int64_t batch, int64_t tokens, int64_t heads,
+                               int64_t dim, int64_t page, int64_t pages, int64_t columns,
+                               int64_t ldt, const int64_t *k_strides, const int64_t *v_strides,
+                               int32_t type, void *stream);
+
+/* ds_attention_fp8 over a 4-bit cache: the same queries, positions, windows and limits. A block
+ * that is NaN makes NaN of the results of the queries that see its token: a key's of all their elements,
+ * a value's of the block's. (Scale bytes that no append writes, 1 .. 103 and 141 .. 254, give what a
+ * 16-bit float has of their numbers.) scratch: ds_attention_fp4_scratch_bytes (0: none needed). */
+ds_status ds_attention_fp4(const void *q, const uint8_t *k_cache, const uint8_t *v_cache,
+                           const uint8_t *k_scales, const uint8_t *v_scales, const int32_t *table,
+                           const int32_t *length, const int32_t *count, void *o, int64_t batch,
+                           int64_t tokens, int64_t heads, int64_t group, int64_t dim,
+                           int64_t page, int64_t pages, int64_t columns, int64_t ldt,
+                           const int64_t *q_strides, const int64_t *o_strides, float scale,
+                           int64_t window, int32_t type, void *scratch, int64_t scratch_bytes,
+                           void *stream);
+int64_t ds_attention_fp4_scratch_bytes(int64_t batch, int64_t tokens, int64_t heads,
                                        int64_t group, int64_t dim, int64_t page,
                                        int64_t columns);
 

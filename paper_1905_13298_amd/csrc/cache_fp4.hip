@@ -1,0 +1,631 @@
+// A paged cache of keys and values in 4 bits, the way back to floats, and the attention that
+// reads it.
+//
+// A number is E2M1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives), two a byte, the first in the
+// low half, with one E8M0 scale for each token, head and 32 elements. A token has its scales for
+// itself, so that what a page holds never changes when others follow. Keys are rows
+// [page][head][token][dim]; values lie in pieces of 16 bytes, 4 tokens x 8 dimensions
+// [page][head][token / 4][dim / 8][token % 4], which is what a lane turns into an operand of the second
+// product (it contracts tokens); scales are [page][head][dim / 32][token], so that those of neighbouring
+// tokens are one load. Scales lie in 2^-23 .. 2^13, where every number is a 16-bit float exactly.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "attention.hpp"
+#include "conv_plan.hpp"
+#include "fastdiv.hpp"
+
+namespace ds {
+
+namespace {
+
+constexpr int kBlock4 = 32;                       // elements that share a scale
+constexpr int kLow4 = 127 - 23, kHigh4 = 127 + 13, kNan4 = 255;
+
+int64_t blocks4(int64_t dim) { return (dim + kBlock4 - 1) / kBlock4; }
+
+// ---------------------------------------------------------------------------
+// To and from the cache.
+
+struct CacheParams {
+    const int *table, *start, *count;
+    int64_t ldt;
+    int columns, pages, tokens, heads, dim, page_shift, blocks, per;      // per: workgroups of a sequence
+    FastDiv lanes, by_head;            // threads of a vector (8 elements each, whole scale blocks), heads
+    int64_t sb[2], st[2], sh[2];       // strides of k and v: sequence, token, head
+};
+
+// A thread's 8 elements of one vector of k or v: which they are, and where the cache has them.
+struct Place {
+    int b, t, h, lane, slot;
+    int64_t at;                        // page and head, -1: nowhere
+    bool live;
+    __device__ __forceinline__ Place(const CacheParams &p)
+    {
+        b = int(blockIdx.x) / p.per;
+        const int i = (int(blockIdx.x) - b * p.per) * 256 + int(threadIdx.x), vec = fdiv(i, p.lanes);
+        lane = i - vec * int(p.lanes.d);
+        t = fdiv(vec, p.by_head);
+        h = vec - t * p.heads;
+        live = t < p.tokens;
+        at = -1;
+        slot = 0;
+        const int start = p.start[b], n = p.count ? min(p.count[b], p.tokens) : p.tokens;
+        if (start < 0 || t >= n) return;
+        const uint32_t pos = uint32_t(start) + uint32_t(t), col = pos >> p.page_shift;
+        if (col >= uint32_t(p.columns)) return;
+        const int pid = p.table[b * p.ldt + col];
+        if (unsigned(pid) >= unsigned(p.pages)) return;
+        at = int64_t(pid) * p.heads + h;
+        slot = int(pos) & ((1 << p.page_shift) - 1);
+    }
+    // The bytes of the elements' codes, and their scale's.
+    __device__ __forceinline__ int64_t codes(const CacheParams &p, bool values) const
+    {
+        const int64_t base = (at << p.page_shift) * (p.dim / 2);
+        return base + (values ? (slot >> 2) * 2 * p.dim + lane * 16 + (slot & 3) * 4 : slot * (p.dim / 2) + lane * 4);
+    }
+    __device__ __forceinline__ int64_t scale(const CacheParams &p) const
+    {
+        return ((at * p.blocks + (lane >> 2)) << p.page_shift) + slot;
+    }
+};
+
+// 2^(e - 127) of the scale byte e for the conversions, which look at the exponent's bits alone
+// (255: NaN).
+__device__ __forceinline__ float scale4(uint32_t e) { return __uint_as_float(e << 23); }
+
+// The scale byte of the least power of two that brings `amax` (finite, >= 0) to at most 6 = 1.5 * 2^2:
+// a mantissa above 1.5 carries into the exponent.
+__device__ __forceinline__ int scale_byte4(float amax)
+{
+    return min(max(int((__float_as_uint(amax) + 0x3fffffu) >> 23) - 2, kLow4), kHigh4);
+}
+
+// New tokens into their pages: 8 elements a thread, 4 threads a scale. An element that is no finite
+// number makes its block NaN (scale byte 255, codes 0).
+template <typename T>
+__global__ void __launch_bounds__(256)
+append4_kernel(const T *__restrict__ k, const T *__restrict__ v, uint8_t *__restrict__ kc, uint8_t *__restrict__ vc,
+               uint8_t *__restrict__ ks, uint8_t *__restrict__ vs, const CacheParams p)
+{
+    const int which = int(blockIdx.y);
+    const Place at(p);
+    const bool mine = at.at >= 0 && at.lane * 8 < p.dim;
+    float x[8] = {}, top = 0.f;
+    if (mine) load8((which ? v : k) + at.b * p.sb[which] + at.t * p.st[which] + at.h * p.sh[which] + at.lane * 8, 8, x);
+    bool fine = true;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        fine = fine && fabsf(x[i]) < __builtin_inff();
+        top = fmaxf(top, fabsf(x[i]));
+    }
+    top = lanes_max<4>(fine ? top : __builtin_inff());
+    fine = top < __builtin_inff();
+    const int e = fine ? scale_byte4(top) : kNan4;
+    if (!mine) return;
+    const float s = scale4(uint32_t(e));
+    uint32_t q = 0;
+    if (fine) {
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, x[0], x[1], s, 0);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, x[2], x[3], s, 1);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, x[4], x[5], s, 2);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, x[6], x[7], s, 3);
+    }
+    *reinterpret_cast<uint32_t *>((which ? vc : kc) + at.codes(p, which)) = q;
+    if ((at.lane & 3) == 0) (which ? vs : ks)[at.scale(p)] = uint8_t(e);
+}
+
+// Eight numbers of a scale, exactly (2^-24 .. 6 * 2^13: 16-bit floats; NaN of scale byte 255).
+__device__ __forceinline__ void widen4(uint32_t codes, float s, float (&x)[8])
+{
+    const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 1);
+    const auto c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 3);
+    x[0] = a[0], x[1] = a[1], x[2] = b[0], x[3] = b[1], x[4] = c[0], x[5] = c[1], x[6] = d[0], x[7] = d[1];
+}
+
+// Tokens of a cache as floats [sequence][token][head][dim], 0 where there is none.
+template <typename T>
+__global__ void __launch_bounds__(256)
+read4_kernel(T *__restrict__ k, T *__restrict__ v, const uint8_t *__restrict__ kc, const uint8_t *__restrict__ vc,
+             const uint8_t *__restrict__ ks, const uint8_t *__restrict__ vs, const CacheParams p)
+{
+    const int which = int(blockIdx.y);
+    const Place at(p);
+    if (!at.live || at.lane * 8 >= p.dim) return;
+    float x[8] = {};
+    if (at.at >= 0)
+        widen4(*reinterpret_cast<const uint32_t *>((which ? vc : kc) + at.codes(p, which)), scale4((which ? vs : ks)[at.scale(p)]), x);
+    store8((which ? v : k) + at.b * p.sb[which] + at.t * p.st[which] + at.h * p.sh[which] + at.lane * 8, 8, x);
+}
+
+// ---------------------------------------------------------------------------
+// Attention. A kv head's queries are its `rows` = tokens x group vectors, and a wave
+// handles 16 of them at a time with 64 keys:
+//
+//   S^T = K Q^T (the matrix instruction's rows are keys, its columns queries), so that a
+//   lane holds 16 consecutive keys of one query;
+//   t = S * scale * log2(e), p = 2^(t - m), m such that the largest p of a row is from 2^9 to 2^15;
+//   O^T += V^T P (rows: dimensions, columns: queries), l += p.
+//
+// The key of row r of a 16-key tile t is 4 r + t: lane group g (lane / 16) holds the products of keys
+// 16 g .. 16 g + 15, and those are the ones that it contracts in the second product, 8 at a time; and a
+// lane's four keys of the first product have their scales side by side. Dimension r of tile j of
+// the second product is (DP / 16) r + j (within 128), so that a lane's dimensions are neighbours in
+// memory too. Keys become numbers of the queries' type exactly, with their scales; p and the values
+// are 16-bit floats with 10 bits of mantissa: values exactly, p rounded once, to 2^-11 of itself down to
+// 2^-23 of the row's largest and to 2^-34 of that one below (l has all of it in 32 bits).
+
+// Eight numbers as an operand.
+template <typename T>
+__device__ __forceinline__ typename Vec8<T>::type operand4(uint32_t codes, float s)
+{
+    if constexpr (__is_same(T, _Float16)) {
+        const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, s, 1);
+        const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, s, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, s, 3);
+        return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+    } else {
+        const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 1);
+        const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 3);
+        return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+    }
+}
+
+// Scale byte i of a word.
+__device__ __forceinline__ float scale_of(uint32_t word, int i)
+{
+    return __uint_as_float(i == 0 ? word << 23 : i == 1 ? word << 15 : i == 2 ? word << 7 : word >> 1);
+}
+
+// 0x80 in each byte of x that is 255, the scale that is NaN. A weight of 0 does not keep a NaN out of a
+// sum: where some queries see a step's keys and others do not, such scales are taken out, and come back
+// as NaN in the results of the queries that see them (a product of where they are with what is seen).
+__device__ __forceinline__ uint32_t nan_scales(uint32_t x) { return ((x & 0x7f7f7f7fu) + 0x01010101u) & x & 0x80808080u; }
+
+// Two dimensions (byte `sel` of each) of 8 tokens, the numbers of a dimension together: 4 tokens a
+// piece, a word each, scales s.
+template <int SEL>
+__device__ __forceinline__ void turn4(const i32x4 &a, const i32x4 &b, const float (&s)[8], f16x8 &even, f16x8 &odd)
+{
+    uint32_t x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const f16x2 y = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(uint32_t(i < 4 ? a[i] : b[i - 4]), s[i], SEL);
+        x[i] = __builtin_bit_cast(uint32_t, y);
+    }
+    i32x4 lo, hi;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        lo[i] = int(__builtin_amdgcn_perm(x[2 * i + 1], x[2 * i], 0x05040100u));
+        hi[i] = int(__builtin_amdgcn_perm(x[2 * i + 1], x[2 * i], 0x07060302u));
+    }
+    even = __builtin_bit_cast(f16x8, lo);
+    odd = __builtin_bit_cast(f16x8, hi);
+}
+
+// 16 queries of a kv head: a block of 4 waves takes a share of the keys, each wave every fourth
+// 64 of it straight from memory to registers, and joins them at its end.
+template <typename T, int DP>
+__global__ void __launch_bounds__(256)
+attention4_few_kernel(const AttentionParams p, int blocks)
+{
+    constexpr int kWaves = 4;
+    constexpr int QC = DP / 32;            // chunks of 32 of the first product's contraction, words of a lane's part of a key
+    constexpr int DT = DP / 16;            // tiles of 16 dimensions of the second product
+    constexpr int NS = DP == 256 ? 2 : 1;  // scale blocks of a lane's part of a key, or value
+    typedef typename Vec8<T>::type v8;
+    __shared__ float ml[2][kWaves][16];
+    __shared__ f32x4 osum[kWaves][DT][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), r = lane & 15, g = lane >> 4;
+    const int split = int(blockIdx.x), bh = int(blockIdx.y), b = bh / p.heads, h = bh - b * p.heads;
+    const int D = p.dim, page = 1 << p.page_shift, row = int(blockIdx.z) * 16 + r;
+    const Sequence seq(p, b);
+    v8 qf[QC];
+    int low, high;
+    load_query<T, DP, 8, DP / 4, QC>(p, seq, b, h, row, g, low, high, qf);
+    // (Rows that see no key, which are 0 in the end, have no say.)
+    int tlo = high > 0 ? low : 0x7fffffff, thi = high, alo = low, ahi = high > 0 ? high : 0x7fffffff;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) {
+        tlo = min(tlo, __shfl_xor(tlo, o));
+        thi = max(thi, __shfl_xor(thi, o));
+        alo = max(alo, __shfl_xor(alo, o));
+        ahi = min(ahi, __shfl_xor(ahi, o));
+    }
+    // Keys that some query sees: [tlo, thi); that every one sees: [alo, ahi).
+    tlo = __builtin_amdgcn_readfirstlane(tlo);
+    thi = __builtin_amdgcn_readfirstlane(thi);
+    alo = __builtin_amdgcn_readfirstlane(alo);
+    ahi = __builtin_amdgcn_readfirstlane(ahi);
+    const int s0 = thi > 0 ? tlo / kStep : 0, s1 = (thi + kStep - 1) / kStep;
+    const int each = (s1 - s0 + p.splits - 1) / p.splits;
+    const int from = s0 + split * each, to = min(s1, from + each);
+
+    f32x4 acc[DT];
+    float m = -__builtin_inff(), l = 0.f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) acc[d] = f32x4{};
+    // Page of the 16 keys from `key` on (they share it), or -1 where there is none.
+    auto page_of = [&](int key) {
+        const int col = key >> p.page_shift;
+        const int pid = key < thi ? p.table[b * p.ldt + col] : -1;
+        return unsigned(pid) < unsigned(p.pages) ? pid : -1;
+    };
+    for (int step = from + wave; step < to; step += kWaves) {
+        const int base = step * kStep;
+        const int krun = base + (r >> 2) * 16, vrun = base + g * 16;
+        const int kp = page_of(krun), vp = page_of(vrun);
+        const int64_t kat = int64_t(max(kp, 0)) * p.heads + h, vat = int64_t(max(vp, 0)) * p.heads + h;
+        const int kslot = (krun & (page - 1)) + (r & 3) * 4, vslot = vrun & (page - 1);
+        uint32_t kraw[4][QC], kse[NS];
+        i32x4 vraw[NS][4];
+        uint32_t vse[NS][4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int c = 0; c < QC; c += 2) {
+                const int d = g * (DP / 4) + c * 8;
+                i32x2 x{};
+                if (kp >= 0 && d < D) x = *reinterpret_cast<const i32x2 *>(p.kc + (kat * page + kslot + t) * (D / 2) + d / 2);
+                kraw[t][c] = uint32_t(x[0]);
+                kraw[t][c + 1] = uint32_t(x[1]);
+            }
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+            const int d = g * (DP / 4) + i * 32;
+            kse[i] = kp >= 0 && d < D ? *reinterpret_cast<const uint32_t *>(p.ks + (kat * blocks + d / 32) * page + kslot) : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+            const int d = DP == 64 ? r * 4 : i * 128 + r * 8;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                vraw[i][q] = vp >= 0 && d < D ? *reinterpret_cast<const i32x4 *>(p.vc + vat * page * (D / 2) + (vslot / 4 + q) * 2 * D + d / 8 * 16) : i32x4{};
+                // (Heads of up to 64: half of a piece's dimensions are this lane's.)
+                if (DP == 64) vraw[i][q] = (r & 1) ? i32x4(vraw[i][q] >> 16) : vraw[i][q];
+            }
+            i32x4 e{};
+            if (vp >= 0 && d < D) e = *reinterpret_cast<const i32x4 *>(p.vs + (vat * blocks + d / 32) * page + vslot);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) vse[i][q] = uint32_t(e[q]);
+        }
+        f32x4 s[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int c = 0; c < QC; ++c)
+                s[t] = mma(operand4<T>(kraw[t][c], scale_of(kse[c * NS / QC], t)), qf[c], c == 0 ? f32x4{} : s[t]);
+        // Element i of s[t]: key vrun + 4 i + t.
+        if (!__all(vp >= 0 && vrun >= low && vrun + 16 <= high)) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int key = vrun + (i & 3) * 4 + (i >> 2);
+                s[i >> 2][i & 3] = vp >= 0 && key >= low && key < high ? s[i >> 2][i & 3] : -__builtin_inff();
+            }
+        }
+        const float sub = or_zero(m);
+        float e[16], top = -__builtin_inff();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) e[i] = fmaf(s[i & 3][i >> 2], p.scale, -sub);        // (key vrun + i)
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) top = fmaxf(top, fmaxf(e[i], e[i + 1]));
+        raise(m, l, max_over_32(max_over_16(top)),
+              [&](float by) {
+#pragma unroll
+                  for (int i = 0; i < 16; ++i) e[i] -= by;
+              },
+              [&](float alpha) {
+#pragma unroll
+                  for (int d = 0; d < DT; ++d) acc[d] *= alpha;
+              });
+        f16x8 pf[2];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            e[i] = __builtin_amdgcn_exp2f(e[i]);
+            l += e[i];
+            pf[i >> 3][i & 7] = _Float16(e[i]);
+        }
+        if (base + kStep > thi || base < tlo) {
+            // Keys that no query sees may hold anything: their values count as 0 (whatever the code, 2^-127
+            // of it is 0 as a 16-bit float).
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int i = 0; i < NS; ++i) vse[i][q] &= uint32_t(key_mask(vrun + 4 * q, tlo, thi));
+        }
+        if (base + kStep > ahi || base < alo) {
+            uint32_t nan = 0;
+#pragma unroll
+            for (int i = 0; i < NS; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) nan |= nan_scales(vse[i][q]);
+            if (__any(nan != 0)) {
+                f16x8 seen[2];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) seen[i >> 3][i & 7] = _Float16(vp >= 0 && vrun + i >= low && vrun + i < high ? 1.f : 0.f);
+#pragma unroll
+                for (int i = 0; i < NS; ++i) {
+                    f32x4 n{};
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        f16x8 where;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) where[j] = _Float16((vse[i][2 * c + j / 4] >> (8 * (j & 3)) & 255u) == 255u ? 1.f : 0.f);
+                        n = mma(where, seen[c], n);
+                    }
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) vse[i][q] &= ~((nan_scales(vse[i][q]) >> 7) * 0xffu);
+                    // A lane's dimensions have their scale in common: the same in all of their tiles.
+#pragma unroll
+                    for (int d = i * (DT / NS); d < (i + 1) * (DT / NS); ++d)
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) acc[d][w] += n[w] > 0.f ? __builtin_nanf("") : 0.f;
+                }
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int i = 0; i < NS; ++i) {
+                float sv[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sv[j] = scale_of(vse[i][2 * c + j / 4], j & 3);
+                auto pair = [&](auto sel) {
+                    constexpr int SEL = decltype(sel)::value;
+                    f16x8 even, odd;
+                    turn4<SEL>(vraw[i][2 * c], vraw[i][2 * c + 1], sv, even, odd);
+                    f32x4 &x = acc[i * (DT / NS) + 2 * SEL], &y = acc[i * (DT / NS) + 2 * SEL + 1];
+                    x = mma(even, pf[c], x);
+                    y = mma(odd, pf[c], y);
+                };
+                pair(std::integral_constant<int, 0>{});
+                pair(std::integral_constant<int, 1>{});
+                if constexpr (DP > 64) {
+                    pair(std::integral_constant<int, 2>{});
+                    pair(std::integral_constant<int, 3>{});
+                }
+            }
+    }
+    if (high == 0) {      // a row that sees no key, whatever the others see
+#pragma unroll
+        for (int d = 0; d < DT; ++d) acc[d] = f32x4{};
+    }
+    // The waves' sums together: a lane's l is its own keys'.
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (g == 0) {
+        ml[0][wave][r] = m;
+        ml[1][wave][r] = l;
+    }
+    __syncthreads();
+    float top = ml[0][0][r];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, ml[0][w][r]);
+    const float sub = or_zero(top), mine = __builtin_amdgcn_exp2f(m - sub);
+    float total = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) total = fmaf(ml[1][w][r], __builtin_amdgcn_exp2f(ml[0][w][r] - sub), total);
+    // Four dimensions that are neighbours, tiles 4 d .. 4 d + 3 of one row, a piece.
+#pragma unroll
+    for (int d = 0; d < DT; d += 4)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) osum[wave][d + w][lane] = f32x4{acc[d][w], acc[d + 1][w], acc[d + 2][w], acc[d + 3][w]} * mine;
+    __syncthreads();
+    if (row >= p.rows) return;
+    float *part = p.part ? p.part + ((int64_t(bh) * p.rows + row) * p.splits + split) * (D + 2) : nullptr;
+    if (part && wave == 0 && g == 0) {
+        part[D] = top;
+        part[D + 1] = total;
+    }
+    const float inv = inverse(total);
+    for (int d = wave; d < DT; d += kWaves) {
+        // Tiles d & -4 .. + 3 of row 4 g + d % 4.
+        const int line = g * 4 + (d & 3), tile = d & -4;
+        const int dim = DP == 64 ? line * 4 : tile / 8 * 128 + line * 8 + (tile & 4);
+        if (dim >= D) continue;
+        f32x4 o = osum[0][d][lane];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) o += osum[w][d][lane];
+        store_row<T>(p, b, h, row, part, dim, o, inv);
+    }
+}
+
+// How a call is split: over the rows first, then over the keys until 512 blocks (two a CU) have at
+// least 8 steps of 64 keys each.
+Plan plan_attention4(int64_t batch, int64_t tokens, int64_t heads, int64_t group, int64_t columns, int64_t page)
+{
+    Plan a;
+    a.rows = tokens * group;
+    a.waves = 0;
+    a.row_tiles = int((a.rows + 15) / 16);
+    const int64_t blocks = std::max<int64_t>(batch * heads * a.row_tiles, 1), steps = (columns * page + kStep - 1) / kStep;
+    a.splits = int(std::max<int64_t>(1, std::min<int64_t>({(511 + blocks) / blocks, (steps + 7) / 8, 256})));
+    return a;
+}
+
+template <typename T, int DP>
+void run_attention4(const AttentionParams &p, const Plan &a, int64_t batch, hipStream_t s)
+{
+    const int bhs = int(batch * p.heads);
+    hipLaunchKernelGGL((attention4_few_kernel<T, DP>), dim3(a.splits, bhs, a.row_tiles), dim3(256), 0, s, p, int(blocks4(p.dim)));
+    if (a.splits > 1)
+        hipLaunchKernelGGL((attention_join_kernel<T, DP / 4>), dim3(uint32_t(bhs * a.rows)), dim3(256), 0, s, p);
+}
+
+template <typename T>
+void run_attention4(const AttentionParams &p, const Plan &a, int64_t batch, hipStream_t s)
+{
+    if (p.dim <= 64) run_attention4<T, 64>(p, a, batch, s);
+    else if (p.dim <= 128) run_attention4<T, 128>(p, a, batch, s);
+    else run_attention4<T, 256>(p, a, batch, s);
+}
+
+int page_shift(int64_t page)
+{
+    int shift = 4;
+    while ((int64_t(1) << shift) < page) ++shift;
+    return shift;
+}
+
+// What an append and a read have in common; bytes: those that k and v span.
+ds_status cache_params(CacheParams &p, int64_t (&bytes)[2], const int32_t *table, const int32_t *start, const int32_t *count, int64_t batch,
+                       int64_t tokens, int64_t heads, int64_t dim, int64_t page, int64_t pages, int64_t columns, int64_t ldt,
+                       const int64_t *k_strides, const int64_t *v_strides, int64_t es)
+{
+    const int64_t lanes = blocks4(dim) * 4;
+    if (tokens * heads > (kMaxElems - 255) / lanes) return fail(DS_ERR_UNSUPPORTED, "too many vectors of a sequence in one call");
+    const int64_t per = (tokens * heads * lanes + 255) / 256;
+    if (!grid_fits(batch * per, 256)) return fail(DS_ERR_UNSUPPORTED, "too many vectors in one call");
+    p = CacheParams{table, start, count, ldt, int(columns), int(pages), int(tokens), int(heads), int(dim), page_shift(page),
+                    int(blocks4(dim)), int(per), make_fastdiv(uint32_t(lanes)), make_fastdiv(uint32_t(heads)), {}, {}, {}};
+    for (int i = 0; i < 2; ++i) {
+        const int64_t *s = i ? v_strides : k_strides;
+        if (s[0] < 0 || s[1] < 0 || s[2] < 0) return fail(DS_ERR_INVALID_ARG, "strides must be >= 0");
+        p.sb[i] = s[0];
+        p.st[i] = s[1];
+        p.sh[i] = s[2];
+        bytes[i] = span(batch, tokens, heads, s, dim, es);
+    }
+    return DS_SUCCESS;
+}
+
+// Cache and scale addresses for whole words.
+ds_status check_aligned(const uint8_t *k_cache, const uint8_t *v_cache, const uint8_t *k_scales, const uint8_t *v_scales)
+{
+    for (const void *p : {k_cache, v_cache, k_scales, v_scales})
+        if (reinterpret_cast<uintptr_t>(p) % 16) return fail(DS_ERR_INVALID_ARG, "a cache and its scales must begin on 16 bytes");
+    return DS_SUCCESS;
+}
+
+}  // namespace
+
+}  // namespace ds
+
+using namespace ds;
+
+extern "C" ds_status ds_kv_cache_fp4_append(const void *k, const void *v, uint8_t *k_cache, uint8_t *v_cache, uint8_t *k_scales,
+                                            uint8_t *v_scales, const int32_t *table, const int32_t *start, const int32_t *count,
+                                            int64_t batch, int64_t tokens, int64_t heads, int64_t dim, int64_t page, int64_t pages,
+                                            int64_t columns, int64_t ldt, const int64_t *k_strides, const int64_t *v_strides,
+                                            int32_t type, void *stream)
+{
+    if (batch != 0 && tokens != 0 &&
+        (!k || !v || !k_cache || !v_cache || !k_scales || !v_scales || !table || !start || !k_strides || !v_strides))
+        return fail(DS_ERR_NULL_POINTER, "a required pointer is NULL");
+    if (ds_status st = check_cache(batch, tokens, heads, dim, page, pages, columns, ldt)) return st;
+    const int64_t es = float_bytes(type);
+    if (!es) return fail(DS_ERR_INVALID_ARG, "type must be DS_TYPE_F32, DS_TYPE_F16 or DS_TYPE_BF16");
+    if (batch == 0 || tokens == 0) return ok();
+    if (ds_status st = check_aligned(k_cache, v_cache, k_scales, v_scales)) return st;
+    CacheParams p;
+    int64_t bytes[2];
+    if (ds_status st = cache_params(p, bytes, table, start, count, batch, tokens, heads, dim, page, pages, columns, ldt, k_strides, v_strides, es))
+        return st;
+    const int64_t cb = pages * heads * page * dim / 2, sb = pages * heads * page * blocks4(dim);
+    if (ds_status st = check_tensors({{k, bytes[0], "k", false}, {v, bytes[1], "v", false}, {table, span(batch, ldt, columns, 4), "table", false},
+                                      {start, batch * 4, "start", false}, {count, batch * 4, "count", false},
+                                      {k_cache, cb, "k_cache", true}, {v_cache, cb, "v_cache", true},
+                                      {k_scales, sb, "k_scales", true}, {v_scales, sb, "v_scales", true}}))
+        return st;
+    const auto go = [&](auto t) {
+        using T = decltype(t);
+        hipLaunchKernelGGL(append4_kernel<T>, dim3(uint32_t(batch * p.per), 2), dim3(256), 0, static_cast<hipStream_t>(stream),
+                           static_cast<const T *>(k), static_cast<const T *>(v), k_cache, v_cache, k_scales, v_scales, p);
+    };
+    if (type == DS_TYPE_F32) go(float{});
+    else if (type == DS_TYPE_F16) go(_Float16{});
+    else go(__bf16{});
+    return launched("ds_kv_cache_fp4_append");
+}
+
+extern "C" ds_status ds_kv_cache_fp4_read(const uint8_t *k_cache, const uint8_t *v_cache, const uint8_t *k_scales, const uint8_t *v_scales,
+                                          const int32_t *table, const int32_t *start, const int32_t *count, void *k, void *v,
+                                          int64_t batch, int64_t tokens, int64_t heads, int64_t dim, int64_t page, int64_t pages,
+                                          int64_t columns, int64_t ldt, const int64_t *k_strides, const int64_t *v_strides,
+                                          int32_t type, void *stream)
+{
+    if (batch != 0 && tokens != 0 &&
+        (!k || !v || !k_cache || !v_cache || !k_scales || !v_scales || !table || !start || !k_strides || !v_strides))
+        return fail(DS_ERR_NULL_POINTER, "a required pointer is NULL");
+    if (ds_status st = check_cache(batch, tokens, heads, dim, page, pages, columns, ldt)) return st;
+    const int64_t es = float_bytes(type);
+    if (!es) return fail(DS_ERR_INVALID_ARG, "type must be DS_TYPE_F32, DS_TYPE_F16 or DS_TYPE_BF16");
+    if (batch == 0 || tokens == 0) return ok();
+    if (ds_status st = check_aligned(k_cache, v_cache, k_scales, v_scales)) return st;
+    CacheParams p;
+    int64_t bytes[2];
+    if (ds_status st = cache_params(p, bytes, table, start, count, batch, tokens, heads, dim, page, pages, columns, ldt, k_strides, v_strides, es))
+        return st;
+    const int64_t cb = pages * heads * page * dim / 2, sb = pages * heads * page * blocks4(dim);
+    if (ds_status st = check_tensors({{k_cache, cb, "k_cache", false}, {v_cache, cb, "v_cache", false}, {k_scales, sb, "k_scales", false},
+                                      {v_scales, sb, "v_scales", false}, {table, span(batch, ldt, columns, 4), "table", false},
+                                      {start, batch * 4, "start", false}, {count, batch * 4, "count", false},
+                                      {k, bytes[0], "k", true}, {v, bytes[1], "v", true}}))
+        return st;
+    const auto go = [&](auto t) {
+        using T = decltype(t);
+        hipLaunchKernelGGL(read4_kernel<T>, dim3(uint32_t(batch * p.per), 2), dim3(256), 0, static_cast<hipStream_t>(stream),
+                           static_cast<T *>(k), static_cast<T *>(v), k_cache, v_cache, k_scales, v_scales, p);
+    };
+    if (type == DS_TYPE_F32) go(float{});
+    else if (type == DS_TYPE_F16) go(_Float16{});
+    else go(__bf16{});
+    return launched("ds_kv_cache_fp4_read");
+}
+
+extern "C" int64_t ds_attention_fp4_scratch_bytes(int64_t batch, int64_t tokens, int64_t heads, int64_t group, int64_t dim,
+                                                  int64_t page, int64_t columns)
+{
+    if (batch <= 0 || tokens <= 0 || heads <= 0 || group <= 0 || dim <= 0 || page <= 0 || columns <= 0) return 0;
+    return 4 * part_floats(plan_attention4(batch, tokens, heads, group, columns, page), batch, heads, dim);
+}
+
+extern "C" ds_status ds_attention_fp4(const void *q, const uint8_t *k_cache, const uint8_t *v_cache, const uint8_t *k_scales,
+                                      const uint8_t *v_scales, const int32_t *table, const int32_t *length,
+                                      const int32_t *count, void *o, int64_t batch, int64_t tokens, int64_t heads,
+                                      int64_t group, int64_t dim, int64_t page, int64_t pages, int64_t columns, int64_t ldt,
+                                      const int64_t *q_strides, const int64_t *o_strides, float scale, int64_t window,
+                                      int32_t type, void *scratch, int64_t scratch_bytes, void *stream)
+{
+    if (batch != 0 && tokens != 0 &&
+        (!q || !k_cache || !v_cache || !k_scales || !v_scales || !table || !length || !o || !q_strides || !o_strides))
+        return fail(DS_ERR_NULL_POINTER, "a required pointer is NULL");
+    if (ds_status st = check_cache(batch, tokens, heads, dim, page, pages, columns, ldt)) return st;
+    if (group <= 0) return fail(DS_ERR_INVALID_SHAPE, "group must be > 0");
+    if (type != DS_TYPE_F16 && type != DS_TYPE_BF16) return fail(DS_ERR_INVALID_ARG, "type must be DS_TYPE_F16 or DS_TYPE_BF16");
+    if (window < 0 || window > kMaxElems) return fail(DS_ERR_INVALID_ARG, "window must be in [0, 2^31)");
+    if (!std::isfinite(scale)) return fail(DS_ERR_INVALID_ARG, "scale must be finite");
+    if (batch == 0 || tokens == 0) return ok();
+    if (ds_status st = check_aligned(k_cache, v_cache, k_scales, v_scales)) return st;
+    if (batch * heads > 65535) return fail(DS_ERR_UNSUPPORTED, "more than 65535 sequences times heads");
+    if (group > 65535 || tokens * group > kMaxElems / 64) return fail(DS_ERR_UNSUPPORTED, "too many queries of a head");
+    const Plan a = plan_attention4(batch, tokens, heads, group, columns, page);
+    if (batch * heads * a.rows * a.splits > kMaxElems / 2 || a.row_tiles > 65535) return fail(DS_ERR_UNSUPPORTED, "too many queries");
+    int64_t bytes[2];
+    for (int i = 0; i < 2; ++i) {
+        const int64_t *s = i ? o_strides : q_strides;
+        if (s[0] < 0 || s[1] < 0 || s[2] < 0) return fail(DS_ERR_INVALID_ARG, "strides must be >= 0");
+        bytes[i] = span(batch, tokens, heads * group, s, dim, 2);
+    }
+    const int64_t cb = pages * heads * page * dim / 2, sb = pages * heads * page * blocks4(dim), need = 4 * part_floats(a, batch, heads, dim);
+    if (need > 0 && !scratch) return fail(DS_ERR_NULL_POINTER, "scratch must not be NULL");
+    if (need > scratch_bytes) return fail(DS_ERR_BUFFER_TOO_SMALL, "scratch has %lld bytes, %lld are needed", (long long)scratch_bytes, (long long)need);
+    if (ds_status st = check_tensors({{q, bytes[0], "q", false}, {k_cache, cb, "k_cache", false}, {v_cache, cb, "v_cache", false},
+                                      {k_scales, sb, "k_scales", false}, {v_scales, sb, "v_scales", false},
+                                      {table, span(batch, ldt, columns, 4), "table", false}, {length, batch * 4, "length", false},
+                                      {count, batch * 4, "count", false}, {o, bytes[1], "o", true},
+                                      {need ? scratch : nullptr, need, "scratch", true}}))
+        return st;
+    // (The factor is above 0: a key that is not seen has -inf, which stays that.)
+    const AttentionParams p{q, k_cache, v_cache, k_scales, v_scales, table, length, count, o,
+                            need ? static_cast<float *>(scratch) : nullptr, ldt, q_strides[0], q_strides[1], q_strides[2],
+                            o_strides[0], o_strides[1], o_strides[2], int(columns), int(pages), int(tokens), int(heads),
+                            int(group), int(dim), page_shift(page), int(window), a.splits, int(a.rows), a.row_tiles,
+                            std::max(std::fabs(scale) * 1.44269504f, 0x1p-126f), scale < 0};
+    const auto s = static_cast<hipStream_t>(stream);
+    if (type == DS_TYPE_F16) run_attention4<_Float16>(p, a, batch, s);
+    else run_attention4<__bf16>(p, a, batch, s);
+    return launched("ds_attention_fp4");
+}

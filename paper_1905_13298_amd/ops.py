@@ -2,8 +2,8 @@
 
 PyTorch provides the device memory and the stream; every computation runs in
 the HIP library. Tensors must be contiguous int32 CUDA (ROCm) tensors; packed
-weights are int32 tensors holding the uint32 words bit for bit. The 8-bit
-operators (rms_norm .. attention_fp8) take floating-point tensors whose rows may
+weights are int32 tensors holding the uint32 words bit for bit. The 8-bit and 4-bit
+operators (rms_norm .. attention_fp4) take floating-point tensors whose rows may
 be strided: float32, float16 and bfloat16, float8_e4m3fn or float8_e5m2 with
 float8_e8m0fnu scales (powers of two).
 """
@@ -26,7 +26,9 @@ __all__ = ["DeepShiftError", "code_bits_flag", "describe_conv2d", "packed_row_wo
            "layer_plan", "run_layer_plan", "set_tuning", "get_tuning", "tuning", "DS_MUL_I24",
            "JitConvMul", "jit_conv_mul_image", "DS_ACT_I16", "DS_ACT_I8", "act_bits_flag",
            "rms_norm", "rms_norm_backward", "quantize_fp8", "quantize_weights_fp8", "shift_weights_to_fp8",
-           "linear_fp8", "linear_fp8_backward_data", "kv_cache", "kv_cache_append", "attention_fp8"]
+           "linear_fp8", "linear_fp8_backward_data", "kv_cache", "kv_cache_append", "attention_fp8",
+           "rotary_frequencies", "rotary_norm", "rotary_norm_backward", "kv_cache_fp4", "kv_cache_fp4_append",
+           "kv_cache_fp4_read", "attention_fp4"]
 
 DS_RELU = 1
 
@@ -781,7 +783,7 @@ class JitConvMul(JitConv):
 # ---------------------------------------------------------------------------
 # 8-bit operators of a decoder layer.
 
-_TYPE = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.float8_e4m3fn: 3, torch.float8_e5m2: 4}
+_TYPE = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.float8_e4m3fn: 3, torch.float8_e5m2: 4, torch.float64: 5}
 _FLOATS = (torch.bfloat16, torch.float16, torch.float32)
 _E4M3, _E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
 _functions = {}
@@ -1093,5 +1095,189 @@ def attention_fp8(q, k_cache, v_cache, k_scales, v_scales, table, length, count=
     scratch, size = _scratch8("ds_attention_fp8_scratch_bytes", shape, dev)
     _launch("ds_attention_fp8", dev, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(),
             table.data_ptr(), length.data_ptr(), _ptr(count), o.data_ptr(), *shape[:6], pages, shape[6], ldt, _vectors(q, "q"),
+            _vectors(o, "o"), 1 / math.sqrt(dim) if scale is None else scale, window, _TYPE[q.dtype], _ptr(scratch), size)
+    return o
+
+
+def rotary_frequencies(pairs: int, theta: float = 10000.0, device="cuda:0"):
+    """Frequencies [pairs] (float64, radians a position) for rotary_norm: theta^(-i / pairs)."""
+    if pairs <= 0 or not theta > 0:
+        raise ValueError("pairs and theta must be > 0")
+    return torch.pow(torch.tensor(float(theta), dtype=torch.float64), -torch.arange(pairs, dtype=torch.float64) / pairs).to(device)
+
+
+def _heads(t, name: str, dtypes, shape=None):
+    """A tensor [batch, tokens, heads, dim] of vectors whose elements are consecutive, and its strides."""
+    _dev_as(t, name, dtypes, shape)
+    if t.dim() != 4:
+        raise ValueError(f"{name} must be [batch, tokens, heads, dim]")
+    return _vectors(t, name)
+
+
+def _rotary(q, k, positions, frequencies, q_weight, k_weight, sections):
+    """What rotary_norm and its gradient pass alike: ((batch, .., axes) and sections, the positions' strides, the weights' type)."""
+    batch, tokens, heads, dim = q.shape
+    kv_heads = 0 if k is None else k.shape[2]
+    _dev_as(positions, "positions", _INT32)
+    axes = 1 if positions.dim() == 2 else positions.shape[0] if positions.dim() == 3 else 0
+    if not axes or positions.shape[-2:] != (batch, tokens):
+        raise ValueError(f"positions must be [{batch}, {tokens}] or [axes, {batch}, {tokens}], got {tuple(positions.shape)}")
+    if axes > 1 and (sections is None or len(sections) != axes):
+        raise ValueError(f"{axes} axes need as many sections")
+    if axes == 1 and sections is not None and tuple(sections) != (frequencies.shape[0],):
+        raise ValueError("one axis has all pairs")
+    _vector(frequencies, "frequencies", (torch.float32, torch.float64), frequencies.numel())
+    if sections is not None and any(not 0 <= n <= frequencies.numel() for n in sections):
+        raise ValueError("a section has from 0 to all pairs")
+    wtype = q.dtype
+    for weight, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if weight is not None:
+            _vector(weight, name, (q.dtype, torch.float32), dim)
+            wtype = weight.dtype
+    if q_weight is not None and k_weight is not None and q_weight.dtype != k_weight.dtype:
+        raise TypeError(f"q_weight is {q_weight.dtype}, k_weight {k_weight.dtype}")
+    if k is None and k_weight is not None:
+        raise ValueError("k_weight without k")
+    _same_device(q.device, k, positions, frequencies, q_weight, k_weight)
+    strides = positions.stride()
+    return ((batch, tokens, heads, kv_heads, dim, frequencies.numel(), axes),
+            None if axes == 1 else (ctypes.c_int32 * axes)(*sections), _Strides(strides[0] if axes > 1 else 0, *strides[-2:]), wtype)
+
+
+def rotary_norm(q, k, positions, frequencies, q_weight=None, k_weight=None, sections=None, interleaved: bool = False, eps: float = 1e-6):
+    """Query and key heads, normed and turned by their tokens' positions: (q', k') of q [batch, tokens, heads, dim] and
+    k [batch, tokens, kv heads, dim] (None: no keys), of their type.
+
+    With a weight [dim] (of q's type or float32) each vector x becomes x / sqrt(mean(x^2) + eps) * weight, without one it stays; then
+    its pair i is turned by positions * frequencies[i] (rotary_frequencies; float32 or float64 radians a position, up to dim / 2 of them):
+    elements i and i + pairs, or 2 i and 2 i + 1 with `interleaved`. Elements past the pairs are not turned. positions: int32
+    [batch, tokens], or [axes, batch, tokens] with `sections`, the number of pairs that go by each axis, in order. dim: even, up to 256."""
+    sq = _heads(q, "q", _FLOATS)
+    sk = None if k is None else _heads(k, "k", (q.dtype,), (*q.shape[:2], k.shape[2] if k.dim() == 4 else 0, q.shape[3]))
+    shape, sections, sp, wtype = _rotary(q, k, positions, frequencies, q_weight, k_weight, sections)
+    dev = q.device
+    qo = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    ko = None if k is None else torch.empty(k.shape, dtype=q.dtype, device=dev)
+    _launch("ds_rotary_norm", dev, q.data_ptr(), _ptr(k), positions.data_ptr(), frequencies.data_ptr(), _ptr(q_weight), _ptr(k_weight),
+            qo.data_ptr(), _ptr(ko), *shape, sections, sq, sk, sp, _vectors(qo, "q"), None if k is None else _vectors(ko, "k"), interleaved, eps,
+            _TYPE[q.dtype], _TYPE[wtype], _TYPE[frequencies.dtype])
+    return qo, ko
+
+
+def rotary_norm_backward(dq_out, dk_out, q, k, positions, frequencies, q_weight=None, k_weight=None, sections=None,
+                         interleaved: bool = False, eps: float = 1e-6):
+    """Gradients (dq, dk, dq_weight, dk_weight) of rotary_norm from those of its results and the call's arguments (None for what
+    the call had not). q and k themselves matter where they have a weight."""
+    sdq = _heads(dq_out, "dq_out", _FLOATS)
+    sq = _heads(q, "q", (dq_out.dtype,), dq_out.shape)
+    if (k is None) != (dk_out is None):
+        raise ValueError("k and dk_out belong together")
+    sdk = sk = None
+    if k is not None:
+        sk = _heads(k, "k", (q.dtype,), (*q.shape[:2], k.shape[2] if k.dim() == 4 else 0, q.shape[3]))
+        sdk = _heads(dk_out, "dk_out", (q.dtype,), k.shape)
+    shape, sections, sp, wtype = _rotary(q, k, positions, frequencies, q_weight, k_weight, sections)
+    dev = q.device
+    _same_device(dev, dq_out, dk_out)
+    dq = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    dk = None if k is None else torch.empty(k.shape, dtype=q.dtype, device=dev)
+    dqw = None if q_weight is None else torch.empty_like(q_weight)
+    dkw = None if k_weight is None else torch.empty_like(k_weight)
+    scratch, size = (None, 0) if dqw is None and dkw is None else _scratch8("ds_rotary_norm_backward_scratch_bytes", (shape[0], shape[1], shape[4]), dev)
+    _launch("ds_rotary_norm_backward", dev, dq_out.data_ptr(), _ptr(dk_out), q.data_ptr(), _ptr(k), positions.data_ptr(), frequencies.data_ptr(),
+            _ptr(q_weight), _ptr(k_weight), dq.data_ptr(), _ptr(dk), _ptr(dqw), _ptr(dkw), *shape, sections, sdq, sdk, sq, sk, sp, _vectors(dq, "dq"),
+            None if k is None else _vectors(dk, "dk"), interleaved, eps, _TYPE[q.dtype], _TYPE[wtype], _TYPE[frequencies.dtype],
+            _ptr(scratch), size)
+    return dq, dk, dqw, dkw
+
+
+def kv_cache_fp4(pages: int, heads: int, page: int, dim: int, device="cuda:0"):
+    """An empty paged 4-bit cache, two numbers a byte (uint8): (k_cache [pages, heads, page, dim / 2],
+    v_cache [pages, heads, page / 4, dim / 8, 4, 4], k_scales and v_scales [pages, heads, ceil(dim / 32), page] (float8_e8m0fnu))."""
+    if page not in (16, 32, 64, 128) or dim <= 0 or dim % 16 or dim > 256 or pages <= 0 or heads <= 0:
+        raise ValueError("page must be 16, 32, 64 or 128, dim a multiple of 16 up to 256, pages and heads > 0")
+    new = lambda *s: torch.zeros(s, dtype=torch.uint8, device=device)  # noqa: E731
+    scales = lambda: new(pages, heads, (dim + 31) // 32, page).view(_E8M0)  # noqa: E731
+    return new(pages, heads, page, dim // 2), new(pages, heads, page // 4, dim // 8, 4, 4), scales(), scales()
+
+
+def _check_cache_fp4(k_cache, v_cache, k_scales, v_scales, table, batch: int):
+    """(pages, heads, page, dim) of a 4-bit cache and the row stride of its table."""
+    _dev_as(k_cache, "k_cache", (torch.uint8,))
+    if k_cache.dim() != 4:
+        raise ValueError("k_cache must be [pages, heads, page, dim / 2]")
+    pages, heads, page, half = k_cache.shape
+    _dev_as(v_cache, "v_cache", (torch.uint8,), (pages, heads, page // 4, half // 4, 4, 4))
+    scales = (pages, heads, (half + 15) // 16, page)
+    _dev_as(k_scales, "k_scales", (_E8M0,), scales)
+    _dev_as(v_scales, "v_scales", (_E8M0,), scales)
+    if not (k_cache.is_contiguous() and v_cache.is_contiguous() and k_scales.is_contiguous() and v_scales.is_contiguous()):
+        raise ValueError("a cache and its scales must be contiguous")
+    ldt = _rows(table, "table", _INT32)
+    if table.shape[0] != batch:
+        raise ValueError(f"table has {table.shape[0]} rows for {batch} sequences")
+    return pages, heads, page, 2 * half, ldt
+
+
+def kv_cache_fp4_append(k, v, k_cache, v_cache, k_scales, v_scales, table, start, count=None):
+    """kv_cache_append into a 4-bit cache (kv_cache_fp4), in place. A token's 32 elements of a head share a scale, the least power of
+    two within 2^-23 .. 2^13 that brings them to at most 6 (NaN, for all of them, where one is infinite or NaN), so that what the cache
+    holds of other tokens stays as it is."""
+    sk = _heads(k, "k", _FLOATS)
+    sv = _heads(v, "v", (k.dtype,), k.shape)
+    batch, tokens = k.shape[:2]
+    pages, heads, page, dim, ldt = _check_cache_fp4(k_cache, v_cache, k_scales, v_scales, table, batch)
+    if k.shape[2] != heads or k.shape[3] != dim:
+        raise ValueError(f"k has heads and dim {tuple(k.shape[2:])}, the cache {(heads, dim)}")
+    _vector(start, "start", _INT32, batch)
+    if count is not None:
+        _vector(count, "count", _INT32, batch)
+    dev = k.device
+    _same_device(dev, v, k_cache, v_cache, k_scales, v_scales, table, start, count)
+    _launch("ds_kv_cache_fp4_append", dev, k.data_ptr(), v.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), k_scales.data_ptr(),
+            v_scales.data_ptr(), table.data_ptr(), start.data_ptr(), _ptr(count), batch, tokens, heads, dim, page, pages,
+            table.shape[1], ldt, sk, sv, _TYPE[k.dtype])
+
+
+def kv_cache_fp4_read(k_cache, v_cache, k_scales, v_scales, table, start, tokens: int, count=None, dtype=torch.bfloat16):
+    """(k, v) [batch, tokens, heads, dim] of a 4-bit cache, exactly, in `dtype`: tokens 0 .. count[b] - 1 (all without count)
+    are positions start[b], start[b] + 1, .. of sequence b, the others 0, as are those past the table, of a page outside the
+    cache, or of a sequence whose start is negative."""
+    batch = _dev_as(start, "start", _INT32).numel()
+    pages, heads, page, dim, ldt = _check_cache_fp4(k_cache, v_cache, k_scales, v_scales, table, batch)
+    _vector(start, "start", _INT32, batch)
+    if count is not None:
+        _vector(count, "count", _INT32, batch)
+    if dtype not in _FLOATS:
+        raise TypeError("dtype must be float32, float16 or bfloat16")
+    if tokens < 0:
+        raise ValueError("tokens must be >= 0")
+    dev = k_cache.device
+    _same_device(dev, v_cache, k_scales, v_scales, table, start, count)
+    k, v = (torch.empty((batch, tokens, heads, dim), dtype=dtype, device=dev) for _ in range(2))
+    _launch("ds_kv_cache_fp4_read", dev, k_cache.data_ptr(), v_cache.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), table.data_ptr(),
+            start.data_ptr(), _ptr(count), k.data_ptr(), v.data_ptr(), batch, tokens, heads, dim, page, pages, table.shape[1], ldt,
+            _vectors(k, "k"), _vectors(v, "v"), _TYPE[dtype])
+    return k, v
+
+
+def attention_fp4(q, k_cache, v_cache, k_scales, v_scales, table, length, count=None, scale: float | None = None, window: int = 0):
+    """attention_fp8 over a 4-bit cache (kv_cache_fp4)."""
+    _dev_as(q, "q", (torch.bfloat16, torch.float16))
+    sq = _heads(q, "q", (q.dtype,))
+    batch, tokens, hq, qdim = q.shape
+    pages, heads, page, dim, ldt = _check_cache_fp4(k_cache, v_cache, k_scales, v_scales, table, batch)
+    if qdim != dim or hq % heads:
+        raise ValueError(f"q has {hq} heads of {qdim}, the cache {heads} of {dim}")
+    _vector(length, "length", _INT32, batch)
+    if count is not None:
+        _vector(count, "count", _INT32, batch)
+    dev = q.device
+    _same_device(dev, k_cache, v_cache, k_scales, v_scales, table, length, count)
+    o = torch.empty((batch, tokens, hq, dim), dtype=q.dtype, device=dev)
+    shape = (batch, tokens, heads, hq // heads, dim, page, table.shape[1])
+    scratch, size = _scratch8("ds_attention_fp4_scratch_bytes", shape, dev)
+    _launch("ds_attention_fp4", dev, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(),
+            table.data_ptr(), length.data_ptr(), _ptr(count), o.data_ptr(), *shape[:6], pages, shape[6], ldt, sq,
             _vectors(o, "o"), 1 / math.sqrt(dim) if scale is None else scale, window, _TYPE[q.dtype], _ptr(scratch), size)
     return o

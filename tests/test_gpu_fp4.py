@@ -1,0 +1,541 @@
+"""The 4-bit cache and its attention on the GPU against their definitions in 64 bits.
+
+The append and the read are exact: codes, scales and floats are compared bit for bit (a zero's sign apart).
+The attention's tolerance counts half a unit in the last place of an output (bfloat16 2^-8, float16 2^-11,
+relative) and what its terms may be off by: see `attention_reference`.
+"""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+E8M0 = torch.float8_e8m0fnu
+HALF_ULP = {BF16: 2.0 ** -8, F16: 2.0 ** -11, F32: 2.0 ** -24}
+TINY = {BF16: 2.0 ** -133, F16: 2.0 ** -25, F32: 2.0 ** -149}
+SIZES = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], dtype=torch.float64)
+LOW, HIGH, NAN = 104, 140, 255
+
+
+@pytest.fixture(scope="module")
+def ops():
+    from paper_1905_13298_amd import ops as o
+    return o
+
+
+def normal(seed, *shape, std=1.0):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed)) * std
+
+
+def near(got, want, terms=0.0):
+    """got within its type's rounding of `want` and of what the terms are off by."""
+    t = got.dtype
+    assert torch.isfinite(got).all()
+    off = (got.cpu().double() - want).abs()
+    tol = want.abs() * HALF_ULP[t] * 1.01 + TINY[t] + terms * (1 + HALF_ULP[t])
+    assert torch.all(off <= tol), float((off / tol.clamp(min=1e-300)).max())
+
+
+def to4(x):
+    """(codes [.., dim], scale bytes [.., blocks]) of x by the definition, in 64 bits."""
+    dim = x.shape[-1]
+    y = torch.nn.functional.pad(x.double(), (0, -dim % 32)).reshape(*x.shape[:-1], -1, 32)
+    fine = torch.isfinite(y).all(-1)
+    top = torch.where(fine[..., None], y, 0.0).abs().amax(-1)
+    e = torch.full_like(top, HIGH)
+    for byte in range(HIGH - 1, LOW - 1, -1):
+        e = torch.where(top <= 6 * 2.0 ** (byte - 127), byte, e)
+    y = (torch.where(fine[..., None], y, 0.0) / torch.exp2(e - 127)[..., None]).clamp(-6, 6)       # (1e30 is as far from 6 as from 0 in 64 bits)
+    away = (y.abs()[..., None] - SIZES).abs()
+    least = away.amin(-1, keepdim=True)
+    tied = away == least
+    code = torch.where(tied[..., 0::2].any(-1), tied[..., 0::2].int().argmax(-1) * 2, tied.int().argmax(-1))     # even at a tie
+    code = code | (torch.signbit(y) & fine[..., None]).int() * 8
+    return code.reshape(*x.shape[:-1], -1)[..., :dim], torch.where(fine, e, NAN).long()
+
+
+def tokens_of(cache):
+    """(codes [pages, heads, page, dim], scale bytes [pages, heads, page, blocks]) of a cache's keys, and values."""
+    out = []
+    for codes, scales in ((cache[0], cache[2]), (cache[1], cache[3])):
+        b = codes.cpu()
+        if b.dim() == 6:
+            b = b.permute(0, 1, 2, 4, 3, 5).reshape(*b.shape[:2], b.shape[2] * 4, -1)
+        out.append((torch.stack([b & 15, b >> 4], -1).flatten(-2).long(), scales.cpu().view(torch.uint8).transpose(2, 3).long()))
+    return out
+
+
+def numbers(code, e):
+    v = SIZES[code & 7] * torch.where(code > 7, -1.0, 1.0)
+    power = torch.where(e == NAN, math.nan, torch.exp2((e - 127).double()))
+    return v * power.repeat_interleave(32, -1)[..., :code.shape[-1]]
+
+
+def filled_cache(ops, pages, heads, page, dim, seed=0):
+    cache = ops.kv_cache_fp4(pages, heads, page, dim, DEV)
+    table = torch.arange(pages, dtype=torch.int32, device=DEV)[:, None]
+    k = normal(seed, pages, page, heads, dim) * torch.exp2(normal(seed + 1, pages, page, 1, 1))
+    v = normal(seed + 2, pages, page, heads, dim) * torch.exp2(normal(seed + 3, pages, page, 1, 1))
+    ops.kv_cache_fp4_append(k.to(DEV), v.to(DEV), *cache, table, torch.zeros(pages, dtype=torch.int32, device=DEV))
+    return cache
+
+
+def append_reference(held, new, table, start, count, page):
+    """One cache's codes and scales after the append, a token at a time."""
+    code, e = held[0].clone(), held[1].clone()
+    batch, tokens = new.shape[:2]
+    c, s = to4(new)
+    for b in range(batch):
+        for t in range(min(int(count[b]), tokens) if start[b] >= 0 else 0):
+            col, slot = divmod(int(start[b]) + t, page)
+            if col < table.shape[1] and 0 <= int(table[b, col]) < code.shape[0]:
+                code[int(table[b, col]), :, slot] = c[b, t]
+                e[int(table[b, col]), :, slot] = s[b, t]
+    return code, e
+
+
+def same_numbers(a, b):
+    """The same codes (+0 is -0) and scales."""
+    (ca, ea), (cb, eb) = a, b
+    return torch.equal(ca, cb) and torch.equal(ea, eb)
+
+
+# ---------------------------------------------------------------------------
+# Append and read.
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+@pytest.mark.parametrize("dim,heads", [(16, 1), (32, 2), (64, 3), (80, 2), (128, 2), (256, 1)])
+@pytest.mark.parametrize("tokens", [1, 5, 70, 150])
+def test_append_and_read(ops, page, dim, heads, tokens):
+    batch, columns = 5, (400 + page - 1) // page
+    gen = torch.Generator().manual_seed(page + dim + tokens)
+    pages = batch * columns + 2
+    cache = filled_cache(ops, pages, heads, page, dim)
+    table = torch.randperm(pages, generator=gen)[:batch * columns].reshape(batch, columns).to(torch.int32)
+    start = torch.tensor([0, 1, page - 1, page, 211], dtype=torch.int32)
+    count = torch.tensor([tokens, tokens, max(tokens - 1, 1), 0, tokens], dtype=torch.int32)
+    dtype = (BF16, F16, F32)[(dim + tokens) % 3]
+    big = (normal(5, 2, batch, tokens, heads, dim + 3) * torch.exp2(normal(6, 2, batch, tokens, 1, 1) * 3)).to(dtype)
+    k, v = (big[i, ..., i:i + dim] for i in range(2))
+    before = tokens_of(cache)
+    want = [append_reference(before[i], (k, v)[i], table, start, count, page) for i in range(2)]
+    d = big.to(DEV)
+    ops.kv_cache_fp4_append(d[0, ..., 0:dim], d[1, ..., 1:1 + dim], *cache, table.to(DEV), start.to(DEV), count.to(DEV))
+    for got, w in zip(tokens_of(cache), want):
+        assert same_numbers(got, w)
+    # Back: the same tokens, and some before and behind them, in each type, through a table with wider rows.
+    wide = torch.full((batch, columns + 4), -1, dtype=torch.int32)
+    wide[:, 1:1 + columns] = table
+    first = (start - 3).clamp(min=0)
+    for out in (BF16, F16, F32):
+        got = ops.kv_cache_fp4_read(*cache, wide.to(DEV)[:, 1:1 + columns], first.to(DEV), tokens + 5, (count + 4).to(DEV), dtype=out)
+        for g, w in zip(got, want):
+            held = numbers(*w)
+            assert g.dtype == out and g.shape == (batch, tokens + 5, heads, dim)
+            for b in range(batch):
+                for t in range(tokens + 5):
+                    at = int(first[b]) + t
+                    there = t < min(int(count[b]) + 4, tokens + 5) and at // page < columns
+                    x = held[int(table[b, at // page]), :, at % page] if there else torch.zeros(heads, dim, dtype=torch.float64)
+                    assert torch.equal(g[b, t].cpu().double(), x)
+
+
+def test_append_boundaries(ops):
+    """Every tie and its neighbours, at both ends of the scales and between, and blocks' largest elements around a scale's limit."""
+    page, dim = 16, 64
+    ties = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0])
+    base = torch.cat([ties, torch.nextafter(ties, ties * 0), torch.nextafter(ties, ties * 9)])
+    rows = []
+    for e in (-23, -7, 0, 13):
+        x = torch.zeros(dim)
+        x[:21], x[21], x[32:53], x[53] = base, 6.0, -base, 4.5
+        rows.append(x * 2.0 ** e)
+    for top in (6.0, 6.0000005, 5.9999995, 3.0, 3.0000002, 12 * 2.0 ** 11, 6.1 * 2.0 ** 13, 1e30, 6 * 2.0 ** -24, 2.0 ** -25, 2.1 * 2.0 ** -25, 1e-30, 1e-40, 0.0):
+        x = torch.zeros(dim)
+        x[3], x[40] = top, -top
+        rows.append(x)
+    x = torch.stack(rows)[None, :, None]
+    n = x.shape[1]
+    cache = ops.kv_cache_fp4(2, 1, page, dim, DEV)
+    table, zero = torch.arange(2, dtype=torch.int32, device=DEV)[None], torch.zeros(1, dtype=torch.int32, device=DEV)
+    ops.kv_cache_fp4_append(x.to(DEV), x.flip(-1).to(DEV), *cache, table, zero)
+    for (code, e), y in zip(tokens_of(cache), (x, x.flip(-1))):
+        want = to4(y[0, :, 0])
+        assert same_numbers((code.reshape(32, dim)[:n], e.reshape(32, 2)[:n]), want)
+    k, _ = ops.kv_cache_fp4_read(*cache, table, zero, n, dtype=F32)
+    assert k[0, 11, 0, 3] == 49152 and k[0, 10, 0, 3] == 49152
+
+
+def test_append_drops_what_has_no_page_and_marks_what_is_no_number(ops):
+    page, dim, heads = 16, 80, 2
+    cache = filled_cache(ops, 4, heads, page, dim)
+    table = torch.tensor([[-1, 3], [7, 0], [2, 1]], dtype=torch.int32)     # columns without a page, and past the table
+    k = normal(1, 3, 40, heads, dim)
+    k[0, 20, 0, 70], k[0, 21, 1, 1], k[0, 22, 0, 32] = float("inf"), float("nan"), -float("inf")
+    start, count = torch.tensor([0, 0, -1], dtype=torch.int32), torch.full((3,), 40, dtype=torch.int32)
+    before = tokens_of(cache)
+    want = [append_reference(before[i], k, table, start, count, page) for i in range(2)]
+    ops.kv_cache_fp4_append(k.to(DEV), k.to(DEV), *cache, table.to(DEV), start.to(DEV))
+    after = tokens_of(cache)
+    for i in range(2):
+        assert same_numbers(after[i], want[i])
+        for p in (1, 2):
+            assert torch.equal(after[i][0][p], before[i][0][p]) and torch.equal(after[i][1][p], before[i][1][p])
+    assert after[0][1][3, 0, 4].tolist()[2] == NAN and after[0][1][3, 0, 4].tolist()[:2] != [NAN, NAN]
+    got, _ = ops.kv_cache_fp4_read(*cache, table.to(DEV), start.to(DEV), 40)
+    nan = torch.isnan(got).cpu()
+    assert nan[0, 20, 0].tolist() == [False] * 64 + [True] * 16 and nan[0, 21, 1].tolist() == [True] * 32 + [False] * 48
+    assert nan[0, 22, 0].tolist() == [False] * 32 + [True] * 32 + [False] * 16 and int(nan.sum()) == 16 + 32 + 32
+    assert torch.all(got[2] == 0) and torch.all(got[0, :16] == 0) and torch.all(got[1, :16] == 0) and torch.all(got[:, 32:] == 0)
+
+
+# ---------------------------------------------------------------------------
+# Attention.
+
+
+def attention_reference(q, cache, table, length, count, window, scale):
+    """(o, what it may be off by) in 64 bits, a query head at a time."""
+    (kc, ke), (vc, ve) = tokens_of(cache)
+    kv, vv = numbers(kc, ke), numbers(vc, ve)
+    pages, heads, page, dim = kv.shape
+    batch, tokens, hq, _ = q.shape
+    group = hq // heads
+    o, off = torch.zeros(batch, tokens, hq, dim, dtype=torch.float64), torch.zeros(batch, tokens, hq, dim, dtype=torch.float64)
+    for b in range(batch):
+        length_b = max(int(length[b]), 0)
+        c = min(max(int(count[b]), 0), tokens)
+        n = min(length_b, table.shape[1] * page)
+        if c == 0 or n == 0:
+            continue
+        pid = table[b, :(n + page - 1) // page].long()
+        good = ((pid >= 0) & (pid < pages)).repeat_interleave(page)[:n]
+        pid = torch.where((pid >= 0) & (pid < pages), pid, 0)
+        pos = torch.arange(length_b - c, length_b)[:, None]
+        j = torch.arange(n)[None, :]
+        seen = (j <= pos) & good[None, :]
+        if window:
+            seen &= j > pos - window
+        some = seen.any(1, keepdim=True)
+        any_seen = seen.any(0)[:, None]
+        for h in range(heads):
+            k, v = (torch.where(any_seen, a[pid, h].reshape(-1, dim)[:n], 0.0) for a in (kv, vv))
+            for g in range(group):
+                x = q[b, :c, h * group + g].double()
+                s = torch.where(seen, scale * (x @ k.T), -math.inf)
+                top = torch.where(some, s.amax(1, keepdim=True), 0.0)
+                p = torch.exp(s - top)
+                total = p.sum(1, keepdim=True).clamp(min=1e-300)
+                o[b, :c, h * group + g] = torch.where(some, p @ v / total, 0.0)
+                # Weights off by 2^-11 (16-bit floats) and by the scores' own errors, twice (sum and weights): 2^-23 a term of a
+                # score and 2^-22 of itself; the sums by 2^-23 for each 16 keys and some more; and a weight is cut at half the
+                # least 16-bit float, 2^-25 where the largest weight is at least 2^9, for each key.
+                ds = ((dim + 4) * 2.0 ** -23 * abs(scale) * (x.abs() @ k.abs().T) + s.abs().nan_to_num(posinf=0) * 2.0 ** -22).nan_to_num()
+                rel = 2.0 ** -11 + 2 * (ds * seen).amax(1, keepdim=True) + (8 + n / 16) * 2.0 ** -23
+                cut = n * 2.0 ** -34 * float(v.abs().max())
+                off[b, :c, h * group + g] = torch.where(some, rel * (p @ v.abs()) / total + cut / total, 0.0)
+    return o, off
+
+
+def attention_case(ops, dim, page, heads, group, tokens, lengths, window=0, dtype=BF16, count=None, seed=0, holes=False, scale=None, short=0):
+    batch, longest = len(lengths), max(max(lengths), 1)
+    columns = max(1, (longest + page - 1) // page + 1 - short)
+    pages = batch * columns + 3
+    cache = filled_cache(ops, pages, heads, page, dim, seed)
+    gen = torch.Generator().manual_seed(seed + 1)
+    table = torch.randperm(pages, generator=gen)[:batch * columns].reshape(batch, columns).to(torch.int32)
+    if holes:
+        table[:, 1::3] = -1
+        table[0, 0] = pages + 5
+    length = torch.tensor(lengths, dtype=torch.int32)
+    n = torch.full((batch,), tokens, dtype=torch.int32) if count is None else torch.tensor(count, dtype=torch.int32)
+    q = normal(seed + 2, batch, tokens, heads * group, dim).to(dtype)
+    o = ops.attention_fp4(q.to(DEV), *cache, table.to(DEV), length.to(DEV), None if count is None else n.to(DEV), window=window, scale=scale)
+    want, off = attention_reference(q, cache, table, length, n, window, 1 / math.sqrt(dim) if scale is None else scale)
+    near(o, want, off)
+    return o
+
+
+@pytest.mark.parametrize("dim", [16, 48, 64, 80, 128, 144, 256])
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_attention_one_token(ops, dim, page, dtype):
+    attention_case(ops, dim, page, 2, 4, 1, [0, 1, 15, 16, 17, 63, 64, 65, 130, 700], dtype=dtype, seed=dim)
+
+
+@pytest.mark.parametrize("heads,group", [(1, 1), (1, 7), (2, 8), (1, 16), (1, 17), (3, 5), (1, 40)])
+@pytest.mark.parametrize("tokens", [1, 2, 9])
+def test_attention_heads_and_tokens(ops, heads, group, tokens):
+    attention_case(ops, 64, 32, heads, group, tokens, [tokens, 100, 333], seed=heads * group)
+
+
+@pytest.mark.parametrize("dim", [48, 64, 80, 128, 208, 256])
+@pytest.mark.parametrize("tokens,lengths", [(130, [130, 300, 131]), (65, [65, 64, 800]), (257, [257]), (20, [20, 777])])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_attention_many_tokens(ops, dim, tokens, lengths, dtype):
+    attention_case(ops, dim, 64 if dim % 32 else 16, 1, 2, tokens, lengths, count=[min(tokens, n) for n in lengths], seed=tokens, dtype=dtype)
+
+
+@pytest.mark.parametrize("window", [1, 16, 63, 64, 100])
+@pytest.mark.parametrize("tokens", [1, 3, 40])
+def test_attention_window(ops, window, tokens):
+    attention_case(ops, 64, 16, 2, 2, tokens, [tokens, 90, 500], window=window, seed=window)
+
+
+@pytest.mark.parametrize("tokens", [2, 30])
+def test_attention_more_queries_than_tokens_and_longer_than_the_table(ops, tokens):
+    """Queries before a sequence's first token see nothing; tokens past the table count for positions and are not seen."""
+    attention_case(ops, 64, 16, 1, 2, tokens, [0, 1, tokens - 1, 200], seed=4)
+    attention_case(ops, 128, 32, 1, 2, tokens, [100, 300, 40], seed=6, short=3)
+    attention_case(ops, 128, 32, 1, 2, tokens, [100, 300, 40], seed=6, short=3, window=50)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.2, 1.5])
+@pytest.mark.parametrize("tokens", [1, 20])
+def test_attention_scales_of_the_softmax(ops, scale, tokens):
+    attention_case(ops, 64, 32, 1, 3, tokens, [100, 333], seed=9, scale=scale)
+
+
+def test_attention_ragged_counts_and_empty_rows(ops):
+    for tokens in (6, 40):
+        o = attention_case(ops, 64, 32, 2, 3, tokens, [0, 3, 200, 6, 50], count=[0, 3, 1, 0, 6], seed=5)
+        assert torch.all(o[0] == 0) and torch.all(o[1, 3:] == 0) and torch.all(o[2, 1:] == 0) and torch.all(o[3] == 0)
+
+
+@pytest.mark.parametrize("tokens", [1, 20])
+def test_attention_pages_outside_the_cache_are_not_seen(ops, tokens):
+    attention_case(ops, 64, 32, 1, 4, tokens, [20, 100, 400], holes=True, seed=8)
+
+
+@pytest.mark.parametrize("lengths", [[20000], [9000, 17, 12345]])
+@pytest.mark.parametrize("tokens", [1, 7])
+def test_attention_long_axis(ops, lengths, tokens):
+    """Long enough that the keys are split and joined."""
+    attention_case(ops, 128, 64, 1, 4, tokens, lengths, seed=3)
+
+
+@pytest.mark.parametrize("tokens", [1, 30])
+def test_attention_ends_of_the_scales(ops, tokens):
+    """Keys and values of the least and the largest numbers that a cache holds."""
+    dim, page, n = 64, 16, 90
+    cache = ops.kv_cache_fp4(6, 1, page, dim, DEV)
+    e = torch.tensor([-24.0, 15.0, -20.0, 3.0])[torch.arange(n) % 4]
+    k, v = normal(1, 1, n, 1, dim) * torch.exp2(e.flip(0) - 4)[None, :, None, None], normal(2, 1, n, 1, dim) * torch.exp2(e)[None, :, None, None]
+    v[:, 60:] = normal(3, 1, 30, 1, dim) * 2.0 ** -23
+    table, zero = torch.arange(6, dtype=torch.int32)[None], torch.zeros(1, dtype=torch.int32, device=DEV)
+    ops.kv_cache_fp4_append(k.to(DEV), v.to(DEV), *cache, table.to(DEV), zero)
+    for dtype, window in ((BF16, 0), (F16, 0), (F16, 20)):
+        q = (normal(4, 1, tokens, 2, dim) * 2.0 ** -8).to(dtype)
+        length = torch.tensor([n], dtype=torch.int32)
+        o = ops.attention_fp4(q.to(DEV), *cache, table.to(DEV), length.to(DEV), window=window)
+        # Row by row, since a row's largest value sets what is cut.
+        for t in range(0, tokens, 7):
+            at = torch.tensor([n - tokens + t + 1], dtype=torch.int32)
+            want, off = attention_reference(q[:, t:t + 1], cache, table, at, torch.ones(1), window, 1 / 8)
+            near(o[:, t:t + 1], want, off)
+
+
+def test_attention_weights_far_below_the_largest(ops):
+    """One key with a large weight, very many with small ones that add up to as much."""
+    dim, page, n = 64, 128, 8192
+    cache = ops.kv_cache_fp4(n // page, 1, page, dim, DEV)
+    k, v = torch.zeros(1, n, 1, dim), torch.full((1, n, 1, dim), -1.0)
+    k[0, 100, 0, 0] = 64.0                                           # weight e^8 times 2^.. the others'
+    v[0, 100] = 1.0
+    table = torch.arange(n // page, dtype=torch.int32)[None]
+    ops.kv_cache_fp4_append(k.to(DEV), v.to(DEV), *cache, table.to(DEV), torch.zeros(1, dtype=torch.int32, device=DEV))
+    length = torch.tensor([n], dtype=torch.int32)
+    for tokens, by in ((1, 1.0), (1, 1.125), (40, 1.125)):
+        q = torch.zeros(1, tokens, 1, dim, dtype=F16)
+        q[..., 0] = by
+        o = ops.attention_fp4(q.to(DEV), *cache, table.to(DEV), length.to(DEV))
+        want, off = attention_reference(q, cache, table, length, torch.full((1,), tokens), 0, 1 / 8)
+        near(o, want, off)
+
+
+def hide(cache, page_of, slots, page):
+    """NaN scales and arbitrary codes for the tokens `slots` of the sequence whose pages start at page_of."""
+    for slot in slots:
+        p, at = page_of + slot // page, slot % page
+        cache[0][p, :, at] = 0xA7
+        cache[1][p, :, at // 4, :, at % 4] = 0x7A
+        cache[2].view(torch.uint8)[p, :, :, at] = NAN
+        cache[3].view(torch.uint8)[p, :, :, at] = NAN
+
+
+@pytest.mark.parametrize("tokens", [1, 3, 40])
+@pytest.mark.parametrize("dim", [64, 80, 256])
+def test_attention_ignores_what_no_query_sees(ops, tokens, dim):
+    """NaN past a sequence's last token, and in keys and values that a window hides from every query."""
+    page = 32
+    cache = filled_cache(ops, 8, 2, page, dim)
+    table = torch.arange(8, dtype=torch.int32).reshape(2, 4)
+    length = torch.tensor([57, 90], dtype=torch.int32)
+    q = normal(2, 2, tokens, 4, dim).to(BF16)
+    args = (table.to(DEV), length.to(DEV))
+    whole, windowed = ops.attention_fp4(q.to(DEV), *cache, *args), ops.attention_fp4(q.to(DEV), *cache, *args, window=9)
+    for b, n in enumerate((57, 90)):
+        hide(cache, b * 4, range(n, 128), page)
+    assert torch.equal(ops.attention_fp4(q.to(DEV), *cache, *args), whole)
+    for b, n in enumerate((57, 90)):
+        hide(cache, b * 4, range(0, n - tokens - 8), page)
+    assert torch.equal(ops.attention_fp4(q.to(DEV), *cache, *args, window=9), windowed)
+
+
+@pytest.mark.parametrize("tokens,group", [(1, 4), (5, 3), (40, 1), (130, 2)])
+@pytest.mark.parametrize("dim", [48, 128, 256])
+def test_attention_nan_reaches_the_queries_that_see_it(ops, tokens, group, dim):
+    page, n = 32, 300
+    cache = filled_cache(ops, 10, 1, page, dim)
+    table, length = torch.arange(10, dtype=torch.int32, device=DEV)[None], torch.tensor([n], dtype=torch.int32, device=DEV)
+    q = normal(2, 1, tokens, group, dim).to(BF16).to(DEV)
+    for window in (0, 30):
+        clean = ops.attention_fp4(q, *cache, table, length, window=window)
+        for which, at in ((3, n - 2), (3, n - tokens), (2, n - 2), (3, n - tokens - 20), (2, n - tokens - 20)):
+            scales = cache[which].view(torch.uint8)
+            block = 1
+            keep = int(scales[at // page, 0, block, at % page])
+            scales[at // page, 0, block, at % page] = NAN
+            got = ops.attention_fp4(q, *cache, table, length, window=window)
+            scales[at // page, 0, block, at % page] = keep
+            pos = torch.arange(n - tokens, n)
+            sees = (pos >= at) & ((pos - window < at) if window else (pos >= 0))
+            for t in range(tokens):
+                nan = torch.isnan(got[0, t]).cpu()
+                if not sees[t]:
+                    assert torch.equal(got[0, t], clean[0, t])
+                elif which == 2:
+                    assert nan.all()
+                else:
+                    assert nan[:, 32:64].all() and torch.equal(got[0, t, :, :32], clean[0, t, :, :32]) and torch.equal(got[0, t, :, 64:], clean[0, t, :, 64:])
+
+
+@pytest.mark.parametrize("tokens", [1, 20])
+def test_attention_infinite_and_nan_queries(ops, tokens):
+    dim = 64
+    cache = filled_cache(ops, 4, 1, 32, dim)
+    table, length = torch.arange(4, dtype=torch.int32)[None].to(DEV), torch.tensor([100], dtype=torch.int32, device=DEV)
+    q = normal(2, 1, tokens, 4, dim).to(BF16)
+    want = ops.attention_fp4(q.to(DEV), *cache, table, length)
+    q[0, tokens // 2, 2, 5] = float("nan")
+    q[0, tokens // 2, 1, 7] = float("inf")
+    got = ops.attention_fp4(q.to(DEV), *cache, table, length)
+    keep = torch.ones(tokens, 4, dtype=torch.bool)
+    keep[tokens // 2, 1:3] = False
+    assert torch.isnan(got[0, tokens // 2, 2]).all()
+    assert torch.equal(got[0].cpu()[keep], want[0].cpu()[keep])
+
+
+@pytest.mark.parametrize("tokens", [5, 40])
+def test_attention_strides(ops, tokens):
+    dim, heads, group = 80, 2, 3
+    cache = filled_cache(ops, 8, heads, 32, dim)
+    table = torch.arange(8, dtype=torch.int32).reshape(2, 4)
+    wide = torch.full((2, 9), -1, dtype=torch.int32)
+    wide[:, 2:6] = table
+    length = torch.tensor([128, 77], dtype=torch.int32, device=DEV)
+    q = normal(2, tokens, 2, heads * group, dim + 7).to(F16).to(DEV)
+    view = q.transpose(0, 1)[..., 3:3 + dim]
+    got = ops.attention_fp4(view, *cache, wide.to(DEV)[:, 2:6], length)
+    assert torch.equal(got, ops.attention_fp4(view.contiguous(), *cache, table.to(DEV), length))
+
+
+@pytest.mark.parametrize("tokens", [1, 40])
+def test_attention_over_a_cache_past_4_gib(ops, tokens):
+    """Page offsets beyond 2^32 bytes, in keys and values."""
+    heads, page, dim = 8, 128, 128
+    pages = (2 ** 32 + 2 ** 28) // (heads * page * dim // 2)
+    cache = ops.kv_cache_fp4(pages, heads, page, dim, DEV)
+    last = torch.tensor([[pages - 1, 0, pages - 2]], dtype=torch.int32, device=DEV)
+    k, v = (normal(i, 1, 300, heads, dim).to(DEV) for i in (1, 2))
+    zero = torch.zeros(1, dtype=torch.int32, device=DEV)
+    ops.kv_cache_fp4_append(k, v, *cache, last, zero)
+    small = ops.kv_cache_fp4(3, heads, page, dim, DEV)
+    table, length = torch.arange(3, dtype=torch.int32, device=DEV)[None], torch.tensor([300], dtype=torch.int32, device=DEV)
+    ops.kv_cache_fp4_append(k, v, *small, table, zero)
+    q = normal(3, 1, tokens, heads, dim).to(BF16).to(DEV)
+    assert torch.equal(ops.attention_fp4(q, *cache, last, length), ops.attention_fp4(q, *small, table, length))
+    for a, b in zip(ops.kv_cache_fp4_read(*cache, last, zero, 300), ops.kv_cache_fp4_read(*small, table, zero, 300)):
+        assert torch.equal(a, b)
+
+
+# ---------------------------------------------------------------------------
+# Streams, graphs, refusals.
+
+
+def test_other_streams_and_graphs(ops):
+    """On a stream of the caller's, and replayed from two graphs, between the caller's own work: the eager results."""
+    cache = filled_cache(ops, 64, 2, 32, 64)
+    table = torch.arange(64, dtype=torch.int32, device=DEV).reshape(2, 32)
+    start = torch.tensor([900, 17], dtype=torch.int32, device=DEV)
+    x = normal(1, 2, 1, 8, 64).to(BF16).to(DEV)
+
+    def step(group):
+        ops.kv_cache_fp4_append(x[:, :, :2], x[:, :, 2:4], *cache, table, start)
+        k, v = ops.kv_cache_fp4_read(*cache, table, start, 1)
+        return ops.attention_fp4(x[:, :, :2 * group], *cache, table, start + 1), k, v
+
+    want = [step(2), step(4)]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        got = [step(2), step(4)]
+    s.synchronize()
+    for a, b in zip(got, want):
+        assert all(torch.equal(c, d) for c, d in zip(a, b))
+    graphs, outs = [], []
+    for group in (2, 4):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            outs.append(step(group))
+    for i in range(4):
+        x.copy_(normal(10 + i, 2, 1, 8, 64).to(BF16))
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        got = [[t.clone() for t in o] for o in outs]
+        for a, b in zip(got, [step(2), step(4)]):
+            assert all(torch.equal(c, d) for c, d in zip(a, b))
+
+
+def test_refusals(ops):
+    cache = ops.kv_cache_fp4(4, 2, 16, 64, DEV)
+    eight = ops.kv_cache(4, 2, 16, 64, DEV)
+    table, one = torch.zeros(1, 4, dtype=torch.int32, device=DEV), torch.ones(1, dtype=torch.int32, device=DEV)
+    q = torch.zeros(1, 1, 4, 64, dtype=BF16, device=DEV)
+    k = torch.zeros(1, 1, 2, 64, dtype=BF16, device=DEV)
+    bad = [
+        lambda: ops.kv_cache_fp4_append(k, k, *cache, table, None),
+        lambda: ops.kv_cache_fp4_append(k, k[..., :32], *cache, table, one),
+        lambda: ops.kv_cache_fp4_append(k, k, *eight, table, one),
+        lambda: ops.kv_cache_fp4_append(k, k, *cache, table.long(), one),
+        lambda: ops.kv_cache_fp4_append(k[0], k[0], *cache, table, one),
+        lambda: ops.kv_cache_fp4_append(k, k, *cache, table, one, one[:0]),
+        lambda: ops.kv_cache_fp4_append(k.int(), k.int(), *cache, table, one),
+        lambda: ops.kv_cache_fp4_append(k, k, cache[0], cache[0], *cache[2:], table, one),
+        lambda: ops.kv_cache_fp4_append(k, k, *cache[:3], cache[3][:, :, :, :8], table, one),
+        lambda: ops.kv_cache_fp4_read(*cache, table, one, -1),
+        lambda: ops.kv_cache_fp4_read(*cache, table, one, 4, dtype=torch.int32),
+        lambda: ops.kv_cache_fp4_read(*cache, table, one.cpu(), 4),
+        lambda: ops.kv_cache_fp4_read(*cache, torch.cat([table, table]), one, 4),
+        lambda: ops.attention_fp4(q.float(), *cache, table, one),
+        lambda: ops.attention_fp4(q[:, :, :3], *cache, table, one),
+        lambda: ops.attention_fp4(q[..., :32], *cache, table, one),
+        lambda: ops.attention_fp4(q[0], *cache, table, one),
+        lambda: ops.attention_fp4(q.transpose(2, 3), *cache, table, one),
+        lambda: ops.attention_fp4(q, *cache, table, one.cpu()),
+        lambda: ops.attention_fp4(q, *eight, table, one),
+        lambda: ops.attention_fp4(q, *cache, table, one, window=-1),
+        lambda: ops.attention_fp4(q, *cache, table, one, scale=float("inf")),
+    ]
+    for i, f in enumerate(bad):
+        with pytest.raises((TypeError, ValueError, ops.DeepShiftError)):
+            f()
+            pytest.fail(f"case {i} was accepted")
+    empty = ops.kv_cache_fp4_read(*cache, table, one, 0)
+    assert empty[0].shape == (1, 0, 2, 64)
+    assert ops.attention_fp4(q[:, :0], *cache, table, one).shape == (1, 0, 4, 64)
+    ops.kv_cache_fp4_append(k[:0], k[:0], *cache, table[:0], one[:0])
