@@ -12,6 +12,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "attention.hpp"
 #include "conv_plan.hpp"
@@ -205,6 +206,16 @@ __device__ __forceinline__ void turn4(const i32x4 &a, const i32x4 &b, const floa
     odd = __builtin_bit_cast(f16x8, hi);
 }
 
+// f(0) .. f(N - 1) with the number as a constant.
+template <int FROM, int TO, typename F>
+__device__ __forceinline__ void unroll(F &&f)
+{
+    if constexpr (FROM < TO) {
+        f(std::integral_constant<int, FROM>{});
+        unroll<FROM + 1, TO>(f);
+    }
+}
+
 // 16 queries of a kv head: a block of 4 waves takes a share of the keys, each wave every fourth
 // 64 of it straight from memory to registers, and joins them at its end.
 template <typename T, int DP>
@@ -220,7 +231,7 @@ attention4_few_kernel(const AttentionParams p, int blocks)
     __shared__ f32x4 osum[kWaves][DT][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), r = lane & 15, g = lane >> 4;
     const int split = int(blockIdx.x), bh = int(blockIdx.y), b = bh / p.heads, h = bh - b * p.heads;
-    const int D = p.dim, page = 1 << p.page_shift, row = int(blockIdx.z) * 16 + r;
+    const int D = p.dim, page = 1 << p.page_shift, row = r;
     const Sequence seq(p, b);
     v8 qf[QC];
     int low, high;
@@ -432,16 +443,360 @@ attention4_few_kernel(const AttentionParams p, int blocks)
     }
 }
 
+// Many queries of a kv head: a block's waves have 32 of them each and share the keys, 64 at a
+// time. A wave reads its part of them a step ahead, turns them into 16-bit floats, once for
+// the whole block, and puts them into LDS: keys as rows [key][dim], values as rows [dim][key],
+// the 16-byte pieces of a row in an order of its own, so that the lanes of a read (0-3, 12-15,
+// 20-27 at once, and so on) meet in no bank.
+//
+// The products are 32 x 32: one query a lane and 32 keys of it, 8 of each 16. Row 8 w + 4 hf + e of tile
+// tt is key 32 tt + 16 (w / 2) + 8 hf + 4 (w % 2) + e: lane half hf then holds the keys that it
+// contracts in the second product.
+template <typename T, int DP, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, DP <= 128 ? 2 : 1)
+attention4_many_kernel(const AttentionParams p, int blocks, int bhs)
+{
+    constexpr int QC = DP / 16, DT = DP / 32, kRuns = 4 / WAVES;
+    constexpr int kWords = DP / 32;            // words (8 codes) of a lane's part of a run's keys, and of its values' tokens
+    constexpr int NS = DP == 256 ? 2 : 1;      // scale blocks of it
+    constexpr int kKeys = kStep * DP * 2;      // bytes of a step's keys, or values
+    typedef typename Vec8<T>::type v8;
+    __shared__ __align__(16) uint8_t lds[2][2 * kKeys];
+    __shared__ int nans[2][WAVES];             // whether a wave's part of the values has any
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), r = lane & 31, hf = lane >> 5, g = lane >> 4;
+    // An eighth of the work to each XCD, a head's blocks together, so that they read its
+    // keys through one L2, the same head of every sequence next, whose lengths may differ; the
+    // last rows, which see the most keys, first.
+    const int per = p.row_tiles * p.splits, all = bhs * per, share = (all + 7) >> 3;
+    const int at = (int(blockIdx.x) & 7) * share + (int(blockIdx.x) >> 3);
+    if ((int(blockIdx.x) >> 3) >= share || at >= all) return;
+    const int unit = at / per, rest = at - unit * per, tile = p.row_tiles - 1 - rest / p.splits, split = rest % p.splits;
+    const int batch = bhs / p.heads, h = unit / batch, b = unit - h * batch, bh = b * p.heads + h;
+    const int D = p.dim, page = 1 << p.page_shift;
+    const Sequence seq(p, b);
+    v8 qf[QC];
+    int low, high;
+    const int row = (tile * WAVES + wave) * 32 + r;
+    const bool live = load_query<T, DP, 16, 8, QC>(p, seq, b, h, row, hf, low, high, qf);
+    // A row without a query sees every key, which costs less than no key, and is 0 in the end.
+    if (!live) high = 0x7fffffff;
+    // The block's keys: from the first that its first query sees to its last query's own.
+    const int t0 = tile * WAVES * 32 / p.group, t1 = min(((tile + 1) * WAVES * 32 - 1) / p.group, seq.count - 1);
+    const int thi = t0 < seq.count ? min(max(seq.first + t1 + 1, 0), seq.keys) : 0;
+    const int tlo = p.window ? max(max(seq.first + t0 + 1, 0) - p.window, 0) : 0;
+    // Steps of which one of its queries does not see every key.
+    const int alo = p.window ? max(max(seq.first + t1 + 1, 0) - p.window, 0) : 0, ahi = min(max(seq.first + t0 + 1, 0), seq.keys);
+    auto mixed = [&](int step) { return step * kStep < alo || step * kStep + kStep > ahi; };
+    const int s0 = thi > tlo ? tlo / kStep : 0, s1 = thi > tlo ? (thi + kStep - 1) / kStep : 0;
+    const int each = (s1 - s0 + p.splits - 1) / p.splits;
+    const int from = s0 + split * each, to = min(s1, from + each);
+
+    f32x16 acc[DT];
+    float m = -__builtin_inff(), l = 0.f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) acc[d] = f32x16{};
+    // The table's entry of the g-th 16 keys of a step; a page of the cache or -1.
+    const int *const table = p.table + b * p.ldt;
+    auto entry = [&](int step) {
+        const int key = step * kStep + g * 16;
+        return step < to && key < thi ? table[key >> p.page_shift] : -1;
+    };
+    auto on_page = [&](int pid) { return unsigned(pid) < unsigned(p.pages) ? pid : -1; };
+    auto on_pages = [&](int pids) { return bool(__all(pids >= 0)); };
+    // A lane's part of a run of 16 keys: a quarter of the dimensions of key lane / 4, and of the values
+    // 4 tokens x 8 dimensions (of heads of up to 64 half of them, of more than 128 two such pieces). What lies past
+    // `dim` is read somewhere inside. Where there is no page, page 0 is read instead.
+    const int kkey = lane >> 2, kdim = (lane & 3) * (DP / 4), quad = lane >> 4, vgroup = lane & 15;
+    uint32_t kraw[kRuns][kWords], kse[kRuns][NS], vse[kRuns][NS];
+    i32x4 vraw[kRuns][NS];
+    uint32_t koff[kWords / 2], kso[NS], voff[NS], vso[NS];
+#pragma unroll
+    for (int i = 0; i < kWords / 2; ++i) koff[i] = uint32_t(kkey * (D / 2) + min(kdim + i * 16, D - 16) / 2);
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+        const int d = min(DP == 64 ? vgroup * 4 : i * 128 + vgroup * 8, D - 8);
+        kso[i] = uint32_t(min(kdim / 32 + i, blocks - 1) * page + kkey);
+        voff[i] = uint32_t(quad * 2 * D + d / 8 * 16);
+        vso[i] = uint32_t(d / 32 * page + quad * 4);
+    }
+    const int64_t head_bytes = int64_t(D / 2) * page, head_scales = int64_t(blocks) * page;
+    const uint8_t *const kh = p.kc + h * head_bytes, *const vh = p.vc + h * head_bytes;
+    const uint8_t *const ksh = p.ks + h * head_scales, *const vsh = p.vs + h * head_scales;
+    const int64_t page_bytes = p.heads * head_bytes, page_scales = p.heads * head_scales;
+    auto fetch = [&](int step, int pids) {
+#pragma unroll
+        for (int q = 0; q < kRuns; ++q) {
+            const int which = wave * kRuns + q, pid = max(__builtin_amdgcn_readlane(pids, which * 16), 0);
+            const int slot = (step * kStep + which * 16) & (page - 1);
+            const uint8_t *k = kh + pid * page_bytes + slot * (D / 2), *v = vh + pid * page_bytes + slot * (D / 2);
+            const uint8_t *ks = ksh + pid * page_scales + slot, *vs = vsh + pid * page_scales + slot;
+            if (kWords >= 4 && D == DP) {
+#pragma unroll
+                for (int i = 0; i < kWords / 4; ++i) {
+                    const i32x4 x = *reinterpret_cast<const i32x4 *>(k + koff[2 * i]);
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) kraw[q][4 * i + w] = uint32_t(x[w]);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < kWords / 2; ++i) {
+                    const i32x2 x = *reinterpret_cast<const i32x2 *>(k + koff[i]);
+                    kraw[q][2 * i] = uint32_t(x[0]);
+                    kraw[q][2 * i + 1] = uint32_t(x[1]);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < NS; ++i) {
+                vraw[q][i] = *reinterpret_cast<const i32x4 *>(v + voff[i]);
+                kse[q][i] = ks[kso[i]];
+                vse[q][i] = *reinterpret_cast<const uint32_t *>(vs + vso[i]);
+            }
+        }
+    };
+    // The order of a key's pieces: its row in a tile, from 16 on again (rows of 128 bytes share a bank row
+    // by twos); of a dimension's pieces: such that both a read's 16 dimensions and a write's, every
+    // fourth or eighth, are spread.
+    auto order = [](int key) { return ((key & 3) | ((key >> 3) & 1) << 2 | ((key >> 2) & 1) << 3) >> (DP < 128 ? 1 : 0); };
+    auto vorder = [](int d) { return ((d >> 1) ^ (d >> 4)) & 7; };
+    // Keys that no query sees may hold anything: their values count as 0 (whatever the code, 2^-127 of it is
+    // 0 as a 16-bit float). So does what was read of a key past `dim`.
+    auto clear = [&](int step, int pids) {
+        if (__builtin_expect(D == DP && step * kStep >= tlo && step * kStep + kStep <= thi && on_pages(pids), 1)) return;
+#pragma unroll
+        for (int q = 0; q < kRuns; ++q) {
+            const int which = wave * kRuns + q, run = step * kStep + which * 16;
+            const bool there = __builtin_amdgcn_readlane(pids, which * 16) >= 0;
+#pragma unroll
+            for (int i = 0; i < NS; ++i) vse[q][i] &= uint32_t(there ? key_mask(run + 4 * quad, tlo, thi) : 0);
+#pragma unroll
+            for (int i = 0; i < kWords; ++i)
+                if (kdim + i * 8 >= D) kraw[q][i] = 0;
+        }
+    };
+    auto note_nans = [&](int step, int buf) {
+        if (!mixed(step)) return;
+        uint32_t nan = 0;
+#pragma unroll
+        for (int q = 0; q < kRuns; ++q)
+#pragma unroll
+            for (int i = 0; i < NS; ++i) nan |= nan_scales(vse[q][i]);
+        nans[buf][wave] = __any(nan != 0);
+    };
+    // Part u of what fetch() read, to LDS: 8 dimensions of a key, or 2 of 4 tokens' values, turned
+    // around. (Every other lane writes its two rows in the other order, so that all banks have work.)
+    constexpr int kParts = kRuns * kWords * 2;
+    const int odd = DP == 64 ? (vgroup >> 3) & 1 : vgroup & 1;
+    const uint32_t first = odd ? 0x07060302u : 0x05040100u, second = odd ? 0x05040100u : 0x07060302u;
+    auto put = [&](auto part, int buf) {
+        constexpr int u = decltype(part)::value;
+        constexpr int q = u / (2 * kWords), c = u / 2 % kWords;
+        const int which = wave * kRuns + q;
+        uint8_t *const ks = lds[buf], *const vs = ks + kKeys;
+        if constexpr (u % 2 == 0) {
+            const int key = which * 16 + kkey, piece = (lane & 3) * kWords + c;
+            *reinterpret_cast<v8 *>(ks + key * DP * 2 + (piece ^ order(key)) * 16) = operand4<T>(kraw[q][c], scale4(kse[q][c * NS / kWords]));
+        } else {
+            constexpr int i = DP == 256 ? c / 4 : 0, sel = c % 4;
+            const int d = (DP == 64 ? vgroup * 4 : i * 128 + vgroup * 8) + sel * 2;
+            uint32_t x[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const uint32_t w = uint32_t(vraw[q][i][t]);
+                const f16x2 y = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(DP == 64 ? w >> (16 * (vgroup & 1)) : w, scale_of(vse[q][i], t), sel);
+                x[t] = __builtin_bit_cast(uint32_t, y);
+            }
+            uint8_t *const to = vs + ((which * 2 + (quad >> 1)) ^ vorder(d)) * 16 + (quad & 1) * 8;
+            *reinterpret_cast<i32x2 *>(to + (d + odd) * 128) =
+                i32x2{int(__builtin_amdgcn_perm(x[1], x[0], first)), int(__builtin_amdgcn_perm(x[3], x[2], first))};
+            *reinterpret_cast<i32x2 *>(to + (d + 1 - odd) * 128) =
+                i32x2{int(__builtin_amdgcn_perm(x[1], x[0], second)), int(__builtin_amdgcn_perm(x[3], x[2], second))};
+        }
+    };
+    // Pages of this step and the next, and the table's entry of the one after.
+    int pid0 = -1, pid1 = -1, next = -1;
+    if (from < to) {
+        pid1 = on_page(entry(from));
+        fetch(from, pid1);
+        next = entry(from + 1);
+        clear(from, pid1);
+        note_nans(from, 0);
+        unroll<0, kParts>([&](auto u) { put(u, 0); });
+        pid0 = pid1;
+        pid1 = on_page(next);
+        next = entry(from + 2);
+        fetch(from + 1, pid1);
+    }
+    // A step mixes what does not depend on each other, product by product (each is issued in
+    // a few clocks and takes 32): into the first products the transfer of the next step's keys
+    // to LDS, into the second ones the weights that the products after them need. What they
+    // read from LDS is read eight products ahead.
+    constexpr int kFirst = 2 * QC, kSecond = 4 * DT, kAhead = 8;
+    const int krow = (r >> 4) * 16 + ((r >> 2) & 1) * 8 + ((r >> 3) & 1) * 4 + (r & 3);     // row r's key in tile 0
+    auto body = [&](int step, auto which_buf) {
+        constexpr int buf = decltype(which_buf)::value;
+        const int base = step * kStep;
+        wait_lds();
+        barrier();
+        const uint8_t *const kt = lds[buf] + krow * DP * 2, *const vt = lds[buf] + kKeys + r * 128;
+        auto key_part = [&](int n) { return *reinterpret_cast<const v8 *>(kt + (n % 2) * 32 * DP * 2 + ((n / 2 * 2 + hf) ^ order(krow)) * 16); };
+        auto value_part = [&](int n) {
+            return *reinterpret_cast<const f16x8 *>(vt + n % DT * 32 * 128 + ((n / DT * 2 + hf) ^ vorder(n % DT * 32 + r)) * 16);
+        };
+        if (mixed(step)) {
+            int nan = 0;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) nan |= nans[buf][w];
+            if (__builtin_amdgcn_readfirstlane(nan)) {      // the same in every wave
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    f32x16 n{};
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const bool there = __builtin_amdgcn_readlane(pid0, q * 16) >= 0;
+                        const f16x8 v = value_part(q * DT + d);
+                        f16x8 where, seen;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int key = base + q * 16 + hf * 8 + i;
+                            where[i] = _Float16(v[i] != v[i] ? 1.f : 0.f);
+                            seen[i] = _Float16(there && key >= low && key < high ? 1.f : 0.f);
+                        }
+                        n = mma32(where, seen, n);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[d][i] += n[i] > 0.f ? __builtin_nanf("") : 0.f;
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                wait_lds();
+                barrier();
+                for (int i = int(threadIdx.x); i < kKeys / 16; i += 64 * WAVES) {
+                    f16x8 *const at = reinterpret_cast<f16x8 *>(lds[buf] + kKeys + i * 16);
+                    f16x8 v = *at;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = v[e] != v[e] ? _Float16(0.f) : v[e];
+                    *at = v;
+                }
+                wait_lds();
+                barrier();
+            }
+        }
+        v8 kf[kAhead];
+#pragma unroll
+        for (int n = 0; n < kAhead; ++n) kf[n] = key_part(n);
+        const bool held = on_pages(pid0);
+        const int now = pid0;
+        if (step + 1 < to) {
+            clear(step + 1, pid1);
+            note_nans(step + 1, buf ^ 1);
+        }
+        f32x16 s[2];
+        unroll<0, kFirst>([&](auto nth) {
+            constexpr int n = decltype(nth)::value;
+            s[n % 2] = mma32(kf[n % kAhead], qf[n / 2], n < 2 ? f32x16{} : s[n % 2]);
+            if constexpr (n + kAhead < kFirst) kf[n % kAhead] = key_part(n + kAhead);
+            unroll<n * kParts / kFirst, (n + 1) * kParts / kFirst>([&](auto u) { put(u, buf ^ 1); });
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        f16x8 vf[kAhead];
+#pragma unroll
+        for (int n = 0; n < kAhead; ++n) vf[n] = value_part(n);
+        pid0 = pid1;
+        if (step + 1 < to) {
+            pid1 = on_page(next);
+            next = entry(step + 3);
+            fetch(step + 2, pid1);
+        }
+        // Element i of s[t]: key 16 (2 t + i / 8) + 8 hf + i % 8.
+        if (!held || !__all(base >= low && base + kStep <= high)) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const bool there = __builtin_amdgcn_readlane(now, q * 16) >= 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int key = base + q * 16 + hf * 8 + i;
+                    float &v = reinterpret_cast<float *>(&s[q >> 1])[(q & 1) * 8 + i];
+                    v = there && key >= low && key < high ? v : -__builtin_inff();
+                }
+            }
+        }
+        float top = -__builtin_inff();
+        const float sub = or_zero(m);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) s[i / 16][i % 16] = fmaf(s[i / 16][i % 16], p.scale, -sub);
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) top = fmaxf(top, fmaxf(s[i / 16][i % 16], s[i / 16][i % 16 + 1]));
+        raise(m, l, max_over_32(top),
+              [&](float by) {
+#pragma unroll
+                  for (int i = 0; i < 32; ++i) s[i / 16][i % 16] -= by;
+              },
+              [&](float alpha) {
+#pragma unroll
+                  for (int d = 0; d < DT; ++d) acc[d] *= alpha;
+              });
+        f16x8 pf[4];
+        float sum[4] = {};
+        auto weigh = [&](int q, int i) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const float e = __builtin_amdgcn_exp2f(s[q >> 1][(q & 1) * 8 + i + k]);
+                sum[q] += e;
+                pf[q][i + k] = _Float16(e);
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) weigh(0, i);
+#pragma unroll
+        for (int n = 0; n < kSecond; ++n) {
+            const int q = n / DT, d = n % DT;
+            acc[d] = mma32(vf[n % kAhead], pf[q], acc[d]);
+            if (n + kAhead < kSecond) vf[n % kAhead] = value_part(n + kAhead);
+            if (q < 3) {
+#pragma unroll
+                for (int i = d * 4 / DT * 2; i < (d + 1) * 4 / DT * 2; i += 2) weigh(q + 1, i);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    };
+    for (int step = from; step < to; step += 2) {
+        body(step, std::integral_constant<int, 0>{});
+        if (step + 1 < to) body(step + 1, std::integral_constant<int, 1>{});
+    }
+    l += __shfl_xor(l, 32);
+    if (row >= p.rows) return;
+    if (!live || high == 0) {
+        m = -__builtin_inff();
+        l = 0.f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) acc[d] = f32x16{};
+    }
+    float *part = p.part ? p.part + ((int64_t(bh) * p.rows + row) * p.splits + split) * (D + 2) : nullptr;
+    if (part && hf == 0) {
+        part[D] = m;
+        part[D + 1] = l;
+    }
+    const float inv = inverse(l);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const int at = d * 32 + w * 8 + hf * 4;
+            if (at < D) store_row<T>(p, b, h, row, part, at, f32x4{acc[d][4 * w], acc[d][4 * w + 1], acc[d][4 * w + 2], acc[d][4 * w + 3]}, inv);
+        }
+}
+
 // How a call is split: over the rows first, then over the keys until 512 blocks (two a CU) have at
 // least 8 steps of 64 keys each.
 Plan plan_attention4(int64_t batch, int64_t tokens, int64_t heads, int64_t group, int64_t columns, int64_t page)
 {
     Plan a;
     a.rows = tokens * group;
-    a.waves = 0;
-    a.row_tiles = int((a.rows + 15) / 16);
+    a.waves = a.rows <= 16 ? 0 : a.rows <= 64 ? 2 : 4;
+    a.row_tiles = a.waves ? int((a.rows + 32 * a.waves - 1) / (32 * a.waves)) : 1;
     const int64_t blocks = std::max<int64_t>(batch * heads * a.row_tiles, 1), steps = (columns * page + kStep - 1) / kStep;
-    a.splits = int(std::max<int64_t>(1, std::min<int64_t>({(511 + blocks) / blocks, (steps + 7) / 8, 256})));
+    a.splits = int(std::max<int64_t>(1, std::min<int64_t>({a.waves ? 512 / blocks : (511 + blocks) / blocks, (steps + 7) / 8, 256})));
     return a;
 }
 
@@ -449,7 +804,13 @@ template <typename T, int DP>
 void run_attention4(const AttentionParams &p, const Plan &a, int64_t batch, hipStream_t s)
 {
     const int bhs = int(batch * p.heads);
-    hipLaunchKernelGGL((attention4_few_kernel<T, DP>), dim3(a.splits, bhs, a.row_tiles), dim3(256), 0, s, p, int(blocks4(p.dim)));
+    const int blocks = int(blocks4(p.dim));
+    if (a.waves == 0) {
+        hipLaunchKernelGGL((attention4_few_kernel<T, DP>), dim3(a.splits, bhs), dim3(256), 0, s, p, blocks);
+    } else {
+        const dim3 grid(uint32_t((int64_t(bhs) * a.row_tiles * a.splits + 7) / 8 * 8));
+        hipLaunchKernelGGL((a.waves == 2 ? attention4_many_kernel<T, DP, 2> : attention4_many_kernel<T, DP, 4>), grid, dim3(64 * a.waves), 0, s, p, blocks, bhs);
+    }
     if (a.splits > 1)
         hipLaunchKernelGGL((attention_join_kernel<T, DP / 4>), dim3(uint32_t(bhs * a.rows)), dim3(256), 0, s, p);
 }
@@ -602,7 +963,7 @@ extern "C" ds_status ds_attention_fp4(const void *q, const uint8_t *k_cache, con
     if (batch * heads > 65535) return fail(DS_ERR_UNSUPPORTED, "more than 65535 sequences times heads");
     if (group > 65535 || tokens * group > kMaxElems / 64) return fail(DS_ERR_UNSUPPORTED, "too many queries of a head");
     const Plan a = plan_attention4(batch, tokens, heads, group, columns, page);
-    if (batch * heads * a.rows * a.splits > kMaxElems / 2 || a.row_tiles > 65535) return fail(DS_ERR_UNSUPPORTED, "too many queries");
+    if (batch * heads * a.rows * a.splits > kMaxElems / 2) return fail(DS_ERR_UNSUPPORTED, "too many queries");
     int64_t bytes[2];
     for (int i = 0; i < 2; ++i) {
         const int64_t *s = i ? o_strides : q_strides;
