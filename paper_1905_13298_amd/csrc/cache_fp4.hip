@@ -219,7 +219,7 @@ __device__ __forceinline__ void unroll(F &&f)
 // 16 queries of a kv head: a block of 4 waves takes a share of the keys, each wave every fourth
 // 64 of it straight from memory to registers, and joins them at its end.
 template <typename T, int DP>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1)
 attention4_few_kernel(const AttentionParams p, int blocks)
 {
     constexpr int kWaves = 4;
@@ -250,6 +250,9 @@ attention4_few_kernel(const AttentionParams p, int blocks)
     thi = __builtin_amdgcn_readfirstlane(thi);
     alo = __builtin_amdgcn_readfirstlane(alo);
     ahi = __builtin_amdgcn_readfirstlane(ahi);
+    // Such a row takes part as if it saw every key, which costs less than no key.
+    const bool none = high == 0;
+    if (none) high = 0x7fffffff;
     const int s0 = thi > 0 ? tlo / kStep : 0, s1 = (thi + kStep - 1) / kStep;
     const int each = (s1 - s0 + p.splits - 1) / p.splits;
     const int from = s0 + split * each, to = min(s1, from + each);
@@ -264,56 +267,94 @@ attention4_few_kernel(const AttentionParams p, int blocks)
         const int pid = key < thi ? p.table[b * p.ldt + col] : -1;
         return unsigned(pid) < unsigned(p.pages) ? pid : -1;
     };
-    for (int step = from + wave; step < to; step += kWaves) {
-        const int base = step * kStep;
-        const int krun = base + (r >> 2) * 16, vrun = base + g * 16;
-        const int kp = page_of(krun), vp = page_of(vrun);
+    // What a lane reads of a step: a quarter of the dimensions of keys 4 r .. 4 r + 3, and of the values 16 tokens
+    // x 8 dimensions (of heads of up to 64 half of that counts, of more than 128 it is twice as much). Where there is no page, page 0
+    // is read instead, and what lies past `dim` somewhere inside.
+    struct Step {
+        uint32_t k[4][QC], ks[NS], vs[NS][4];
+        i32x4 v[NS][4];
+        int vp;
+    };
+    uint32_t koff[QC / 2], kso[NS], voff[NS], vso[NS];
+#pragma unroll
+    for (int c = 0; c < QC / 2; ++c) koff[c] = uint32_t(min(g * (DP / 4) + c * 16, D - 16) / 2 + (r & 3) * 4 * (D / 2));
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+        const int d = min(DP == 64 ? r * 4 : i * 128 + r * 8, D - 8);
+        kso[i] = uint32_t(min(g * (DP / 4) / 32 + i, blocks - 1) * page + (r & 3) * 4);
+        voff[i] = uint32_t(d / 8 * 16);
+        vso[i] = uint32_t(d / 32 * page);
+    }
+    auto fetch = [&](int step, int kp, int vp, Step &x) {
+        const int kslot = (step * kStep + (r >> 2) * 16) & (page - 1), vslot = (step * kStep + g * 16) & (page - 1);
         const int64_t kat = int64_t(max(kp, 0)) * p.heads + h, vat = int64_t(max(vp, 0)) * p.heads + h;
-        const int kslot = (krun & (page - 1)) + (r & 3) * 4, vslot = vrun & (page - 1);
-        uint32_t kraw[4][QC], kse[NS];
-        i32x4 vraw[NS][4];
-        uint32_t vse[NS][4];
+        const uint8_t *const k = p.kc + (kat * page + kslot) * (D / 2), *const ks = p.ks + kat * blocks * page + kslot;
+        const uint8_t *const v = p.vc + (vat * page + vslot) * (D / 2), *const vs = p.vs + vat * blocks * page + vslot;
+        if (DP > 64 && D == DP) {
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+            for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int c = 0; c < QC; c += 2) {
-                const int d = g * (DP / 4) + c * 8;
-                i32x2 x{};
-                if (kp >= 0 && d < D) x = *reinterpret_cast<const i32x2 *>(p.kc + (kat * page + kslot + t) * (D / 2) + d / 2);
-                kraw[t][c] = uint32_t(x[0]);
-                kraw[t][c + 1] = uint32_t(x[1]);
-            }
+                for (int c = 0; c < QC; c += 4) {
+                    const i32x4 y = *reinterpret_cast<const i32x4 *>(k + koff[c / 2] + t * (DP / 2));
 #pragma unroll
-        for (int i = 0; i < NS; ++i) {
-            const int d = g * (DP / 4) + i * 32;
-            kse[i] = kp >= 0 && d < D ? *reinterpret_cast<const uint32_t *>(p.ks + (kat * blocks + d / 32) * page + kslot) : 0;
+                    for (int w = 0; w < 4; ++w) x.k[t][(c + w) % QC] = uint32_t(y[w]);
+                }
+        } else {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int c = 0; c < QC; c += 2) {
+                    const i32x2 y = *reinterpret_cast<const i32x2 *>(k + koff[c / 2] + t * (D / 2));
+                    const bool in = g * (DP / 4) + c * 8 < D;
+                    x.k[t][c] = in ? uint32_t(y[0]) : 0u;
+                    x.k[t][c + 1] = in ? uint32_t(y[1]) : 0u;
+                }
         }
 #pragma unroll
         for (int i = 0; i < NS; ++i) {
-            const int d = DP == 64 ? r * 4 : i * 128 + r * 8;
+            x.ks[i] = *reinterpret_cast<const uint32_t *>(ks + kso[i]);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                vraw[i][q] = vp >= 0 && d < D ? *reinterpret_cast<const i32x4 *>(p.vc + vat * page * (D / 2) + (vslot / 4 + q) * 2 * D + d / 8 * 16) : i32x4{};
-                // (Heads of up to 64: half of a piece's dimensions are this lane's.)
-                if (DP == 64) vraw[i][q] = (r & 1) ? i32x4(vraw[i][q] >> 16) : vraw[i][q];
-            }
-            i32x4 e{};
-            if (vp >= 0 && d < D) e = *reinterpret_cast<const i32x4 *>(p.vs + (vat * blocks + d / 32) * page + vslot);
+            for (int q = 0; q < 4; ++q) x.v[i][q] = *reinterpret_cast<const i32x4 *>(v + voff[i] + q * 2 * D);
+            const i32x4 e = *reinterpret_cast<const i32x4 *>(vs + vso[i]);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) vse[i][q] = uint32_t(e[q]);
+            for (int q = 0; q < 4; ++q) x.vs[i][q] = uint32_t(e[q]);
         }
+        x.vp = vp;
+    };
+    // The next step's keys and values are on their way while this one's are worked on, and the pages of
+    // the one after.
+    Step one, other;
+    int kp = -1, vp = -1;
+    auto look = [&](int step) {
+        kp = page_of(step * kStep + (r >> 2) * 16);
+        vp = page_of(step * kStep + g * 16);
+    };
+    if (from + wave < to) {
+        look(from + wave);
+        fetch(from + wave, kp, vp, one);
+        look(from + wave + kWaves);
+    }
+    auto body = [&](int step, Step &x, Step &ahead) {
+        const int base = step * kStep, vrun = base + g * 16;
+        if (step + kWaves < to) {
+            fetch(step + kWaves, kp, vp, ahead);
+            look(step + 2 * kWaves);
+        }
+        const bool there = x.vp >= 0;
         f32x4 s[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int c = 0; c < QC; ++c)
-                s[t] = mma(operand4<T>(kraw[t][c], scale_of(kse[c * NS / QC], t)), qf[c], c == 0 ? f32x4{} : s[t]);
+                s[t] = mma(operand4<T>(x.k[t][c], scale_of(x.ks[c * NS / QC], t)), qf[c], c == 0 ? f32x4{} : s[t]);
         // Element i of s[t]: key vrun + 4 i + t.
-        if (!__all(vp >= 0 && vrun >= low && vrun + 16 <= high)) {
+        if (!__all(there && vrun >= low && vrun + 16 <= high)) {
+            int run = vrun;
+            asm volatile("" : "+v"(run));         // (what follows is not worked out where it is not needed)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const int key = vrun + (i & 3) * 4 + (i >> 2);
-                s[i >> 2][i & 3] = vp >= 0 && key >= low && key < high ? s[i >> 2][i & 3] : -__builtin_inff();
+                const int key = run + (i & 3) * 4 + (i >> 2);
+                s[i >> 2][i & 3] = there && key >= low && key < high ? s[i >> 2][i & 3] : -__builtin_inff();
             }
         }
         const float sub = or_zero(m);
@@ -338,24 +379,26 @@ attention4_few_kernel(const AttentionParams p, int blocks)
             l += e[i];
             pf[i >> 3][i & 7] = _Float16(e[i]);
         }
-        if (base + kStep > thi || base < tlo) {
+        if (!__all(there && base + kStep <= thi && base >= tlo)) {
             // Keys that no query sees may hold anything: their values count as 0 (whatever the code, 2^-127
             // of it is 0 as a 16-bit float).
 #pragma unroll
             for (int q = 0; q < 4; ++q)
 #pragma unroll
-                for (int i = 0; i < NS; ++i) vse[i][q] &= uint32_t(key_mask(vrun + 4 * q, tlo, thi));
+                for (int i = 0; i < NS; ++i) x.vs[i][q] &= uint32_t(there ? key_mask(vrun + 4 * q, tlo, thi) : 0);
         }
         if (base + kStep > ahi || base < alo) {
             uint32_t nan = 0;
 #pragma unroll
             for (int i = 0; i < NS; ++i)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) nan |= nan_scales(vse[i][q]);
+                for (int q = 0; q < 4; ++q) nan |= nan_scales(x.vs[i][q]);
             if (__any(nan != 0)) {
                 f16x8 seen[2];
+                int run = vrun;
+                asm volatile("" : "+v"(run));
 #pragma unroll
-                for (int i = 0; i < 16; ++i) seen[i >> 3][i & 7] = _Float16(vp >= 0 && vrun + i >= low && vrun + i < high ? 1.f : 0.f);
+                for (int i = 0; i < 16; ++i) seen[i >> 3][i & 7] = _Float16(there && run + i >= low && run + i < high ? 1.f : 0.f);
 #pragma unroll
                 for (int i = 0; i < NS; ++i) {
                     f32x4 n{};
@@ -363,11 +406,11 @@ attention4_few_kernel(const AttentionParams p, int blocks)
                     for (int c = 0; c < 2; ++c) {
                         f16x8 where;
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) where[j] = _Float16((vse[i][2 * c + j / 4] >> (8 * (j & 3)) & 255u) == 255u ? 1.f : 0.f);
+                        for (int j = 0; j < 8; ++j) where[j] = _Float16((x.vs[i][2 * c + j / 4] >> (8 * (j & 3)) & 255u) == 255u ? 1.f : 0.f);
                         n = mma(where, seen[c], n);
                     }
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) vse[i][q] &= ~((nan_scales(vse[i][q]) >> 7) * 0xffu);
+                    for (int q = 0; q < 4; ++q) x.vs[i][q] &= ~((nan_scales(x.vs[i][q]) >> 7) * 0xffu);
                     // A lane's dimensions have their scale in common: the same in all of their tiles.
 #pragma unroll
                     for (int d = i * (DT / NS); d < (i + 1) * (DT / NS); ++d)
@@ -380,16 +423,21 @@ attention4_few_kernel(const AttentionParams p, int blocks)
         for (int c = 0; c < 2; ++c)
 #pragma unroll
             for (int i = 0; i < NS; ++i) {
+                i32x4 va = x.v[i][2 * c], vb = x.v[i][2 * c + 1];
+                if (DP == 64 && (r & 1)) {         // the other half of the pieces' dimensions
+                    va >>= 16;
+                    vb >>= 16;
+                }
                 float sv[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) sv[j] = scale_of(vse[i][2 * c + j / 4], j & 3);
+                for (int j = 0; j < 8; ++j) sv[j] = scale_of(x.vs[i][2 * c + j / 4], j & 3);
                 auto pair = [&](auto sel) {
                     constexpr int SEL = decltype(sel)::value;
                     f16x8 even, odd;
-                    turn4<SEL>(vraw[i][2 * c], vraw[i][2 * c + 1], sv, even, odd);
-                    f32x4 &x = acc[i * (DT / NS) + 2 * SEL], &y = acc[i * (DT / NS) + 2 * SEL + 1];
-                    x = mma(even, pf[c], x);
-                    y = mma(odd, pf[c], y);
+                    turn4<SEL>(va, vb, sv, even, odd);
+                    f32x4 &a = acc[i * (DT / NS) + 2 * SEL], &b = acc[i * (DT / NS) + 2 * SEL + 1];
+                    a = mma(even, pf[c], a);
+                    b = mma(odd, pf[c], b);
                 };
                 pair(std::integral_constant<int, 0>{});
                 pair(std::integral_constant<int, 1>{});
@@ -398,8 +446,14 @@ attention4_few_kernel(const AttentionParams p, int blocks)
                     pair(std::integral_constant<int, 3>{});
                 }
             }
+    };
+    for (int step = from + wave; step < to; step += 2 * kWaves) {
+        body(step, one, other);
+        if (step + kWaves < to) body(step + kWaves, other, one);
     }
-    if (high == 0) {      // a row that sees no key, whatever the others see
+    if (none) {
+        m = -__builtin_inff();
+        l = 0.f;
 #pragma unroll
         for (int d = 0; d < DT; ++d) acc[d] = f32x4{};
     }
@@ -452,6 +506,9 @@ attention4_few_kernel(const AttentionParams p, int blocks)
 // The products are 32 x 32: one query a lane and 32 keys of it, 8 of each 16. Row 8 w + 4 hf + e of tile
 // tt is key 32 tt + 16 (w / 2) + 8 hf + 4 (w % 2) + e: lane half hf then holds the keys that it
 // contracts in the second product.
+//
+// Bound by the matrix instructions and the exponentials between them, which two waves of a SIMD overlap in
+// part: 2 x 1000 queries of 32 heads over up to 8000 keys of 8 heads of 128 take 246 us, 970 TFLOP/s.
 template <typename T, int DP, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES, DP <= 128 ? 2 : 1)
 attention4_many_kernel(const AttentionParams p, int blocks, int bhs)
@@ -583,21 +640,23 @@ attention4_many_kernel(const AttentionParams p, int blocks, int bhs)
         nans[buf][wave] = __any(nan != 0);
     };
     // Part u of what fetch() read, to LDS: 8 dimensions of a key, or 2 of 4 tokens' values, turned
-    // around. (Every other lane writes its two rows in the other order, so that all banks have work.)
+    // around. (Every other lane writes its two rows in the other order, so that all banks have work.) A part's place
+    // differs from the first one's in bits that are 0 there or are exclusive-ored by the order; it is formed anew
+    // each time, since registers are short.
     constexpr int kParts = kRuns * kWords * 2;
     const int odd = DP == 64 ? (vgroup >> 3) & 1 : vgroup & 1;
     const uint32_t first = odd ? 0x07060302u : 0x05040100u, second = odd ? 0x05040100u : 0x07060302u;
+    int kput = (wave * kRuns * 16 + kkey) * DP * 2 + (((lane & 3) * kWords) ^ order(kkey)) * 16;
+    int vput = kKeys + vgroup * (DP == 64 ? 4 : 8) * 128 + odd * 128 +
+               ((wave * kRuns * 2 + (quad >> 1)) ^ vorder(vgroup * (DP == 64 ? 4 : 8))) * 16 + (quad & 1) * 8;
+    int vnext = odd ? -128 : 128;
     auto put = [&](auto part, int buf) {
         constexpr int u = decltype(part)::value;
         constexpr int q = u / (2 * kWords), c = u / 2 % kWords;
-        const int which = wave * kRuns + q;
-        uint8_t *const ks = lds[buf], *const vs = ks + kKeys;
         if constexpr (u % 2 == 0) {
-            const int key = which * 16 + kkey, piece = (lane & 3) * kWords + c;
-            *reinterpret_cast<v8 *>(ks + key * DP * 2 + (piece ^ order(key)) * 16) = operand4<T>(kraw[q][c], scale4(kse[q][c * NS / kWords]));
+            *reinterpret_cast<v8 *>(lds[buf] + ((kput ^ c * 16) + q * 16 * DP * 2)) = operand4<T>(kraw[q][c], scale4(kse[q][c * NS / kWords]));
         } else {
             constexpr int i = DP == 256 ? c / 4 : 0, sel = c % 4;
-            const int d = (DP == 64 ? vgroup * 4 : i * 128 + vgroup * 8) + sel * 2;
             uint32_t x[4];
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
@@ -605,11 +664,9 @@ attention4_many_kernel(const AttentionParams p, int blocks, int bhs)
                 const f16x2 y = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(DP == 64 ? w >> (16 * (vgroup & 1)) : w, scale_of(vse[q][i], t), sel);
                 x[t] = __builtin_bit_cast(uint32_t, y);
             }
-            uint8_t *const to = vs + ((which * 2 + (quad >> 1)) ^ vorder(d)) * 16 + (quad & 1) * 8;
-            *reinterpret_cast<i32x2 *>(to + (d + odd) * 128) =
-                i32x2{int(__builtin_amdgcn_perm(x[1], x[0], first)), int(__builtin_amdgcn_perm(x[3], x[2], first))};
-            *reinterpret_cast<i32x2 *>(to + (d + 1 - odd) * 128) =
-                i32x2{int(__builtin_amdgcn_perm(x[1], x[0], second)), int(__builtin_amdgcn_perm(x[3], x[2], second))};
+            uint8_t *const to = lds[buf] + ((vput ^ (q * 2 ^ sel) * 16) + (i * 128 + sel * 2) * 128);
+            *reinterpret_cast<i32x2 *>(to) = i32x2{int(__builtin_amdgcn_perm(x[1], x[0], first)), int(__builtin_amdgcn_perm(x[3], x[2], first))};
+            *reinterpret_cast<i32x2 *>(to + vnext) = i32x2{int(__builtin_amdgcn_perm(x[1], x[0], second)), int(__builtin_amdgcn_perm(x[3], x[2], second))};
         }
     };
     // Pages of this step and the next, and the table's entry of the one after.
@@ -629,12 +686,15 @@ attention4_many_kernel(const AttentionParams p, int blocks, int bhs)
     // A step mixes what does not depend on each other, product by product (each is issued in
     // a few clocks and takes 32): into the first products the transfer of the next step's keys
     // to LDS, into the second ones the weights that the products after them need. What they
-    // read from LDS is read eight products ahead.
-    constexpr int kFirst = 2 * QC, kSecond = 4 * DT, kAhead = 8;
+    // read from LDS is read four products ahead (eight: 249 us for 246, heads of 256 269 for 230: registers).
+    // A wave goes first while it has its first products, so that the two of a SIMD come to do different
+    // things (246 us, without 261).
+    constexpr int kFirst = 2 * QC, kSecond = 4 * DT, kAhead = 4;
     const int krow = (r >> 4) * 16 + ((r >> 2) & 1) * 8 + ((r >> 3) & 1) * 4 + (r & 3);     // row r's key in tile 0
     auto body = [&](int step, auto which_buf) {
         constexpr int buf = decltype(which_buf)::value;
         const int base = step * kStep;
+        asm("" : "+v"(kput), "+v"(vput));
         wait_lds();
         barrier();
         const uint8_t *const kt = lds[buf] + krow * DP * 2, *const vt = lds[buf] + kKeys + r * 128;
@@ -691,6 +751,7 @@ attention4_many_kernel(const AttentionParams p, int blocks, int bhs)
             note_nans(step + 1, buf ^ 1);
         }
         f32x16 s[2];
+        __builtin_amdgcn_s_setprio(1);
         unroll<0, kFirst>([&](auto nth) {
             constexpr int n = decltype(nth)::value;
             s[n % 2] = mma32(kf[n % kAhead], qf[n / 2], n < 2 ? f32x16{} : s[n % 2]);
@@ -698,6 +759,7 @@ attention4_many_kernel(const AttentionParams p, int blocks, int bhs)
             unroll<n * kParts / kFirst, (n + 1) * kParts / kFirst>([&](auto u) { put(u, buf ^ 1); });
             __builtin_amdgcn_sched_barrier(0);
         });
+        __builtin_amdgcn_s_setprio(0);
         f16x8 vf[kAhead];
 #pragma unroll
         for (int n = 0; n < kAhead; ++n) vf[n] = value_part(n);
