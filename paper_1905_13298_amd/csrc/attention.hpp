@@ -30,6 +30,7 @@ struct AttentionParams {
     int window, splits, rows, row_tiles;
     float scale;                 // |softmax scale| * log2(e)
     int negative;                // the scale is: the queries are taken with the other sign
+    int least;                   // steps of a split, where it has any
 };
 
 template <typename T> struct Vec8;
@@ -143,27 +144,30 @@ __device__ __forceinline__ void store_row(const AttentionParams &p, int b, int h
 
 __device__ __forceinline__ float inverse(float total) { return total > 0.f ? 1.f / total : total == 0.f ? 0.f : total; }
 
-// The splits of a row together: a block of 4 waves per row, LANES lanes (4 dimensions each)
-// per split, so that 16 or 8 or 4 splits are read at once. A few us (64 splits of 32 rows: 3), behind
-// the launch that writes them.
-template <typename T, int LANES>
-__global__ void __launch_bounds__(256)
+// The splits of a row together: a block of THREADS per row, LANES lanes (4 dimensions each)
+// per split, so that 16 or 8 or 4 splits (of 256 threads) are read at once. A few us (64 splits of 32 rows: 3), behind
+// the launch that writes them. A split without keys may have no results, only its maximum of -inf.
+template <typename T, int LANES, int THREADS = 256>
+__global__ void __launch_bounds__(THREADS)
 attention_join_kernel(const AttentionParams p)
 {
-    constexpr int kAtOnce = 256 / LANES;
-    __shared__ float red[2][4];
-    __shared__ f32x4 sums[256];
+    constexpr int kAtOnce = THREADS / LANES, kWaves = THREADS / 64;
+    __shared__ float red[2][kWaves];
+    __shared__ f32x4 sums[THREADS];
     const int64_t at = blockIdx.x;
     const int D = p.dim, d = int(threadIdx.x % LANES) * 4, mine = int(threadIdx.x) / LANES;
     const float *part = p.part + at * p.splits * (D + 2);
     float top = -__builtin_inff();
-    for (int s = threadIdx.x; s < p.splits; s += 256) top = fmaxf(top, part[s * (D + 2) + D]);
+    for (int s = threadIdx.x; s < p.splits; s += THREADS) top = fmaxf(top, part[s * (D + 2) + D]);
     top = lanes_max<64>(top);
     if ((threadIdx.x & 63) == 0) red[0][threadIdx.x >> 6] = top;
     __syncthreads();
-    const float sub = or_zero(fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3])));
+    top = red[0][0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, red[0][w]);
+    const float sub = or_zero(top);
     float total = 0.f;
-    for (int s = threadIdx.x; s < p.splits; s += 256)
+    for (int s = threadIdx.x; s < p.splits; s += THREADS)
         total = fmaf(part[s * (D + 2) + D + 1], __builtin_amdgcn_exp2f(part[s * (D + 2) + D] - sub), total);
     total = lanes_sum<64>(total);
     if ((threadIdx.x & 63) == 0) red[1][threadIdx.x >> 6] = total;
@@ -171,10 +175,11 @@ attention_join_kernel(const AttentionParams p)
     if (d < D) {
 #pragma unroll 4
         for (int s = mine; s < p.splits; s += kAtOnce) {
-            const float f = __builtin_amdgcn_exp2f(part[s * (D + 2) + D] - sub);
+            const float m = part[s * (D + 2) + D], f = __builtin_amdgcn_exp2f(m - sub);
             f32x4 x;
             __builtin_memcpy(&x, part + s * (D + 2) + d, 16);
-            o += x * f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] += m == -__builtin_inff() ? 0.f : x[i] * f;
         }
     }
     sums[threadIdx.x] = o;
@@ -182,8 +187,11 @@ attention_join_kernel(const AttentionParams p)
     if (mine != 0 || d >= D) return;
 #pragma unroll
     for (int i = 1; i < kAtOnce; ++i) o += sums[i * LANES + threadIdx.x];
+    total = red[1][0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) total += red[1][w];
     const int64_t bh = at / p.rows;
-    store_row<T>(p, int(bh / p.heads), int(bh % p.heads), int(at - bh * p.rows), nullptr, d, o, inverse(red[1][0] + red[1][1] + red[1][2] + red[1][3]));
+    store_row<T>(p, int(bh / p.heads), int(bh % p.heads), int(at - bh * p.rows), nullptr, d, o, inverse(total));
 }
 
 bool page_ok(int64_t page) { return page == 16 || page == 32 || page == 64 || page == 128; }
@@ -204,6 +212,7 @@ ds_status check_cache(int64_t batch, int64_t tokens, int64_t heads, int64_t dim,
 struct Plan {
     int waves, splits, row_tiles;      // waves 0: few queries of a head
     int64_t rows;
+    int least = 1;                     // steps of a split, where it has any
 };
 
 int64_t part_floats(const Plan &a, int64_t batch, int64_t heads, int64_t dim)

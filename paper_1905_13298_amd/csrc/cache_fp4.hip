@@ -216,8 +216,10 @@ __device__ __forceinline__ void unroll(F &&f)
     }
 }
 
-// 16 queries of a kv head: a block of 4 waves takes a share of the keys, each wave every fourth
-// 64 of it straight from memory to registers, and joins them at its end.
+// Up to 16 queries of a kv head (tokens being decoded): a block of 4 waves takes a share of the keys, each wave
+// every fourth 64 of it straight from memory to registers (no two waves share any), and joins them at its end.
+// Bound by reading the cache once, and by the blocks' starts and ends: 131072 keys of 8 heads of 128, 143 MB, 30.3 us
+// (4.7 TB/s) and 4.1 of joining; its VALU instructions, a third of them conversions, would take a third of that.
 template <typename T, int DP>
 __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1)
 attention4_few_kernel(const AttentionParams p, int blocks)
@@ -233,29 +235,21 @@ attention4_few_kernel(const AttentionParams p, int blocks)
     const int split = int(blockIdx.x), bh = int(blockIdx.y), b = bh / p.heads, h = bh - b * p.heads;
     const int D = p.dim, page = 1 << p.page_shift, row = r;
     const Sequence seq(p, b);
-    v8 qf[QC];
-    int low, high;
-    load_query<T, DP, 8, DP / 4, QC>(p, seq, b, h, row, g, low, high, qf);
-    // (Rows that see no key, which are 0 in the end, have no say.)
-    int tlo = high > 0 ? low : 0x7fffffff, thi = high, alo = low, ahi = high > 0 ? high : 0x7fffffff;
-#pragma unroll
-    for (int o = 8; o > 0; o >>= 1) {
-        tlo = min(tlo, __shfl_xor(tlo, o));
-        thi = max(thi, __shfl_xor(thi, o));
-        alo = max(alo, __shfl_xor(alo, o));
-        ahi = min(ahi, __shfl_xor(ahi, o));
-    }
-    // Keys that some query sees: [tlo, thi); that every one sees: [alo, ahi).
-    tlo = __builtin_amdgcn_readfirstlane(tlo);
-    thi = __builtin_amdgcn_readfirstlane(thi);
-    alo = __builtin_amdgcn_readfirstlane(alo);
-    ahi = __builtin_amdgcn_readfirstlane(ahi);
-    // Such a row takes part as if it saw every key, which costs less than no key.
-    const bool none = high == 0;
-    if (none) high = 0x7fffffff;
-    const int s0 = thi > 0 ? tlo / kStep : 0, s1 = (thi + kStep - 1) / kStep;
-    const int each = (s1 - s0 + p.splits - 1) / p.splits;
+    // Keys that some query sees lie in [tlo, thi); every query that sees any sees [alo, ahi).
+    const int t1 = min(seq.count, p.tokens) - 1, t0 = min(max(-seq.first, 0), max(t1, 0));      // the first query that is not before the first key
+    const int thi = t1 >= t0 ? min(max(seq.first + t1 + 1, 0), seq.keys) : 0, ahi = min(max(seq.first + t0 + 1, 0), seq.keys);
+    const int tlo = p.window ? max(seq.first + t0 + 1 - p.window, 0) : 0, alo = p.window ? max(seq.first + t1 + 1 - p.window, 0) : 0;
+    const int s0 = thi > tlo ? tlo / kStep : 0, s1 = thi > tlo ? (thi + kStep - 1) / kStep : 0;
+    const int each = max((s1 - s0 + p.splits - 1) / p.splits, p.least);
     const int from = s0 + split * each, to = min(s1, from + each);
+    float *const part = p.part ? p.part + ((int64_t(bh) * p.rows + r) * p.splits + split) * (D + 2) : nullptr;
+    if (part && from >= to) {      // nothing here: no results, only that there are none
+        if (wave == 0 && g == 0 && r < p.rows) {
+            part[D] = -__builtin_inff();
+            part[D + 1] = 0.f;
+        }
+        return;
+    }
 
     f32x4 acc[DT];
     float m = -__builtin_inff(), l = 0.f;
@@ -321,25 +315,25 @@ attention4_few_kernel(const AttentionParams p, int blocks)
         }
         x.vp = vp;
     };
-    // The next step's keys and values are on their way while this one's are worked on, and the pages of
-    // the one after.
-    Step one, other;
+    // The next step's pages are looked up while this one's keys and values are worked on. (Those themselves a step
+    // ahead: 38.1 us instead of 35.2 for 131072 keys, 64.7 and 61.1 for 48 x 1: registers for a third wave of a SIMD.)
     int kp = -1, vp = -1;
     auto look = [&](int step) {
         kp = page_of(step * kStep + (r >> 2) * 16);
         vp = page_of(step * kStep + g * 16);
     };
-    if (from + wave < to) {
-        look(from + wave);
-        fetch(from + wave, kp, vp, one);
-        look(from + wave + kWaves);
-    }
-    auto body = [&](int step, Step &x, Step &ahead) {
+    look(from + wave);
+    v8 qf[QC];
+    int low, high;
+    load_query<T, DP, 8, DP / 4, QC>(p, seq, b, h, row, g, low, high, qf);
+    // A row that sees no key, and is 0 in the end, takes part as if it saw every one, which costs less.
+    const bool none = high == 0;
+    if (none) high = 0x7fffffff;
+    for (int step = from + wave; step < to; step += kWaves) {
+        Step x;
         const int base = step * kStep, vrun = base + g * 16;
-        if (step + kWaves < to) {
-            fetch(step + kWaves, kp, vp, ahead);
-            look(step + 2 * kWaves);
-        }
+        fetch(step, kp, vp, x);
+        look(step + kWaves);
         const bool there = x.vp >= 0;
         f32x4 s[4];
 #pragma unroll
@@ -446,10 +440,6 @@ attention4_few_kernel(const AttentionParams p, int blocks)
                     pair(std::integral_constant<int, 3>{});
                 }
             }
-    };
-    for (int step = from + wave; step < to; step += 2 * kWaves) {
-        body(step, one, other);
-        if (step + kWaves < to) body(step + kWaves, other, one);
     }
     if (none) {
         m = -__builtin_inff();
@@ -479,7 +469,6 @@ attention4_few_kernel(const AttentionParams p, int blocks)
         for (int w = 0; w < 4; ++w) osum[wave][d + w][lane] = f32x4{acc[d][w], acc[d + 1][w], acc[d + 2][w], acc[d + 3][w]} * mine;
     __syncthreads();
     if (row >= p.rows) return;
-    float *part = p.part ? p.part + ((int64_t(bh) * p.rows + row) * p.splits + split) * (D + 2) : nullptr;
     if (part && wave == 0 && g == 0) {
         part[D] = top;
         part[D + 1] = total;
@@ -850,7 +839,12 @@ attention4_many_kernel(const AttentionParams p, int blocks, int bhs)
 }
 
 // How a call is split: over the rows first, then over the keys until 512 blocks (two a CU) have at
-// least 8 steps of 64 keys each.
+// least 8 steps of 64 keys each. Measured (8 heads of 128, 4 query heads each; us): one query over 131072 keys 34.7,
+// with 768 blocks 36.9, with 1024 43; 16 x 1 over up to 8192 23.5, 22.7 and 28. Where sequences and heads alone
+// make more than 256 blocks of few queries, whose lengths may differ, until 1536 have at least 16 steps each: 48 x 1 over
+// up to 8192 55.5, until 512 60.4, until 3072 70; 64 x 1 over up to 16000 131, 16 splits each 170. (Splits have the same
+// number of steps, so that a sequence much longer than 63 others is what a call waits for.)
+// Up to 16 rows run attention4_few_kernel; from 17 to 64 rows blocks of two waves, above of four.
 Plan plan_attention4(int64_t batch, int64_t tokens, int64_t heads, int64_t group, int64_t columns, int64_t page)
 {
     Plan a;
@@ -858,7 +852,10 @@ Plan plan_attention4(int64_t batch, int64_t tokens, int64_t heads, int64_t group
     a.waves = a.rows <= 16 ? 0 : a.rows <= 64 ? 2 : 4;
     a.row_tiles = a.waves ? int((a.rows + 32 * a.waves - 1) / (32 * a.waves)) : 1;
     const int64_t blocks = std::max<int64_t>(batch * heads * a.row_tiles, 1), steps = (columns * page + kStep - 1) / kStep;
-    a.splits = int(std::max<int64_t>(1, std::min<int64_t>({a.waves ? 512 / blocks : (511 + blocks) / blocks, (steps + 7) / 8, 256})));
+    const bool uneven = a.waves == 0 && blocks > 256;
+    a.least = uneven ? 16 : 8;
+    const int64_t most = uneven ? (1535 + blocks) / blocks : a.waves ? 512 / blocks : (511 + blocks) / blocks;
+    a.splits = int(std::max<int64_t>(1, std::min<int64_t>({most, (steps + a.least - 1) / a.least, 256})));
     return a;
 }
 
@@ -1046,7 +1043,7 @@ extern "C" ds_status ds_attention_fp4(const void *q, const uint8_t *k_cache, con
                             need ? static_cast<float *>(scratch) : nullptr, ldt, q_strides[0], q_strides[1], q_strides[2],
                             o_strides[0], o_strides[1], o_strides[2], int(columns), int(pages), int(tokens), int(heads),
                             int(group), int(dim), page_shift(page), int(window), a.splits, int(a.rows), a.row_tiles,
-                            std::max(std::fabs(scale) * 1.44269504f, 0x1p-126f), scale < 0};
+                            std::max(std::fabs(scale) * 1.44269504f, 0x1p-126f), scale < 0, a.least};
     const auto s = static_cast<hipStream_t>(stream);
     if (type == DS_TYPE_F16) run_attention4<_Float16>(p, a, batch, s);
     else run_attention4<__bf16>(p, a, batch, s);
