@@ -746,7 +746,8 @@ ds_status ds_rotary_norm_backward(const void *dq_out, const void *dk_out, const 
                                   int32_t interleaved, float eps, int32_t type,
                                   int32_t weight_type, int32_t frequency_type, void *scratch,
                                   int64_t scratch_bytes, void *stream);
-int64_t ds_rotary_norm_backward_scratch_bytes(int64_t batch, int64_t tokens, int64_t dim);
+int64_t ds_rotary_norm_backward_scratch_bytes(int64_t batch, int64_t tokens, int64_t heads,
+                                              int64_t kv_heads, int64_t dim);
 
 /* A paged cache of keys and values in 4 bits: E2M1 numbers (0, 0.5, 1, 1.5, 2, 3, 4, 6 with codes 0 .. 7,
  * and 8 for the sign), two a byte, the first in the low half, and an E8M0 scale for each token, head and

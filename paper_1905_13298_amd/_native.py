@@ -73,7 +73,7 @@ SIGNATURES = {
     "ds_attention_fp8_scratch_bytes": (_I64, [_I64] * 7),
     "ds_rotary_norm": (ctypes.c_int, [_P] * 8 + [_I64] * 7 + [_P] * 6 + [_I32, _F32] + [_I32] * 3 + [_P]),
     "ds_rotary_norm_backward": (ctypes.c_int, [_P] * 12 + [_I64] * 7 + [_P] * 8 + [_I32, _F32] + [_I32] * 3 + [_P, _I64, _P]),
-    "ds_rotary_norm_backward_scratch_bytes": (_I64, [_I64] * 3),
+    "ds_rotary_norm_backward_scratch_bytes": (_I64, [_I64] * 5),
     "ds_kv_cache_fp4_append": (ctypes.c_int, [_P] * 9 + [_I64] * 8 + [_P] * 2 + [_I32, _P]),
     "ds_kv_cache_fp4_read": (ctypes.c_int, [_P] * 9 + [_I64] * 8 + [_P] * 2 + [_I32, _P]),
     "ds_attention_fp4": (ctypes.c_int, [_P] * 9 + [_I64] * 9 + [_P] * 2 + [_F32, _I64, _I32, _P, _I64, _P]),

@@ -14,6 +14,7 @@
 #include <cmath>
 
 #include "conv_plan.hpp"
+#include "fastdiv.hpp"
 #include "fp8.hpp"
 
 namespace ds {
@@ -27,17 +28,21 @@ struct RotaryParams {
     const void *frequencies;
     int64_t pa, pb, pt;                // strides of the positions: axis, sequence, token
     int64_t in[2][3], out[2][3], grad[2][3];   // of q and k, their results, and (gradient) what comes in: sequence, token, head
-    int64_t rows;                      // batch * tokens
-    int tokens, heads[2], dim, pairs, interleaved, wide;     // wide: the frequencies have 64 bits
+    int rows;                          // batch * tokens
+    FastDiv tokens;
+    int heads[2], dim, pairs, interleaved, wide;     // wide: the frequencies have 64 bits
     int until[kMaxAxes];               // the pair that an axis ends before
     float eps;
+    int per, chunks;                   // groups of heads that a wave takes, and how many times that q has
+    int blocks;                        // of the gradient's launch, those of q
 };
 
 // A lane's 16 elements of a vector: 8 pairs from pair 8 * lane on. Pairs past `pairs`, of the elements
-// that are not turned, are made up likewise. WHOLE: the lane's elements are two runs of 8 that
-// begin at `first` and `second`; otherwise one by one.
+// that are not turned, are made up likewise. RUN: so many of the lane's first (and second) elements
+// lie together: 8, 4 or 1.
+template <int RUN>
 struct Lane {
-    int j0, first, second, half, pairs, rest, interleaved;
+    int j0, half, pairs, rest, interleaved;
     __device__ __forceinline__ Lane(const RotaryParams &p, int lane)
     {
         half = p.dim / 2;
@@ -45,8 +50,6 @@ struct Lane {
         rest = half - pairs;
         interleaved = p.interleaved;
         j0 = lane * 8;
-        first = where(j0, 0);
-        second = interleaved ? j0 * 2 + 8 : where(j0, 1);
     }
     // The element of a pair.
     __device__ __forceinline__ int where(int j, int which) const
@@ -55,46 +58,61 @@ struct Lane {
         return j < pairs ? j + which * pairs : pairs + j + which * rest;
     }
     // The pairs' elements a[i], b[i].
-    template <bool WHOLE, typename T>
+    template <typename T>
     __device__ __forceinline__ void load(const T *p, float (&a)[8], float (&b)[8]) const
     {
-        if constexpr (WHOLE) {
-            float x[8], y[8];
-            load8(p + first, 8, x);
-            load8(p + second, 8, y);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float e = i < 4 ? x[(2 * i) & 7] : y[(2 * i) & 7], o = i < 4 ? x[(2 * i + 1) & 7] : y[(2 * i + 1) & 7];
-                a[i] = interleaved ? e : x[i];
-                b[i] = interleaved ? o : y[i];
-            }
-        } else {
+        if constexpr (RUN == 1) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 a[i] = j0 + i < half ? float(p[where(j0 + i, 0)]) : 0.f;
                 b[i] = j0 + i < half ? float(p[where(j0 + i, 1)]) : 0.f;
             }
-        }
-    }
-    template <bool WHOLE, typename T>
-    __device__ __forceinline__ void store(T *p, const float (&a)[8], const float (&b)[8]) const
-    {
-        if constexpr (WHOLE) {
-            float x[8], y[8];
+        } else {
+            // Two pieces of RUN elements for RUN pairs.
+            T x[8], y[8];
+#pragma unroll
+            for (int i = 0; i < 8; i += RUN) {
+                if (RUN < 8 && j0 + i >= half) {
+#pragma unroll
+                    for (int e = 0; e < RUN; ++e) x[i + e] = y[i + e] = T(0.f);
+                    continue;
+                }
+                __builtin_memcpy(x + i, p + where(j0 + i, 0), RUN * sizeof(T));
+                __builtin_memcpy(y + i, p + (interleaved ? 2 * (j0 + i) + RUN : where(j0 + i, 1)), RUN * sizeof(T));
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float lo = i & 1 ? b[i / 2] : a[i / 2], hi = i & 1 ? b[4 + i / 2] : a[4 + i / 2];
-                x[i] = interleaved ? lo : a[i];
-                y[i] = interleaved ? hi : b[i];
+                const int of = i / RUN * RUN, in = i % RUN * 2;        // (interleaved: place in the two pieces)
+                const T e = in < RUN ? x[of + in % RUN] : y[of + in % RUN], o = in < RUN ? x[of + in % RUN + 1] : y[of + in % RUN + 1];
+                a[i] = float(interleaved ? e : x[i]);
+                b[i] = float(interleaved ? o : y[i]);
             }
-            store8(p + first, 8, x);
-            store8(p + second, 8, y);
-        } else {
+        }
+    }
+    template <typename T>
+    __device__ __forceinline__ void store(T *p, const float (&a)[8], const float (&b)[8]) const
+    {
+        if constexpr (RUN == 1) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 if (j0 + i >= half) continue;
                 p[where(j0 + i, 0)] = T(a[i]);
                 p[where(j0 + i, 1)] = T(b[i]);
+            }
+        } else {
+            T x[8], y[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int of = i / RUN * RUN, in = i % RUN;
+                const float lo = in & 1 ? b[of + in / 2] : a[of + in / 2], hi = in & 1 ? b[of + RUN / 2 + in / 2] : a[of + RUN / 2 + in / 2];
+                x[i] = T(interleaved ? lo : a[i]);
+                y[i] = T(interleaved ? hi : b[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; i += RUN) {
+                if (RUN < 8 && j0 + i >= half) continue;
+                __builtin_memcpy(p + where(j0 + i, 0), x + i, RUN * sizeof(T));
+                __builtin_memcpy(p + (interleaved ? 2 * (j0 + i) + RUN : where(j0 + i, 1)), y + i, RUN * sizeof(T));
             }
         }
     }
@@ -115,167 +133,171 @@ __device__ __forceinline__ void turn_of(double t, float &cosine, float &sine)
     sine = q & 2 ? -w : w;
 }
 
-// The angles of a lane's pairs for one token.
-__device__ __forceinline__ void angles(const RotaryParams &p, const Lane &lane, int64_t b, int64_t t, float (&cosine)[8], float (&sine)[8])
+// The angles of a lane's pairs for one token. The wave's lanes work each out once and hand them on to the lanes
+// of all its heads (every lane for itself: 55 us instead of 37 where a wave has one group of heads of 4 x 2001 tokens).
+template <int LPV, int RUN>
+__device__ __forceinline__ void angles(const RotaryParams &p, const Lane<RUN> &lane, int b, int t, float (&cosine)[8], float (&sine)[8])
 {
+    constexpr int kEach = LPV > 8 ? LPV / 8 : 1;         // pairs of a lane: those from 8 l + kEach * sub on
+    const int l = lane.j0 / 8, sub = int(threadIdx.x & 63) / LPV;
     const int *at = p.positions + b * p.pb + t * p.pt;
+    float c[kEach], s[kEach];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int j = lane.j0 + i;
-        cosine[i] = 1.f;
-        sine[i] = 0.f;
+    for (int i = 0; i < kEach; ++i) {
+        const int j = lane.j0 + (sub * kEach + i) % 8;
+        c[i] = 1.f;
+        s[i] = 0.f;
         if (j >= p.pairs) continue;
         const int axis = (j >= p.until[0]) + (j >= p.until[1]) + (j >= p.until[2]);
         const double f = p.wide ? static_cast<const double *>(p.frequencies)[j] : double(static_cast<const float *>(p.frequencies)[j]);
-        turn_of(double(at[axis * p.pa]) * (f * 0.15915494309189533577), cosine[i], sine[i]);
+        turn_of(double(at[axis * p.pa]) * (f * 0.15915494309189533577), c[i], s[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        cosine[i] = __shfl(c[i % kEach], i / kEach * LPV + l);
+        sine[i] = __shfl(s[i % kEach], i / kEach * LPV + l);
     }
 }
 
-// A wave has one token at a time and LPV lanes for each of 64 / LPV heads at once, so that a
-// token's angles are found once for all of its heads.
-template <typename T, typename W, int LPV, bool WHOLE>
+// A wave has one token and LPV lanes for each of 64 / LPV heads of q or k at once, a group; it takes up to 4 groups of its
+// token, where there are tokens enough, so that angles and weight are found once for them. Bound by bandwidth: 4 x 2001 tokens
+// of 32 + 8 heads of 128, 164 MB, 30.1 us (5.4 TB/s, some of it from the caches); 8 x 1 tokens 3.2 us, the launch's trip.
+template <typename T, typename W, int LPV, int RUN>
 __global__ void __launch_bounds__(256)
 rotary_kernel(const T *__restrict__ q, const T *__restrict__ k, const W *__restrict__ qw, const W *__restrict__ kw, T *__restrict__ qo,
               T *__restrict__ ko, const RotaryParams p)
 {
     constexpr int kHeads = 64 / LPV;
     const int lane = int(threadIdx.x & 63), sub = lane / LPV;
-    const int64_t row = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    const int row = __builtin_amdgcn_readfirstlane(int(blockIdx.x) * 4 + int(threadIdx.x >> 6));
     if (row >= p.rows) return;
-    const int64_t b = row / p.tokens, t = row - b * p.tokens;
-    const Lane me(p, lane % LPV);
+    const int b = fdiv(row, p.tokens), t = row - b * int(p.tokens.d);
+    const Lane<RUN> me(p, lane % LPV);
     const bool some = me.j0 < me.half;
-    float cosine[8], sine[8];
-    angles(p, me, b, t, cosine, sine);
+    const int which = int(blockIdx.y) >= p.chunks, first = (int(blockIdx.y) - which * p.chunks) * p.per * kHeads, heads = p.heads[which];
+    const W *const weight = which ? kw : qw;
+    const T *const src = (which ? k : q) + b * p.in[which][0] + t * p.in[which][1];
+    T *const dst = (which ? ko : qo) + b * p.out[which][0] + t * p.out[which][1];
+    float cosine[8], sine[8], wa[8] = {}, wb[8] = {};
+    if (weight && some) me.load(weight, wa, wb);
+    angles<LPV>(p, me, b, t, cosine, sine);
     const float inv = 1.f / float(p.dim);
+    for (int h0 = first; h0 < min(first + p.per * kHeads, heads); h0 += kHeads) {
+        const int h = h0 + sub;
+        const bool mine = some && h < heads;
+        float x[8] = {}, y[8] = {};
+        if (mine) me.load(src + h * p.in[which][2], x, y);
+        if (weight) {
+            float sum = 0.f;
 #pragma unroll
-    for (int which = 0; which < 2; ++which) {
-        const W *const weight = which ? kw : qw;
-        const T *const src = (which ? k : q) + b * p.in[which][0] + t * p.in[which][1];
-        T *const dst = (which ? ko : qo) + b * p.out[which][0] + t * p.out[which][1];
-        float wa[8] = {}, wb[8] = {};
-        if (weight && some) me.load<WHOLE>(weight, wa, wb);
-        for (int h0 = 0; h0 < p.heads[which]; h0 += kHeads) {
-            const int h = h0 + sub;
-            const bool mine = some && h < p.heads[which];
-            float x[8] = {}, y[8] = {};
-            if (mine) me.load<WHOLE>(src + h * p.in[which][2], x, y);
-            if (weight) {
-                float sum = 0.f;
+            for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], fmaf(y[e], y[e], sum));
+            const float r = 1.f / sqrtf(fmaf(lanes_sum<LPV>(sum), inv, p.eps));
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], fmaf(y[i], y[i], sum));
-                const float r = 1.f / sqrtf(fmaf(lanes_sum<LPV>(sum), inv, p.eps));
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    x[i] *= r * wa[i];
-                    y[i] *= r * wb[i];
-                }
+            for (int e = 0; e < 8; ++e) {
+                x[e] *= r * wa[e];
+                y[e] *= r * wb[e];
             }
-            if (!mine) continue;
-            float u[8], v[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                u[i] = fmaf(x[i], cosine[i], -(y[i] * sine[i]));
-                v[i] = fmaf(y[i], cosine[i], x[i] * sine[i]);
-            }
-            me.store<WHOLE>(dst + h * p.out[which][2], u, v);
         }
+        if (!mine) continue;
+        float u[8], v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            u[e] = fmaf(x[e], cosine[e], -(y[e] * sine[e]));
+            v[e] = fmaf(y[e], cosine[e], x[e] * sine[e]);
+        }
+        me.store(dst + h * p.out[which][2], u, v);
     }
 }
 
-// The gradient: a wave goes through every so many tokens and keeps its sums for the weights, which the
-// block's waves add up in LDS, in a fixed order, into a row of `part` [block][q, k][dim].
-template <typename T, typename W, int LPV, bool WHOLE>
+// The gradient: a block has q or k; its waves go through every so many tokens' chunks and keep their sums for the
+// weight, which they add up in LDS, in a fixed order, into the block's row of `part`. Bound by bandwidth: 4 x 2048 tokens of 32 + 8
+// heads of 128, 252 MB, 52 us (4.8 TB/s) and 4 of adding up the rows.
+template <typename T, typename W, int LPV, int RUN>
 __global__ void __launch_bounds__(256)
 rotary_grad_kernel(const T *__restrict__ dq, const T *__restrict__ dk, const T *__restrict__ q, const T *__restrict__ k,
                    const W *__restrict__ qw, const W *__restrict__ kw, T *__restrict__ dqo, T *__restrict__ dko, float *__restrict__ part,
                    const RotaryParams p)
 {
     constexpr int kHeads = 64 / LPV;
-    __shared__ float red[4][2][LPV * 16];
-    const int lane = int(threadIdx.x & 63), wave = int(threadIdx.x >> 6), sub = lane / LPV;
-    const Lane me(p, lane % LPV);
+    __shared__ float red[4][LPV * 16];
+    const int lane = int(threadIdx.x & 63), wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), sub = lane / LPV;
+    const Lane<RUN> me(p, lane % LPV);
     const bool some = me.j0 < me.half;
     const float inv = 1.f / float(p.dim);
-    float sums[2][2][8] = {};
-    for (int64_t row = int64_t(blockIdx.x) * 4 + wave; row < p.rows; row += int64_t(gridDim.x) * 4) {
-        const int64_t b = row / p.tokens, t = row - b * p.tokens;
+    const int which = int(blockIdx.x) >= p.blocks, at = int(blockIdx.x) - which * p.blocks, blocks = which ? int(gridDim.x) - p.blocks : p.blocks;
+    const int heads = p.heads[which], chunk = p.per * kHeads, chunks = (heads + chunk - 1) / chunk;
+    const W *const weight = which ? kw : qw;
+    float wa[8] = {}, wb[8] = {}, da[8] = {}, db[8] = {};
+    if (weight && some) me.load(weight, wa, wb);
+    for (int64_t unit = at * 4 + wave; unit < int64_t(p.rows) * chunks; unit += blocks * 4) {
+        const int row = chunks == 1 ? int(unit) : int(unit / chunks), first = chunks == 1 ? 0 : int(unit - int64_t(row) * chunks) * chunk;
+        const int b = fdiv(row, p.tokens), t = row - b * int(p.tokens.d);
+        const T *const dy = (which ? dk : dq) + b * p.grad[which][0] + t * p.grad[which][1];
+        const T *const src = (which ? k : q) + b * p.in[which][0] + t * p.in[which][1];
+        T *const dst = (which ? dko : dqo) + b * p.out[which][0] + t * p.out[which][1];
         float cosine[8], sine[8];
-        angles(p, me, b, t, cosine, sine);
+        angles<LPV>(p, me, b, t, cosine, sine);
+        for (int h0 = first; h0 < min(first + chunk, heads); h0 += kHeads) {
+            const int h = h0 + sub;
+            const bool mine = some && h < heads;
+            float u[8] = {}, v[8] = {}, x[8] = {}, y[8] = {};
+            if (mine) {
+                me.load(dy + h * p.grad[which][2], u, v);
+                if (weight) me.load(src + h * p.in[which][2], x, y);
+            }
 #pragma unroll
-        for (int which = 0; which < 2; ++which) {
-            const W *const weight = which ? kw : qw;
-            const T *const dy = (which ? dk : dq) + b * p.grad[which][0] + t * p.grad[which][1];
-            const T *const src = (which ? k : q) + b * p.in[which][0] + t * p.in[which][1];
-            T *const dst = (which ? dko : dqo) + b * p.out[which][0] + t * p.out[which][1];
-            float wa[8] = {}, wb[8] = {};
-            if (weight && some) me.load<WHOLE>(weight, wa, wb);
-            for (int h0 = 0; h0 < p.heads[which]; h0 += kHeads) {
-                const int h = h0 + sub;
-                const bool mine = some && h < p.heads[which];
-                float u[8] = {}, v[8] = {}, x[8] = {}, y[8] = {};
-                if (mine) {
-                    me.load<WHOLE>(dy + h * p.grad[which][2], u, v);
-                    if (weight) me.load<WHOLE>(src + h * p.in[which][2], x, y);
-                }
+            for (int i = 0; i < 8; ++i) {
+                const float a = u[i], c = v[i];
+                u[i] = fmaf(a, cosine[i], c * sine[i]);
+                v[i] = fmaf(c, cosine[i], -(a * sine[i]));
+            }
+            if (weight) {
+                float sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], fmaf(y[i], y[i], sum));
+                const float r = 1.f / sqrtf(fmaf(lanes_sum<LPV>(sum), inv, p.eps));
+                sum = 0.f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float a = u[i], c = v[i];
-                    u[i] = fmaf(a, cosine[i], c * sine[i]);
-                    v[i] = fmaf(c, cosine[i], -(a * sine[i]));
+                    x[i] *= r;
+                    y[i] *= r;
+                    da[i] = fmaf(u[i], x[i], da[i]);
+                    db[i] = fmaf(v[i], y[i], db[i]);
+                    u[i] *= wa[i];
+                    v[i] *= wb[i];
+                    sum = fmaf(u[i], x[i], fmaf(v[i], y[i], sum));
                 }
-                if (weight) {
-                    float sum = 0.f;
+                const float mean = lanes_sum<LPV>(sum) * inv;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], fmaf(y[i], y[i], sum));
-                    const float r = 1.f / sqrtf(fmaf(lanes_sum<LPV>(sum), inv, p.eps));
-                    sum = 0.f;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        x[i] *= r;
-                        y[i] *= r;
-                        sums[which][0][i] = fmaf(u[i], x[i], sums[which][0][i]);
-                        sums[which][1][i] = fmaf(v[i], y[i], sums[which][1][i]);
-                        u[i] *= wa[i];
-                        v[i] *= wb[i];
-                        sum = fmaf(u[i], x[i], fmaf(v[i], y[i], sum));
-                    }
-                    const float mean = lanes_sum<LPV>(sum) * inv;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        u[i] = r * (u[i] - x[i] * mean);
-                        v[i] = r * (v[i] - y[i] * mean);
-                    }
+                for (int i = 0; i < 8; ++i) {
+                    u[i] = r * (u[i] - x[i] * mean);
+                    v[i] = r * (v[i] - y[i] * mean);
                 }
-                if (mine) me.store<WHOLE>(dst + h * p.out[which][2], u, v);
             }
+            if (mine) me.store(dst + h * p.out[which][2], u, v);
         }
     }
     if (!part) return;
 #pragma unroll
-    for (int which = 0; which < 2; ++which)
+    for (int e = 0; e < 2; ++e)
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
+        for (int i = 0; i < 8; ++i) {
+            float s = e ? db[i] : da[i];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float s = sums[which][e][i];
-#pragma unroll
-                for (int o = LPV; o < 64; o <<= 1) s += __shfl_xor(s, o);
-                if (sub == 0) red[wave][which][(lane * 2 + e) * 8 + i] = s;
-            }
+            for (int o = LPV; o < 64; o <<= 1) s += __shfl_xor(s, o);
+            if (sub == 0) red[wave][(lane * 2 + e) * 8 + i] = s;
+        }
     __syncthreads();
-    for (int at = int(threadIdx.x); at < 2 * LPV * 16; at += 256) {
-        const int which = at / (LPV * 16), rest = at - which * LPV * 16, j = rest / 16 * 8 + rest % 8, e = rest / 8 % 2;
-        if (j >= me.half) continue;
-        const float s = (red[0][which][rest] + red[1][which][rest]) + (red[2][which][rest] + red[3][which][rest]);
-        part[(int64_t(blockIdx.x) * 2 + which) * p.dim + me.where(j, e)] = s;
-    }
+    const int i = int(threadIdx.x), j = i / 16 * 8 + i % 8;
+    if (i < LPV * 16 && j < me.half)
+        part[int64_t(blockIdx.x) * p.dim + me.where(j, i / 8 % 2)] = (red[0][i] + red[1][i]) + (red[2][i] + red[3][i]);
 }
 
-// dweight = the sum over `parts` rows of part [row][q, k][dim]: a block adds 32 columns, 32 threads each.
+// dweight = the sum over the rows of part that the blocks of q (or of k, behind them) have written: a block adds 32
+// columns, 32 threads each.
 template <typename W>
 __global__ void __launch_bounds__(1024)
-rotary_grad_weight_kernel(const float *__restrict__ part, W *__restrict__ dqw, W *__restrict__ dkw, int parts, int dim)
+rotary_grad_weight_kernel(const float *__restrict__ part, W *__restrict__ dqw, W *__restrict__ dkw, int q_rows, int k_rows, int dim)
 {
     __shared__ float red[32][33];
     const int x = int(threadIdx.x & 31), y = int(threadIdx.x >> 5), which = int(blockIdx.y), c = int(blockIdx.x) * 32 + x;
@@ -284,7 +306,7 @@ rotary_grad_weight_kernel(const float *__restrict__ part, W *__restrict__ dqw, W
     float sum = 0.f;
     if (c < dim) {
 #pragma unroll 8
-        for (int i = y; i < parts; i += 32) sum += part[(int64_t(i) * 2 + which) * dim + c];
+        for (int i = (which ? q_rows : 0) + y; i < q_rows + (which ? k_rows : 0); i += 32) sum += part[int64_t(i) * dim + c];
     }
     red[y][x] = sum;
     __syncthreads();
@@ -296,15 +318,16 @@ rotary_grad_weight_kernel(const float *__restrict__ part, W *__restrict__ dqw, W
 }
 
 // f with the element type, the weights' (the same or float32), the lanes of a vector (8 pairs each) and
-// whether a lane's elements are two whole runs.
+// how many of a lane's elements lie together.
 template <typename F>
 void for_layout(const RotaryParams &p, int32_t type, int32_t wtype, F &&f)
 {
-    const bool whole = p.interleaved ? p.dim % 16 == 0 : p.pairs % 8 == 0 && p.dim % 16 == 0;
+    const int apart = p.interleaved ? p.dim / 2 : p.pairs | p.dim / 2;
     const auto layout = [&](auto t, auto w) {
         const auto lanes = [&](auto l) {
-            if (whole) f(t, w, l, std::true_type{});
-            else f(t, w, l, std::false_type{});
+            if (apart % 8 == 0) f(t, w, l, std::integral_constant<int, 8>{});
+            else if (apart % 4 == 0) f(t, w, l, std::integral_constant<int, 4>{});
+            else f(t, w, l, std::integral_constant<int, 1>{});
         };
         if (p.dim <= 64) lanes(std::integral_constant<int, 4>{});
         else if (p.dim <= 128) lanes(std::integral_constant<int, 8>{});
@@ -320,7 +343,30 @@ void for_layout(const RotaryParams &p, int32_t type, int32_t wtype, F &&f)
 }
 
 // Blocks of the gradient's launch, a row of the weights' sums each: four waves, a token each at a time.
-int rotary_grad_blocks(int64_t rows) { return int(std::min<int64_t>((rows + 3) / 4, 512)); }
+// Heads of a group (a wave has them at once), and how many groups it takes of a token.
+int heads_at_once(int64_t dim) { return dim <= 64 ? 16 : dim <= 128 ? 8 : 4; }
+
+struct Split {
+    int per, chunks[2];                // groups of heads that a wave takes; chunks of q and of k
+    int blocks[2];                     // of the gradient's launch: a row of the weights' sums each
+};
+
+// A wave takes up to 4 groups of a token (4 x 2001 tokens of 4 + 1 groups: 30.1 us, with 2 33.4, with 1 39.9), as long as 4096
+// waves have work (2 x 1221 tokens of 2 + 2 groups: 2 each 6.9 us, 1 each 8.1). The gradient has up to 1024 blocks, four a CU,
+// shared between q and k by their groups: 4 x 2048 tokens 56.2 us, with 768 56.9, with 512 66.0, with 256 103.
+Split split_heads(int64_t rows, int64_t heads, int64_t kv_heads, int64_t dim)
+{
+    Split a;
+    const int64_t once = heads_at_once(dim), groups = (heads + once - 1) / once, kv_groups = (kv_heads + once - 1) / once;
+    a.per = int(std::max<int64_t>(1, std::min<int64_t>(4, rows * (groups + kv_groups) / 4096)));
+    a.chunks[0] = int((groups + a.per - 1) / a.per);
+    a.chunks[1] = int((kv_groups + a.per - 1) / a.per);
+    for (int i = 0; i < 2; ++i) {
+        const int64_t share = std::max<int64_t>(1, 1024 * (i ? kv_groups : groups) / (groups + kv_groups));
+        a.blocks[i] = int(std::min<int64_t>((rows * a.chunks[i] + 3) / 4, share));
+    }
+    return a;
+}
 
 // What both directions check; bytes: those that q and k, and their results, span.
 ds_status rotary_params(RotaryParams &p, int64_t batch, int64_t tokens, int64_t heads, int64_t kv_heads, int64_t dim, int64_t pairs,
@@ -338,11 +384,11 @@ ds_status rotary_params(RotaryParams &p, int64_t batch, int64_t tokens, int64_t 
     if (frequency_type != DS_TYPE_F32 && frequency_type != DS_TYPE_F64)
         return fail(DS_ERR_INVALID_ARG, "frequencies must be DS_TYPE_F32 or DS_TYPE_F64");
     if (!(eps >= 0.f)) return fail(DS_ERR_INVALID_ARG, "eps must be >= 0");
-    if (heads > 65535 || kv_heads > 65535 || batch > kMaxElems || tokens > kMaxElems || batch * tokens > kMaxElems)
+    if (heads > 65535 || kv_heads > 65535 || batch > kMaxElems || tokens > kMaxElems || batch * tokens > kMaxElems - 4096)
         return fail(DS_ERR_UNSUPPORTED, "too many heads or tokens");
     p = RotaryParams{};
-    p.rows = batch * tokens;
-    p.tokens = int(tokens);
+    p.rows = int(batch * tokens);
+    p.tokens = make_fastdiv(uint32_t(std::max<int64_t>(tokens, 1)));
     p.heads[0] = int(heads);
     p.heads[1] = int(kv_heads);
     p.dim = int(dim);
@@ -392,7 +438,7 @@ extern "C" ds_status ds_rotary_norm(const void *q, const void *k, const int32_t 
     RotaryParams p;
     if (ds_status st = rotary_params(p, batch, tokens, heads, kv_heads, dim, pairs, axes, sections, interleaved, eps, type, weight_type, frequency_type))
         return st;
-    const int64_t blocks = (p.rows + 3) / 4;
+    const int64_t blocks = (int64_t(p.rows) + 3) / 4;
     if (!grid_fits(blocks, 256)) return fail(DS_ERR_UNSUPPORTED, "too many tokens for a launch");
     if (p.rows == 0) return ok();
     int64_t ps[3];
@@ -414,10 +460,13 @@ extern "C" ds_status ds_rotary_norm(const void *q, const void *k, const int32_t 
                                       {frequencies, pairs * (p.wide ? 8 : 4), "frequencies", false}, {q_weight, wb, "q_weight", false},
                                       {k_weight, wb, "k_weight", false}, {q_out, out[0], "q_out", true}, {k_out, out[1], "k_out", true}}))
         return st;
-    for_layout(p, type, weight_type, [&](auto t, auto w, auto lanes, auto whole) {
+    const Split a = split_heads(p.rows, heads, kv_heads, dim);
+    p.per = a.per;
+    p.chunks = a.chunks[0];
+    for_layout(p, type, weight_type, [&](auto t, auto w, auto lanes, auto run) {
         using T = decltype(t);
         using W = decltype(w);
-        hipLaunchKernelGGL((rotary_kernel<T, W, decltype(lanes)::value, decltype(whole)::value>), dim3(uint32_t(blocks)), dim3(256), 0,
+        hipLaunchKernelGGL((rotary_kernel<T, W, decltype(lanes)::value, decltype(run)::value>), dim3(uint32_t(blocks), uint32_t(a.chunks[0] + a.chunks[1])), dim3(256), 0,
                            static_cast<hipStream_t>(stream), static_cast<const T *>(q), static_cast<const T *>(k),
                            static_cast<const W *>(q_weight), static_cast<const W *>(k_weight), static_cast<T *>(q_out),
                            static_cast<T *>(k_out), p);
@@ -425,10 +474,13 @@ extern "C" ds_status ds_rotary_norm(const void *q, const void *k, const int32_t 
     return launched("ds_rotary_norm");
 }
 
-extern "C" int64_t ds_rotary_norm_backward_scratch_bytes(int64_t batch, int64_t tokens, int64_t dim)
+extern "C" int64_t ds_rotary_norm_backward_scratch_bytes(int64_t batch, int64_t tokens, int64_t heads, int64_t kv_heads, int64_t dim)
 {
-    if (batch <= 0 || tokens <= 0 || dim <= 0 || dim > 256 || batch > kMaxElems || tokens > kMaxElems || batch * tokens > kMaxElems) return 0;
-    return int64_t(rotary_grad_blocks(batch * tokens)) * 2 * dim * 4;
+    if (batch <= 0 || tokens <= 0 || heads <= 0 || kv_heads < 0 || heads > 65535 || kv_heads > 65535 || dim <= 0 || dim > 256 || batch > kMaxElems ||
+        tokens > kMaxElems || batch * tokens > kMaxElems)
+        return 0;
+    const Split a = split_heads(batch * tokens, heads, kv_heads, dim);
+    return int64_t(a.blocks[0] + a.blocks[1]) * dim * 4;
 }
 
 extern "C" ds_status ds_rotary_norm_backward(const void *dq_out, const void *dk_out, const void *q, const void *k, const int32_t *positions,
@@ -454,7 +506,7 @@ extern "C" ds_status ds_rotary_norm_backward(const void *dq_out, const void *dk_
         return fail(DS_ERR_INVALID_ARG, "a gradient of a weight that is not given");
     const int64_t es = float_bytes(type), wb = dim * float_bytes(weight_type);
     const bool sums = dq_weight || dk_weight;
-    const int64_t need = sums ? ds_rotary_norm_backward_scratch_bytes(batch, tokens, dim) : 0;
+    const int64_t need = sums ? ds_rotary_norm_backward_scratch_bytes(batch, tokens, heads, kv_heads, dim) : 0;
     if (need > 0 && !scratch) return fail(DS_ERR_NULL_POINTER, "gradients of weights need scratch");
     if (need > scratch_bytes) return fail(DS_ERR_BUFFER_TOO_SMALL, "scratch has %lld bytes, %lld are needed", (long long)scratch_bytes, (long long)need);
     if (p.rows == 0 && !sums) return ok();
@@ -482,19 +534,22 @@ extern "C" ds_status ds_rotary_norm_backward(const void *dq_out, const void *dk_
                                       {dk, out[1], "dk", true}, {dq_weight, wb, "dq_weight", true}, {dk_weight, wb, "dk_weight", true},
                                       {need ? scratch : nullptr, need, "scratch", true}}))
         return st;
-    const int blocks = p.rows > 0 ? rotary_grad_blocks(p.rows) : 0;
+    const Split a = split_heads(p.rows, heads, kv_heads, dim);
+    const int blocks = a.blocks[0] + a.blocks[1];           // (0 without tokens)
+    p.per = a.per;
+    p.blocks = a.blocks[0];
     const auto s = static_cast<hipStream_t>(stream);
-    for_layout(p, type, weight_type, [&](auto t, auto w, auto lanes, auto whole) {
+    for_layout(p, type, weight_type, [&](auto t, auto w, auto lanes, auto run) {
         using T = decltype(t);
         using W = decltype(w);
         if (blocks > 0)
-            hipLaunchKernelGGL((rotary_grad_kernel<T, W, decltype(lanes)::value, decltype(whole)::value>), dim3(uint32_t(blocks)), dim3(256), 0, s,
+            hipLaunchKernelGGL((rotary_grad_kernel<T, W, decltype(lanes)::value, decltype(run)::value>), dim3(uint32_t(blocks)), dim3(256), 0, s,
                                static_cast<const T *>(dq_out), static_cast<const T *>(dk_out), static_cast<const T *>(q),
                                static_cast<const T *>(k), static_cast<const W *>(q_weight), static_cast<const W *>(k_weight),
                                static_cast<T *>(dq), static_cast<T *>(dk), sums ? static_cast<float *>(scratch) : nullptr, p);
         if (sums)
             hipLaunchKernelGGL(rotary_grad_weight_kernel<W>, dim3(uint32_t((dim + 31) / 32), 2), dim3(1024), 0, s,
-                               static_cast<const float *>(scratch), static_cast<W *>(dq_weight), static_cast<W *>(dk_weight), blocks, int(dim));
+                               static_cast<const float *>(scratch), static_cast<W *>(dq_weight), static_cast<W *>(dk_weight), a.blocks[0], a.blocks[1], int(dim));
     });
     return launched("ds_rotary_norm_backward");
 }

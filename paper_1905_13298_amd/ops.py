@@ -1183,7 +1183,7 @@ def rotary_norm_backward(dq_out, dk_out, q, k, positions, frequencies, q_weight=
     dk = None if k is None else torch.empty(k.shape, dtype=q.dtype, device=dev)
     dqw = None if q_weight is None else torch.empty_like(q_weight)
     dkw = None if k_weight is None else torch.empty_like(k_weight)
-    scratch, size = (None, 0) if dqw is None and dkw is None else _scratch8("ds_rotary_norm_backward_scratch_bytes", (shape[0], shape[1], shape[4]), dev)
+    scratch, size = (None, 0) if dqw is None and dkw is None else _scratch8("ds_rotary_norm_backward_scratch_bytes", shape[:5], dev)
     _launch("ds_rotary_norm_backward", dev, dq_out.data_ptr(), _ptr(dk_out), q.data_ptr(), _ptr(k), positions.data_ptr(), frequencies.data_ptr(),
             _ptr(q_weight), _ptr(k_weight), dq.data_ptr(), _ptr(dk), _ptr(dqw), _ptr(dkw), *shape, sections, sdq, sdk, sq, sk, sp, _vectors(dq, "dq"),
             None if k is None else _vectors(dk, "dk"), interleaved, eps, _TYPE[q.dtype], _TYPE[wtype], _TYPE[frequencies.dtype],

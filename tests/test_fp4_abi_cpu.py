@@ -85,8 +85,9 @@ def test_calls_without_tokens_do_nothing():
 
 def test_scratch_sizes():
     lib = _native.lib()
-    assert lib.ds_rotary_norm_backward_scratch_bytes(0, 4, 64) == 0 and lib.ds_rotary_norm_backward_scratch_bytes(1, 4, 1 << 20) == 0
-    assert lib.ds_rotary_norm_backward_scratch_bytes(1, 4, 64) == 2 * 64 * 4
+    need = lib.ds_rotary_norm_backward_scratch_bytes
+    assert need(0, 4, 2, 2, 64) == 0 and need(1, 4, 2, 2, 1 << 20) == 0 and need(1, 4, 0, 2, 64) == 0
+    assert need(1, 4, 2, 2, 64) == 2 * 64 * 4 and need(1, 4, 2, 0, 64) == 64 * 4
     assert lib.ds_attention_fp4_scratch_bytes(0, 1, 1, 1, 64, 16, 4) == 0
     assert lib.ds_attention_fp4_scratch_bytes(1, 1, 8, 4, 128, 64, 4096) > 0
 
