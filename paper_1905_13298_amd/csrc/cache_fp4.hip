@@ -38,35 +38,37 @@ struct CacheParams {
     int64_t sb[2], st[2], sh[2];       // strides of k and v: sequence, token, head
 };
 
-// A thread's 8 elements of one vector of k or v: which they are, and where the cache has them.
+// A thread's share of k or v: 8 elements of N tokens, where N is 4 those of one multiple of 4 positions, whose values
+// and scales lie together in the cache. Which they are, and where the cache has them.
+template <int N>
 struct Place {
-    int b, t, h, lane, slot;
+    int b, t, h, lane, slot;           // t, slot: of the first of the N (t may be negative)
+    int low, high;                     // the tokens t + low .. t + high - 1 are meant
     int64_t at;                        // page and head, -1: nowhere
-    bool live;
     __device__ __forceinline__ Place(const CacheParams &p)
     {
         b = int(blockIdx.x) / p.per;
-        const int i = (int(blockIdx.x) - b * p.per) * 256 + int(threadIdx.x), vec = fdiv(i, p.lanes);
+        const int i = (int(blockIdx.x) - b * p.per) * 256 + int(threadIdx.x), vec = fdiv(i, p.lanes), nth = fdiv(vec, p.by_head);
         lane = i - vec * int(p.lanes.d);
-        t = fdiv(vec, p.by_head);
-        h = vec - t * p.heads;
-        live = t < p.tokens;
+        h = vec - nth * p.heads;
+        const int start = p.start[b], n = p.count ? min(p.count[b], p.tokens) : p.tokens;
+        t = nth * N - (start & (N - 1));
+        low = max(-t, 0);
+        high = min(n - t, N);
         at = -1;
         slot = 0;
-        const int start = p.start[b], n = p.count ? min(p.count[b], p.tokens) : p.tokens;
-        if (start < 0 || t >= n) return;
-        const uint32_t pos = uint32_t(start) + uint32_t(t), col = pos >> p.page_shift;
+        if (start < 0 || high <= low) return;
+        const uint32_t pos = uint32_t(start) - uint32_t(start & (N - 1)) + uint32_t(nth) * N, col = pos >> p.page_shift;
         if (col >= uint32_t(p.columns)) return;
         const int pid = p.table[b * p.ldt + col];
         if (unsigned(pid) >= unsigned(p.pages)) return;
         at = int64_t(pid) * p.heads + h;
         slot = int(pos) & ((1 << p.page_shift) - 1);
     }
-    // The bytes of the elements' codes, and their scale's.
+    // The bytes of the first token's codes (keys: the next ones dim / 2 further; values: 4), and of the scales.
     __device__ __forceinline__ int64_t codes(const CacheParams &p, bool values) const
     {
-        const int64_t base = (at << p.page_shift) * (p.dim / 2);
-        return base + (values ? (slot >> 2) * 2 * p.dim + lane * 16 + (slot & 3) * 4 : slot * (p.dim / 2) + lane * 4);
+        return (at << p.page_shift) * (p.dim / 2) + (values ? (slot >> 2) * 2 * p.dim + lane * 16 + (slot & 3) * 4 : slot * (p.dim / 2) + lane * 4);
     }
     __device__ __forceinline__ int64_t scale(const CacheParams &p) const
     {
@@ -78,6 +80,12 @@ struct Place {
 // (255: NaN).
 __device__ __forceinline__ float scale4(uint32_t e) { return __uint_as_float(e << 23); }
 
+// The same of scale byte i of a word (the conversions do not look at the sign and the mantissa).
+__device__ __forceinline__ float scale_of(uint32_t word, int i)
+{
+    return __uint_as_float(i == 0 ? word << 23 : i == 1 ? word << 15 : i == 2 ? word << 7 : word >> 1);
+}
+
 // The scale byte of the least power of two that brings `amax` (finite, >= 0) to at most 6 = 1.5 * 2^2:
 // a mantissa above 1.5 carries into the exponent.
 __device__ __forceinline__ int scale_byte4(float amax)
@@ -85,38 +93,71 @@ __device__ __forceinline__ int scale_byte4(float amax)
     return min(max(int((__float_as_uint(amax) + 0x3fffffu) >> 23) - 2, kLow4), kHigh4);
 }
 
-// New tokens into their pages: 8 elements a thread, 4 threads a scale. An element that is no finite
-// number makes its block NaN (scale byte 255, codes 0).
-template <typename T>
+// The largest of four neighbouring lanes' values (>= 0, or infinite), in all four.
+__device__ __forceinline__ float max_of_4(float v)
+{
+    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xb1, 0xf, 0xf, true)));       // lanes 1, 0, 3, 2
+    return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4e, 0xf, 0xf, true)));    // lanes 2, 3, 0, 1
+}
+
+// New tokens into their pages: 8 elements of N tokens a thread, 4 threads a scale. An element that is no finite
+// number makes its block NaN (scale byte 255, codes 0). Bound by bandwidth: 4 x 2001 tokens of 8 heads of 128 in 16 bits,
+// 42 MB, 11.5 us (3.6 TB/s, the launch's 2 us among them); 64 x 1 3.2.
+template <typename T, int N>
 __global__ void __launch_bounds__(256)
 append4_kernel(const T *__restrict__ k, const T *__restrict__ v, uint8_t *__restrict__ kc, uint8_t *__restrict__ vc,
                uint8_t *__restrict__ ks, uint8_t *__restrict__ vs, const CacheParams p)
 {
     const int which = int(blockIdx.y);
-    const Place at(p);
+    const Place<N> at(p);
     const bool mine = at.at >= 0 && at.lane * 8 < p.dim;
-    float x[8] = {}, top = 0.f;
-    if (mine) load8((which ? v : k) + at.b * p.sb[which] + at.t * p.st[which] + at.h * p.sh[which] + at.lane * 8, 8, x);
-    bool fine = true;
+    const T *const src = (which ? v : k) + at.b * p.sb[which] + at.t * p.st[which] + at.h * p.sh[which] + at.lane * 8;
+    Eight<T> x[N];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        fine = fine && fabsf(x[i]) < __builtin_inff();
-        top = fmaxf(top, fabsf(x[i]));
+    for (int j = 0; j < N; ++j) {
+        x[j].clear();
+        if (mine && j >= at.low && j < at.high) __builtin_memcpy(x[j].v, src + j * p.st[which], sizeof x[j].v);
     }
-    top = lanes_max<4>(fine ? top : __builtin_inff());
-    fine = top < __builtin_inff();
-    const int e = fine ? scale_byte4(top) : kNan4;
+    uint32_t q[N], scales = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        bool fine = true;
+        float top = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            fine = fine && fabsf(x[j].at(i)) < __builtin_inff();
+            top = fmaxf(top, fabsf(x[j].at(i)));
+        }
+        top = max_of_4(fine ? top : __builtin_inff());
+        fine = top < __builtin_inff();
+        const uint32_t e = fine ? uint32_t(scale_byte4(top)) : uint32_t(kNan4);
+        const float s = scale4(e);
+        q[j] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, x[j].at(0), x[j].at(1), s, 0);
+        q[j] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q[j], x[j].at(2), x[j].at(3), s, 1);
+        q[j] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q[j], x[j].at(4), x[j].at(5), s, 2);
+        q[j] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q[j], x[j].at(6), x[j].at(7), s, 3);
+        q[j] = fine ? q[j] : 0u;
+        scales |= e << (8 * j);
+    }
     if (!mine) return;
-    const float s = scale4(uint32_t(e));
-    uint32_t q = 0;
-    if (fine) {
-        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, x[0], x[1], s, 0);
-        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, x[2], x[3], s, 1);
-        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, x[4], x[5], s, 2);
-        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, x[6], x[7], s, 3);
+    uint8_t *const codes = (which ? vc : kc) + at.codes(p, which), *const e = (which ? vs : ks) + at.scale(p);
+    const bool whole = N == 4 && at.low == 0 && at.high == 4;
+    if (which && whole) {
+        __builtin_memcpy(__builtin_assume_aligned(codes, 4 * N), q, sizeof q);
+    } else {
+        const int step = which ? 4 : p.dim / 2;
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (j >= at.low && j < at.high) *reinterpret_cast<uint32_t *>(codes + j * step) = q[j];
     }
-    *reinterpret_cast<uint32_t *>((which ? vc : kc) + at.codes(p, which)) = q;
-    if ((at.lane & 3) == 0) (which ? vs : ks)[at.scale(p)] = uint8_t(e);
+    if ((at.lane & 3) != 0) return;
+    if (whole) {
+        *reinterpret_cast<uint32_t *>(e) = scales;
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (j >= at.low && j < at.high) e[j] = uint8_t(scales >> (8 * j));
+    }
 }
 
 // Eight numbers of a scale, exactly (2^-24 .. 6 * 2^13: 16-bit floats; NaN of scale byte 255).
@@ -127,19 +168,36 @@ __device__ __forceinline__ void widen4(uint32_t codes, float s, float (&x)[8])
     x[0] = a[0], x[1] = a[1], x[2] = b[0], x[3] = b[1], x[4] = c[0], x[5] = c[1], x[6] = d[0], x[7] = d[1];
 }
 
-// Tokens of a cache as floats [sequence][token][head][dim], 0 where there is none.
-template <typename T>
+// Tokens of a cache as floats [sequence][token][head][dim], 0 where there is none: 8 elements of N tokens a
+// thread. Bound by bandwidth: 6 x 20000 tokens of 8 heads of 128 to 16 bits, 608 MB, 115 us (5.3 TB/s).
+template <typename T, int N>
 __global__ void __launch_bounds__(256)
 read4_kernel(T *__restrict__ k, T *__restrict__ v, const uint8_t *__restrict__ kc, const uint8_t *__restrict__ vc,
              const uint8_t *__restrict__ ks, const uint8_t *__restrict__ vs, const CacheParams p)
 {
     const int which = int(blockIdx.y);
-    const Place at(p);
-    if (!at.live || at.lane * 8 >= p.dim) return;
-    float x[8] = {};
-    if (at.at >= 0)
-        widen4(*reinterpret_cast<const uint32_t *>((which ? vc : kc) + at.codes(p, which)), scale4((which ? vs : ks)[at.scale(p)]), x);
-    store8((which ? v : k) + at.b * p.sb[which] + at.t * p.st[which] + at.h * p.sh[which] + at.lane * 8, 8, x);
+    const Place<N> at(p);
+    if (at.lane * 8 >= p.dim) return;
+    uint32_t q[N] = {}, scales = 0;
+    if (at.at >= 0) {
+        const uint8_t *const codes = (which ? vc : kc) + at.codes(p, which);
+        if (which) {
+            __builtin_memcpy(q, __builtin_assume_aligned(codes, 4 * N), sizeof q);
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j) q[j] = *reinterpret_cast<const uint32_t *>(codes + j * (p.dim / 2));
+        }
+        const uint8_t *const e = (which ? vs : ks) + at.scale(p);
+        scales = N == 4 ? *reinterpret_cast<const uint32_t *>(e) : *e;
+    }
+    T *const dst = (which ? v : k) + at.b * p.sb[which] + at.t * p.st[which] + at.h * p.sh[which] + at.lane * 8;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        if (at.t + j < 0 || at.t + j >= p.tokens) continue;
+        float x[8] = {};
+        if (at.at >= 0 && j >= at.low && j < at.high) widen4(q[j], scale_of(scales, j), x);
+        store8(dst + j * p.st[which], 8, x);
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -172,12 +230,6 @@ __device__ __forceinline__ typename Vec8<T>::type operand4(uint32_t codes, float
         const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 3);
         return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
     }
-}
-
-// Scale byte i of a word.
-__device__ __forceinline__ float scale_of(uint32_t word, int i)
-{
-    return __uint_as_float(i == 0 ? word << 23 : i == 1 ? word << 15 : i == 2 ? word << 7 : word >> 1);
 }
 
 // 0x80 in each byte of x that is 255, the scale that is NaN. A weight of 0 does not keep a NaN out of a
@@ -889,14 +941,22 @@ int page_shift(int64_t page)
     return shift;
 }
 
+// Whether a thread has 4 tokens, where that leaves work for the whole chip. Append and read of 4 x 2001 tokens (8 heads
+// of 128, pages of 64) 20.2 us, with 1 24.4; 2000 (dim 80) 8.6 and 9.1; 64 x 4 5.9 and 5.4; 64 x 1 5.3 and 4.5; a read
+// of 6 x 20000 116 and 183.
+bool four_tokens(int64_t batch, int64_t tokens, int64_t heads, int64_t dim)
+{
+    return tokens > 1 && double(batch) * double(tokens) * double(heads) * double(dim) >= (1 << 20);
+}
+
 // What an append and a read have in common; bytes: those that k and v span.
-ds_status cache_params(CacheParams &p, int64_t (&bytes)[2], const int32_t *table, const int32_t *start, const int32_t *count, int64_t batch,
+ds_status cache_params(bool four, CacheParams &p, int64_t (&bytes)[2], const int32_t *table, const int32_t *start, const int32_t *count, int64_t batch,
                        int64_t tokens, int64_t heads, int64_t dim, int64_t page, int64_t pages, int64_t columns, int64_t ldt,
                        const int64_t *k_strides, const int64_t *v_strides, int64_t es)
 {
-    const int64_t lanes = blocks4(dim) * 4;
-    if (tokens * heads > (kMaxElems - 255) / lanes) return fail(DS_ERR_UNSUPPORTED, "too many vectors of a sequence in one call");
-    const int64_t per = (tokens * heads * lanes + 255) / 256;
+    const int64_t lanes = blocks4(dim) * 4, shares = four ? (tokens + 2) / 4 + 1 : tokens;        // (a sequence's start is any)
+    if (shares * heads > (kMaxElems - 255) / lanes) return fail(DS_ERR_UNSUPPORTED, "too many vectors of a sequence in one call");
+    const int64_t per = (shares * heads * lanes + 255) / 256;
     if (!grid_fits(batch * per, 256)) return fail(DS_ERR_UNSUPPORTED, "too many vectors in one call");
     p = CacheParams{table, start, count, ldt, int(columns), int(pages), int(tokens), int(heads), int(dim), page_shift(page),
                     int(blocks4(dim)), int(per), make_fastdiv(uint32_t(lanes)), make_fastdiv(uint32_t(heads)), {}, {}, {}};
@@ -939,9 +999,10 @@ extern "C" ds_status ds_kv_cache_fp4_append(const void *k, const void *v, uint8_
     if (!es) return fail(DS_ERR_INVALID_ARG, "type must be DS_TYPE_F32, DS_TYPE_F16 or DS_TYPE_BF16");
     if (batch == 0 || tokens == 0) return ok();
     if (ds_status st = check_aligned(k_cache, v_cache, k_scales, v_scales)) return st;
+    const bool four = four_tokens(batch, tokens, heads, dim);
     CacheParams p;
     int64_t bytes[2];
-    if (ds_status st = cache_params(p, bytes, table, start, count, batch, tokens, heads, dim, page, pages, columns, ldt, k_strides, v_strides, es))
+    if (ds_status st = cache_params(four, p, bytes, table, start, count, batch, tokens, heads, dim, page, pages, columns, ldt, k_strides, v_strides, es))
         return st;
     const int64_t cb = pages * heads * page * dim / 2, sb = pages * heads * page * blocks4(dim);
     if (ds_status st = check_tensors({{k, bytes[0], "k", false}, {v, bytes[1], "v", false}, {table, span(batch, ldt, columns, 4), "table", false},
@@ -951,7 +1012,7 @@ extern "C" ds_status ds_kv_cache_fp4_append(const void *k, const void *v, uint8_
         return st;
     const auto go = [&](auto t) {
         using T = decltype(t);
-        hipLaunchKernelGGL(append4_kernel<T>, dim3(uint32_t(batch * p.per), 2), dim3(256), 0, static_cast<hipStream_t>(stream),
+        hipLaunchKernelGGL((four ? append4_kernel<T, 4> : append4_kernel<T, 1>), dim3(uint32_t(batch * p.per), 2), dim3(256), 0, static_cast<hipStream_t>(stream),
                            static_cast<const T *>(k), static_cast<const T *>(v), k_cache, v_cache, k_scales, v_scales, p);
     };
     if (type == DS_TYPE_F32) go(float{});
@@ -974,9 +1035,10 @@ extern "C" ds_status ds_kv_cache_fp4_read(const uint8_t *k_cache, const uint8_t 
     if (!es) return fail(DS_ERR_INVALID_ARG, "type must be DS_TYPE_F32, DS_TYPE_F16 or DS_TYPE_BF16");
     if (batch == 0 || tokens == 0) return ok();
     if (ds_status st = check_aligned(k_cache, v_cache, k_scales, v_scales)) return st;
+    const bool four = four_tokens(batch, tokens, heads, dim);
     CacheParams p;
     int64_t bytes[2];
-    if (ds_status st = cache_params(p, bytes, table, start, count, batch, tokens, heads, dim, page, pages, columns, ldt, k_strides, v_strides, es))
+    if (ds_status st = cache_params(four, p, bytes, table, start, count, batch, tokens, heads, dim, page, pages, columns, ldt, k_strides, v_strides, es))
         return st;
     const int64_t cb = pages * heads * page * dim / 2, sb = pages * heads * page * blocks4(dim);
     if (ds_status st = check_tensors({{k_cache, cb, "k_cache", false}, {v_cache, cb, "v_cache", false}, {k_scales, sb, "k_scales", false},
@@ -986,7 +1048,7 @@ extern "C" ds_status ds_kv_cache_fp4_read(const uint8_t *k_cache, const uint8_t 
         return st;
     const auto go = [&](auto t) {
         using T = decltype(t);
-        hipLaunchKernelGGL(read4_kernel<T>, dim3(uint32_t(batch * p.per), 2), dim3(256), 0, static_cast<hipStream_t>(stream),
+        hipLaunchKernelGGL((four ? read4_kernel<T, 4> : read4_kernel<T, 1>), dim3(uint32_t(batch * p.per), 2), dim3(256), 0, static_cast<hipStream_t>(stream),
                            static_cast<T *>(k), static_cast<T *>(v), k_cache, v_cache, k_scales, v_scales, p);
     };
     if (type == DS_TYPE_F32) go(float{});

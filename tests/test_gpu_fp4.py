@@ -144,6 +144,34 @@ def test_append_and_read(ops, page, dim, heads, tokens):
                     assert torch.equal(g[b, t].cpu().double(), x)
 
 
+@pytest.mark.parametrize("dim,heads,tokens,page", [(128, 4, 600, 64), (80, 3, 1001, 16), (32, 8, 1102, 128), (256, 8, 259, 32)])
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+def test_append_and_read_of_many_tokens(ops, dim, heads, tokens, page, dtype):
+    """Enough for threads with 4 tokens each: ragged ends, a page that is none, a sequence that is none."""
+    batch, columns = 5, (tokens + 400 + page - 1) // page
+    pages = batch * columns + 2
+    cache = filled_cache(ops, pages, heads, page, dim)
+    table = torch.randperm(pages, generator=torch.Generator().manual_seed(dim))[:batch * columns].reshape(batch, columns).to(torch.int32)
+    table[1, 2], table[3, columns - 9:] = -1, pages
+    start = torch.tensor([0, 1, page + 2, 211, -1], dtype=torch.int32)
+    count = torch.tensor([tokens, tokens - 1, tokens - 2, tokens + 3, tokens], dtype=torch.int32)
+    k, v = (normal(5 + i, batch, tokens, heads, dim).to(dtype) for i in range(2))
+    before = tokens_of(cache)
+    want = [append_reference(before[i], (k, v)[i], table, start, count, page) for i in range(2)]
+    args = table.to(DEV), start.to(DEV)
+    ops.kv_cache_fp4_append(k.to(DEV), v.to(DEV), *cache, *args, count.to(DEV))
+    after = tokens_of(cache)
+    for got, w in zip(after, want):
+        assert same_numbers(got, w)
+    pos = start[:, None] + torch.arange(tokens)[None, :]
+    pid = table.gather(1, (pos.clamp(min=0) // page).long()).long()
+    there = (torch.arange(tokens)[None, :] < count[:, None]) & (start[:, None] >= 0) & (pid >= 0) & (pid < pages)
+    got = ops.kv_cache_fp4_read(*cache, *args, tokens, count.to(DEV), dtype=dtype)
+    for g, w in zip(got, want):
+        x = numbers(*w)[pid.clamp(0, pages - 1), :, pos.clamp(min=0) % page]
+        assert torch.equal(g.cpu().double(), torch.where(there[:, :, None, None], x, 0.0))
+
+
 def test_append_boundaries(ops):
     """Every tie and its neighbours, at both ends of the scales and between, and blocks' largest elements around a scale's limit."""
     page, dim = 16, 64
