@@ -268,11 +268,11 @@ __device__ __forceinline__ void unroll(F &&f)
     }
 }
 
-// Up to 16 queries of a kv head (tokens being decoded): a block of 4 waves takes a share of the keys, each wave
+// Up to 16 TILES queries of a kv head (tokens being decoded): a block of 4 waves takes a share of the keys, each wave
 // every fourth 64 of it straight from memory to registers (no two waves share any), and joins them at its end.
 // Bound by reading the cache once, and by the blocks' starts and ends: 131072 keys of 8 heads of 128, 143 MB, 30.3 us
 // (4.7 TB/s) and 4.1 of joining; its VALU instructions, a third of them conversions, would take a third of that.
-template <typename T, int DP>
+template <typename T, int DP, int TILES>
 __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1)
 attention4_few_kernel(const AttentionParams p, int blocks)
 {
@@ -285,7 +285,7 @@ attention4_few_kernel(const AttentionParams p, int blocks)
     __shared__ f32x4 osum[kWaves][DT][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), r = lane & 15, g = lane >> 4;
     const int split = int(blockIdx.x), bh = int(blockIdx.y), b = bh / p.heads, h = bh - b * p.heads;
-    const int D = p.dim, page = 1 << p.page_shift, row = r;
+    const int D = p.dim, page = 1 << p.page_shift;
     const Sequence seq(p, b);
     // Keys that some query sees lie in [tlo, thi); every query that sees any sees [alo, ahi).
     const int t1 = min(seq.count, p.tokens) - 1, t0 = min(max(-seq.first, 0), max(t1, 0));      // the first query that is not before the first key
@@ -294,19 +294,25 @@ attention4_few_kernel(const AttentionParams p, int blocks)
     const int s0 = thi > tlo ? tlo / kStep : 0, s1 = thi > tlo ? (thi + kStep - 1) / kStep : 0;
     const int each = max((s1 - s0 + p.splits - 1) / p.splits, p.least);
     const int from = s0 + split * each, to = min(s1, from + each);
-    float *const part = p.part ? p.part + ((int64_t(bh) * p.rows + r) * p.splits + split) * (D + 2) : nullptr;
-    if (part && from >= to) {      // nothing here: no results, only that there are none
-        if (wave == 0 && g == 0 && r < p.rows) {
+    auto part_of = [&](int row) { return p.part + ((int64_t(bh) * p.rows + row) * p.splits + split) * (D + 2); };
+    if (p.part && from >= to) {      // nothing here: no results, only that there are none
+        if (int(threadIdx.x) < p.rows) {
+            float *const part = part_of(int(threadIdx.x));
             part[D] = -__builtin_inff();
             part[D + 1] = 0.f;
         }
         return;
     }
 
-    f32x4 acc[DT];
-    float m = -__builtin_inff(), l = 0.f;
+    f32x4 acc[TILES][DT];
+    float m[TILES], l[TILES];
 #pragma unroll
-    for (int d = 0; d < DT; ++d) acc[d] = f32x4{};
+    for (int u = 0; u < TILES; ++u) {
+        m[u] = -__builtin_inff();
+        l[u] = 0.f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) acc[u][d] = f32x4{};
+    }
     // Page of the 16 keys from `key` on (they share it), or -1 where there is none.
     auto page_of = [&](int key) {
         const int col = key >> p.page_shift;
@@ -375,55 +381,66 @@ attention4_few_kernel(const AttentionParams p, int blocks)
         vp = page_of(step * kStep + g * 16);
     };
     look(from + wave);
-    v8 qf[QC];
-    int low, high;
-    load_query<T, DP, 8, DP / 4, QC>(p, seq, b, h, row, g, low, high, qf);
-    // A row that sees no key, and is 0 in the end, takes part as if it saw every one, which costs less.
-    const bool none = high == 0;
-    if (none) high = 0x7fffffff;
+    v8 qf[TILES][QC];
+    int low[TILES], high[TILES];
+    bool none[TILES];
+#pragma unroll
+    for (int u = 0; u < TILES; ++u) {
+        load_query<T, DP, 8, DP / 4, QC>(p, seq, b, h, u * 16 + r, g, low[u], high[u], qf[u]);
+        // A row that sees no key, and is 0 in the end, takes part as if it saw every one, which costs less.
+        none[u] = high[u] == 0;
+        if (none[u]) high[u] = 0x7fffffff;
+    }
     for (int step = from + wave; step < to; step += kWaves) {
         Step x;
         const int base = step * kStep, vrun = base + g * 16;
         fetch(step, kp, vp, x);
         look(step + kWaves);
         const bool there = x.vp >= 0;
-        f32x4 s[4];
+        f32x4 products[TILES][4];
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int c = 0; c < QC; ++c)
-                s[t] = mma(operand4<T>(x.k[t][c], scale_of(x.ks[c * NS / QC], t)), qf[c], c == 0 ? f32x4{} : s[t]);
-        // Element i of s[t]: key vrun + 4 i + t.
-        if (!__all(there && vrun >= low && vrun + 16 <= high)) {
-            int run = vrun;
-            asm volatile("" : "+v"(run));         // (what follows is not worked out where it is not needed)
+            for (int c = 0; c < QC; ++c) {
+                const v8 key = operand4<T>(x.k[t][c], scale_of(x.ks[c * NS / QC], t));
+#pragma unroll
+                for (int u = 0; u < TILES; ++u) products[u][t] = mma(key, qf[u][c], c == 0 ? f32x4{} : products[u][t]);
+            }
+        f16x8 pf[TILES][2];
+#pragma unroll
+        for (int u = 0; u < TILES; ++u) {
+            f32x4 (&s)[4] = products[u];
+            // Element i of s[t]: key vrun + 4 i + t.
+            if (!__all(there && vrun >= low[u] && vrun + 16 <= high[u])) {
+                int run = vrun;
+                asm volatile("" : "+v"(run));         // (what follows is not worked out where it is not needed)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int key = run + (i & 3) * 4 + (i >> 2);
+                    s[i >> 2][i & 3] = there && key >= low[u] && key < high[u] ? s[i >> 2][i & 3] : -__builtin_inff();
+                }
+            }
+            const float sub = or_zero(m[u]);
+            float e[16], top = -__builtin_inff();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) e[i] = fmaf(s[i & 3][i >> 2], p.scale, -sub);        // (key vrun + i)
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) top = fmaxf(top, fmaxf(e[i], e[i + 1]));
+            raise(m[u], l[u], max_over_32(max_over_16(top)),
+                  [&](float by) {
+#pragma unroll
+                      for (int i = 0; i < 16; ++i) e[i] -= by;
+                  },
+                  [&](float alpha) {
+#pragma unroll
+                      for (int d = 0; d < DT; ++d) acc[u][d] *= alpha;
+                  });
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const int key = run + (i & 3) * 4 + (i >> 2);
-                s[i >> 2][i & 3] = there && key >= low && key < high ? s[i >> 2][i & 3] : -__builtin_inff();
+                e[i] = __builtin_amdgcn_exp2f(e[i]);
+                l[u] += e[i];
+                pf[u][i >> 3][i & 7] = _Float16(e[i]);
             }
-        }
-        const float sub = or_zero(m);
-        float e[16], top = -__builtin_inff();
-#pragma unroll
-        for (int i = 0; i < 16; ++i) e[i] = fmaf(s[i & 3][i >> 2], p.scale, -sub);        // (key vrun + i)
-#pragma unroll
-        for (int i = 0; i < 16; i += 2) top = fmaxf(top, fmaxf(e[i], e[i + 1]));
-        raise(m, l, max_over_32(max_over_16(top)),
-              [&](float by) {
-#pragma unroll
-                  for (int i = 0; i < 16; ++i) e[i] -= by;
-              },
-              [&](float alpha) {
-#pragma unroll
-                  for (int d = 0; d < DT; ++d) acc[d] *= alpha;
-              });
-        f16x8 pf[2];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            e[i] = __builtin_amdgcn_exp2f(e[i]);
-            l += e[i];
-            pf[i >> 3][i & 7] = _Float16(e[i]);
         }
         if (!__all(there && base + kStep <= thi && base >= tlo)) {
             // Keys that no query sees may hold anything: their values count as 0 (whatever the code, 2^-127
@@ -440,29 +457,35 @@ attention4_few_kernel(const AttentionParams p, int blocks)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) nan |= nan_scales(x.vs[i][q]);
             if (__any(nan != 0)) {
-                f16x8 seen[2];
                 int run = vrun;
                 asm volatile("" : "+v"(run));
+                f32x4 n[TILES][NS];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) seen[i >> 3][i & 7] = _Float16(there && run + i >= low && run + i < high ? 1.f : 0.f);
+                for (int u = 0; u < TILES; ++u) {
+                    f16x8 seen[2];
 #pragma unroll
-                for (int i = 0; i < NS; ++i) {
-                    f32x4 n{};
+                    for (int i = 0; i < 16; ++i) seen[i >> 3][i & 7] = _Float16(there && run + i >= low[u] && run + i < high[u] ? 1.f : 0.f);
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        f16x8 where;
+                    for (int i = 0; i < NS; ++i) {
+                        n[u][i] = f32x4{};
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) where[j] = _Float16((x.vs[i][2 * c + j / 4] >> (8 * (j & 3)) & 255u) == 255u ? 1.f : 0.f);
-                        n = mma(where, seen[c], n);
+                        for (int c = 0; c < 2; ++c) {
+                            f16x8 where;
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) where[j] = _Float16((x.vs[i][2 * c + j / 4] >> (8 * (j & 3)) & 255u) == 255u ? 1.f : 0.f);
+                            n[u][i] = mma(where, seen[c], n[u][i]);
+                        }
+                        // A lane's dimensions have their scale in common: the same in all of their tiles.
+#pragma unroll
+                        for (int d = i * (DT / NS); d < (i + 1) * (DT / NS); ++d)
+#pragma unroll
+                            for (int w = 0; w < 4; ++w) acc[u][d][w] += n[u][i][w] > 0.f ? __builtin_nanf("") : 0.f;
                     }
+                }
+#pragma unroll
+                for (int i = 0; i < NS; ++i)
 #pragma unroll
                     for (int q = 0; q < 4; ++q) x.vs[i][q] &= ~((nan_scales(x.vs[i][q]) >> 7) * 0xffu);
-                    // A lane's dimensions have their scale in common: the same in all of their tiles.
-#pragma unroll
-                    for (int d = i * (DT / NS); d < (i + 1) * (DT / NS); ++d)
-#pragma unroll
-                        for (int w = 0; w < 4; ++w) acc[d][w] += n[w] > 0.f ? __builtin_nanf("") : 0.f;
-                }
             }
         }
 #pragma unroll
@@ -481,9 +504,12 @@ attention4_few_kernel(const AttentionParams p, int blocks)
                     constexpr int SEL = decltype(sel)::value;
                     f16x8 even, odd;
                     turn4<SEL>(va, vb, sv, even, odd);
-                    f32x4 &a = acc[i * (DT / NS) + 2 * SEL], &b = acc[i * (DT / NS) + 2 * SEL + 1];
-                    a = mma(even, pf[c], a);
-                    b = mma(odd, pf[c], b);
+#pragma unroll
+                    for (int u = 0; u < TILES; ++u) {
+                        f32x4 &a = acc[u][i * (DT / NS) + 2 * SEL], &b = acc[u][i * (DT / NS) + 2 * SEL + 1];
+                        a = mma(even, pf[u][c], a);
+                        b = mma(odd, pf[u][c], b);
+                    }
                 };
                 pair(std::integral_constant<int, 0>{});
                 pair(std::integral_constant<int, 1>{});
@@ -493,48 +519,55 @@ attention4_few_kernel(const AttentionParams p, int blocks)
                 }
             }
     }
-    if (none) {
-        m = -__builtin_inff();
-        l = 0.f;
 #pragma unroll
-        for (int d = 0; d < DT; ++d) acc[d] = f32x4{};
-    }
-    // The waves' sums together: a lane's l is its own keys'.
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-    if (g == 0) {
-        ml[0][wave][r] = m;
-        ml[1][wave][r] = l;
-    }
-    __syncthreads();
-    float top = ml[0][0][r];
+    for (int u = 0; u < TILES; ++u) {
+        if (u > 0) __syncthreads();
+        const int row = u * 16 + r;
+        if (none[u]) {
+            m[u] = -__builtin_inff();
+            l[u] = 0.f;
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, ml[0][w][r]);
-    const float sub = or_zero(top), mine = __builtin_amdgcn_exp2f(m - sub);
-    float total = 0.f;
+            for (int d = 0; d < DT; ++d) acc[u][d] = f32x4{};
+        }
+        // The waves' sums together: a lane's l is its own keys'.
+        l[u] += __shfl_xor(l[u], 16);
+        l[u] += __shfl_xor(l[u], 32);
+        if (g == 0) {
+            ml[0][wave][r] = m[u];
+            ml[1][wave][r] = l[u];
+        }
+        __syncthreads();
+        float top = ml[0][0][r];
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) total = fmaf(ml[1][w][r], __builtin_amdgcn_exp2f(ml[0][w][r] - sub), total);
-    // Four dimensions that are neighbours, tiles 4 d .. 4 d + 3 of one row, a piece.
+        for (int w = 1; w < kWaves; ++w) top = fmaxf(top, ml[0][w][r]);
+        const float sub = or_zero(top), mine = __builtin_amdgcn_exp2f(m[u] - sub);
+        float total = 0.f;
 #pragma unroll
-    for (int d = 0; d < DT; d += 4)
+        for (int w = 0; w < kWaves; ++w) total = fmaf(ml[1][w][r], __builtin_amdgcn_exp2f(ml[0][w][r] - sub), total);
+        // Four dimensions that are neighbours, tiles 4 d .. 4 d + 3 of one row, a piece.
 #pragma unroll
-        for (int w = 0; w < 4; ++w) osum[wave][d + w][lane] = f32x4{acc[d][w], acc[d + 1][w], acc[d + 2][w], acc[d + 3][w]} * mine;
-    __syncthreads();
-    if (row >= p.rows) return;
-    if (part && wave == 0 && g == 0) {
-        part[D] = top;
-        part[D + 1] = total;
-    }
-    const float inv = inverse(total);
-    for (int d = wave; d < DT; d += kWaves) {
-        // Tiles d & -4 .. + 3 of row 4 g + d % 4.
-        const int line = g * 4 + (d & 3), tile = d & -4;
-        const int dim = DP == 64 ? line * 4 : tile / 8 * 128 + line * 8 + (tile & 4);
-        if (dim >= D) continue;
-        f32x4 o = osum[0][d][lane];
+        for (int d = 0; d < DT; d += 4)
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) o += osum[w][d][lane];
-        store_row<T>(p, b, h, row, part, dim, o, inv);
+            for (int w = 0; w < 4; ++w)
+                osum[wave][d + w][lane] = f32x4{acc[u][d][w], acc[u][d + 1][w], acc[u][d + 2][w], acc[u][d + 3][w]} * mine;
+        __syncthreads();
+        if (row >= p.rows) continue;
+        float *const part = p.part ? part_of(row) : nullptr;
+        if (part && wave == 0 && g == 0) {
+            part[D] = top;
+            part[D + 1] = total;
+        }
+        const float inv = inverse(total);
+        for (int d = wave; d < DT; d += kWaves) {
+            // Tiles d & -4 .. + 3 of row 4 g + d % 4.
+            const int line = g * 4 + (d & 3), tile = d & -4;
+            const int dim = DP == 64 ? line * 4 : tile / 8 * 128 + line * 8 + (tile & 4);
+            if (dim >= D) continue;
+            f32x4 o = osum[0][d][lane];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) o += osum[w][d][lane];
+            store_row<T>(p, b, h, row, part, dim, o, inv);
+        }
     }
 }
 
@@ -895,19 +928,26 @@ attention4_many_kernel(const AttentionParams p, int blocks, int bhs)
 // with 768 blocks 36.9, with 1024 43; 16 x 1 over up to 8192 23.5, 22.7 and 28. Where sequences and heads alone
 // make more than 256 blocks of few queries, whose lengths may differ, until 1536 have at least 16 steps each: 48 x 1 over
 // up to 8192 55.5, until 512 60.4, until 3072 70; 64 x 1 over up to 16000 131, 16 splits each 170. (Splits have the same
-// number of steps, so that a sequence much longer than 63 others is what a call waits for.)
-// Up to 16 rows run attention4_few_kernel; from 17 to 64 rows blocks of two waves, above of four.
-Plan plan_attention4(int64_t batch, int64_t tokens, int64_t heads, int64_t group, int64_t columns, int64_t page)
+// number of steps, so that a sequence much longer than 63 others is what a call waits for.) Few queries whose
+// splits would not give every CU a block have splits of 4 steps: 1 x 1 over 2000 8.7, of 8 10.1.
+// Up to 32 rows (of heads above 128: 16) run attention4_few_kernel, from 17 on in two tiles: 32 x 5 queries over up
+// to 4000 keys 37.5, through LDS 80.6; 5 x 3 of 7 heads each 13.4 and 17.6. To 64 rows blocks of two waves, above of four.
+Plan plan_attention4(int64_t batch, int64_t tokens, int64_t heads, int64_t group, int64_t dim, int64_t columns, int64_t page)
 {
     Plan a;
     a.rows = tokens * group;
-    a.waves = a.rows <= 16 ? 0 : a.rows <= 64 ? 2 : 4;
+    a.waves = a.rows <= (dim <= 128 ? 32 : 16) ? 0 : a.rows <= 64 ? 2 : 4;
     a.row_tiles = a.waves ? int((a.rows + 32 * a.waves - 1) / (32 * a.waves)) : 1;
     const int64_t blocks = std::max<int64_t>(batch * heads * a.row_tiles, 1), steps = (columns * page + kStep - 1) / kStep;
     const bool uneven = a.waves == 0 && blocks > 256;
     a.least = uneven ? 16 : 8;
     const int64_t most = uneven ? (1535 + blocks) / blocks : a.waves ? 512 / blocks : (511 + blocks) / blocks;
-    a.splits = int(std::max<int64_t>(1, std::min<int64_t>({most, (steps + a.least - 1) / a.least, 256})));
+    const auto split = [&] { a.splits = int(std::max<int64_t>(1, std::min<int64_t>({most, (steps + a.least - 1) / a.least, 256}))); };
+    split();
+    if (a.waves == 0 && a.splits > 1 && blocks * a.splits < 256) {
+        a.least = 4;
+        split();
+    }
     return a;
 }
 
@@ -917,7 +957,8 @@ void run_attention4(const AttentionParams &p, const Plan &a, int64_t batch, hipS
     const int bhs = int(batch * p.heads);
     const int blocks = int(blocks4(p.dim));
     if (a.waves == 0) {
-        hipLaunchKernelGGL((attention4_few_kernel<T, DP>), dim3(a.splits, bhs), dim3(256), 0, s, p, blocks);
+        constexpr int most = DP <= 128 ? 2 : 1;
+        hipLaunchKernelGGL((a.rows <= 16 ? attention4_few_kernel<T, DP, 1> : attention4_few_kernel<T, DP, most>), dim3(a.splits, bhs), dim3(256), 0, s, p, blocks);
     } else {
         const dim3 grid(uint32_t((int64_t(bhs) * a.row_tiles * a.splits + 7) / 8 * 8));
         hipLaunchKernelGGL((a.waves == 2 ? attention4_many_kernel<T, DP, 2> : attention4_many_kernel<T, DP, 4>), grid, dim3(64 * a.waves), 0, s, p, blocks, bhs);
@@ -1061,7 +1102,7 @@ extern "C" int64_t ds_attention_fp4_scratch_bytes(int64_t batch, int64_t tokens,
                                                   int64_t page, int64_t columns)
 {
     if (batch <= 0 || tokens <= 0 || heads <= 0 || group <= 0 || dim <= 0 || page <= 0 || columns <= 0) return 0;
-    return 4 * part_floats(plan_attention4(batch, tokens, heads, group, columns, page), batch, heads, dim);
+    return 4 * part_floats(plan_attention4(batch, tokens, heads, group, dim, columns, page), batch, heads, dim);
 }
 
 extern "C" ds_status ds_attention_fp4(const void *q, const uint8_t *k_cache, const uint8_t *v_cache, const uint8_t *k_scales,
@@ -1083,7 +1124,7 @@ extern "C" ds_status ds_attention_fp4(const void *q, const uint8_t *k_cache, con
     if (ds_status st = check_aligned(k_cache, v_cache, k_scales, v_scales)) return st;
     if (batch * heads > 65535) return fail(DS_ERR_UNSUPPORTED, "more than 65535 sequences times heads");
     if (group > 65535 || tokens * group > kMaxElems / 64) return fail(DS_ERR_UNSUPPORTED, "too many queries of a head");
-    const Plan a = plan_attention4(batch, tokens, heads, group, columns, page);
+    const Plan a = plan_attention4(batch, tokens, heads, group, dim, columns, page);
     if (batch * heads * a.rows * a.splits > kMaxElems / 2) return fail(DS_ERR_UNSUPPORTED, "too many queries");
     int64_t bytes[2];
     for (int i = 0; i < 2; ++i) {
