@@ -781,8 +781,8 @@ ds_status ds_kv_cache_fp4_read(const uint8_t *k_cache, const uint8_t *v_cache,
 
 /* ds_attention_fp8 over a 4-bit cache: the same queries, positions, windows and limits. A block
  * that is NaN makes NaN of the results of the queries that see its token: a key's of all their elements,
- * a value's of the block's. (Scale bytes that no append writes, 1 .. 103 and 141 .. 254, give what a
- * 16-bit float has of their numbers.) scratch: ds_attention_fp4_scratch_bytes (0: none needed). */
+ * a value's of the block's. The scale bytes of seen tokens are what an append writes (104 .. 140, 255; others
+ * give no defined results). scratch: ds_attention_fp4_scratch_bytes (0: none needed). */
 ds_status ds_attention_fp4(const void *q, const uint8_t *k_cache, const uint8_t *v_cache,
                            const uint8_t *k_scales, const uint8_t *v_scales, const int32_t *table,
                            const int32_t *length, const int32_t *count, void *o, int64_t batch,

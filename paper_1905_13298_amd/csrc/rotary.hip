@@ -119,8 +119,8 @@ struct Lane {
 };
 
 // Cosine and sine of 2 pi t. The angle is taken in quarter turns from the nearest one, in 64 bits, so
-// that a position of 2^31 leaves as many bits as a position of 0; what remains, up to pi / 4, goes
-// through the Taylor polynomials up to x^9 and x^10, whose next terms are 2.2e-9 of x and 1.1e-10.
+// that a far position costs 2^-53 of its angle (2^-30 at a million radians) and no more; what remains, up to
+// pi / 4, goes through the Taylor polynomials up to x^9 and x^10, whose next terms are 2.2e-9 of x and 1.1e-10.
 __device__ __forceinline__ void turn_of(double t, float &cosine, float &sine)
 {
     const double quarters = t * 4, near = rint(quarters);

@@ -1182,8 +1182,8 @@ def rotary_norm(q, k, positions, frequencies, q_weight=None, k_weight=None, sect
     sk = None if k is None else _keys(k, q)
     shape, sections, sp, wtype = _rotary(q, k, positions, frequencies, q_weight, k_weight, sections)
     dev = q.device
-    qo = torch.empty(q.shape, dtype=q.dtype, device=dev)
-    ko = None if k is None else torch.empty(k.shape, dtype=q.dtype, device=dev)
+    qo = torch.empty_like(q, memory_format=torch.contiguous_format)         # (1.2 us; torch.empty of four sizes 2.2)
+    ko = None if k is None else torch.empty_like(k, memory_format=torch.contiguous_format)
     _launch("ds_rotary_norm", dev, q.data_ptr(), _ptr(k), positions.data_ptr(), frequencies.data_ptr(), _ptr(q_weight), _ptr(k_weight),
             qo.data_ptr(), _ptr(ko), *shape, sections, sq, sk, sp, _packed(shape, 2), _packed(shape, 3), interleaved, eps,
             _TYPE[q.dtype], _TYPE[wtype], _TYPE[frequencies.dtype])
@@ -1205,8 +1205,8 @@ def rotary_norm_backward(dq_out, dk_out, q, k, positions, frequencies, q_weight=
     shape, sections, sp, wtype = _rotary(q, k, positions, frequencies, q_weight, k_weight, sections)
     dev = q.device
     _same_device(dev, dq_out, dk_out)
-    dq = torch.empty(q.shape, dtype=q.dtype, device=dev)
-    dk = None if k is None else torch.empty(k.shape, dtype=q.dtype, device=dev)
+    dq = torch.empty_like(q, memory_format=torch.contiguous_format)
+    dk = None if k is None else torch.empty_like(k, memory_format=torch.contiguous_format)
     dqw = None if q_weight is None else torch.empty_like(q_weight)
     dkw = None if k_weight is None else torch.empty_like(k_weight)
     scratch, size = (None, 0) if dqw is None and dkw is None else _scratch8("ds_rotary_norm_backward_scratch_bytes", shape[:5], dev)
@@ -1280,7 +1280,8 @@ def kv_cache_fp4_read(k_cache, v_cache, k_scales, v_scales, table, start, tokens
         raise ValueError("tokens must be >= 0")
     dev = k_cache.device
     _same_device(dev, v_cache, k_scales, v_scales, table, start, count)
-    k, v = (torch.empty((batch, tokens, heads, dim), dtype=dtype, device=dev) for _ in range(2))
+    k = torch.empty((batch, tokens, heads, dim), dtype=dtype, device=dev)
+    v = torch.empty_like(k)
     _launch("ds_kv_cache_fp4_read", dev, k_cache.data_ptr(), v_cache.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), table.data_ptr(),
             start.data_ptr(), _ptr(count), k.data_ptr(), v.data_ptr(), batch, tokens, heads, dim, page, pages, table.shape[1], ldt,
             _vectors(k, "k"), _vectors(v, "v"), _TYPE[dtype])
@@ -1300,7 +1301,7 @@ def attention_fp4(q, k_cache, v_cache, k_scales, v_scales, table, length, count=
         _vector(count, "count", _INT32, batch)
     dev = q.device
     _same_device(dev, k_cache, v_cache, k_scales, v_scales, table, length, count)
-    o = torch.empty((batch, tokens, hq, dim), dtype=q.dtype, device=dev)
+    o = torch.empty_like(q, memory_format=torch.contiguous_format)
     shape = (batch, tokens, heads, hq // heads, dim, page, table.shape[1])
     scratch, size = _scratch8("ds_attention_fp4_scratch_bytes", shape, dev)
     _launch("ds_attention_fp4", dev, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(),
