@@ -1,5 +1,5 @@
 // What the attentions over paged caches share: how queries and keys are found, the running
-// maximum of a softmax, the results' way out, and the launch that joins the splits of a long axis.
+// maximum of a softmax, and the results' way out.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -143,56 +143,6 @@ __device__ __forceinline__ void store_row(const AttentionParams &p, int b, int h
 }
 
 __device__ __forceinline__ float inverse(float total) { return total > 0.f ? 1.f / total : total == 0.f ? 0.f : total; }
-
-// The splits of a row together: a block of THREADS per row, LANES lanes (4 dimensions each)
-// per split, so that 16 or 8 or 4 splits (of 256 threads) are read at once. A few us (64 splits of 32 rows: 3), behind
-// the launch that writes them. A split without keys may have no results, only its maximum of -inf.
-template <typename T, int LANES, int THREADS = 256>
-__global__ void __launch_bounds__(THREADS)
-attention_join_kernel(const AttentionParams p)
-{
-    constexpr int kAtOnce = THREADS / LANES, kWaves = THREADS / 64;
-    __shared__ float red[2][kWaves];
-    __shared__ f32x4 sums[THREADS];
-    const int64_t at = blockIdx.x;
-    const int D = p.dim, d = int(threadIdx.x % LANES) * 4, mine = int(threadIdx.x) / LANES;
-    const float *part = p.part + at * p.splits * (D + 2);
-    float top = -__builtin_inff();
-    for (int s = threadIdx.x; s < p.splits; s += THREADS) top = fmaxf(top, part[s * (D + 2) + D]);
-    top = lanes_max<64>(top);
-    if ((threadIdx.x & 63) == 0) red[0][threadIdx.x >> 6] = top;
-    __syncthreads();
-    top = red[0][0];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, red[0][w]);
-    const float sub = or_zero(top);
-    float total = 0.f;
-    for (int s = threadIdx.x; s < p.splits; s += THREADS)
-        total = fmaf(part[s * (D + 2) + D + 1], __builtin_amdgcn_exp2f(part[s * (D + 2) + D] - sub), total);
-    total = lanes_sum<64>(total);
-    if ((threadIdx.x & 63) == 0) red[1][threadIdx.x >> 6] = total;
-    f32x4 o{};
-    if (d < D) {
-#pragma unroll 4
-        for (int s = mine; s < p.splits; s += kAtOnce) {
-            const float m = part[s * (D + 2) + D], f = __builtin_amdgcn_exp2f(m - sub);
-            f32x4 x;
-            __builtin_memcpy(&x, part + s * (D + 2) + d, 16);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] += m == -__builtin_inff() ? 0.f : x[i] * f;
-        }
-    }
-    sums[threadIdx.x] = o;
-    __syncthreads();
-    if (mine != 0 || d >= D) return;
-#pragma unroll
-    for (int i = 1; i < kAtOnce; ++i) o += sums[i * LANES + threadIdx.x];
-    total = red[1][0];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) total += red[1][w];
-    const int64_t bh = at / p.rows;
-    store_row<T>(p, int(bh / p.heads), int(bh % p.heads), int(at - bh * p.rows), nullptr, d, o, inverse(total));
-}
 
 bool page_ok(int64_t page) { return page == 16 || page == 32 || page == 64 || page == 128; }
 

@@ -923,6 +923,56 @@ attention4_many_kernel(const AttentionParams p, int blocks, int bhs)
         }
 }
 
+// The splits of a row together, in one trip: a block of 4 waves per row, LANES lanes (4 dimensions each) per split,
+// which keep a running maximum, and the groups' sums together in LDS. 64 splits of 32 rows 3.4 us behind the launch that
+// writes them (4.1 where the maximum is looked for first; 4 of 1536 rows 3.4 and 4.7). A split without keys has no results, only its
+// maximum of -inf.
+template <typename T, int LANES>
+__global__ void __launch_bounds__(256)
+attention4_join_kernel(const AttentionParams p)
+{
+    constexpr int kAtOnce = 256 / LANES;
+    __shared__ float ml[2][kAtOnce];
+    __shared__ f32x4 sums[256];
+    const int64_t at = blockIdx.x;
+    const int D = p.dim, lane = int(threadIdx.x % LANES), mine = int(threadIdx.x) / LANES, d = min(lane * 4, D - 4);
+    const float *const part = p.part + at * p.splits * (D + 2);
+    float m = -__builtin_inff(), l = 0.f;
+    f32x4 o{};
+#pragma unroll 4
+    for (int s = mine; s < p.splits; s += kAtOnce) {
+        const float *const from = part + s * (D + 2);
+        const float sm = from[D], sl = from[D + 1];
+        f32x4 x;
+        __builtin_memcpy(&x, from + d, 16);
+        const float top = fmaxf(m, sm), sub = or_zero(top), a = __builtin_amdgcn_exp2f(m - sub), b = __builtin_amdgcn_exp2f(sm - sub);
+        m = top;
+        l = fmaf(l, a, sl * b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = fmaf(o[i], a, sm == -__builtin_inff() ? 0.f : x[i] * b);
+    }
+    if (lane == 0) {
+        ml[0][mine] = m;
+        ml[1][mine] = l;
+    }
+    sums[threadIdx.x] = o;
+    __syncthreads();
+    if (mine != 0 || lane * 4 >= D) return;
+    float top = ml[0][0], total = 0.f;
+#pragma unroll
+    for (int i = 1; i < kAtOnce; ++i) top = fmaxf(top, ml[0][i]);
+    const float sub = or_zero(top);
+    f32x4 sum{};
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+        const float f = __builtin_amdgcn_exp2f(ml[0][i] - sub);
+        total = fmaf(ml[1][i], f, total);
+        sum += sums[i * LANES + lane] * f;
+    }
+    const int64_t bh = at / p.rows;
+    store_row<T>(p, int(bh / p.heads), int(bh % p.heads), int(at - bh * p.rows), nullptr, lane * 4, sum, inverse(total));
+}
+
 // How a call is split: over the rows first, then over the keys until 512 blocks (two a CU) have at
 // least 8 steps of 64 keys each. Measured (8 heads of 128, 4 query heads each; us): one query over 131072 keys 34.7,
 // with 768 blocks 36.9, with 1024 43; 16 x 1 over up to 8192 23.5, 22.7 and 28. Where sequences and heads alone
@@ -964,7 +1014,7 @@ void run_attention4(const AttentionParams &p, const Plan &a, int64_t batch, hipS
         hipLaunchKernelGGL((a.waves == 2 ? attention4_many_kernel<T, DP, 2> : attention4_many_kernel<T, DP, 4>), grid, dim3(64 * a.waves), 0, s, p, blocks, bhs);
     }
     if (a.splits > 1)
-        hipLaunchKernelGGL((attention_join_kernel<T, DP / 4>), dim3(uint32_t(bhs * a.rows)), dim3(256), 0, s, p);
+        hipLaunchKernelGGL((attention4_join_kernel<T, DP / 4>), dim3(uint32_t(bhs * a.rows)), dim3(256), 0, s, p);
 }
 
 template <typename T>

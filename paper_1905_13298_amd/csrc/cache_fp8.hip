@@ -724,6 +724,49 @@ attention_many_kernel(const AttentionParams p, int bhs)
         }
 }
 
+// The splits of a row together: a block of 4 waves per row, LANES lanes (4 dimensions each)
+// per split, so that 16 or 8 or 4 splits are read at once. A few us (64 splits of 32 rows: 3), behind
+// the launch that writes them.
+template <typename T, int LANES>
+__global__ void __launch_bounds__(256)
+attention_join_kernel(const AttentionParams p)
+{
+    constexpr int kAtOnce = 256 / LANES;
+    __shared__ float red[2][4];
+    __shared__ f32x4 sums[256];
+    const int64_t at = blockIdx.x;
+    const int D = p.dim, d = int(threadIdx.x % LANES) * 4, mine = int(threadIdx.x) / LANES;
+    const float *part = p.part + at * p.splits * (D + 2);
+    float top = -__builtin_inff();
+    for (int s = threadIdx.x; s < p.splits; s += 256) top = fmaxf(top, part[s * (D + 2) + D]);
+    top = lanes_max<64>(top);
+    if ((threadIdx.x & 63) == 0) red[0][threadIdx.x >> 6] = top;
+    __syncthreads();
+    const float sub = or_zero(fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3])));
+    float total = 0.f;
+    for (int s = threadIdx.x; s < p.splits; s += 256)
+        total = fmaf(part[s * (D + 2) + D + 1], __builtin_amdgcn_exp2f(part[s * (D + 2) + D] - sub), total);
+    total = lanes_sum<64>(total);
+    if ((threadIdx.x & 63) == 0) red[1][threadIdx.x >> 6] = total;
+    f32x4 o{};
+    if (d < D) {
+#pragma unroll 4
+        for (int s = mine; s < p.splits; s += kAtOnce) {
+            const float f = __builtin_amdgcn_exp2f(part[s * (D + 2) + D] - sub);
+            f32x4 x;
+            __builtin_memcpy(&x, part + s * (D + 2) + d, 16);
+            o += x * f;
+        }
+    }
+    sums[threadIdx.x] = o;
+    __syncthreads();
+    if (mine != 0 || d >= D) return;
+#pragma unroll
+    for (int i = 1; i < kAtOnce; ++i) o += sums[i * LANES + threadIdx.x];
+    const int64_t bh = at / p.rows;
+    store_row<T>(p, int(bh / p.heads), int(bh % p.heads), int(at - bh * p.rows), nullptr, d, o, inverse(red[1][0] + red[1][1] + red[1][2] + red[1][3]));
+}
+
 // How a call is split: over the rows first, then over the keys until 512 blocks (two a CU) have at
 // least 8 steps of 64 keys each. Measured (8 heads of 128, 4 query heads each; us): one query over 131072
 // keys 57, with 256 blocks 61, with 1024 61, unsplit 1202; 16 x 1 over up to 8192 40, 55, 43 and, with 2048,
