@@ -582,9 +582,10 @@ attention4_few_kernel(const AttentionParams p, int blocks)
 // contracts in the second product.
 //
 // Bound by the matrix instructions and the exponentials between them, which two waves of a SIMD overlap in
-// part: 2 x 1000 queries of 32 heads over up to 8000 keys of 8 heads of 128 take 246 us, 970 TFLOP/s.
+// part, and by turning keys and values into floats (without it 217 us): 2 x 1000 queries of 32 heads over up to 8000
+// keys of 8 heads of 128 take 246 us, 970 TFLOP/s. (Blocks of eight waves, which turn half as much each, 281.)
 template <typename T, int DP, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES, DP <= 128 ? 2 : 1)
+__global__ void __launch_bounds__(64 * WAVES, DP == 256 || (DP == 128 && WAVES == 2) ? 1 : 2)
 attention4_many_kernel(const AttentionParams p, int blocks, int bhs)
 {
     constexpr int QC = DP / 16, DT = DP / 32, kRuns = 4 / WAVES;
