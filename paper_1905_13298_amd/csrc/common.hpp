@@ -1,5 +1,5 @@
 // Host-side helpers shared by the entry points: error reporting and argument
-// validation. Nothing here touches the device except device_range_ok().
+// validation. Nothing here touches the device except device_range_ok() and device_allocation().
 #pragma once
 
 #include <cstdarg>
@@ -105,6 +105,9 @@ inline bool overlap(const void *a, int64_t abytes, const void *b, int64_t bbytes
 // True when [p, p + bytes) lies inside one device allocation known to the HIP
 // runtime. Rejects host pointers and buffers too small for the shape.
 bool device_range_ok(const void *p, int64_t bytes);
+
+// The device allocation that p lies in; false where the HIP runtime knows none.
+bool device_allocation(const void *p, uintptr_t &base, uint64_t &size);
 
 
 struct Range {

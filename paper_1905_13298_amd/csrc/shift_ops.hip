@@ -11,16 +11,26 @@
 
 namespace ds {
 
-bool device_range_ok(const void *p, int64_t bytes)
+bool device_allocation(const void *p, uintptr_t &base, uint64_t &size)
 {
-    hipDeviceptr_t base = nullptr;
-    size_t size = 0;
-    if (hipMemGetAddressRange(&base, &size, const_cast<void *>(p)) != hipSuccess) {
+    hipDeviceptr_t b = nullptr;
+    size_t n = 0;
+    if (hipMemGetAddressRange(&b, &n, const_cast<void *>(p)) != hipSuccess) {
         (void)hipGetLastError();  // clear the sticky error of a failed lookup
         return false;
     }
-    auto b = reinterpret_cast<uintptr_t>(base), q = reinterpret_cast<uintptr_t>(p);
-    return q >= b && q - b + uint64_t(bytes) <= uint64_t(size);
+    base = reinterpret_cast<uintptr_t>(b);
+    size = n;
+    return true;
+}
+
+bool device_range_ok(const void *p, int64_t bytes)
+{
+    uintptr_t b = 0;
+    uint64_t size = 0;
+    if (!device_allocation(p, b, size)) return false;
+    const auto q = reinterpret_cast<uintptr_t>(p);
+    return q >= b && q - b + uint64_t(bytes) <= size;
 }
 
 // Validates the sizes of a convolution problem and fills `g` (no pointers).

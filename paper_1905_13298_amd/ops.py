@@ -1227,16 +1227,20 @@ def kv_cache_fp4(pages: int, heads: int, page: int, dim: int, device="cuda:0"):
     return new(pages, heads, page, dim // 2), new(pages, heads, page // 4, dim // 8, 4, 4), scales(), scales()
 
 
+_UINT8, _SCALES = (torch.uint8,), (_E8M0,)
+
+
 def _check_cache_fp4(k_cache, v_cache, k_scales, v_scales, table, batch: int):
     """(pages, heads, page, dim) of a 4-bit cache and the row stride of its table."""
-    _dev_as(k_cache, "k_cache", (torch.uint8,))
+    _dev_as(k_cache, "k_cache", _UINT8)
     if k_cache.dim() != 4:
         raise ValueError("k_cache must be [pages, heads, page, dim / 2]")
     pages, heads, page, half = k_cache.shape
-    _dev_as(v_cache, "v_cache", (torch.uint8,), (pages, heads, page // 4, half // 4, 4, 4))
-    scales = (pages, heads, (half + 15) // 16, page)
-    _dev_as(k_scales, "k_scales", (_E8M0,), scales)
-    _dev_as(v_scales, "v_scales", (_E8M0,), scales)
+    for t, name, dtypes, shape in ((v_cache, "v_cache", _UINT8, (pages, heads, page // 4, half // 4, 4, 4)),
+                                   (k_scales, "k_scales", _SCALES, (pages, heads, (half + 15) // 16, page)),
+                                   (v_scales, "v_scales", _SCALES, (pages, heads, (half + 15) // 16, page))):
+        if not isinstance(t, torch.Tensor) or t.dtype is not dtypes[0] or t.shape != shape:
+            _dev_as(t, name, dtypes, shape)          # says what is wrong
     if not (k_cache.is_contiguous() and v_cache.is_contiguous() and k_scales.is_contiguous() and v_scales.is_contiguous()):
         raise ValueError("a cache and its scales must be contiguous")
     ldt = _rows(table, "table", _INT32)
