@@ -790,12 +790,17 @@ _E4M3, _E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
 _functions = {}
 
 
-def _launch(name: str, dev: torch.device, *args) -> None:
-    """Calls entry point `name` with the current stream of `dev` as its last argument. A decoded token's calls take
-    as long as the host does, so nothing is looked up twice and the device is set only where it is another."""
+def _function(name: str):
     fn = _functions.get(name)
     if fn is None:
         fn = _functions[name] = getattr(lib(), name)
+    return fn
+
+
+def _launch(name: str, dev: torch.device, *args) -> None:
+    """Calls entry point `name` with the current stream of `dev` as its last argument. A decoded token's calls take
+    as long as the host does, so nothing is looked up twice and the device is set only where it is another."""
+    fn = _function(name)
     index = dev.index
     if index == torch._C._cuda_getDevice():
         status = fn(*args, torch._C._cuda_getCurrentRawStream(index))
@@ -910,7 +915,7 @@ def rms_norm_backward(dy, h, weight, rstd, dh=None):
 
 def _scratch8(entry: str, shape, dev):
     """A call's scratch, which it cannot do without."""
-    size = getattr(lib(), entry)(*shape)
+    size = _function(entry)(*shape)
     return (torch.empty(size, dtype=torch.uint8, device=dev), size) if size > 0 else (None, 0)
 
 
