@@ -268,7 +268,7 @@ __device__ __forceinline__ void unroll(F &&f)
     }
 }
 
-// Up to 16 TILES queries of a kv head (tokens being decoded): a block of 4 waves takes a share of the keys, each wave
+// Up to 16 TILES queries of a kv head at a time (tokens being decoded): a block of 4 waves takes a share of the keys, each wave
 // every fourth 64 of it straight from memory to registers (no two waves share any), and joins them at its end.
 // Bound by reading the cache once, and by the blocks' starts and ends: 131072 keys of 8 heads of 128, 143 MB, 30.3 us
 // (4.7 TB/s) and 4.1 of joining; its VALU instructions, a third of them conversions, would take a third of that.
@@ -285,7 +285,7 @@ attention4_few_kernel(const AttentionParams p, int blocks)
     __shared__ f32x4 osum[kWaves][DT][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), r = lane & 15, g = lane >> 4;
     const int split = int(blockIdx.x), bh = int(blockIdx.y), b = bh / p.heads, h = bh - b * p.heads;
-    const int D = p.dim, page = 1 << p.page_shift;
+    const int D = p.dim, page = 1 << p.page_shift, row0 = int(blockIdx.z) * 16 * TILES;
     const Sequence seq(p, b);
     // Keys that some query sees lie in [tlo, thi); every query that sees any sees [alo, ahi).
     const int t1 = min(seq.count, p.tokens) - 1, t0 = min(max(-seq.first, 0), max(t1, 0));      // the first query that is not before the first key
@@ -296,8 +296,8 @@ attention4_few_kernel(const AttentionParams p, int blocks)
     const int from = s0 + split * each, to = min(s1, from + each);
     auto part_of = [&](int row) { return p.part + ((int64_t(bh) * p.rows + row) * p.splits + split) * (D + 2); };
     if (p.part && from >= to) {      // nothing here: no results, only that there are none
-        if (int(threadIdx.x) < p.rows) {
-            float *const part = part_of(int(threadIdx.x));
+        if (int(threadIdx.x) < min(16 * TILES, p.rows - row0)) {
+            float *const part = part_of(row0 + int(threadIdx.x));
             part[D] = -__builtin_inff();
             part[D + 1] = 0.f;
         }
@@ -386,7 +386,7 @@ attention4_few_kernel(const AttentionParams p, int blocks)
     bool none[TILES];
 #pragma unroll
     for (int u = 0; u < TILES; ++u) {
-        load_query<T, DP, 8, DP / 4, QC>(p, seq, b, h, u * 16 + r, g, low[u], high[u], qf[u]);
+        load_query<T, DP, 8, DP / 4, QC>(p, seq, b, h, row0 + u * 16 + r, g, low[u], high[u], qf[u]);
         // A row that sees no key, and is 0 in the end, takes part as if it saw every one, which costs less.
         none[u] = high[u] == 0;
         if (none[u]) high[u] = 0x7fffffff;
@@ -522,7 +522,7 @@ attention4_few_kernel(const AttentionParams p, int blocks)
 #pragma unroll
     for (int u = 0; u < TILES; ++u) {
         if (u > 0) __syncthreads();
-        const int row = u * 16 + r;
+        const int row = row0 + u * 16 + r;
         if (none[u]) {
             m[u] = -__builtin_inff();
             l[u] = 0.f;
@@ -571,7 +571,7 @@ attention4_few_kernel(const AttentionParams p, int blocks)
     }
 }
 
-// Many queries of a kv head: a block's waves have 32 of them each and share the keys, 64 at a
+// Many queries of a kv head: a block's four waves have 32 of them each and share the keys, 64 at a
 // time. A wave reads its part of them a step ahead, turns them into 16-bit floats, once for
 // the whole block, and puts them into LDS: keys as rows [key][dim], values as rows [dim][key],
 // the 16-byte pieces of a row in an order of its own, so that the lanes of a read (0-3, 12-15,
@@ -584,17 +584,17 @@ attention4_few_kernel(const AttentionParams p, int blocks)
 // Bound by the matrix instructions and the exponentials between them, which two waves of a SIMD overlap in
 // part, and by turning keys and values into floats (without it 217 us): 2 x 1000 queries of 32 heads over up to 8000
 // keys of 8 heads of 128 take 246 us, 970 TFLOP/s. (Blocks of eight waves, which turn half as much each, 281.)
-template <typename T, int DP, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES, DP == 256 || (DP == 128 && WAVES == 2) ? 1 : 2)
+template <typename T, int DP>
+__global__ void __launch_bounds__(256, DP == 256 ? 1 : 2)
 attention4_many_kernel(const AttentionParams p, int blocks, int bhs)
 {
-    constexpr int QC = DP / 16, DT = DP / 32, kRuns = 4 / WAVES;
+    constexpr int kWaves = 4, QC = DP / 16, DT = DP / 32;
     constexpr int kWords = DP / 32;            // words (8 codes) of a lane's part of a run's keys, and of its values' tokens
     constexpr int NS = DP == 256 ? 2 : 1;      // scale blocks of it
     constexpr int kKeys = kStep * DP * 2;      // bytes of a step's keys, or values
     typedef typename Vec8<T>::type v8;
     __shared__ __align__(16) uint8_t lds[2][2 * kKeys];
-    __shared__ int nans[2][WAVES];             // whether a wave's part of the values has any
+    __shared__ int nans[2][kWaves];             // whether a wave's part of the values has any
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), r = lane & 31, hf = lane >> 5, g = lane >> 4;
     // An eighth of the work to each XCD, a head's blocks together, so that they read its
     // keys through one L2, the same head of every sequence next, whose lengths may differ; the
@@ -608,12 +608,12 @@ attention4_many_kernel(const AttentionParams p, int blocks, int bhs)
     const Sequence seq(p, b);
     v8 qf[QC];
     int low, high;
-    const int row = (tile * WAVES + wave) * 32 + r;
+    const int row = (tile * kWaves + wave) * 32 + r;
     const bool live = load_query<T, DP, 16, 8, QC>(p, seq, b, h, row, hf, low, high, qf);
     // A row without a query sees every key, which costs less than no key, and is 0 in the end.
     if (!live) high = 0x7fffffff;
     // The block's keys: from the first that its first query sees to its last query's own.
-    const int t0 = tile * WAVES * 32 / p.group, t1 = min(((tile + 1) * WAVES * 32 - 1) / p.group, seq.count - 1);
+    const int t0 = tile * kWaves * 32 / p.group, t1 = min(((tile + 1) * kWaves * 32 - 1) / p.group, seq.count - 1);
     const int thi = t0 < seq.count ? min(max(seq.first + t1 + 1, 0), seq.keys) : 0;
     const int tlo = p.window ? max(max(seq.first + t0 + 1, 0) - p.window, 0) : 0;
     // Steps of which one of its queries does not see every key.
@@ -639,8 +639,8 @@ attention4_many_kernel(const AttentionParams p, int blocks, int bhs)
     // 4 tokens x 8 dimensions (of heads of up to 64 half of them, of more than 128 two such pieces). What lies past
     // `dim` is read somewhere inside. Where there is no page, page 0 is read instead.
     const int kkey = lane >> 2, kdim = (lane & 3) * (DP / 4), quad = lane >> 4, vgroup = lane & 15;
-    uint32_t kraw[kRuns][kWords], kse[kRuns][NS], vse[kRuns][NS];
-    i32x4 vraw[kRuns][NS];
+    uint32_t kraw[kWords], kse[NS], vse[NS];
+    i32x4 vraw[NS];
     uint32_t koff[kWords / 2], kso[NS], voff[NS], vso[NS];
 #pragma unroll
     for (int i = 0; i < kWords / 2; ++i) koff[i] = uint32_t(kkey * (D / 2) + min(kdim + i * 16, D - 16) / 2);
@@ -656,33 +656,29 @@ attention4_many_kernel(const AttentionParams p, int blocks, int bhs)
     const uint8_t *const ksh = p.ks + h * head_scales, *const vsh = p.vs + h * head_scales;
     const int64_t page_bytes = p.heads * head_bytes, page_scales = p.heads * head_scales;
     auto fetch = [&](int step, int pids) {
+        const int pid = max(__builtin_amdgcn_readlane(pids, wave * 16), 0), slot = (step * kStep + wave * 16) & (page - 1);
+        const uint8_t *k = kh + pid * page_bytes + slot * (D / 2), *v = vh + pid * page_bytes + slot * (D / 2);
+        const uint8_t *ks = ksh + pid * page_scales + slot, *vs = vsh + pid * page_scales + slot;
+        if (kWords >= 4 && D == DP) {
 #pragma unroll
-        for (int q = 0; q < kRuns; ++q) {
-            const int which = wave * kRuns + q, pid = max(__builtin_amdgcn_readlane(pids, which * 16), 0);
-            const int slot = (step * kStep + which * 16) & (page - 1);
-            const uint8_t *k = kh + pid * page_bytes + slot * (D / 2), *v = vh + pid * page_bytes + slot * (D / 2);
-            const uint8_t *ks = ksh + pid * page_scales + slot, *vs = vsh + pid * page_scales + slot;
-            if (kWords >= 4 && D == DP) {
+            for (int i = 0; i < kWords / 4; ++i) {
+                const i32x4 x = *reinterpret_cast<const i32x4 *>(k + koff[2 * i]);
 #pragma unroll
-                for (int i = 0; i < kWords / 4; ++i) {
-                    const i32x4 x = *reinterpret_cast<const i32x4 *>(k + koff[2 * i]);
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) kraw[q][4 * i + w] = uint32_t(x[w]);
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < kWords / 2; ++i) {
-                    const i32x2 x = *reinterpret_cast<const i32x2 *>(k + koff[i]);
-                    kraw[q][2 * i] = uint32_t(x[0]);
-                    kraw[q][2 * i + 1] = uint32_t(x[1]);
-                }
+                for (int w = 0; w < 4; ++w) kraw[4 * i + w] = uint32_t(x[w]);
             }
+        } else {
 #pragma unroll
-            for (int i = 0; i < NS; ++i) {
-                vraw[q][i] = *reinterpret_cast<const i32x4 *>(v + voff[i]);
-                kse[q][i] = ks[kso[i]];
-                vse[q][i] = *reinterpret_cast<const uint32_t *>(vs + vso[i]);
+            for (int i = 0; i < kWords / 2; ++i) {
+                const i32x2 x = *reinterpret_cast<const i32x2 *>(k + koff[i]);
+                kraw[2 * i] = uint32_t(x[0]);
+                kraw[2 * i + 1] = uint32_t(x[1]);
             }
+        }
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+            vraw[i] = *reinterpret_cast<const i32x4 *>(v + voff[i]);
+            kse[i] = ks[kso[i]];
+            vse[i] = *reinterpret_cast<const uint32_t *>(vs + vso[i]);
         }
     };
     // The order of a key's pieces: its row in a tile, from 16 on again (rows of 128 bytes share a bank row
@@ -694,52 +690,46 @@ attention4_many_kernel(const AttentionParams p, int blocks, int bhs)
     // 0 as a 16-bit float). So does what was read of a key past `dim`.
     auto clear = [&](int step, int pids) {
         if (__builtin_expect(D == DP && step * kStep >= tlo && step * kStep + kStep <= thi && on_pages(pids), 1)) return;
+        const bool there = __builtin_amdgcn_readlane(pids, wave * 16) >= 0;
 #pragma unroll
-        for (int q = 0; q < kRuns; ++q) {
-            const int which = wave * kRuns + q, run = step * kStep + which * 16;
-            const bool there = __builtin_amdgcn_readlane(pids, which * 16) >= 0;
+        for (int i = 0; i < NS; ++i) vse[i] &= uint32_t(there ? key_mask(step * kStep + wave * 16 + 4 * quad, tlo, thi) : 0);
 #pragma unroll
-            for (int i = 0; i < NS; ++i) vse[q][i] &= uint32_t(there ? key_mask(run + 4 * quad, tlo, thi) : 0);
-#pragma unroll
-            for (int i = 0; i < kWords; ++i)
-                if (kdim + i * 8 >= D) kraw[q][i] = 0;
-        }
+        for (int i = 0; i < kWords; ++i)
+            if (kdim + i * 8 >= D) kraw[i] = 0;
     };
     auto note_nans = [&](int step, int buf) {
         if (!mixed(step)) return;
         uint32_t nan = 0;
 #pragma unroll
-        for (int q = 0; q < kRuns; ++q)
-#pragma unroll
-            for (int i = 0; i < NS; ++i) nan |= nan_scales(vse[q][i]);
+        for (int i = 0; i < NS; ++i) nan |= nan_scales(vse[i]);
         nans[buf][wave] = __any(nan != 0);
     };
     // Part u of what fetch() read, to LDS: 8 dimensions of a key, or 2 of 4 tokens' values, turned
     // around. (Every other lane writes its two rows in the other order, so that all banks have work.) A part's place
     // differs from the first one's in bits that are 0 there or are exclusive-ored by the order; it is formed anew
     // each time, since registers are short.
-    constexpr int kParts = kRuns * kWords * 2;
+    constexpr int kParts = kWords * 2;
     const int odd = DP == 64 ? (vgroup >> 3) & 1 : vgroup & 1;
     const uint32_t first = odd ? 0x07060302u : 0x05040100u, second = odd ? 0x05040100u : 0x07060302u;
-    int kput = (wave * kRuns * 16 + kkey) * DP * 2 + (((lane & 3) * kWords) ^ order(kkey)) * 16;
+    int kput = (wave * 16 + kkey) * DP * 2 + (((lane & 3) * kWords) ^ order(kkey)) * 16;
     int vput = kKeys + vgroup * (DP == 64 ? 4 : 8) * 128 + odd * 128 +
-               ((wave * kRuns * 2 + (quad >> 1)) ^ vorder(vgroup * (DP == 64 ? 4 : 8))) * 16 + (quad & 1) * 8;
+               ((wave * 2 + (quad >> 1)) ^ vorder(vgroup * (DP == 64 ? 4 : 8))) * 16 + (quad & 1) * 8;
     int vnext = odd ? -128 : 128;
     auto put = [&](auto part, int buf) {
         constexpr int u = decltype(part)::value;
-        constexpr int q = u / (2 * kWords), c = u / 2 % kWords;
+        constexpr int c = u / 2;
         if constexpr (u % 2 == 0) {
-            *reinterpret_cast<v8 *>(lds[buf] + ((kput ^ c * 16) + q * 16 * DP * 2)) = operand4<T>(kraw[q][c], scale4(kse[q][c * NS / kWords]));
+            *reinterpret_cast<v8 *>(lds[buf] + (kput ^ c * 16)) = operand4<T>(kraw[c], scale4(kse[c * NS / kWords]));
         } else {
             constexpr int i = DP == 256 ? c / 4 : 0, sel = c % 4;
             uint32_t x[4];
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                const uint32_t w = uint32_t(vraw[q][i][t]);
-                const f16x2 y = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(DP == 64 ? w >> (16 * (vgroup & 1)) : w, scale_of(vse[q][i], t), sel);
+                const uint32_t w = uint32_t(vraw[i][t]);
+                const f16x2 y = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(DP == 64 ? w >> (16 * (vgroup & 1)) : w, scale_of(vse[i], t), sel);
                 x[t] = __builtin_bit_cast(uint32_t, y);
             }
-            uint8_t *const to = lds[buf] + ((vput ^ (q * 2 ^ sel) * 16) + (i * 128 + sel * 2) * 128);
+            uint8_t *const to = lds[buf] + ((vput ^ sel * 16) + (i * 128 + sel * 2) * 128);
             *reinterpret_cast<i32x2 *>(to) = i32x2{int(__builtin_amdgcn_perm(x[1], x[0], first)), int(__builtin_amdgcn_perm(x[3], x[2], first))};
             *reinterpret_cast<i32x2 *>(to + vnext) = i32x2{int(__builtin_amdgcn_perm(x[1], x[0], second)), int(__builtin_amdgcn_perm(x[3], x[2], second))};
         }
@@ -780,7 +770,7 @@ attention4_many_kernel(const AttentionParams p, int blocks, int bhs)
         if (mixed(step)) {
             int nan = 0;
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) nan |= nans[buf][w];
+            for (int w = 0; w < kWaves; ++w) nan |= nans[buf][w];
             if (__builtin_amdgcn_readfirstlane(nan)) {      // the same in every wave
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
@@ -805,7 +795,7 @@ attention4_many_kernel(const AttentionParams p, int blocks, int bhs)
                 }
                 wait_lds();
                 barrier();
-                for (int i = int(threadIdx.x); i < kKeys / 16; i += 64 * WAVES) {
+                for (int i = int(threadIdx.x); i < kKeys / 16; i += 64 * kWaves) {
                     f16x8 *const at = reinterpret_cast<f16x8 *>(lds[buf] + kKeys + i * 16);
                     f16x8 v = *at;
 #pragma unroll
@@ -981,14 +971,16 @@ attention4_join_kernel(const AttentionParams p)
 // up to 8192 55.5, until 512 60.4, until 3072 70; 64 x 1 over up to 16000 131, 16 splits each 170. (Splits have the same
 // number of steps, so that a sequence much longer than 63 others is what a call waits for.) Few queries whose
 // splits would not give every CU a block have splits of 4 steps: 1 x 1 over 2000 8.7, of 8 10.1.
-// Up to 32 rows (of heads above 128: 16) run attention4_few_kernel, from 17 on in two tiles: 32 x 5 queries over up
-// to 4000 keys 37.5, through LDS 80.6; 5 x 3 of 7 heads each 13.4 and 17.6. To 64 rows blocks of two waves, above of four.
+// Up to 64 rows run attention4_few_kernel, from 17 on in blocks of 32 rows (of heads above 128: 16): 32 x 5 queries over
+// up to 4000 keys 37.5, through LDS 80.6; 32 x 16 62.8 and 88.3, of heads of 256 (8 x 16) 53.9 and 75.7, of 64 58.9 and 68.5;
+// 5 x 3 of 7 heads each 13.4 and 17.6; 1 x 16 over 8000 15.2 and 26.8. Above, 32 x 32 queries would take 106 for 86.
 Plan plan_attention4(int64_t batch, int64_t tokens, int64_t heads, int64_t group, int64_t dim, int64_t columns, int64_t page)
 {
     Plan a;
     a.rows = tokens * group;
-    a.waves = a.rows <= (dim <= 128 ? 32 : 16) ? 0 : a.rows <= 64 ? 2 : 4;
-    a.row_tiles = a.waves ? int((a.rows + 32 * a.waves - 1) / (32 * a.waves)) : 1;
+    a.waves = a.rows <= 64 ? 0 : 4;
+    const int tile = a.waves ? 32 * a.waves : dim <= 128 && a.rows > 16 ? 32 : 16;
+    a.row_tiles = int((a.rows + tile - 1) / tile);
     const int64_t blocks = std::max<int64_t>(batch * heads * a.row_tiles, 1), steps = (columns * page + kStep - 1) / kStep;
     const bool uneven = a.waves == 0 && blocks > 256;
     a.least = uneven ? 16 : 8;
@@ -1009,10 +1001,10 @@ void run_attention4(const AttentionParams &p, const Plan &a, int64_t batch, hipS
     const int blocks = int(blocks4(p.dim));
     if (a.waves == 0) {
         constexpr int most = DP <= 128 ? 2 : 1;
-        hipLaunchKernelGGL((a.rows <= 16 ? attention4_few_kernel<T, DP, 1> : attention4_few_kernel<T, DP, most>), dim3(a.splits, bhs), dim3(256), 0, s, p, blocks);
+        hipLaunchKernelGGL((a.rows <= 16 ? attention4_few_kernel<T, DP, 1> : attention4_few_kernel<T, DP, most>), dim3(a.splits, bhs, a.row_tiles), dim3(256), 0, s, p, blocks);
     } else {
         const dim3 grid(uint32_t((int64_t(bhs) * a.row_tiles * a.splits + 7) / 8 * 8));
-        hipLaunchKernelGGL((a.waves == 2 ? attention4_many_kernel<T, DP, 2> : attention4_many_kernel<T, DP, 4>), grid, dim3(64 * a.waves), 0, s, p, blocks, bhs);
+        hipLaunchKernelGGL((attention4_many_kernel<T, DP>), grid, dim3(64 * a.waves), 0, s, p, blocks, bhs);
     }
     if (a.splits > 1)
         hipLaunchKernelGGL((attention4_join_kernel<T, DP / 4>), dim3(uint32_t(bhs * a.rows)), dim3(256), 0, s, p);

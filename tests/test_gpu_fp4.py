@@ -307,6 +307,25 @@ def test_attention_many_tokens(ops, dim, tokens, lengths, dtype):
     attention_case(ops, dim, 64 if dim % 32 else 16, 1, 2, tokens, lengths, count=[min(tokens, n) for n in lengths], seed=tokens, dtype=dtype)
 
 
+@pytest.mark.parametrize("dim", [32, 112, 128, 240])
+@pytest.mark.parametrize("group,tokens", [(1, 33), (3, 16), (7, 9), (8, 8), (13, 5), (33, 2)])
+def test_attention_from_33_to_66_rows(ops, dim, group, tokens):
+    """Rows past a block's 32 (or 16) and past 64, with counts that leave some of them empty, pages that are none and a window."""
+    attention_case(ops, dim, 32, 2, group, tokens, [tokens, 500, 3, 1000], count=[tokens, tokens - 2, 2, 1], seed=dim + tokens)
+    attention_case(ops, dim, 128, 1, group, tokens, [700, 90], window=37, seed=dim + tokens, holes=True, dtype=F16)
+
+
+@pytest.mark.parametrize("seed", range(30))
+def test_attention_random_shapes(ops, seed):
+    import random
+    r = random.Random(seed)
+    dim, group, tokens = r.choice([16, 48, 64, 96, 128, 160, 256]), r.choice([1, 2, 3, 4, 7, 8, 16]), r.choice([1, 1, 2, 4, 8, 13, 33, 70])
+    lengths = [r.choice([0, 1, tokens, r.randint(0, 900)]) for _ in range(r.choice([1, 2, 4]))]
+    attention_case(ops, dim, r.choice([16, 32, 64, 128]), r.choice([1, 2, 3]), group, tokens, lengths, window=r.choice([0, 0, 1, r.randint(2, 500)]),
+                   dtype=r.choice([BF16, F16]), count=r.choice([None, [r.randint(-1, tokens + 1) for _ in lengths]]), seed=seed,
+                   holes=r.random() < 0.3, scale=r.choice([None, None, 0.3, -0.1]), short=r.choice([0, 0, 2]))
+
+
 @pytest.mark.parametrize("window", [1, 16, 63, 64, 100])
 @pytest.mark.parametrize("tokens", [1, 3, 40])
 def test_attention_window(ops, window, tokens):
