@@ -212,8 +212,8 @@ read4_kernel(T *__restrict__ k, T *__restrict__ v, const uint8_t *__restrict__ k
 // The key of row r of a 16-key tile t is 4 r + t: lane group g (lane / 16) holds the products of keys
 // 16 g .. 16 g + 15, and those are the ones that it contracts in the second product, 8 at a time; and a
 // lane's four keys of the first product have their scales side by side. Dimension r of tile j of
-// the second product is (DP / 16) r + j (within 128), so that a lane's dimensions are neighbours in
-// memory too. Keys become numbers of the queries' type exactly, with their scales; p and the values
+// the second product is 8 r + j (of heads of up to 64: 4 r + j; above 128 there are two such sets), so that a lane's
+// dimensions are neighbours in memory too. Keys become numbers of the queries' type exactly, with their scales; p and the values
 // are 16-bit floats with 10 bits of mantissa: values exactly, p rounded once, to 2^-11 of itself down to
 // 2^-23 of the row's largest and to 2^-34 of that one below (l has all of it in 32 bits).
 
@@ -271,7 +271,7 @@ __device__ __forceinline__ void unroll(F &&f)
 // Up to 16 TILES queries of a kv head at a time (tokens being decoded): a block of 4 waves takes a share of the keys, each wave
 // every fourth 64 of it straight from memory to registers (no two waves share any), and joins them at its end.
 // Bound by reading the cache once, and by the blocks' starts and ends: 131072 keys of 8 heads of 128, 143 MB, 30.3 us
-// (4.7 TB/s) and 4.1 of joining; its VALU instructions, a third of them conversions, would take a third of that.
+// (4.7 TB/s) and 3.4 of joining; its VALU instructions, a third of them conversions, would take 38 % of that.
 template <typename T, int DP, int TILES>
 __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1)
 attention4_few_kernel(const AttentionParams p, int blocks)
@@ -635,10 +635,15 @@ attention4_many_kernel(const AttentionParams p, int blocks, int bhs)
     };
     auto on_page = [&](int pid) { return unsigned(pid) < unsigned(p.pages) ? pid : -1; };
     auto on_pages = [&](int pids) { return bool(__all(pids >= 0)); };
-    // A lane's part of a run of 16 keys: a quarter of the dimensions of key lane / 4, and of the values
-    // 4 tokens x 8 dimensions (of heads of up to 64 half of them, of more than 128 two such pieces). What lies past
-    // `dim` is read somewhere inside. Where there is no page, page 0 is read instead.
-    const int kkey = lane >> 2, kdim = (lane & 3) * (DP / 4), quad = lane >> 4, vgroup = lane & 15;
+    // A lane's part of a run of 16 keys: a quarter of the dimensions of one key, and of the values 4 tokens x 8 dimensions
+    // (of heads of up to 64 half of them, of more than 128 two such pieces). What lies past `dim` is read somewhere
+    // inside. Where there is no page, page 0 is read instead. Which lane has which part is such that lanes which
+    // write to LDS at once, 128 bytes of them, meet in no bank (with neighbours in a row half of the writes' cycles
+    // were conflicts: 250.9 us for 249.4; 4 x 300 queries of heads of 256 over 4000 keys 229.8 for 221.1).
+    const int bit2 = (lane >> 2) & 1, bit3 = (lane >> 3) & 1, high2 = lane >> 4;
+    const int kkey = DP == 64 ? high2 * 4 + bit2 * 2 + bit3 : DP == 128 ? high2 * 4 + ((lane >> 1) & 3) : bit2 * 8 + bit3 * 4 + (lane & 3);
+    const int quarter = DP == 64 ? lane & 3 : DP == 128 ? bit3 * 2 + (lane & 1) : high2, kdim = quarter * (DP / 4);
+    const int quad = (lane >> 5) * 2 + (lane & 1), vgroup = ((lane >> 4) & 1) * 8 + ((lane >> 1) & 7);
     uint32_t kraw[kWords], kse[NS], vse[NS];
     i32x4 vraw[NS];
     uint32_t koff[kWords / 2], kso[NS], voff[NS], vso[NS];
@@ -683,7 +688,7 @@ attention4_many_kernel(const AttentionParams p, int blocks, int bhs)
     };
     // The order of a key's pieces: its row in a tile, from 16 on again (rows of 128 bytes share a bank row
     // by twos); of a dimension's pieces: such that both a read's 16 dimensions and a write's, every
-    // fourth or eighth, are spread.
+    // fourth or eighth of 8, are spread.
     auto order = [](int key) { return ((key & 3) | ((key >> 3) & 1) << 2 | ((key >> 2) & 1) << 3) >> (DP < 128 ? 1 : 0); };
     auto vorder = [](int d) { return ((d >> 1) ^ (d >> 4)) & 7; };
     // Keys that no query sees may hold anything: their values count as 0 (whatever the code, 2^-127 of it is
@@ -705,16 +710,11 @@ attention4_many_kernel(const AttentionParams p, int blocks, int bhs)
         nans[buf][wave] = __any(nan != 0);
     };
     // Part u of what fetch() read, to LDS: 8 dimensions of a key, or 2 of 4 tokens' values, turned
-    // around. (Every other lane writes its two rows in the other order, so that all banks have work.) A part's place
-    // differs from the first one's in bits that are 0 there or are exclusive-ored by the order; it is formed anew
-    // each time, since registers are short.
+    // around. A part's place differs from the first one's in bits that are 0 there or are exclusive-ored by the
+    // order; it is formed anew each time, since registers are short.
     constexpr int kParts = kWords * 2;
-    const int odd = DP == 64 ? (vgroup >> 3) & 1 : vgroup & 1;
-    const uint32_t first = odd ? 0x07060302u : 0x05040100u, second = odd ? 0x05040100u : 0x07060302u;
-    int kput = (wave * 16 + kkey) * DP * 2 + (((lane & 3) * kWords) ^ order(kkey)) * 16;
-    int vput = kKeys + vgroup * (DP == 64 ? 4 : 8) * 128 + odd * 128 +
-               ((wave * 2 + (quad >> 1)) ^ vorder(vgroup * (DP == 64 ? 4 : 8))) * 16 + (quad & 1) * 8;
-    int vnext = odd ? -128 : 128;
+    int kput = (wave * 16 + kkey) * DP * 2 + ((quarter * kWords) ^ order(kkey)) * 16;
+    int vput = kKeys + vgroup * (DP == 64 ? 4 : 8) * 128 + ((wave * 2 + (quad >> 1)) ^ vorder(vgroup * (DP == 64 ? 4 : 8))) * 16 + (quad & 1) * 8;
     auto put = [&](auto part, int buf) {
         constexpr int u = decltype(part)::value;
         constexpr int c = u / 2;
@@ -730,8 +730,8 @@ attention4_many_kernel(const AttentionParams p, int blocks, int bhs)
                 x[t] = __builtin_bit_cast(uint32_t, y);
             }
             uint8_t *const to = lds[buf] + ((vput ^ sel * 16) + (i * 128 + sel * 2) * 128);
-            *reinterpret_cast<i32x2 *>(to) = i32x2{int(__builtin_amdgcn_perm(x[1], x[0], first)), int(__builtin_amdgcn_perm(x[3], x[2], first))};
-            *reinterpret_cast<i32x2 *>(to + vnext) = i32x2{int(__builtin_amdgcn_perm(x[1], x[0], second)), int(__builtin_amdgcn_perm(x[3], x[2], second))};
+            *reinterpret_cast<i32x2 *>(to) = i32x2{int(__builtin_amdgcn_perm(x[1], x[0], 0x05040100u)), int(__builtin_amdgcn_perm(x[3], x[2], 0x05040100u))};
+            *reinterpret_cast<i32x2 *>(to + 128) = i32x2{int(__builtin_amdgcn_perm(x[1], x[0], 0x07060302u)), int(__builtin_amdgcn_perm(x[3], x[2], 0x07060302u))};
         }
     };
     // Pages of this step and the next, and the table's entry of the one after.
@@ -968,7 +968,7 @@ attention4_join_kernel(const AttentionParams p)
 // least 8 steps of 64 keys each. Measured (8 heads of 128, 4 query heads each; us): one query over 131072 keys 34.7,
 // with 768 blocks 36.9, with 1024 43; 16 x 1 over up to 8192 23.5, 22.7 and 28. Where sequences and heads alone
 // make more than 256 blocks of few queries, whose lengths may differ, until 1536 have at least 16 steps each: 48 x 1 over
-// up to 8192 55.5, until 512 60.4, until 3072 70; 64 x 1 over up to 16000 131, 16 splits each 170. (Splits have the same
+// up to 8192 55.5, until 512 60.4, with 8 splits each 70; 64 x 1 over up to 16000 131, 16 splits each 170. (Splits have the same
 // number of steps, so that a sequence much longer than 63 others is what a call waits for.) Few queries whose
 // splits would not give every CU a block have splits of 4 steps: 1 x 1 over 2000 8.7, of 8 10.1.
 // Up to 64 rows run attention4_few_kernel, from 17 on in blocks of 32 rows (of heads above 128: 16): 32 x 5 queries over
