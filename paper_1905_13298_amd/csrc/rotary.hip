@@ -38,7 +38,7 @@ struct RotaryParams {
 };
 
 // A lane's 16 elements of a vector: 8 pairs from pair 8 * lane on. Pairs past `pairs`, of the elements
-// that are not turned, are made up likewise. RUN: so many of the lane's first (and second) elements
+// that are not turned, are made up likewise; turn() leaves those as they are. RUN: so many of the lane's first (and second) elements
 // lie together: 8, 4 or 1.
 template <int RUN>
 struct Lane {
@@ -56,6 +56,16 @@ struct Lane {
     {
         if (interleaved) return 2 * j + which;
         return j < pairs ? j + which * pairs : pairs + j + which * rest;
+    }
+    // Pair i turned by its angle, back where SIGN is -1. (An element that stays is chosen, not multiplied by 1 and 0: its made-up
+    // partner may be infinite or NaN.)
+    template <int SIGN>
+    __device__ __forceinline__ void turn(int i, float cosine, float sine, float &a, float &b) const
+    {
+        const float x = a, y = b, s = SIGN * sine;
+        const bool turned = j0 + i < pairs;
+        a = turned ? fmaf(x, cosine, -(y * s)) : x;
+        b = turned ? fmaf(y, cosine, x * s) : y;
     }
     // The pairs' elements a[i], b[i].
     template <typename T>
@@ -199,13 +209,9 @@ rotary_kernel(const T *__restrict__ q, const T *__restrict__ k, const W *__restr
             }
         }
         if (!mine) continue;
-        float u[8], v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            u[e] = fmaf(x[e], cosine[e], -(y[e] * sine[e]));
-            v[e] = fmaf(y[e], cosine[e], x[e] * sine[e]);
-        }
-        me.store(dst + h * p.out[which][2], u, v);
+        for (int e = 0; e < 8; ++e) me.template turn<1>(e, cosine[e], sine[e], x[e], y[e]);
+        me.store(dst + h * p.out[which][2], x, y);
     }
 }
 
@@ -246,11 +252,7 @@ rotary_grad_kernel(const T *__restrict__ dq, const T *__restrict__ dk, const T *
                 if (weight) me.load(src + h * p.in[which][2], x, y);
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float a = u[i], c = v[i];
-                u[i] = fmaf(a, cosine[i], c * sine[i]);
-                v[i] = fmaf(c, cosine[i], -(a * sine[i]));
-            }
+            for (int i = 0; i < 8; ++i) me.template turn<-1>(i, cosine[i], sine[i], u[i], v[i]);
             if (weight) {
                 float sum = 0.f;
 #pragma unroll
