@@ -257,7 +257,8 @@ rotary_grad_kernel(const T *__restrict__ dq, const T *__restrict__ dk, const T *
                 float sum = 0.f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], fmaf(y[i], y[i], sum));
-                const float r = 1.f / sqrtf(fmaf(lanes_sum<LPV>(sum), inv, p.eps));
+                // (A lane without elements adds 0 to the weight's sums, also where eps is 0 and its root has no inverse.)
+                const float root = sqrtf(fmaf(lanes_sum<LPV>(sum), inv, p.eps)), r = mine ? 1.f / root : 0.f;
                 sum = 0.f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {

@@ -90,3 +90,23 @@ def test_gradient_behind_a_norm_of_what_is_not_turned(ops, dim, pairs, interleav
         near(got[i], r * (e - n * inner),
              r * (slack * w.abs() + n.abs() * ((slack * w.abs() * n.abs()).mean(-1, keepdim=True) + magnitude * 2.0 ** -18) + e.abs() * 2.0 ** -19))
         near(got[2 + i], (g * n).sum((0, 1, 2)), (both * n.abs()).sum((0, 1, 2)) * 2.0 ** -18)
+
+
+@pytest.mark.parametrize("dim,heads,kv", [(32, 5, 16), (64, 17, 3), (80, 9, 8), (128, 3, 9), (250, 5, 2)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_gradient_without_eps(ops, dim, heads, kv, dtype):  # noqa: F811
+    """eps = 0 over numbers of heads that leave lanes without one."""
+    q, k, positions, f, qw, kw, _ = inputs(dim, 2, 3, heads, kv, dim, dim // 2, 0, True, dtype, 100)
+    dy = [normal(90 + i, *x.shape).to(dtype) for i, x in enumerate((q, k))]
+    got = ops.rotary_norm_backward(*to(DEV, *dy, q, k, positions, f, qw, kw), eps=0.0)
+    a = angles(positions, f, None)
+    for i, (d, x, w) in enumerate(zip(dy, (q, k), (qw, kw))):
+        g, both = turn(d.double(), a, False, back=True)
+        x, w = x.double(), w.double()
+        r = 1 / torch.sqrt((x * x).mean(-1, keepdim=True))
+        n, e = x * r, g * w
+        inner, magnitude = (e * n).mean(-1, keepdim=True), (e * n).abs().mean(-1, keepdim=True)
+        slack = both * 2.0 ** -21
+        near_finite(got[i], r * (e - n * inner),
+                    r * (slack * w.abs() + n.abs() * ((slack * w.abs() * n.abs()).mean(-1, keepdim=True) + magnitude * 2.0 ** -18) + e.abs() * 2.0 ** -19))
+        near_finite(got[2 + i], (g * n).sum((0, 1, 2)), (both * n.abs()).sum((0, 1, 2)) * 2.0 ** -18)
