@@ -668,7 +668,7 @@ int64_t ds_linear_fp8_backward_data_scratch_bytes(int64_t m, int64_t n, int64_t 
  * tokens; dim: a multiple of 16, at most 256. Row b of `table` [batch][columns] (ldt
  * elements apart) lists the pages of sequence b in order; columns x page is at most 2^31 - 4096.
  *
- * ds_kv_cache_append writes tokens 0 .. count[b] - 1 (count NULL or above tokens: all) of
+ * ds_kv_cache_append writes tokens 0 .. count[b] - 1 (count NULL or above tokens: all; below 1: none) of
  * k and v [batch][tokens][heads][dim] at positions start[b], start[b] + 1, .. of sequence b
  * (none where start[b] is negative). A page's scale is the one its new tokens need; where it
  * already holds tokens before start[b], the larger of that and its own, and what it holds is

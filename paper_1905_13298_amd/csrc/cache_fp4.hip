@@ -51,7 +51,7 @@ struct Place {
         const int i = (int(blockIdx.x) - b * p.per) * 256 + int(threadIdx.x), vec = fdiv(i, p.lanes), nth = fdiv(vec, p.by_head);
         lane = i - vec * int(p.lanes.d);
         h = vec - nth * p.heads;
-        const int start = p.start[b], n = p.count ? min(p.count[b], p.tokens) : p.tokens;
+        const int start = p.start[b], n = p.count ? min(max(p.count[b], 0), p.tokens) : p.tokens;     // (n - t stays a 32-bit number)
         t = nth * N - (start & (N - 1));
         low = max(-t, 0);
         high = min(n - t, N);
