@@ -70,6 +70,8 @@ class Rotary:
             raise ValueError(f"{pairs} pairs of heads of {dim}")
         if self.sections is not None and (sum(self.sections) != pairs or min(self.sections) < 0 or len(self.sections) > 4):
             raise ValueError(f"sections {self.sections} of {pairs} pairs")
+        if not self.eps >= 0:
+            raise ValueError(f"eps must be >= 0, got {self.eps}")
         for norm in (self.q_norm, self.k_norm):
             if norm is not None:
                 ops._vector(norm, "a head's norm", (x.dtype, torch.float32), dim)
