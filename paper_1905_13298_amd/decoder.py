@@ -11,6 +11,8 @@ matrices, which are rounded once here.
 """
 from __future__ import annotations
 
+import operator
+
 import torch
 
 from . import ops
@@ -53,7 +55,7 @@ class Rotary:
 
     def __init__(self, frequencies, q_norm=None, k_norm=None, sections=None, interleaved: bool = False, eps: float = 1e-6):
         self.frequencies, self.q_norm, self.k_norm = frequencies, q_norm, k_norm
-        self.sections = None if sections is None else tuple(sections)
+        self.sections = None if sections is None else tuple(operator.index(n) for n in sections)
         self.interleaved, self.eps = interleaved, eps
 
     @property
