@@ -102,6 +102,8 @@ class DecoderLayer:
             raise ValueError(f"{heads} query heads over {kv_heads} heads")
         if cache_bits not in _CACHES:
             raise ValueError(f"a cache holds 8 or 4 bits an element, not {cache_bits}")
+        if not 0 <= operator.index(window) < 2 ** 31:
+            raise ValueError(f"window must be in [0, 2^31), got {window}")
         self.rotary, self.cache_bits = rotary, cache_bits
         hidden = params["norm1"].shape[0]
         self.heads, self.kv_heads, self.dim, self.window = heads, kv_heads, dim, window
