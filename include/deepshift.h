@@ -582,13 +582,15 @@ ds_status ds_get_tuning(const char *name, int32_t *value);
  * brings the block's largest finite magnitude to at most 448 (2^0 for a block of
  * zeros, 2^-48 in a cache), rounds to nearest even, and holds an element that is
  * not finite as NaN, which has no say in its block's scale. The byte 255 is a scale that is
- * no number (no quantiser writes it): its block's products are NaN.
+ * no number (no 8-bit quantiser writes it): its block's products are NaN.
  *
  * Element types of the other tensors: ds_dtype. Strides (ld*) count elements from
  * one row to the next; an 8-bit matrix's rows begin on 16 bytes, a multiple of 16
  * apart, and are readable up to a multiple of 16 (their elements past the columns
  * are never used, the quantisers write zeros up to a multiple of 8). No output may
- * overlap another tensor of the call. Sums, norms and softmax statistics are held
+ * overlap another tensor of the call, a tensor being all that lies from its first element to its
+ * last: outputs that are parts of one buffer's rows are refused. An output's elements are
+ * places of their own (no stride of 0). Sums, norms and softmax statistics are held
  * in 32 bits. Calls are asynchronous on `stream`, allocate nothing, keep nothing
  * and may be captured; scratch is device memory of the caller's that a call may
  * overwrite. Sizes of 0 rows, tokens or sequences are allowed and do nothing. */
