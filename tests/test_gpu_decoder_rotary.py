@@ -4,7 +4,7 @@ import math
 import pytest
 import torch
 
-from .test_gpu_decoder_fp4 import BF16, DEV, build
+from .test_gpu_decoder_fp4 import BF16, DEV, F16, build
 
 pytestmark = pytest.mark.gpu
 
@@ -22,3 +22,43 @@ def test_a_later_layers_eps_is_refused_before_a_cache_is_written(eps, cache_bits
         model(x * 100)
     assert model.length.tolist() == [3, 3]
     assert all(torch.equal(a, b.view(torch.uint8)) for a, b in zip(kept, (t for c in model.caches for t in c)))
+
+
+@pytest.mark.parametrize("sections,interleaved,norms,window,cache_bits,dtype", [
+    (None, True, True, 0, 4, BF16), ((10, 9, 13), False, True, 20, 4, F16), ((32, 0), True, False, 0, 4, BF16), (None, False, False, 33, 8, BF16),
+    ((16, 16), True, True, 0, 8, F16), ((32,), False, True, 0, 8, BF16),
+])
+def test_layers_are_their_operators_one_by_one(sections, interleaved, norms, window, cache_bits, dtype):
+    from paper_1905_13298_amd import ops
+    heads, kv, dim, batch, layers = 6, 2, 64, 2, 2
+    make, _, rs, norm, rng = build(5, layers, 256, heads, kv, dim, 512, dtype, batch, 100, 32, window, sections, interleaved, norms, cache_bits)
+    model, twin = make(), make()
+    append, attention = (ops.kv_cache_fp4_append, ops.attention_fp4) if cache_bits == 4 else (ops.kv_cache_append, ops.attention_fp8)
+    length = torch.zeros(batch, dtype=torch.int32, device=DEV)
+    axes = len(sections) if sections else 1
+    for tokens, count in ((37, [37, 5]), (1, None), (4, [0, 4]), (1, None)):
+        x = torch.from_numpy(rng.standard_normal((batch, tokens, 256))).to(DEV, dtype)
+        n = None if count is None else torch.tensor(count, dtype=torch.int32, device=DEV)
+        at = None if axes == 1 else torch.from_numpy(rng.integers(0, 90, (axes, batch, tokens))).to(DEV, torch.int32)
+        got = model(x, n, positions=at)
+        after = length + (tokens if n is None else n)
+        where = at if at is not None else (length[:, None] + torch.arange(tokens, device=DEV)).to(torch.int32)
+        y, h = x.view(batch * tokens, -1), None
+        for layer, r, cache in zip(twin.layers, rs, twin.caches):
+            qkv, h, _ = layer.qkv(y, h)
+            q, k, v = qkv.view(batch, tokens, -1, dim).split([heads, kv, kv], dim=2)
+            turned = ops.rotary_norm(q, k, where, r.frequencies, r.q_norm, r.k_norm, sections if axes > 1 else None, interleaved)
+            assert not torch.equal(turned[0], q) and not torch.equal(turned[1], k)
+            append(turned[1], v, *cache, twin.table, length, n)
+            o = attention(turned[0], *cache, twin.table, after, n, window=window)
+            a = ops.linear_fp8(*ops.quantize_fp8(o.view(batch * tokens, -1)), *layer.out, out_dtype=dtype)
+            gu, h, _ = layer.gate_up(a, h)
+            gate, up = gu.chunk(2, dim=1)
+            y = ops.linear_fp8(*ops.quantize_fp8(up, gate), *layer.down, out_dtype=dtype)
+        y, _, _, _ = ops.rms_norm(y, norm, h, quantize=False)
+        assert torch.equal(got, y.view(got.shape))
+        length = after
+        assert torch.equal(model.length, length)
+        for mine, theirs in zip(model.caches, twin.caches):
+            for a, b in zip(mine, theirs):
+                assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))

@@ -1,10 +1,12 @@
 """The 4-bit cache and its attention: counts that are no counts, and splits of many sequences. Definitions and tolerances
 are those of test_gpu_fp4.py.
 """
+import random
+
 import pytest
 import torch
 
-from .test_gpu_fp4 import BF16, DEV, append_reference, filled_cache, normal, ops, same_numbers, tokens_of  # noqa: F401
+from .test_gpu_fp4 import BF16, DEV, append_reference, attention_case, filled_cache, normal, ops, same_numbers, tokens_of  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -32,3 +34,13 @@ def test_counts_that_are_no_counts(ops, tokens, count):  # noqa: F811
         for b in range(batch):
             c = min(max(count[b], 0), tokens)
             assert torch.equal(g[b, :c], w[b, :c]) and not g[b, c:].any() and w[b].any()
+
+
+@pytest.mark.parametrize("tokens,group,window", [(1, 3, 0), (1, 1, 700), (9, 2, 0), (20, 2, 0), (33, 1, 300)])
+@pytest.mark.parametrize("dim", [16, 80, 144])
+def test_attention_of_many_sequences_of_unequal_lengths(ops, tokens, group, window, dim):  # noqa: F811
+    """More than 256 blocks of few queries: splits of at least 16 steps, many without keys, joined."""
+    rng = random.Random(tokens + dim)
+    lengths = [rng.choice([0, 1, tokens, 63, rng.randint(1, 400), rng.randint(1, 2100)]) for _ in range(134)] + [2100]
+    attention_case(ops, dim, 64 if dim < 100 else 128, 2 if dim == 16 else 1, group, tokens, lengths * (1 if dim == 16 else 2), window=window, seed=dim,
+                   count=[min(n, tokens) for n in lengths] * (1 if dim == 16 else 2))

@@ -110,3 +110,43 @@ def test_gradient_without_eps(ops, dim, heads, kv, dtype):  # noqa: F811
         near_finite(got[i], r * (e - n * inner),
                     r * (slack * w.abs() + n.abs() * ((slack * w.abs() * n.abs()).mean(-1, keepdim=True) + magnitude * 2.0 ** -18) + e.abs() * 2.0 ** -19))
         near_finite(got[2 + i], (g * n).sum((0, 1, 2)), (both * n.abs()).sum((0, 1, 2)) * 2.0 ** -18)
+
+
+# Tokens and heads of which a wave takes 2, 3, 4, 2 and 2 groups of heads, more than one chunk of them but in the fourth, the last one ragged.
+SEVERAL = [(1, 1700, 37, 9, 128, 64, 0, False), (3, 700, 19, 5, 256, 100, 0, False), (2, 1024, 70, 33, 64, 32, 0, False), (2, 1221, 16, 16, 80, 40, 3, True),
+           (1, 2100, 33, 17, 32, 16, 2, True)]
+
+
+@pytest.mark.parametrize("shape", SEVERAL)
+def test_several_groups_of_heads_a_wave(ops, shape):  # noqa: F811
+    *size, interleaved = shape
+    q, k, positions, f, qw, kw, sections = inputs(sum(size), *size, True, F32, 5000)
+    args = to(DEV, q, k, positions, f, qw, kw)
+    a = angles(positions, f, sections)
+    got = ops.rotary_norm(*args, sections=sections, interleaved=interleaved, eps=1e-5)
+    for g, x, w in zip(got, (q, k), (qw, kw)):
+        want, both = turn(normed(x.double(), w.double(), 1e-5), a, interleaved)
+        near_finite(g, want, both * 2.0 ** -19)
+    plain = ops.rotary_norm(*args[:4], sections=sections, interleaved=interleaved)
+    for g, x in zip(plain, (q, k)):
+        want, both = turn(x.double(), a, interleaved)
+        near_finite(g, want, both * 2.0 ** -19)
+
+
+@pytest.mark.parametrize("shape", SEVERAL)
+def test_gradient_of_several_groups_of_heads_a_wave(ops, shape):  # noqa: F811
+    """A weight's sum has at most 51 roundings (8 in a lane, 4 between lanes, 2 between waves, 37 over the blocks) and its terms are off by 24 * 2^-24
+    of |a| + |b|: less than 2^-17."""
+    *size, interleaved = shape
+    q, k, positions, f, qw, kw, sections = inputs(sum(size) + 5, *size, True, F32, 5000)
+    dy = [normal(90 + i, *x.shape) for i, x in enumerate((q, k))]
+    got = ops.rotary_norm_backward(*to(DEV, *dy, q, k, positions, f, qw, kw), sections=sections, interleaved=interleaved, eps=1e-5)
+    a = angles(positions, f, sections)
+    for i, (d, x, w) in enumerate(zip(dy, (q, k), (qw, kw))):
+        g, both = turn(d.double(), a, interleaved, back=True)
+        x, w = x.double(), w.double()
+        r = 1 / torch.sqrt((x * x).mean(-1, keepdim=True) + 1e-5)
+        n, e = x * r, g * w
+        inner, magnitude = (e * n).mean(-1, keepdim=True), (e * n).abs().mean(-1, keepdim=True)
+        near_finite(got[i], r * (e - n * inner), r * (both * w.abs() + n.abs() * ((both * w.abs() * n.abs()).mean(-1, keepdim=True) + magnitude)) * 2.0 ** -18)
+        near_finite(got[2 + i], (g * n).sum((0, 1, 2)), (both * n.abs()).sum((0, 1, 2)) * 2.0 ** -17)
