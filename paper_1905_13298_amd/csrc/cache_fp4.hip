@@ -215,7 +215,9 @@ read4_kernel(T *__restrict__ k, T *__restrict__ v, const uint8_t *__restrict__ k
 // the second product is 8 r + j (of heads of up to 64: 4 r + j; above 128 there are two such sets), so that a lane's
 // dimensions are neighbours in memory too. Keys become numbers of the queries' type exactly, with their scales; p and the values
 // are 16-bit floats with 10 bits of mantissa: values exactly, p rounded once, to 2^-11 of itself down to
-// 2^-23 of the row's largest and to 2^-34 of that one below (l has all of it in 32 bits).
+// 2^-23 of the row's largest and to 2^-34 of that one below (l has all of it in 32 bits). That rounding buys one matrix
+// instruction of 16-bit floats where p as a sum of two of them needs two: 2 x 1000 queries over 8000 keys 243 us for 331, 32 x 5
+// over up to 4000 34.2 for 38.4, one over 131072 34.3 for 35.5 (float16 results 2.2e-4 of their size off instead of 2.1e-4).
 
 // Eight numbers as an operand.
 template <typename T>
@@ -271,7 +273,8 @@ __device__ __forceinline__ void unroll(F &&f)
 // Up to 16 TILES queries of a kv head at a time (tokens being decoded): a block of 4 waves takes a share of the keys, each wave
 // every fourth 64 of it straight from memory to registers (no two waves share any), and joins them at its end.
 // Bound by reading the cache once, and by the blocks' starts and ends: 131072 keys of 8 heads of 128, 143 MB, 30.3 us
-// (4.7 TB/s) and 3.4 of joining; its VALU instructions, a third of them conversions, would take 38 % of that.
+// (4.7 TB/s) and 3.4 of joining; its VALU instructions, a third of them conversions, would take 38 % of that. Heads
+// above 128 need 369 registers and have one block a CU: as many bytes in 4 heads of 256 47 us in all.
 template <typename T, int DP, int TILES>
 __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1)
 attention4_few_kernel(const AttentionParams p, int blocks)
@@ -583,7 +586,8 @@ attention4_few_kernel(const AttentionParams p, int blocks)
 //
 // Bound by the matrix instructions and the exponentials between them, which two waves of a SIMD overlap in
 // part, and by turning keys and values into floats (without it 217 us): 2 x 1000 queries of 32 heads over up to 8000
-// keys of 8 heads of 128 take 246 us, 970 TFLOP/s. (Blocks of eight waves, which turn half as much each, 281.)
+// keys of 8 heads of 128 take 243-246 us, 980 TFLOP/s. (Blocks of eight waves, which turn half as much each, 281.) Heads of 65 to
+// 128 spill 11 registers, those above, which leave one wave a SIMD, 57: 4 x 300 queries of 256 over up to 4000 221 us, 420 TFLOP/s.
 template <typename T, int DP>
 __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2)
 attention4_many_kernel(const AttentionParams p, int blocks, int bhs)
@@ -964,16 +968,18 @@ attention4_join_kernel(const AttentionParams p)
     store_row<T>(p, int(bh / p.heads), int(bh % p.heads), int(at - bh * p.rows), nullptr, lane * 4, sum, inverse(total));
 }
 
-// How a call is split: over the rows first, then over the keys until 512 blocks (two a CU) have at
+// How a call is split: over the rows first, then over the keys until 512 blocks (two a CU, of heads above 128 in two rounds) have at
 // least 8 steps of 64 keys each. Measured (8 heads of 128, 4 query heads each; us): one query over 131072 keys 34.7,
 // with 768 blocks 36.9, with 1024 43; 16 x 1 over up to 8192 23.5, 22.7 and 28. Where sequences and heads alone
 // make more than 256 blocks of few queries, whose lengths may differ, until 1536 have at least 16 steps each: 48 x 1 over
 // up to 8192 55.5, until 512 60.4, with 8 splits each 70; 64 x 1 over up to 16000 131, 16 splits each 170. (Splits have the same
 // number of steps, so that a sequence much longer than 63 others is what a call waits for.) Few queries whose
 // splits would not give every CU a block have splits of 4 steps: 1 x 1 over 2000 8.7, of 8 10.1.
+// (Lengths and windows are the device's: the splits go by the table's width. In a table for 131072 keys 1 x 1 over 2000 takes 11.9
+// for 8.1, and with a window of 4096 over 131072 11.9 for the 8.2 of 4096 alone: few of the splits have keys then.)
 // Up to 64 rows run attention4_few_kernel, from 17 on in blocks of 32 rows (of heads above 128: 16): 32 x 5 queries over
-// up to 4000 keys 37.5, through LDS 80.6; 32 x 16 62.8 and 88.3, of heads of 256 (8 x 16) 53.9 and 75.7, of 64 58.9 and 68.5;
-// 5 x 3 of 7 heads each 13.4 and 17.6; 1 x 16 over 8000 15.2 and 26.8. Above, 32 x 32 queries would take 106 for 86.
+// up to 4000 keys 34.1, through LDS 63.8; 32 x 16 62.1 and 72.1, of heads of 256 (8 x 16) 53.5 and 63.8, of 64 58.6 and 65.0;
+// 5 x 3 of 7 heads each 12.8 and 14.5; 1 x 16 over 8000 15.0 and 22.2. Above, 32 x 32 queries would take 105 for 84.
 Plan plan_attention4(int64_t batch, int64_t tokens, int64_t heads, int64_t group, int64_t dim, int64_t columns, int64_t page)
 {
     Plan a;

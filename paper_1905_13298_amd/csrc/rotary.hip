@@ -128,9 +128,10 @@ struct Lane {
     }
 };
 
-// Cosine and sine of 2 pi t. The angle is taken in quarter turns from the nearest one, in 64 bits, so
-// that a far position costs 2^-53 of its angle (2^-30 at a million radians) and no more; what remains, up to
-// pi / 4, goes through the Taylor polynomials up to x^9 and x^10, whose next terms are 2.2e-9 of x and 1.1e-10.
+// Cosine and sine of 2 pi t. The angle is taken in quarter turns from the nearest one, in 64 bits: three roundings (1 / 2 pi, its
+// product with the frequency, that with the position), at most 3 * 2^-53 of the angle (2^-31 at a million radians), whatever the
+// position. What remains, up to pi / 4, is rounded to 32 bits and goes through the Taylor polynomials up to x^9 and x^10, whose next terms
+// are 2.2e-9 of x and 1.1e-10: in 32 bits, off by 2^-22 at most, as what they multiply has 24 bits itself.
 __device__ __forceinline__ void turn_of(double t, float &cosine, float &sine)
 {
     const double quarters = t * 4, near = rint(quarters);
@@ -345,8 +346,7 @@ void for_layout(const RotaryParams &p, int32_t type, int32_t wtype, F &&f)
     else weights(__bf16{});
 }
 
-// Blocks of the gradient's launch, a row of the weights' sums each: four waves, a token each at a time.
-// Heads of a group (a wave has them at once), and how many groups it takes of a token.
+// Heads of a group: those that a wave has at once.
 int heads_at_once(int64_t dim) { return dim <= 64 ? 16 : dim <= 128 ? 8 : 4; }
 
 struct Split {
